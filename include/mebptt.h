@@ -13,6 +13,8 @@
  *                     executes the schedule on the GPU inside the caller's slot pool and
  *                     returns dW, db, dh0, dc0 (and optionally dx and the outputs h_1..h_t).
  *
+ * A third part, "operators of a selective state space block", stands by itself: no plan, no slots.
+ *
  * Conventions
  *   - Every function returns MEBPTT_OK (0) or a negative mebptt_status; it never throws or
  *     aborts.  On a validation error no device work has been enqueued.  mebptt_last_error()
@@ -416,6 +418,150 @@ int mebptt_run_static(const mebptt_lstm_desc* desc, const mebptt_plan_t* plan,
                       void* slots, size_t slots_bytes,
                       float* dW_ih, float* dW_hh, float* db, float* dh0, float* dc0,
                       float* dx, float* y_out, mebptt_stats* stats, void* stream);
+
+/* ---- operators of a selective state space block ------------------------------------------------
+ * A recurrent core whose recurrence is diagonal and depends on its input, and what stands around it in
+ * a residual block: root-mean-square norm with the residual's addition, product of 8-bit integers with
+ * scales (the block's projections when it serves), short causal convolution, selective scan.  The first,
+ * third and fourth have a backward pass; the last two have a form for single tokens with their states in a pool.
+ *
+ * All of them: pointers are device memory of the caller unless marked host; the calls only enqueue work on
+ * `stream` (a hipStream_t, NULL = the default stream) of the current device and create nothing; sums, statistics and
+ * states are 32 bits wide whatever the activations' type; results do not depend on timing (no floating-point
+ * atomics).  A size of zero (rows, t, B, M) is a valid call that computes what is left of it.  Outputs must not
+ * overlap inputs or each other unless said so.  Workspaces are 256-byte aligned and hold nothing between
+ * calls.  Errors: EINVAL, EWORKSPACE, EHIP; nothing is enqueued on a validation error. */
+enum { MEBPTT_FP32 = 0, MEBPTT_BF16 = 1, MEBPTT_INT8 = 2 };
+
+/* A sequence of activations: element (step s, sequence b, channel c), all from 0, is at data[s * stride_t + b * stride_b + c]
+ * (strides in elements).  Covers [t, B, C], [B, t, C] and column blocks of a wider array.  Rows of an output must not
+ * overlap.  Elements need only their own alignment; channel counts, strides and pointers that keep every row on a
+ * 16-byte boundary are faster. */
+typedef struct {
+  void* data;
+  int64_t stride_t, stride_b;
+} mebptt_seq;
+
+/* RMS norm of rows of `width` values:  r = x + residual,  y = r * rsqrt(mean(r^2) + eps) * weight. */
+typedef struct {
+  int64_t rows;
+  int32_t width;          /* 1 .. 16384 */
+  int32_t x_dtype;        /* MEBPTT_FP32 or MEBPTT_BF16: x, and dy, dx of the backward pass */
+  int32_t residual_dtype; /* the same choice for residual, residual_out and their gradients */
+  int32_t y_dtype;        /* MEBPTT_FP32, MEBPTT_BF16 or MEBPTT_INT8 */
+  float eps;              /* >= 0 */
+} mebptt_norm_desc;
+/* read:  x [rows, width], row stride ldx (elements, >= width; all ld alike); residual (NULL: r = x); weight [width] fp32 (NULL: ones).
+ * write: y; y_scale [rows] fp32 (MEBPTT_INT8 only, else ignored); residual_out = r rounded to its type (NULL: not written);
+ *        rstd [rows] fp32 (NULL: not written).  residual_out may be residual itself (and, types and ld being the same, x),
+ *        y may be x (types and ld being the same).
+ * The statistics and y come from r before it is rounded to residual_out's type.  MEBPTT_INT8: y_scale = max|y| / 127 of the row and
+ * y = round to nearest even(y / y_scale), -127 .. 127; a row of zeros has scale 0, a row with a value that is not finite has
+ * scale NaN, both with zeros in y. */
+int mebptt_norm_forward(const mebptt_norm_desc* desc, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                        const float* weight, void* y, int64_t ldy, float* y_scale, void* residual_out, int64_t ldo,
+                        float* rstd, void* stream);
+/* Gradients of mebptt_norm_forward (y_dtype is not looked at).
+ * read:  r [rows, width] of residual_dtype: what residual_out received (x itself if there was no residual; the types must then be
+ *        the same), rstd, weight (NULL: ones), dy (x_dtype), dresidual_out (residual_dtype, the gradient that
+ *        arrives at residual_out; NULL: none).
+ * write: dx (x_dtype) and dresidual (residual_dtype), one gradient in two types, either may be NULL and dresidual may be
+ *        dresidual_out itself; dweight [width] fp32 (NULL: not computed). */
+size_t mebptt_norm_workspace_bytes(const mebptt_norm_desc* desc);
+int mebptt_norm_backward(const mebptt_norm_desc* desc, const void* r, int64_t ldr, const float* weight, const float* rstd,
+                         const void* dy, int64_t lddy, const void* dresidual_out, int64_t lddo, void* dx, int64_t lddx,
+                         void* dresidual, int64_t lddr, float* dweight, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/* out[m][n] = a_scale[m] * b_scale[n] * sum_k a[m][k] * b[n][k] + bias[n]: a token's and a channel's scale each.  The sums are
+ * exact 32-bit integers, which bounds K; they are scaled in fp32 and rounded once.
+ * read:  a [M, K] int8, row stride lda; a_scale [M] fp32; b [N, K] int8, row stride ldb (a weight matrix as it is
+ *        stored); b_scale [N] fp32; bias [N] fp32 or NULL.  write: out [M, N], row stride ldo.
+ * K = 0 gives the bias. */
+typedef struct {
+  int64_t M;         /* 0 .. 2^29 */
+  int32_t N, K;      /* N 1 .. 2^21, K 0 .. 131071 */
+  int32_t out_dtype; /* MEBPTT_FP32 or MEBPTT_BF16 */
+} mebptt_int8_desc;
+size_t mebptt_int8_workspace_bytes(const mebptt_int8_desc* desc);
+int mebptt_int8_product(const mebptt_int8_desc* desc, const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b,
+                        int64_t ldb, const float* b_scale, const float* bias, void* out, int64_t ldo, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* Depthwise causal convolution:  y_s = act(bias + sum_{j < taps} weight[:, j] * x_{s - taps + 1 + j}), act(v) = v * sigmoid(v) or v.
+ * Inputs before the first step come from state_in (its last row is the one just before), zeros without it.  With lengths,
+ * sequence b has lengths[b] steps (clamped to 0 .. t): what stands in x beyond them is not looked at, y (and dx) is zero there,
+ * and the state is that after the sequence's own last step. */
+typedef struct {
+  int32_t t, B, C;
+  int32_t taps;  /* 1 .. 8 */
+  int32_t dtype; /* MEBPTT_FP32 or MEBPTT_BF16: x, y, the states, and their gradients */
+  int32_t silu;  /* 0: act(v) = v */
+} mebptt_conv_desc;
+/* read: x, weight [C, taps] fp32, bias [C] fp32 or NULL, lengths [B] or NULL, state_in [B, taps - 1, C] or NULL.
+ * write: y, state_out [B, taps - 1, C] (NULL: not written; may be state_in itself). */
+int mebptt_conv_forward(const mebptt_conv_desc* desc, mebptt_seq x, const float* weight, const float* bias,
+                        const int32_t* lengths, const void* state_in, mebptt_seq y, void* state_out, void* stream);
+/* read: the above (state_in as it was before the forward call), dy, dstate_out [B, taps - 1, C] (NULL: zeros).
+ * write: dx, dweight [C, taps], dbias [C] (NULL: not written), dstate_in [B, taps - 1, C] (NULL: not written). */
+size_t mebptt_conv_workspace_bytes(const mebptt_conv_desc* desc);
+int mebptt_conv_backward(const mebptt_conv_desc* desc, mebptt_seq x, const float* weight, const float* bias,
+                         const int32_t* lengths, const void* state_in, mebptt_seq dy, const void* dstate_out, mebptt_seq dx,
+                         float* dweight, float* dbias, void* dstate_in, void* workspace, size_t workspace_bytes,
+                         void* stream);
+/* One token for each of B sequences whose states are rows of a pool [slots, taps - 1, C]: sequence b's state is read from row index[b]
+ * of state_in and written to the same row of state_out (which may be state_in itself).  index NULL: row b.  A sequence whose index
+ * lies outside 0 .. slots - 1 has no state: its y is zero and nothing else is touched.  The indices of the others must differ.
+ * x and y: [B, C] with row strides ldx, ldy.  desc->t must be 1. */
+int mebptt_conv_step(const mebptt_conv_desc* desc, const void* x, int64_t ldx, const float* weight, const float* bias,
+                     const void* state_in, int64_t slots, const int32_t* index, void* y, int64_t ldy, void* state_out,
+                     void* stream);
+
+/* Selective scan over D channels of N states each.  With G groups, channel d reads row d / (D / G) of B and C:
+ *     w_s = delta_s + delta_bias, through softplus if asked;   h_s = exp(w_s A) h_{s-1} + w_s u_s B_s;
+ *     y_s = (sum_n C_s h_s + skip u_s) * (z_s sigmoid(z_s) if there is a z).
+ * Lengths as in the convolution; h_out is the state after a sequence's own last step. */
+typedef struct {
+  int32_t t, B, D;
+  int32_t N;        /* 1 .. 64 */
+  int32_t G;        /* divides D */
+  int32_t dtype;    /* MEBPTT_FP32 or MEBPTT_BF16: u, delta, z, B, C, y and their gradients */
+  int32_t softplus;
+  int32_t stretch;  /* the backward pass's memory for time: the states of every `stretch`-th step are kept, the ones between
+                       recomputed.  16, 32, 64, 128 or 256; not looked at without `states`. */
+} mebptt_scan_desc;
+typedef struct {
+  mebptt_seq u, delta;     /* D channels */
+  mebptt_seq z;            /* D channels; data NULL: no gate */
+  mebptt_seq Bm, Cm;       /* G * N channels, group after group */
+  const float* A;          /* [D, N], not above 0 where the recurrence is to be stable */
+  const float* skip;       /* [D] or NULL */
+  const float* delta_bias; /* [D] or NULL */
+  const int32_t* lengths;  /* [B] or NULL */
+  const float* h0;         /* [B, D, N] or NULL: zeros */
+} mebptt_scan_inputs;
+typedef struct {
+  mebptt_seq du, ddelta;
+  mebptt_seq dz;            /* written if there is a z */
+  mebptt_seq dBm, dCm;
+  float *dA, *dskip, *ddelta_bias; /* dskip, ddelta_bias: may be NULL */
+  float* dh0;                      /* may be NULL */
+} mebptt_scan_grads;
+/* Bytes of the states that a forward call keeps for a backward call; of the workspace of either call (backward != 0: of the latter). */
+size_t mebptt_scan_state_bytes(const mebptt_scan_desc* desc);
+size_t mebptt_scan_workspace_bytes(const mebptt_scan_desc* desc, int32_t backward);
+/* `in` (host) is read during the call only.  write: y; h_out [B, D, N] (NULL: not written; may be h0 itself); states (NULL when no backward call follows;
+ * 256-byte aligned). */
+int mebptt_scan_forward(const mebptt_scan_desc* desc, const mebptt_scan_inputs* in, mebptt_seq y, float* h_out, void* states,
+                        size_t states_bytes, void* workspace, size_t workspace_bytes, void* stream);
+/* read: the forward call's inputs and the states that it kept, dy, dh_out [B, D, N] (NULL: zeros).  write: all of `grads` (host). */
+int mebptt_scan_backward(const mebptt_scan_desc* desc, const mebptt_scan_inputs* in, mebptt_seq dy, const float* dh_out,
+                         const void* states, size_t states_bytes, const mebptt_scan_grads* grads, void* workspace,
+                         size_t workspace_bytes, void* stream);
+/* One token for each of B sequences, states in a pool [slots, D, N] and indices as in mebptt_conv_step.  desc->t must be 1; the
+ * sequences' stride_t, and in->lengths and in->h0, are not looked at. */
+int mebptt_scan_step(const mebptt_scan_desc* desc, const mebptt_scan_inputs* in, const float* state_in, int64_t slots,
+                     const int32_t* index, mebptt_seq y, float* state_out, void* stream);
 
 /* ---- measurement hooks ---------------------------------------------------------------------
  * Kernel classes of the hot path, for timing with HIP events on the run's own stream. */

@@ -86,6 +86,40 @@ class mebptt_profile(C.Structure):
                 ("sweep_forward_steps", C.c_int64), ("batch_steps", C.c_int64), ("batch_ms", C.c_double)]
 
 
+FP32, BF16, INT8 = 0, 1, 2
+
+
+class mebptt_seq(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_t", C.c_int64), ("stride_b", C.c_int64)]
+
+
+class mebptt_norm_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("x_dtype", C.c_int32), ("residual_dtype", C.c_int32),
+                ("y_dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class mebptt_int8_desc(C.Structure):
+    _fields_ = [("M", C.c_int64), ("N", C.c_int32), ("K", C.c_int32), ("out_dtype", C.c_int32)]
+
+
+class mebptt_conv_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("t", "B", "C", "taps", "dtype", "silu")]
+
+
+class mebptt_scan_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("t", "B", "D", "N", "G", "dtype", "softplus", "stretch")]
+
+
+class mebptt_scan_inputs(C.Structure):
+    _fields_ = ([(n, mebptt_seq) for n in ("u", "delta", "z", "Bm", "Cm")]
+                + [(n, C.c_void_p) for n in ("A", "skip", "delta_bias", "lengths", "h0")])
+
+
+class mebptt_scan_grads(C.Structure):
+    _fields_ = ([(n, mebptt_seq) for n in ("du", "ddelta", "dz", "dBm", "dCm")]
+                + [(n, C.c_void_p) for n in ("dA", "dskip", "ddelta_bias", "dh0")])
+
+
 # name -> (restype, argtypes): every symbol the header declares
 _P = C.c_void_p
 _DESC = C.POINTER(mebptt_lstm_desc)
@@ -134,6 +168,28 @@ SIGNATURES = {
     "mebptt_resident_wait_limit": (C.c_int, [C.c_int64]),
     "mebptt_resident_patience": (C.c_int, [C.c_int64]),
     "mebptt_shutdown": (C.c_int, []),
+    "mebptt_norm_forward": (C.c_int, [C.POINTER(mebptt_norm_desc), _P, C.c_int64, _P, C.c_int64, _P, _P, C.c_int64, _P, _P,
+                                      C.c_int64, _P, _P]),
+    "mebptt_norm_workspace_bytes": (C.c_size_t, [C.POINTER(mebptt_norm_desc)]),
+    "mebptt_norm_backward": (C.c_int, [C.POINTER(mebptt_norm_desc), _P, C.c_int64, _P, _P, _P, C.c_int64, _P, C.c_int64, _P,
+                                       C.c_int64, _P, C.c_int64, _P, _P, C.c_size_t, _P]),
+    "mebptt_int8_workspace_bytes": (C.c_size_t, [C.POINTER(mebptt_int8_desc)]),
+    "mebptt_int8_product": (C.c_int, [C.POINTER(mebptt_int8_desc), _P, C.c_int64, _P, _P, C.c_int64, _P, _P, _P, C.c_int64, _P,
+                                      C.c_size_t, _P]),
+    "mebptt_conv_forward": (C.c_int, [C.POINTER(mebptt_conv_desc), mebptt_seq, _P, _P, _P, _P, mebptt_seq, _P, _P]),
+    "mebptt_conv_workspace_bytes": (C.c_size_t, [C.POINTER(mebptt_conv_desc)]),
+    "mebptt_conv_backward": (C.c_int, [C.POINTER(mebptt_conv_desc), mebptt_seq, _P, _P, _P, _P, mebptt_seq, _P, mebptt_seq, _P,
+                                       _P, _P, _P, C.c_size_t, _P]),
+    "mebptt_conv_step": (C.c_int, [C.POINTER(mebptt_conv_desc), _P, C.c_int64, _P, _P, _P, C.c_int64, _P, _P, C.c_int64, _P,
+                                   _P]),
+    "mebptt_scan_state_bytes": (C.c_size_t, [C.POINTER(mebptt_scan_desc)]),
+    "mebptt_scan_workspace_bytes": (C.c_size_t, [C.POINTER(mebptt_scan_desc), C.c_int32]),
+    "mebptt_scan_forward": (C.c_int, [C.POINTER(mebptt_scan_desc), C.POINTER(mebptt_scan_inputs), mebptt_seq, _P, _P, C.c_size_t,
+                                      _P, C.c_size_t, _P]),
+    "mebptt_scan_backward": (C.c_int, [C.POINTER(mebptt_scan_desc), C.POINTER(mebptt_scan_inputs), mebptt_seq, _P, _P, C.c_size_t,
+                                       C.POINTER(mebptt_scan_grads), _P, C.c_size_t, _P]),
+    "mebptt_scan_step": (C.c_int, [C.POINTER(mebptt_scan_desc), C.POINTER(mebptt_scan_inputs), _P, C.c_int64, _P, mebptt_seq, _P,
+                                   _P]),
     "mebptt_null_launch_us": (C.c_int, [C.c_int32, _P, C.POINTER(C.c_double)]),
     "mebptt_measure_sync": (C.c_int, [C.c_int32, C.c_int32, _P, C.POINTER(C.c_double), C.POINTER(C.c_int32)]),
     "mebptt_chunk_steps": (C.c_int32, [_DESC]),
@@ -509,3 +565,251 @@ def mebptt_measure_gemms(desc: mebptt_lstm_desc, workspace, reps: int = 20, stre
     _check(lib().mebptt_measure_gemms(C.byref(desc), _ptr(workspace), _nbytes(workspace), reps, _stream(stream),
                                       C.byref(a), C.byref(b)))
     return a.value, b.value
+
+
+# ---- operators of a selective state space block ------------------------------------------------------
+#
+# Tensors are checked here for type, shape and device, which the library cannot see; it checks everything else.  Sequences
+# are [t, B, channels], of any strides over t and B; states, parameters and their gradients are contiguous.
+
+
+def _torch_dtype(code: int):
+    import torch
+    return {FP32: torch.float32, BF16: torch.bfloat16, INT8: torch.int8}[code]
+
+
+def _given(t, name: str, shape, dtype, device, optional: bool = False):
+    """`t` as an argument of this shape and type, on the device of the call's other tensors."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{name} is required")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} is needed")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has type {t.dtype}, {dtype} is needed")
+    if t.device != device or t.device.type != "cuda":
+        raise ValueError(f"{name} is on {t.device}, one GPU's memory is needed")
+    return t
+
+
+def _whole(t, name: str, shape, dtype, device, optional: bool = False) -> Optional[int]:
+    """Pointer of a contiguous tensor."""
+    if _given(t, name, shape, dtype, device, optional) is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _rows(t, name: str, rows: int, width: int, dtype, device, optional: bool = False):
+    """(pointer, row stride) of a [rows, width] tensor whose rows are contiguous."""
+    if _given(t, name, (rows, width), dtype, device, optional) is None:
+        return None, 0
+    if t.numel() and width > 1 and t.stride(1) != 1:
+        raise ValueError(f"rows of {name} must be contiguous")
+    return t.data_ptr(), t.stride(0) if rows > 1 else width
+
+
+def _seq(t, name: str, steps: int, B: int, channels: int, dtype, device, optional: bool = False) -> mebptt_seq:
+    """A [t, B, channels] tensor whose channels are contiguous."""
+    if _given(t, name, (steps, B, channels), dtype, device, optional) is None:
+        return mebptt_seq(None, 0, 0)
+    if t.numel() and channels > 1 and t.stride(2) != 1:
+        raise ValueError(f"the channels of {name} must be contiguous")
+    # the stride of an axis of one is whatever it is: never used, and not to be looked at
+    return mebptt_seq(t.data_ptr() or None, t.stride(0) if steps > 1 else B * channels, t.stride(1) if B > 1 else channels)
+
+
+def _room(t, name: str, device):
+    """(pointer, bytes) of a workspace; None where the call needs none."""
+    if t is None:
+        return None, 0
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and on the GPU of the call's other tensors")
+    return t.data_ptr(), _nbytes(t)
+
+
+def make_norm_desc(rows: int, width: int, x_dtype: int, residual_dtype: int, y_dtype: int, eps: float = 1e-5) -> mebptt_norm_desc:
+    return mebptt_norm_desc(rows, width, x_dtype, residual_dtype, y_dtype, eps)
+
+
+def mebptt_norm_workspace_bytes(desc: mebptt_norm_desc) -> int:
+    return lib().mebptt_norm_workspace_bytes(C.byref(desc))
+
+
+def mebptt_norm_forward(desc: mebptt_norm_desc, x, residual, weight, y, y_scale=None, residual_out=None, rstd=None,
+                        stream: Optional[int] = None) -> None:
+    """r = x + residual, y = RMS norm of r times `weight`; residual_out receives r, rstd the rows' 1 / rms (for the backward call),
+    y_scale the rows' scales of an 8-bit y."""
+    import torch
+    M, W, dev, f32 = desc.rows, desc.width, x.device, torch.float32
+    xt, rt = _torch_dtype(desc.x_dtype), _torch_dtype(desc.residual_dtype)
+    px, ldx = _rows(x, "x", M, W, xt, dev)
+    pr, ldr = _rows(residual, "residual", M, W, rt, dev, optional=True)
+    py, ldy = _rows(y, "y", M, W, _torch_dtype(desc.y_dtype), dev)
+    po, ldo = _rows(residual_out, "residual_out", M, W, rt, dev, optional=True)
+    _check(lib().mebptt_norm_forward(C.byref(desc), px, ldx, pr, ldr, _whole(weight, "weight", (W,), f32, dev, True), py, ldy,
+                                     _whole(y_scale, "y_scale", (M,), f32, dev, True), po, ldo,
+                                     _whole(rstd, "rstd", (M,), f32, dev, True), _stream(stream)))
+
+
+def mebptt_norm_backward(desc: mebptt_norm_desc, r, weight, rstd, dy, dresidual_out, dx, dresidual, dweight, workspace,
+                         stream: Optional[int] = None) -> None:
+    """Gradients of mebptt_norm_forward from r (its residual_out, or x without a residual) and rstd."""
+    import torch
+    M, W, dev, f32 = desc.rows, desc.width, r.device, torch.float32
+    xt, rt = _torch_dtype(desc.x_dtype), _torch_dtype(desc.residual_dtype)
+    pr, ldr = _rows(r, "r", M, W, rt, dev)
+    pg, ldg = _rows(dy, "dy", M, W, xt, dev)
+    pi, ldi = _rows(dresidual_out, "dresidual_out", M, W, rt, dev, optional=True)
+    pd, ldd = _rows(dx, "dx", M, W, xt, dev, optional=True)
+    po, ldo = _rows(dresidual, "dresidual", M, W, rt, dev, optional=True)
+    _check(lib().mebptt_norm_backward(C.byref(desc), pr, ldr, _whole(weight, "weight", (W,), f32, dev, True),
+                                      _whole(rstd, "rstd", (M,), f32, dev), pg, ldg, pi, ldi, pd, ldd, po, ldo,
+                                      _whole(dweight, "dweight", (W,), f32, dev, True), *_room(workspace, "workspace", dev),
+                                      _stream(stream)))
+
+
+def make_int8_desc(M: int, N: int, K: int, out_dtype: int) -> mebptt_int8_desc:
+    return mebptt_int8_desc(M, N, K, out_dtype)
+
+
+def mebptt_int8_workspace_bytes(desc: mebptt_int8_desc) -> int:
+    return lib().mebptt_int8_workspace_bytes(C.byref(desc))
+
+
+def mebptt_int8_product(desc: mebptt_int8_desc, a, a_scale, b, b_scale, bias, out, workspace=None, stream: Optional[int] = None) -> None:
+    """out = a_scale[:, None] * b_scale * (a @ b.T) + bias: a [M, K] and b [N, K] int8, scales and bias float32."""
+    import torch
+    M, N, K, dev, f32 = desc.M, desc.N, desc.K, a.device, torch.float32
+    pa, lda = _rows(a, "a", M, K, torch.int8, dev)
+    pb, ldb = _rows(b, "b", N, K, torch.int8, dev)
+    po, ldo = _rows(out, "out", M, N, _torch_dtype(desc.out_dtype), dev)
+    _check(lib().mebptt_int8_product(C.byref(desc), pa, lda, _whole(a_scale, "a_scale", (M,), f32, dev), pb, ldb,
+                                     _whole(b_scale, "b_scale", (N,), f32, dev), _whole(bias, "bias", (N,), f32, dev, True), po, ldo,
+                                     *_room(workspace, "workspace", dev), _stream(stream)))
+
+
+def make_conv_desc(t: int, B: int, C_: int, taps: int, dtype: int, silu: int = 1) -> mebptt_conv_desc:
+    return mebptt_conv_desc(t, B, C_, taps, dtype, silu)
+
+
+def mebptt_conv_workspace_bytes(desc: mebptt_conv_desc) -> int:
+    return lib().mebptt_conv_workspace_bytes(C.byref(desc))
+
+
+def _conv_params(desc, weight, bias, dev):
+    import torch
+    return (_whole(weight, "weight", (desc.C, desc.taps), torch.float32, dev),
+            _whole(bias, "bias", (desc.C,), torch.float32, dev, True))
+
+
+def mebptt_conv_forward(desc: mebptt_conv_desc, x, weight, bias, lengths, state_in, y, state_out=None,
+                        stream: Optional[int] = None) -> None:
+    """Depthwise causal convolution of [t, B, C]; states are the last taps - 1 inputs, [B, taps - 1, C]."""
+    import torch
+    dev, T = x.device, _torch_dtype(desc.dtype)
+    state = (desc.B, desc.taps - 1, desc.C)
+    _check(lib().mebptt_conv_forward(C.byref(desc), _seq(x, "x", desc.t, desc.B, desc.C, T, dev), *_conv_params(desc, weight, bias, dev),
+                                     _whole(lengths, "lengths", (desc.B,), torch.int32, dev, True),
+                                     _whole(state_in, "state_in", state, T, dev, True), _seq(y, "y", desc.t, desc.B, desc.C, T, dev),
+                                     _whole(state_out, "state_out", state, T, dev, True), _stream(stream)))
+
+
+def mebptt_conv_backward(desc: mebptt_conv_desc, x, weight, bias, lengths, state_in, dy, dstate_out, dx, dweight, dbias, dstate_in,
+                         workspace, stream: Optional[int] = None) -> None:
+    import torch
+    dev, T, f32 = x.device, _torch_dtype(desc.dtype), torch.float32
+    state, shape = (desc.B, desc.taps - 1, desc.C), (desc.t, desc.B, desc.C)
+    _check(lib().mebptt_conv_backward(C.byref(desc), _seq(x, "x", *shape, T, dev), *_conv_params(desc, weight, bias, dev),
+                                      _whole(lengths, "lengths", (desc.B,), torch.int32, dev, True),
+                                      _whole(state_in, "state_in", state, T, dev, True), _seq(dy, "dy", *shape, T, dev),
+                                      _whole(dstate_out, "dstate_out", state, T, dev, True), _seq(dx, "dx", *shape, T, dev),
+                                      _whole(dweight, "dweight", (desc.C, desc.taps), f32, dev),
+                                      _whole(dbias, "dbias", (desc.C,), f32, dev, True),
+                                      _whole(dstate_in, "dstate_in", state, T, dev, True), *_room(workspace, "workspace", dev),
+                                      _stream(stream)))
+
+
+def _pool(state_in, state_out, row, dtype, dev, needed: bool):
+    """(pointer, slots, pointer) of a pool of states and of the pool that receives them."""
+    if state_in is None and not needed:
+        return None, 1 << 31, None
+    slots = state_in.shape[0] if state_in is not None else 0
+    return (_whole(state_in, "state_in", (slots, *row), dtype, dev), slots, _whole(state_out, "state_out", (slots, *row), dtype, dev))
+
+
+def mebptt_conv_step(desc: mebptt_conv_desc, x, weight, bias, state_in, index, y, state_out, stream: Optional[int] = None) -> None:
+    """One token: x, y [B, C]; state_in, state_out [slots, taps - 1, C] (one tensor or two); index [B] int32 names every sequence's
+    slot, None: its own number."""
+    import torch
+    dev, T = x.device, _torch_dtype(desc.dtype)
+    px, ldx = _rows(x, "x", desc.B, desc.C, T, dev)
+    py, ldy = _rows(y, "y", desc.B, desc.C, T, dev)
+    pin, slots, pout = _pool(state_in, state_out, (desc.taps - 1, desc.C), T, dev, desc.taps > 1)
+    _check(lib().mebptt_conv_step(C.byref(desc), px, ldx, *_conv_params(desc, weight, bias, dev), pin, slots,
+                                  _whole(index, "index", (desc.B,), torch.int32, dev, True), py, ldy, pout, _stream(stream)))
+
+
+def make_scan_desc(t: int, B: int, D: int, N: int, G: int, dtype: int, softplus: int = 1, stretch: int = 64) -> mebptt_scan_desc:
+    return mebptt_scan_desc(t, B, D, N, G, dtype, softplus, stretch)
+
+
+def mebptt_scan_state_bytes(desc: mebptt_scan_desc) -> int:
+    return lib().mebptt_scan_state_bytes(C.byref(desc))
+
+
+def mebptt_scan_workspace_bytes(desc: mebptt_scan_desc, backward: bool) -> int:
+    return lib().mebptt_scan_workspace_bytes(C.byref(desc), 1 if backward else 0)
+
+
+def _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dev) -> mebptt_scan_inputs:
+    import torch
+    T, f32, D, N = _torch_dtype(desc.dtype), torch.float32, desc.D, desc.N
+    seq = lambda t, name, c, optional=False: _seq(t, name, desc.t, desc.B, c, T, dev, optional)  # noqa: E731
+    return mebptt_scan_inputs(seq(u, "u", D), seq(delta, "delta", D), seq(z, "z", D, True), seq(Bm, "Bm", desc.G * N),
+                              seq(Cm, "Cm", desc.G * N), _whole(A, "A", (D, N), f32, dev), _whole(skip, "skip", (D,), f32, dev, True),
+                              _whole(delta_bias, "delta_bias", (D,), f32, dev, True),
+                              _whole(lengths, "lengths", (desc.B,), torch.int32, dev, True),
+                              _whole(h0, "h0", (desc.B, D, N), f32, dev, True))
+
+
+def mebptt_scan_forward(desc: mebptt_scan_desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, y, h_out=None, states=None,
+                        workspace=None, stream: Optional[int] = None) -> None:
+    """Selective scan.  u, delta, z, y [t, B, D]; Bm, Cm [t, B, G N]; A [D, N]; h0, h_out [B, D, N]; `states` (uint8) keeps what a
+    backward call needs."""
+    import torch
+    dev = u.device
+    given = _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dev)
+    _check(lib().mebptt_scan_forward(C.byref(desc), C.byref(given), _seq(y, "y", desc.t, desc.B, desc.D, _torch_dtype(desc.dtype), dev),
+                                     _whole(h_out, "h_out", (desc.B, desc.D, desc.N), torch.float32, dev, True),
+                                     *_room(states, "states", dev), *_room(workspace, "workspace", dev), _stream(stream)))
+
+
+def mebptt_scan_backward(desc: mebptt_scan_desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dy, dh_out, states, du, ddelta,
+                         dA, dB, dC, dskip, dz, ddelta_bias, dh0, workspace, stream: Optional[int] = None) -> None:
+    import torch
+    dev, T, f32 = u.device, _torch_dtype(desc.dtype), torch.float32
+    D, N, state = desc.D, desc.N, (desc.B, desc.D, desc.N)
+    given = _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dev)
+    seq = lambda t, name, c, optional=False: _seq(t, name, desc.t, desc.B, c, T, dev, optional)  # noqa: E731
+    grads = mebptt_scan_grads(seq(du, "du", D), seq(ddelta, "ddelta", D), seq(dz, "dz", D, z is None), seq(dB, "dB", desc.G * N),
+                              seq(dC, "dC", desc.G * N), _whole(dA, "dA", (D, N), f32, dev), _whole(dskip, "dskip", (D,), f32, dev, True),
+                              _whole(ddelta_bias, "ddelta_bias", (D,), f32, dev, True), _whole(dh0, "dh0", state, f32, dev, True))
+    _check(lib().mebptt_scan_backward(C.byref(desc), C.byref(given), seq(dy, "dy", D), _whole(dh_out, "dh_out", state, f32, dev, True),
+                                      *_room(states, "states", dev), C.byref(grads), *_room(workspace, "workspace", dev),
+                                      _stream(stream)))
+
+
+def mebptt_scan_step(desc: mebptt_scan_desc, u, delta, A, Bm, Cm, skip, z, delta_bias, state_in, index, y, state_out,
+                     stream: Optional[int] = None) -> None:
+    """One token: u, delta, z, y [B, D]; Bm, Cm [B, G N]; state_in, state_out [slots, D, N] float32 (one tensor or two); index as
+    in mebptt_conv_step."""
+    import torch
+    dev = u.device
+    one = lambda t: None if t is None else t.unsqueeze(0)  # noqa: E731
+    given = _scan_inputs(desc, one(u), one(delta), A, one(Bm), one(Cm), skip, one(z), delta_bias, None, None, dev)
+    pin, slots, pout = _pool(state_in, state_out, (desc.D, desc.N), torch.float32, dev, True)
+    _check(lib().mebptt_scan_step(C.byref(desc), C.byref(given), pin, slots, _whole(index, "index", (desc.B,), torch.int32, dev, True),
+                                  _seq(one(y), "y", 1, desc.B, desc.D, _torch_dtype(desc.dtype), dev), pout, _stream(stream)))

@@ -83,7 +83,7 @@ __device__ inline void store(__bf16* p, const float (&v)[V]) {
   }
 }
 
-__device__ inline float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
+__device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }   // within two units in the last place
 
 // ---- sums ------------------------------------------------------------------------------------------
 

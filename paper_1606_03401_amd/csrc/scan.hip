@@ -36,6 +36,8 @@ struct Forward {
   const float* h0;
   float *h_out, *states;
   int stretch;
+  int chunk, chunks;               // steps per chunk, a multiple of a block's
+  float *starts, *sums;            // [chunks][B][D][N], the first left out; [chunks][B][D]
 };
 
 template <typename T>
@@ -43,15 +45,31 @@ __device__ inline float at(const Seq& q, int64_t s, int64_t b, int64_t c) { retu
 template <typename T>
 __device__ inline void put(const SeqOut& q, int64_t s, int64_t b, int64_t c, float v) { ((T*)q.p)[s * q.t + b * q.b + c] = (T)v; }
 
+// The same with an address in two parts: uniform over the wave, and a lane's own, at most seven rows in bytes.
+template <typename T>
+__device__ inline unsigned lane_bytes(int64_t stride, int row, int c) { return (unsigned)((row * stride + c) * (int64_t)sizeof(T)); }
+__device__ inline unsigned opaque(unsigned v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+template <typename T>
+__device__ inline float elem(const T* base, unsigned bytes) { return (float)*reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes); }
+template <typename T>
+__device__ inline void set_elem(T* base, unsigned bytes, float v) { *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes) = (T)v; }
+
 __device__ inline int length_of(const int32_t* lengths, int b, int t) { return lengths ? min(max(lengths[b], 0), t) : t; }
 
-// log(1 + e^x); small values keep their relative accuracy, steps of a thousandth being what such a model starts with.
-__device__ inline float softplus_of(float x) { return fmaxf(x, 0.0f) + log1pf(__expf(-fabsf(x))); }
+// log(1 + e^x).  Small values keep their relative accuracy, steps of a thousandth being what such a model starts with: what 1 + e lost of e is
+// added to the logarithm of the sum.
+__device__ inline float softplus_of(float x) {
+  const float e = __expf(-fabsf(x)), w = 1.0f + e;
+  return fmaxf(x, 0.0f) + (__builtin_amdgcn_logf(w) * 0.6931471805599453f + (e - (w - 1.0f)));
+}
 
 // Sum over the NL lanes that share a channel, in every one of them.
 template <int CTRL>
 __device__ inline float dpp_add(float v) {
-  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+  return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 template <int NL>
 __device__ inline float lanes_sum(float v) {
@@ -82,121 +100,238 @@ struct ForwardShape {
   static constexpr int NP = NB * NL;                                  // N rounded up
   static constexpr int TS = NL == 1 || NL == 8 ? 8 : NL == 16 ? 4 : 16;   // steps per block
   static constexpr int ITEMS = (TS * CH + WAVE - 1) / WAVE;           // (step, channel) pairs per lane
-  static constexpr int SHARED = (2 * TS * NP + WAVE - 1) / WAVE;      // values of B and C per lane
+  static constexpr int SHARED = (TS * NP + WAVE - 1) / WAVE;          // values of B, and of C, per lane
 };
 
-template <typename T, int NL>
+// One wave's channels over a chunk of steps.  ENDS: only the state at the chunk's end (from a start of zeros, the first chunk's
+// apart) and the sum of w, for the chunks after it.
+//
+// Addresses are a uniform part, advanced per block and per pair, and a lane's own 32 bits.
+template <typename T, int NL, bool ENDS>
 __global__ __launch_bounds__(WAVE) void scan_forward_kernel(Forward p) {
   using S = ForwardShape<NL>;
   constexpr int CH = S::CH, TS = S::TS, NP = S::NP, CPL = S::CPL;
-  __shared__ __align__(16) float wu[TS][CH][2];      // w and w u of a block; y takes w's place
-  __shared__ __align__(16) float bc[TS][2][NP];
+  constexpr int WIDE = CH > WAVE ? CH / WAVE : 1;                      // pairs of one step per lane
+  __shared__ __align__(16) float wu[TS][CH][2];                        // w and w u of a block
+  __shared__ __align__(16) float sb[TS][NP], sc[TS][NP];
+  __shared__ __align__(16) float sy[TS][CH];
   const Scan& in = p.in;
-  const int lane = threadIdx.x, b = blockIdx.y;
+  const int lane = threadIdx.x, b = blockIdx.y, chunk = blockIdx.z;
   const int group = blockIdx.x / in.tiles, per = in.D / in.G;
   const int c0 = group * per + (blockIdx.x % in.tiles) * CH;           // first channel
   const int nch = min(CH, group * per + per - c0);
   const int len = length_of(in.lengths, b, in.t);
+  const int begin = chunk * p.chunk, end = min(in.t, begin + p.chunk);
   const int q = lane % NL, cl = lane / NL * CPL;                       // this lane's states NB q .. and channels cl, cl + 1
 
-  float h[CPL][NB], A2[CPL][NB];
+  float h[CPL][NB], A2[CPL][NB], sum_w[CPL] = {};
+  const float* start = chunk == 0 ? p.h0 : ENDS ? nullptr : p.starts + (int64_t)chunk * in.B * in.D * in.N;
 #pragma unroll
   for (int j = 0; j < CPL; ++j) {
     const int64_t d = min(c0 + cl + j, in.D - 1);
     load_states(in.A + d * in.N, q * NB, in.N, A2[j]);
-    if (p.h0) load_states(p.h0 + ((int64_t)b * in.D + d) * in.N, q * NB, in.N, h[j]);
+    if (start) load_states(start + ((int64_t)b * in.D + d) * in.N, q * NB, in.N, h[j]);
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       A2[j][n] *= LOG2E;
-      if (!p.h0) h[j][n] = 0.0f;
+      if (!start) h[j][n] = 0.0f;
     }
   }
 
-  float ru[S::ITEMS], rd[S::ITEMS], rz[S::ITEMS], rb[S::SHARED];
+  // the pairs of a lane: step i * ROWS + row (WIDE: i / WIDE), channel ch (+ 64 for every second one)
+  constexpr int ROWS = CH < WAVE ? WAVE / CH : 1;
+  const int row = CH < WAVE ? lane / CH : 0, ch = lane % CH;
+  const bool pair = TS * CH >= WAVE || lane < TS * CH;
+  auto step_of = [&](int i) { return i / WIDE * ROWS; };              // uniform part
+  auto channel_of = [&](int i) { return i % WIDE * WAVE; };
+  float bias[WIDE], skip[WIDE];
+#pragma unroll
+  for (int i = 0; i < WIDE; ++i) {
+    const int d = min(c0 + ch + i * WAVE, in.D - 1);
+    bias[i] = in.bias ? in.bias[d] : 0.0f;
+    skip[i] = in.skip ? in.skip[d] : 0.0f;
+  }
+  const unsigned ou_ = lane_bytes<T>(in.u.t, row, ch), od_ = lane_bytes<T>(in.delta.t, row, ch), oz_ = lane_bytes<T>(in.z.t, row, ch),
+                 oy_ = lane_bytes<T>(p.y.t, row, ch);
+  const int srow = lane / NP, sn = lane % NP;
+  const bool shared = TS * NP >= WAVE || lane < TS * NP;
+  const int sk = min(sn, in.N - 1);
+  const unsigned ob_ = lane_bytes<T>(in.Bm.t, srow, sk), oc_ = lane_bytes<T>(in.Cm.t, srow, sk);
   const int64_t gn = (int64_t)group * in.N;
+  const T* const pu = (const T*)in.u.p + b * in.u.b + c0;
+  const T* const pd = (const T*)in.delta.p + b * in.delta.b + c0;
+  const T* const pz = (const T*)in.z.p + b * in.z.b + c0;
+  const T* const pb = (const T*)in.Bm.p + b * in.Bm.b + gn;
+  const T* const pc = (const T*)in.Cm.p + b * in.Cm.b + gn;
+  T* const py = (T*)p.y.p + b * p.y.b + c0;
+
+  // The next block's inputs, fetched while a block is worked on.  A whole block (all its steps within the sequence, all its channels
+  // there) needs no masks; which it is, is the same for the whole wave.
+  float ru[S::ITEMS], rd[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
+  auto whole = [&](int s0) { return TS * CH >= WAVE && TS * NP >= WAVE && s0 + TS <= min(len, end) && nch == CH; };
   auto fetch = [&](int s0) {
+    // (opaque, or the sums of the parts are formed ahead in registers)
+    const unsigned ou = opaque(ou_), od = opaque(od_), oz = opaque(oz_), ob = opaque(ob_), oc = opaque(oc_);
+    const T *au = pu + s0 * in.u.t, *ad = pd + s0 * in.delta.t, *az = pz + s0 * in.z.t, *ab = pb + s0 * in.Bm.t, *ac = pc + s0 * in.Cm.t;
+    const int64_t iu = ROWS * in.u.t, id = ROWS * in.delta.t, iz = ROWS * in.z.t, ib = WAVE / NP * in.Bm.t, ic = WAVE / NP * in.Cm.t;
+    if (whole(s0)) {
 #pragma unroll
-    for (int i = 0; i < S::ITEMS; ++i) {
-      const int k = i * WAVE + lane, s = s0 + k / CH, c = k % CH;
-      const bool live = k < TS * CH && s < len && c < nch;
-      ru[i] = live ? at<T>(in.u, s, b, c0 + c) : 0.0f;
-      rd[i] = live ? at<T>(in.delta, s, b, c0 + c) : 0.0f;
-      rz[i] = live && in.z.p ? at<T>(in.z, s, b, c0 + c) : 0.0f;
-    }
+      for (int i = 0; i < S::ITEMS; ++i) {
+        ru[i] = elem(au + channel_of(i), ou);
+        rd[i] = elem(ad + channel_of(i), od);
+        if (i % WIDE == WIDE - 1) au += iu, ad += id;
+      }
+      if (!ENDS && in.z.p) {
 #pragma unroll
-    for (int i = 0; i < S::SHARED; ++i) {
-      const int k = i * WAVE + lane, s = s0 + k / (2 * NP), n = k % NP;
-      const bool live = k < 2 * TS * NP && s < len && n < in.N;
-      rb[i] = !live ? 0.0f : k / NP % 2 ? at<T>(in.Cm, s, b, gn + n) : at<T>(in.Bm, s, b, gn + n);
+        for (int i = 0; i < S::ITEMS; ++i) {
+          rz[i] = elem(az + channel_of(i), oz);
+          if (i % WIDE == WIDE - 1) az += iz;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < S::SHARED; ++i) {
+        rb[i] = elem(ab, ob);
+        ab += ib;
+        if (!ENDS) rc[i] = elem(ac, oc);
+        ac += ic;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i) {
+        const int c = channel_of(i);
+        ru[i] = rd[i] = rz[i] = 0.0f;
+        if (pair && s0 + step_of(i) + row < len && ch + c < nch) {
+          ru[i] = elem(au + c, ou);
+          rd[i] = elem(ad + c, od);
+          if (!ENDS && in.z.p) rz[i] = elem(az + c, oz);
+        }
+        if (i % WIDE == WIDE - 1) au += iu, ad += id, az += iz;
+      }
+#pragma unroll
+      for (int i = 0; i < S::SHARED; ++i) {
+        rb[i] = rc[i] = 0.0f;
+        if (shared && s0 + i * (WAVE / NP) + srow < len) {
+          rb[i] = elem(ab, ob);
+          if (!ENDS) rc[i] = elem(ac, oc);
+        }
+        ab += ib;
+        ac += ic;
+      }
     }
   };
-  fetch(0);
-  for (int s0 = 0; s0 < in.t; s0 += TS) {
+#pragma unroll
+  for (int i = 0; i < S::ITEMS; ++i) rz[i] = 0.0f;
+  const int stop = ENDS ? min(end, len) : end;                         // (beyond its length a sequence's state stays as it is)
+  if (begin < stop) fetch(begin);
+  for (int s0 = begin; s0 < stop; s0 += TS) {
+    const bool all = whole(s0);
     float cu[S::ITEMS], cz[S::ITEMS];
 #pragma unroll
     for (int i = 0; i < S::ITEMS; ++i) {
-      const int k = i * WAVE + lane, s = s0 + k / CH, c = k % CH;
       cu[i] = ru[i];
       cz[i] = rz[i];
-      float w = rd[i] + (in.bias ? in.bias[min(c0 + c, in.D - 1)] : 0.0f);
-      if (in.softplus) w = softplus_of(w);
-      if (!(s < len && c < nch)) w = 0.0f;             // a step beyond the sequence: h stays as it is
-      if (k < TS * CH) {
-        wu[k / CH][c][0] = w;
-        wu[k / CH][c][1] = w * ru[i];
-      }
+      rd[i] += bias[i % WIDE];
     }
+    if (in.softplus) {
 #pragma unroll
-    for (int i = 0; i < S::SHARED; ++i) {
-      const int k = i * WAVE + lane;
-      if (k < 2 * TS * NP) (&bc[0][0][0])[k] = rb[i];
+      for (int i = 0; i < S::ITEMS; ++i) rd[i] = softplus_of(rd[i]);
+    }
+    if (!all) {
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i)      // a step beyond the sequence
+        if (!(s0 + step_of(i) + row < len && ch + channel_of(i) < nch)) rd[i] = 0.0f;
+    }
+    if (pair) {
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i) *reinterpret_cast<float2*>(&wu[step_of(i) + row][ch + channel_of(i)][0]) = float2{rd[i], rd[i] * cu[i]};
+    }
+    if (shared) {
+#pragma unroll
+      for (int i = 0; i < S::SHARED; ++i) {
+        sb[i * (WAVE / NP) + srow][sn] = sn < in.N ? rb[i] : 0.0f;
+        if (!ENDS) sc[i * (WAVE / NP) + srow][sn] = sn < in.N ? rc[i] : 0.0f;
+      }
     }
     __syncthreads();
-    if (s0 + TS < in.t) fetch(s0 + TS);
-#pragma unroll 4
-    for (int s = 0; s < TS; ++s) {
-      if (p.states && (s0 + s) % p.stretch == 0 && s0 + s < in.t) {
+    if (s0 + TS < stop) fetch(s0 + TS);
+    if (!ENDS && p.states && s0 % p.stretch == 0) {
 #pragma unroll
-        for (int j = 0; j < CPL; ++j)
-          if (cl + j < nch)
-            store_states(p.states + (((int64_t)((s0 + s) / p.stretch) * in.B + b) * in.D + c0 + cl + j) * in.N, q * NB, in.N, h[j]);
-      }
+      for (int j = 0; j < CPL; ++j)
+        if (cl + j < nch)
+          store_states(p.states + (((int64_t)(s0 / p.stretch) * in.B + b) * in.D + c0 + cl + j) * in.N, q * NB, in.N, h[j]);
+    }
+#pragma unroll
+    for (int s = 0; s < TS; ++s) {
       const f32x4 w = *reinterpret_cast<const f32x4*>(&wu[s][cl][0]);
-      const f32x4 vb = *reinterpret_cast<const f32x4*>(&bc[s][0][q * NB]), vc = *reinterpret_cast<const f32x4*>(&bc[s][1][q * NB]);
+      const f32x4 vb = *reinterpret_cast<const f32x4*>(&sb[s][q * NB]);
+      f32x4 vc = {};
+      if constexpr (!ENDS) vc = *reinterpret_cast<const f32x4*>(&sc[s][q * NB]);
       float y[CPL];
 #pragma unroll
       for (int j = 0; j < CPL; ++j) {
-        y[j] = 0.0f;
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const float a = __builtin_amdgcn_exp2f(w[2 * j] * A2[j][n]);
           h[j][n] = a * h[j][n] + w[2 * j + 1] * vb[n];
-          y[j] += h[j][n] * vc[n];
+          if constexpr (!ENDS) y[j] = n ? y[j] + h[j][n] * vc[n] : h[j][n] * vc[n];
         }
-        y[j] = lanes_sum<NL>(y[j]);
+        if constexpr (ENDS) sum_w[j] += w[2 * j];
+        else y[j] = lanes_sum<NL>(y[j]);
       }
-      if (q == 0) {
-#pragma unroll
-        for (int j = 0; j < CPL; ++j) wu[s][cl + j][0] = y[j];
-      }
+      // every lane of a channel writes the same value to the same place
+      if constexpr (!ENDS) *reinterpret_cast<float2*>(&sy[s][cl]) = float2{y[0], y[1]};
     }
     __syncthreads();
+    if constexpr (!ENDS) {
+      float y[S::ITEMS];
+      if (pair) {
 #pragma unroll
-    for (int i = 0; i < S::ITEMS; ++i) {
-      const int k = i * WAVE + lane, s = s0 + k / CH, c = k % CH;
-      if (k < TS * CH && s < in.t && c < nch) {
-        float y = wu[k / CH][c][0];
-        if (in.skip) y += in.skip[c0 + c] * cu[i];
-        if (in.z.p) y *= cz[i] * sigmoid(cz[i]);
-        put<T>(p.y, s, b, c0 + c, s < len ? y : 0.0f);
+        for (int i = 0; i < S::ITEMS; ++i) y[i] = sy[step_of(i) + row][ch + channel_of(i)] + skip[i % WIDE] * cu[i];
+      }
+      if (in.z.p) {
+#pragma unroll
+        for (int i = 0; i < S::ITEMS; ++i) y[i] *= cz[i] * sigmoid(cz[i]);
+      }
+      T* ay = py + s0 * p.y.t;
+      const unsigned oy = opaque(oy_);
+      const int64_t iy = ROWS * p.y.t;
+      if (all) {
+#pragma unroll
+        for (int i = 0; i < S::ITEMS; ++i) {
+          set_elem(ay + channel_of(i), oy, y[i]);
+          if (i % WIDE == WIDE - 1) ay += iy;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::ITEMS; ++i) {
+          const int s = s0 + step_of(i) + row;
+          if (pair && s < end && ch + channel_of(i) < nch) set_elem(ay + channel_of(i), oy, s < len ? y[i] : 0.0f);
+          if (i % WIDE == WIDE - 1) ay += iy;
+        }
       }
     }
-    __syncthreads();
   }
-  if (p.h_out) {
+  float* last = ENDS ? p.starts + (int64_t)(chunk + 1) * in.B * in.D * in.N : chunk + 1 == p.chunks ? p.h_out : nullptr;
 #pragma unroll
-    for (int j = 0; j < CPL; ++j)
-      if (cl + j < nch) store_states(p.h_out + ((int64_t)b * in.D + c0 + cl + j) * in.N, q * NB, in.N, h[j]);
+  for (int j = 0; j < CPL; ++j) {
+    if (cl + j >= nch) continue;
+    const int64_t d = (int64_t)b * in.D + c0 + cl + j;
+    if (last) store_states(last + d * in.N, q * NB, in.N, h[j]);
+    if (ENDS && q == 0) p.sums[(int64_t)chunk * in.B * in.D + d] = sum_w[j];
+  }
+}
+
+// starts[c] holds the state that chunk c - 1 reached from zeros; adds what it started from, decayed by exp(A sum w).
+__global__ __launch_bounds__(256) void scan_join_kernel(float* starts, const float* sums, const float* A, int64_t BD, int D, int N, int chunks) {
+  const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (k >= BD * N) return;
+  const int64_t bd = k / N;
+  const float a2 = A[(bd % D) * N + k % N] * LOG2E;
+  float h = starts[BD * N + k];
+#pragma unroll 8
+  for (int c = 2; c < chunks; ++c) {
+    h = starts[c * BD * N + k] + __builtin_amdgcn_exp2f(a2 * sums[(c - 1) * BD + bd]) * h;
+    starts[c * BD * N + k] = h;
   }
 }
 
@@ -537,15 +672,21 @@ int check_stretch(const mebptt_scan_desc* d) {
   const int s = d->stretch;
   return s == 16 || s == 32 || s == 64 || s == 128 || s == 256 ? MEBPTT_OK : set_error(MEBPTT_EINVAL, "stretch must be 16, 32, 64, 128 or 256");
 }
+// A lane's part of an address is 32 bits, of up to seven rows of four bytes.
+bool stride_fits(const mebptt_seq& s) { return s.stride_t >= 0 && s.stride_t <= (1 << 26); }
 int check_inputs(const mebptt_scan_desc* d, const mebptt_scan_inputs* in) {
   if (!in) return set_error(MEBPTT_EINVAL, "inputs are NULL");
   if (!in->A) return set_error(MEBPTT_EINVAL, "A is NULL");
   if (d->t && d->B && (!in->u.data || !in->delta.data || !in->Bm.data || !in->Cm.data))
     return set_error(MEBPTT_EINVAL, "u, delta, B and C are required");
+  if (d->t > 1)
+    for (const mebptt_seq* q : {&in->u, &in->delta, &in->z, &in->Bm, &in->Cm})
+      if (q->data && !stride_fits(*q)) return set_error(MEBPTT_EINVAL, "stride_t must be 0 .. 2^26");
   return MEBPTT_OK;
 }
 int check_out(const mebptt_scan_desc* d, const mebptt_seq& s, int64_t channels, const char* what) {
   if (d->t && d->B && !s.data) return set_error(MEBPTT_EINVAL, "%s is NULL", what);
+  if (d->t > 1 && !stride_fits(s)) return set_error(MEBPTT_EINVAL, "stride_t must be 0 .. 2^26");
   if (!rows_apart(s, d->t, d->B, channels)) return set_error(MEBPTT_EINVAL, "rows of %s overlap", what);
   return MEBPTT_OK;
 }
@@ -553,6 +694,29 @@ Scan scan_of(const mebptt_scan_desc* d, const mebptt_scan_inputs* in) {
   return {in_seq(in->u), in_seq(in->delta), in_seq(in->z), in_seq(in->Bm), in_seq(in->Cm), in->A, in->skip, in->delta_bias, in->lengths,
           d->t, d->B, d->D, d->N, d->G, d->softplus, 0};
 }
+
+// How many chunks the time axis is cut into: enough workgroups for two waves on each of the 1024 SIMDs, in chunks of at least MIN_CHUNK steps.  The
+// chunks' ends are computed first, which is most of the work once more, so nothing is cut that fills the chip by itself.
+constexpr int MIN_CHUNK = 64;
+int64_t forward_tiles(const mebptt_scan_desc* d) {
+  int64_t tiles = 0;
+  with_lanes(d->N, [&](auto l) {
+    tiles = ceil_div(d->D / d->G, ForwardShape<decltype(l)::value>::CH);
+    return 0;
+  });
+  return tiles;
+}
+struct Cut { int chunk, chunks; };
+Cut cut_of(const mebptt_scan_desc* d, int64_t workgroups, int unit) {
+  const int64_t t = std::max(d->t, 1), want = ceil_div(2048, std::max<int64_t>(1, workgroups));
+  int64_t chunk = std::max<int64_t>(MIN_CHUNK, ceil_div(t, want));
+  chunk = ceil_div(chunk, unit) * unit;
+  const int64_t chunks = ceil_div(t, chunk);
+  return workgroups >= 1024 || chunks < 2 ? Cut{(int)(ceil_div(t, unit) * unit), 1} : Cut{(int)chunk, (int)chunks};
+}
+Cut forward_cut(const mebptt_scan_desc* d) { return cut_of(d, forward_tiles(d) * d->G * d->B, 16); }
+size_t starts_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * d->N * sizeof(float)); }
+size_t sums_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * sizeof(float)); }
 
 int64_t back_tiles(const mebptt_scan_desc* d) {
   int64_t tiles = 0;
@@ -586,7 +750,9 @@ size_t mebptt_scan_state_bytes(const mebptt_scan_desc* d) {
 
 size_t mebptt_scan_workspace_bytes(const mebptt_scan_desc* d, int32_t backward) {
   if (check(d) != MEBPTT_OK) return 0;
-  return backward ? bc_bytes(d) + a_bytes(d) : 0;
+  if (backward) return bc_bytes(d) + a_bytes(d);
+  const int chunks = forward_cut(d).chunks;
+  return starts_bytes(d, chunks) + sums_bytes(d, chunks);
 }
 
 int mebptt_scan_forward(const mebptt_scan_desc* d, const mebptt_scan_inputs* in, mebptt_seq y, float* h_out, void* states,
@@ -601,14 +767,26 @@ int mebptt_scan_forward(const mebptt_scan_desc* d, const mebptt_scan_inputs* in,
   }
   if ((rc = check_workspace(workspace, workspace_bytes, mebptt_scan_workspace_bytes(d, 0)))) return rc;
   if (d->B == 0) return MEBPTT_OK;
-  Forward p = {scan_of(d, in), out_seq(y), in->h0, h_out, (float*)states, d->stretch};
+  const Cut cut = forward_cut(d);
+  Forward p = {scan_of(d, in), out_seq(y), in->h0, h_out, (float*)states, d->stretch, cut.chunk, cut.chunks,
+               (float*)workspace, (float*)((char*)workspace + starts_bytes(d, cut.chunks))};
+  hipStream_t s = (hipStream_t)stream;
   return with_lanes(d->N, [&](auto l) {
     constexpr int NL = decltype(l)::value;
     p.in.tiles = (int)ceil_div(d->D / d->G, ForwardShape<NL>::CH);
-    const dim3 grid((unsigned)(p.in.tiles * d->G), d->B);
-    if (d->dtype == MEBPTT_FP32) scan_forward_kernel<float, NL><<<grid, WAVE, 0, (hipStream_t)stream>>>(p);
-    else scan_forward_kernel<__bf16, NL><<<grid, WAVE, 0, (hipStream_t)stream>>>(p);
-    return launched("mebptt_scan_forward");
+    const unsigned wide = (unsigned)(p.in.tiles * d->G);
+    auto go = [&](auto elem) {
+      using T = decltype(elem);
+      if (cut.chunks > 1) {
+        scan_forward_kernel<T, NL, true><<<dim3(wide, d->B, cut.chunks - 1), WAVE, 0, s>>>(p);
+        const int64_t BD = (int64_t)d->B * d->D;
+        if (cut.chunks > 2)
+          scan_join_kernel<<<(unsigned)ceil_div(BD * d->N, 256), 256, 0, s>>>(p.starts, p.sums, in->A, BD, d->D, d->N, cut.chunks);
+      }
+      scan_forward_kernel<T, NL, false><<<dim3(wide, d->B, cut.chunks), WAVE, 0, s>>>(p);
+      return launched("mebptt_scan_forward");
+    };
+    return d->dtype == MEBPTT_FP32 ? go(float{}) : go(__bf16{});
   });
 }
 

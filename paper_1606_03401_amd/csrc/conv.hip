@@ -387,7 +387,9 @@ int mebptt_conv_backward(const mebptt_conv_desc* d, mebptt_seq x, const float* w
   else
     rc = vec ? backward<__bf16, BACK_V>(p, d->taps, parts, s) : backward<__bf16, 1>(p, d->taps, parts, s);
   if (rc) return rc;
-  return sum_parts_split((const float*)workspace, parts, (int64_t)d->C * d->taps, dweight, d->C, dbias, s);
+  const int64_t cols[2] = {(int64_t)d->C * d->taps, d->C};
+  float* const outs[2] = {dweight, dbias};
+  return sum_parts((const float*)workspace, parts, 2, cols, outs, s);
 }
 
 int mebptt_conv_step(const mebptt_conv_desc* d, const void* x, int64_t ldx, const float* weight, const float* bias,

@@ -303,25 +303,35 @@ int check_ld(const void* p, int64_t ld, int width, const char* what) {
   return p && ld < width ? set_error(MEBPTT_EINVAL, "row stride of %s is below the width", what) : MEBPTT_OK;
 }
 
-// [P][cols + cols2] -> [cols], [cols2]: 32 columns per workgroup, 32 threads per column, whose sums meet in LDS.
-constexpr int SUM_COLS = 32, SUM_ROWS = 32;
-__global__ __launch_bounds__(SUM_COLS* SUM_ROWS) void sum_parts_kernel(const float* parts, int64_t P, int64_t cols, float* out,
-                                                                            int64_t cols2, float* out2) {
-  __shared__ float lds[SUM_ROWS][SUM_COLS + 1];
+// [P][all] -> three outputs: 16 columns per workgroup, 64 threads per column, whose sums meet in LDS.
+constexpr int SUM_COLS = 16, SUM_ROWS = 64;
+struct Sum {
+  const float* parts;
+  int64_t P, all, end0, end1;
+  float* outs[3];
+};
+__global__ __launch_bounds__(SUM_COLS* SUM_ROWS) void sum_parts_kernel(Sum p) {
+  __shared__ float lds[SUM_ROWS][SUM_COLS];
   const int x = threadIdx.x % SUM_COLS, y = threadIdx.x / SUM_COLS;
-  const int64_t all = cols + cols2;
-  for (int64_t c0 = (int64_t)blockIdx.x * SUM_COLS; c0 < all; c0 += (int64_t)gridDim.x * SUM_COLS) {
+  for (int64_t c0 = (int64_t)blockIdx.x * SUM_COLS; c0 < p.all; c0 += (int64_t)gridDim.x * SUM_COLS) {
     const int64_t c = c0 + x;
     float s = 0.0f;
-    if (c < all)
-      for (int64_t p = y; p < P; p += SUM_ROWS) s += parts[p * all + c];
+    if (c < p.all) {
+#pragma unroll 8
+      for (int64_t i = y; i < p.P; i += SUM_ROWS) s += p.parts[i * p.all + c];
+    }
     lds[y][x] = s;
     __syncthreads();
-    if (y == 0 && c < all) {
+    if (y < 4) {
 #pragma unroll
-      for (int i = 1; i < SUM_ROWS; ++i) s += lds[i][x];
-      if (c < cols) out[c] = s;
-      else if (out2) out2[c - cols] = s;
+      for (int i = 4; i < SUM_ROWS; i += 4) s += lds[i + y][x];
+      lds[y][x] = s;
+    }
+    __syncthreads();
+    if (y == 0 && c < p.all) {
+      s = lds[0][x] + lds[1][x] + lds[2][x] + lds[3][x];
+      float* out = c < p.end0 ? p.outs[0] : c < p.end1 ? p.outs[1] : p.outs[2];
+      if (out) out[c - (c < p.end0 ? 0 : c < p.end1 ? p.end0 : p.end1)] = s;
     }
     __syncthreads();
   }
@@ -329,10 +339,13 @@ __global__ __launch_bounds__(SUM_COLS* SUM_ROWS) void sum_parts_kernel(const flo
 
 }  // namespace
 
-int mebptt::ops::sum_parts_split(const float* parts, int64_t P, int64_t cols, float* out, int64_t cols2, float* out2, hipStream_t stream) {
-  if (cols + cols2 <= 0) return MEBPTT_OK;
-  const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(cols + cols2, SUM_COLS), 1 << 20);
-  sum_parts_kernel<<<grid, SUM_COLS * SUM_ROWS, 0, stream>>>(parts, P, cols, out, cols2, out2);
+int mebptt::ops::sum_parts(const float* parts, int64_t P, int n, const int64_t* cols, float* const* outs, hipStream_t stream) {
+  Sum p = {parts, P, cols[0], cols[0], cols[0], {outs[0], nullptr, nullptr}};
+  if (n > 1) p.outs[1] = outs[1], p.all = p.end1 = cols[0] + cols[1];
+  if (n > 2) p.outs[2] = outs[2], p.all += cols[2];
+  if (p.all <= 0) return MEBPTT_OK;
+  const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(p.all, SUM_COLS), 1 << 20);
+  sum_parts_kernel<<<grid, SUM_COLS * SUM_ROWS, 0, stream>>>(p);
   return launched("sum of parts");
 }
 
@@ -395,7 +408,9 @@ int mebptt_norm_backward(const mebptt_norm_desc* d, const void* r, int64_t ldr, 
       rc = d->residual_dtype == MEBPTT_FP32 ? backward<__bf16, float>(p, vec, groups, s) : backward<__bf16, __bf16>(p, vec, groups, s);
     if (rc) return rc;
   }
-  return dweight ? sum_parts((const float*)workspace, groups, d->width, dweight, s) : MEBPTT_OK;
+  if (!dweight) return MEBPTT_OK;
+  const int64_t cols = d->width;
+  return sum_parts((const float*)workspace, groups, 1, &cols, &dweight, s);
 }
 
 }  // extern "C"

@@ -13,6 +13,7 @@
 namespace mebptt {
 namespace ops {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
@@ -37,6 +38,10 @@ __device__ inline void load(const float* p, float (&v)[V]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[e + i] = x[i];
     }
+  } else if constexpr (V == 2) {
+    const f32x2 x = *reinterpret_cast<const f32x2*>(p);
+    v[0] = x[0];
+    v[1] = x[1];
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = p[e];
@@ -62,6 +67,8 @@ __device__ inline void store(float* p, const float (&v)[V]) {
   if constexpr (V % 4 == 0) {
 #pragma unroll
     for (int e = 0; e < V; e += 4) *reinterpret_cast<f32x4*>(p + e) = f32x4{v[e], v[e + 1], v[e + 2], v[e + 3]};
+  } else if constexpr (V == 2) {
+    *reinterpret_cast<f32x2*>(p) = f32x2{v[0], v[1]};
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) p[e] = v[e];
@@ -138,12 +145,9 @@ inline int check_workspace(const void* workspace, size_t bytes, size_t needed) {
   return MEBPTT_OK;
 }
 
-// Sums of P partial rows in one fixed order, in a launch of their own: a row's first `cols` floats go to out, its next `cols2` to out2
-// (NULL: nowhere).
-int sum_parts_split(const float* parts, int64_t P, int64_t cols, float* out, int64_t cols2, float* out2, hipStream_t stream);
-inline int sum_parts(const float* parts, int64_t P, int64_t cols, float* out, hipStream_t stream) {
-  return sum_parts_split(parts, P, cols, out, 0, nullptr, stream);
-}
+// Sums of P partial rows in one fixed order, in a launch of their own: a row's first cols[0] floats go to outs[0], its next cols[1] to
+// outs[1], and so on (NULL: nowhere), at most three.
+int sum_parts(const float* parts, int64_t P, int n, const int64_t* cols, float* const* outs, hipStream_t stream);
 
 }  // namespace ops
 }  // namespace mebptt

@@ -30,16 +30,6 @@ struct Scan {
   int t, B, D, N, G, softplus;
   int tiles;                       // workgroups per group of channels
 };
-struct Forward {
-  Scan in;
-  SeqOut y;
-  const float* h0;
-  float *h_out, *states;
-  int stretch;
-  int chunk, chunks;               // steps per chunk, a multiple of a block's
-  float *starts, *sums;            // [chunks][B][D][N], the first left out; [chunks][B][D]
-};
-
 template <typename T>
 __device__ inline float at(const Seq& q, int64_t s, int64_t b, int64_t c) { return (float)((const T*)q.p)[s * q.t + b * q.b + c]; }
 template <typename T>
@@ -80,83 +70,101 @@ __device__ inline float lanes_sum(float v) {
   return v;
 }
 
-// NB consecutive states of a channel's N.
-__device__ inline void load_states(const float* p, int n0, int N, float (&v)[NB]) {
+// K consecutive states of a channel's N.
+template <int K>
+__device__ inline void load_states(const float* p, int n0, int N, float (&v)[K]) {
 #pragma unroll
-  for (int n = 0; n < NB; ++n) v[n] = n0 + n < N ? p[n0 + n] : 0.0f;
+  for (int n = 0; n < K; ++n) v[n] = n0 + n < N ? p[n0 + n] : 0.0f;
 }
-__device__ inline void store_states(float* p, int n0, int N, const float (&v)[NB]) {
+template <int K>
+__device__ inline void store_states(float* p, int n0, int N, const float (&v)[K]) {
 #pragma unroll
-  for (int n = 0; n < NB; ++n)
+  for (int n = 0; n < K; ++n)
     if (n0 + n < N) p[n0 + n] = v[n];
 }
 
 // ---- forward ---------------------------------------------------------------------------------------
 
-template <int NL>
+struct Forward {
+  Scan in;
+  SeqOut y;
+  const float* h0;
+  float *h_out, *states;
+  int stretch;
+  int chunk, chunks;               // steps per chunk, a multiple of a block's
+  float *starts, *sums;            // [chunks][B][D][N]: what the chunk before reached by itself; [chunks][B][D]: sum of w
+};
+
+constexpr int FORWARD_WAVES = 4;   // waves of neighbouring channels per workgroup: they share cache lines, and nothing else
+
+template <int NL_, int NB_>
 struct ForwardShape {
-  static constexpr int CPL = 2;                                       // channels per lane, which share what it reads of B and C
-  static constexpr int CH = WAVE / NL * CPL;                          // channels per workgroup of one wave
+  static constexpr int NL = NL_, NB = NB_;                            // lanes per channel, states per lane
+  static constexpr int CH = WAVE / NL;                                // channels per wave
   static constexpr int NP = NB * NL;                                  // N rounded up
-  static constexpr int TS = NL == 1 || NL == 8 ? 8 : NL == 16 ? 4 : 16;   // steps per block
+  static constexpr int TS = NL <= 8 ? 16 : 8;                         // steps per block
   static constexpr int ITEMS = (TS * CH + WAVE - 1) / WAVE;           // (step, channel) pairs per lane
   static constexpr int SHARED = (TS * NP + WAVE - 1) / WAVE;          // values of B, and of C, per lane
 };
 
-// One wave's channels over a chunk of steps.  ENDS: only the state at the chunk's end (from a start of zeros, the first chunk's
-// apart) and the sum of w, for the chunks after it.
-//
-// Addresses are a uniform part, advanced per block and per pair, and a lane's own 32 bits.
-template <typename T, int NL, bool ENDS>
-__global__ __launch_bounds__(WAVE) void scan_forward_kernel(Forward p) {
-  using S = ForwardShape<NL>;
-  constexpr int CH = S::CH, TS = S::TS, NP = S::NP, CPL = S::CPL;
-  constexpr int WIDE = CH > WAVE ? CH / WAVE : 1;                      // pairs of one step per lane
-  __shared__ __align__(16) float wu[TS][CH][2];                        // w and w u of a block
-  __shared__ __align__(16) float sb[TS][NP], sc[TS][NP];
-  __shared__ __align__(16) float sy[TS][CH];
+// What the lanes of one wave hand each other through LDS is in order by itself; the compiler has to keep it so.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// One wave's channels over a chunk of steps.  ENDS: only the state at the chunk's end (from zeros, the first chunk's from h0) and the
+// sum of w, for the chunks after it.  Addresses are a uniform part, advanced per block and per pair, and a lane's own 32 bits.
+template <typename T, typename S, bool ENDS>
+__global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forward p) {
+  constexpr int CH = S::CH, TS = S::TS, NP = S::NP, NL = S::NL, NB = S::NB;
+  struct Lds { float wu[TS][CH][2], sb[TS][NP], sc[ENDS ? 1 : TS][NP], sy[ENDS ? 1 : TS][CH]; };   // w and w u of a block, B, C, y
+  __shared__ __align__(16) Lds lds[FORWARD_WAVES];
   const Scan& in = p.in;
-  const int lane = threadIdx.x, b = blockIdx.y, chunk = blockIdx.z;
+  const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), b = blockIdx.y, chunk = blockIdx.z;
+  auto& [wu, sb, sc, sy] = lds[wave];
   const int group = blockIdx.x / in.tiles, per = in.D / in.G;
-  const int c0 = group * per + (blockIdx.x % in.tiles) * CH;           // first channel
+  const int c0 = group * per + (blockIdx.x % in.tiles * FORWARD_WAVES + wave) * CH;   // first channel
   const int nch = min(CH, group * per + per - c0);
+  if (nch <= 0) return;                                                // (waves of a workgroup never wait for each other)
   const int len = length_of(in.lengths, b, in.t);
   const int begin = chunk * p.chunk, end = min(in.t, begin + p.chunk);
-  const int q = lane % NL, cl = lane / NL * CPL;                       // this lane's states NB q .. and channels cl, cl + 1
+  const int q = lane % NL, cl = lane / NL;                             // this lane's states NB q .. and channel
+  const int64_t d = min(c0 + cl, in.D - 1), bd = (int64_t)b * in.D + d, all_states = (int64_t)in.B * in.D * in.N;
 
-  float h[CPL][NB], A2[CPL][NB], sum_w[CPL] = {};
-  const float* start = chunk == 0 ? p.h0 : ENDS ? nullptr : p.starts + (int64_t)chunk * in.B * in.D * in.N;
+  float h[NB], A2[NB], sum_w = 0.0f;
+  load_states(in.A + d * in.N, q * NB, in.N, A2);
 #pragma unroll
-  for (int j = 0; j < CPL; ++j) {
-    const int64_t d = min(c0 + cl + j, in.D - 1);
-    load_states(in.A + d * in.N, q * NB, in.N, A2[j]);
-    if (start) load_states(start + ((int64_t)b * in.D + d) * in.N, q * NB, in.N, h[j]);
+  for (int n = 0; n < NB; ++n) {
+    A2[n] *= LOG2E;
+    h[n] = 0.0f;
+  }
+  if (chunk == 0) {
+    if (p.h0) load_states(p.h0 + bd * in.N, q * NB, in.N, h);
+  } else if (!ENDS) {
+    // what the chunks before this one reached, each by itself, decayed by exp(A sum w) of those after it
+    for (int k = 1; k <= chunk; k += 8) {
+      float e[8][NB], w[8];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      A2[j][n] *= LOG2E;
-      if (!start) h[j][n] = 0.0f;
+      for (int i = 0; i < 8; ++i) {
+        const int m = min(k + i, chunk);
+        load_states(p.starts + m * all_states + bd * in.N, q * NB, in.N, e[i]);
+        w[i] = p.sums[(int64_t)(m - 1) * in.B * in.D + bd];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k + i <= chunk) {
+#pragma unroll
+          for (int n = 0; n < NB; ++n) h[n] = e[i][n] + __builtin_amdgcn_exp2f(w[i] * A2[n]) * h[n];
+        }
     }
   }
 
-  // the pairs of a lane: step i * ROWS + row (WIDE: i / WIDE), channel ch (+ 64 for every second one)
-  constexpr int ROWS = CH < WAVE ? WAVE / CH : 1;
-  const int row = CH < WAVE ? lane / CH : 0, ch = lane % CH;
-  const bool pair = TS * CH >= WAVE || lane < TS * CH;
-  auto step_of = [&](int i) { return i / WIDE * ROWS; };              // uniform part
-  auto channel_of = [&](int i) { return i % WIDE * WAVE; };
-  float bias[WIDE], skip[WIDE];
-#pragma unroll
-  for (int i = 0; i < WIDE; ++i) {
-    const int d = min(c0 + ch + i * WAVE, in.D - 1);
-    bias[i] = in.bias ? in.bias[d] : 0.0f;
-    skip[i] = in.skip ? in.skip[d] : 0.0f;
-  }
-  const unsigned ou_ = lane_bytes<T>(in.u.t, row, ch), od_ = lane_bytes<T>(in.delta.t, row, ch), oz_ = lane_bytes<T>(in.z.t, row, ch),
-                 oy_ = lane_bytes<T>(p.y.t, row, ch);
-  const int srow = lane / NP, sn = lane % NP;
-  const bool shared = TS * NP >= WAVE || lane < TS * NP;
-  const int sk = min(sn, in.N - 1);
-  const unsigned ob_ = lane_bytes<T>(in.Bm.t, srow, sk), oc_ = lane_bytes<T>(in.Cm.t, srow, sk);
+  // the pairs of a lane: step i * ROWS + row, channel ch; its values of B and C: step i * SROWS + srow, state sn
+  constexpr int ROWS = WAVE / CH, SROWS = WAVE / NP;
+  const int row = lane / CH, ch = lane % CH, srow = lane / NP, sn = lane % NP;
+  const bool pair = TS * CH >= WAVE || lane < TS * CH, shared = TS * NP >= WAVE || lane < TS * NP;
+  const float bias = in.bias ? in.bias[min(c0 + ch, in.D - 1)] : 0.0f, skip = in.skip ? in.skip[min(c0 + ch, in.D - 1)] : 0.0f;
   const int64_t gn = (int64_t)group * in.N;
   const T* const pu = (const T*)in.u.p + b * in.u.b + c0;
   const T* const pd = (const T*)in.delta.p + b * in.delta.b + c0;
@@ -170,22 +178,26 @@ __global__ __launch_bounds__(WAVE) void scan_forward_kernel(Forward p) {
   float ru[S::ITEMS], rd[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
   auto whole = [&](int s0) { return TS * CH >= WAVE && TS * NP >= WAVE && s0 + TS <= min(len, end) && nch == CH; };
   auto fetch = [&](int s0) {
-    // (opaque, or the sums of the parts are formed ahead in registers)
-    const unsigned ou = opaque(ou_), od = opaque(od_), oz = opaque(oz_), ob = opaque(ob_), oc = opaque(oc_);
+    // (opaque: the sums of an address's parts are not to be formed ahead, in registers)
+    const int sk = min(sn, in.N - 1);
+    const unsigned ou = opaque(lane_bytes<T>(in.u.t, row, ch)), od = opaque(lane_bytes<T>(in.delta.t, row, ch)),
+                   oz = opaque(lane_bytes<T>(in.z.t, row, ch)), ob = opaque(lane_bytes<T>(in.Bm.t, srow, sk)),
+                   oc = opaque(lane_bytes<T>(in.Cm.t, srow, sk));
     const T *au = pu + s0 * in.u.t, *ad = pd + s0 * in.delta.t, *az = pz + s0 * in.z.t, *ab = pb + s0 * in.Bm.t, *ac = pc + s0 * in.Cm.t;
-    const int64_t iu = ROWS * in.u.t, id = ROWS * in.delta.t, iz = ROWS * in.z.t, ib = WAVE / NP * in.Bm.t, ic = WAVE / NP * in.Cm.t;
+    const int64_t iu = ROWS * in.u.t, id = ROWS * in.delta.t, iz = ROWS * in.z.t, ib = SROWS * in.Bm.t, ic = SROWS * in.Cm.t;
     if (whole(s0)) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        ru[i] = elem(au + channel_of(i), ou);
-        rd[i] = elem(ad + channel_of(i), od);
-        if (i % WIDE == WIDE - 1) au += iu, ad += id;
+        ru[i] = elem(au, ou);
+        rd[i] = elem(ad, od);
+        au += iu;
+        ad += id;
       }
       if (!ENDS && in.z.p) {
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) {
-          rz[i] = elem(az + channel_of(i), oz);
-          if (i % WIDE == WIDE - 1) az += iz;
+          rz[i] = elem(az, oz);
+          az += iz;
         }
       }
 #pragma unroll
@@ -198,19 +210,20 @@ __global__ __launch_bounds__(WAVE) void scan_forward_kernel(Forward p) {
     } else {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        const int c = channel_of(i);
         ru[i] = rd[i] = rz[i] = 0.0f;
-        if (pair && s0 + step_of(i) + row < len && ch + c < nch) {
-          ru[i] = elem(au + c, ou);
-          rd[i] = elem(ad + c, od);
-          if (!ENDS && in.z.p) rz[i] = elem(az + c, oz);
+        if (pair && s0 + i * ROWS + row < len && ch < nch) {
+          ru[i] = elem(au, ou);
+          rd[i] = elem(ad, od);
+          if (!ENDS && in.z.p) rz[i] = elem(az, oz);
         }
-        if (i % WIDE == WIDE - 1) au += iu, ad += id, az += iz;
+        au += iu;
+        ad += id;
+        az += iz;
       }
 #pragma unroll
       for (int i = 0; i < S::SHARED; ++i) {
         rb[i] = rc[i] = 0.0f;
-        if (shared && s0 + i * (WAVE / NP) + srow < len) {
+        if (shared && s0 + i * SROWS + srow < len) {
           rb[i] = elem(ab, ob);
           if (!ENDS) rc[i] = elem(ac, oc);
         }
@@ -230,7 +243,7 @@ __global__ __launch_bounds__(WAVE) void scan_forward_kernel(Forward p) {
     for (int i = 0; i < S::ITEMS; ++i) {
       cu[i] = ru[i];
       cz[i] = rz[i];
-      rd[i] += bias[i % WIDE];
+      rd[i] += bias;
     }
     if (in.softplus) {
 #pragma unroll
@@ -239,100 +252,73 @@ __global__ __launch_bounds__(WAVE) void scan_forward_kernel(Forward p) {
     if (!all) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i)      // a step beyond the sequence
-        if (!(s0 + step_of(i) + row < len && ch + channel_of(i) < nch)) rd[i] = 0.0f;
+        if (!(s0 + i * ROWS + row < len && ch < nch)) rd[i] = 0.0f;
     }
     if (pair) {
 #pragma unroll
-      for (int i = 0; i < S::ITEMS; ++i) *reinterpret_cast<float2*>(&wu[step_of(i) + row][ch + channel_of(i)][0]) = float2{rd[i], rd[i] * cu[i]};
+      for (int i = 0; i < S::ITEMS; ++i) *reinterpret_cast<f32x2*>(&wu[i * ROWS + row][ch][0]) = f32x2{rd[i], rd[i] * cu[i]};
     }
     if (shared) {
 #pragma unroll
       for (int i = 0; i < S::SHARED; ++i) {
-        sb[i * (WAVE / NP) + srow][sn] = sn < in.N ? rb[i] : 0.0f;
-        if (!ENDS) sc[i * (WAVE / NP) + srow][sn] = sn < in.N ? rc[i] : 0.0f;
+        sb[i * SROWS + srow][sn] = sn < in.N ? rb[i] : 0.0f;
+        if (!ENDS) sc[i * SROWS + srow][sn] = sn < in.N ? rc[i] : 0.0f;
       }
     }
-    __syncthreads();
+    wave_sync();
     if (s0 + TS < stop) fetch(s0 + TS);
     if (!ENDS && p.states && s0 % p.stretch == 0) {
-#pragma unroll
-      for (int j = 0; j < CPL; ++j)
-        if (cl + j < nch)
-          store_states(p.states + (((int64_t)(s0 / p.stretch) * in.B + b) * in.D + c0 + cl + j) * in.N, q * NB, in.N, h[j]);
+      if (cl < nch) store_states(p.states + (int64_t)(s0 / p.stretch) * all_states + bd * in.N, q * NB, in.N, h);
     }
 #pragma unroll
     for (int s = 0; s < TS; ++s) {
-      const f32x4 w = *reinterpret_cast<const f32x4*>(&wu[s][cl][0]);
-      const f32x4 vb = *reinterpret_cast<const f32x4*>(&sb[s][q * NB]);
-      f32x4 vc = {};
-      if constexpr (!ENDS) vc = *reinterpret_cast<const f32x4*>(&sc[s][q * NB]);
-      float y[CPL];
+      const f32x2 w = *reinterpret_cast<const f32x2*>(&wu[s][cl][0]);
+      float vb[NB], vc[NB], y = 0.0f;
+      load<NB>(&sb[s][q * NB], vb);
+      if constexpr (!ENDS) load<NB>(&sc[s][q * NB], vc);
 #pragma unroll
-      for (int j = 0; j < CPL; ++j) {
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const float a = __builtin_amdgcn_exp2f(w[2 * j] * A2[j][n]);
-          h[j][n] = a * h[j][n] + w[2 * j + 1] * vb[n];
-          if constexpr (!ENDS) y[j] = n ? y[j] + h[j][n] * vc[n] : h[j][n] * vc[n];
-        }
-        if constexpr (ENDS) sum_w[j] += w[2 * j];
-        else y[j] = lanes_sum<NL>(y[j]);
+      for (int n = 0; n < NB; ++n) {
+        const float a = __builtin_amdgcn_exp2f(w[0] * A2[n]);
+        h[n] = a * h[n] + w[1] * vb[n];
+        if constexpr (!ENDS) y = n ? y + h[n] * vc[n] : h[n] * vc[n];
       }
-      // every lane of a channel writes the same value to the same place
-      if constexpr (!ENDS) *reinterpret_cast<float2*>(&sy[s][cl]) = float2{y[0], y[1]};
+      // (every lane of a channel writes the same value to the same place)
+      if constexpr (ENDS) sum_w += w[0];
+      else sy[s][cl] = lanes_sum<NL>(y);
     }
-    __syncthreads();
+    wave_sync();
     if constexpr (!ENDS) {
       float y[S::ITEMS];
-      if (pair) {
 #pragma unroll
-        for (int i = 0; i < S::ITEMS; ++i) y[i] = sy[step_of(i) + row][ch + channel_of(i)] + skip[i % WIDE] * cu[i];
-      }
+      for (int i = 0; i < S::ITEMS; ++i) y[i] = pair ? sy[i * ROWS + row][ch] + skip * cu[i] : 0.0f;
       if (in.z.p) {
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) y[i] *= cz[i] * sigmoid(cz[i]);
       }
       T* ay = py + s0 * p.y.t;
-      const unsigned oy = opaque(oy_);
+      const unsigned oy = opaque(lane_bytes<T>(p.y.t, row, ch));
       const int64_t iy = ROWS * p.y.t;
       if (all) {
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) {
-          set_elem(ay + channel_of(i), oy, y[i]);
-          if (i % WIDE == WIDE - 1) ay += iy;
+          set_elem(ay, oy, y[i]);
+          ay += iy;
         }
       } else {
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) {
-          const int s = s0 + step_of(i) + row;
-          if (pair && s < end && ch + channel_of(i) < nch) set_elem(ay + channel_of(i), oy, s < len ? y[i] : 0.0f);
-          if (i % WIDE == WIDE - 1) ay += iy;
+          const int s = s0 + i * ROWS + row;
+          if (pair && s < end && ch < nch) set_elem(ay, oy, s < len ? y[i] : 0.0f);
+          ay += iy;
         }
       }
+      wave_sync();
     }
   }
-  float* last = ENDS ? p.starts + (int64_t)(chunk + 1) * in.B * in.D * in.N : chunk + 1 == p.chunks ? p.h_out : nullptr;
-#pragma unroll
-  for (int j = 0; j < CPL; ++j) {
-    if (cl + j >= nch) continue;
-    const int64_t d = (int64_t)b * in.D + c0 + cl + j;
-    if (last) store_states(last + d * in.N, q * NB, in.N, h[j]);
-    if (ENDS && q == 0) p.sums[(int64_t)chunk * in.B * in.D + d] = sum_w[j];
-  }
-}
-
-// starts[c] holds the state that chunk c - 1 reached from zeros; adds what it started from, decayed by exp(A sum w).
-__global__ __launch_bounds__(256) void scan_join_kernel(float* starts, const float* sums, const float* A, int64_t BD, int D, int N, int chunks) {
-  const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (k >= BD * N) return;
-  const int64_t bd = k / N;
-  const float a2 = A[(bd % D) * N + k % N] * LOG2E;
-  float h = starts[BD * N + k];
-#pragma unroll 8
-  for (int c = 2; c < chunks; ++c) {
-    h = starts[c * BD * N + k] + __builtin_amdgcn_exp2f(a2 * sums[(c - 1) * BD + bd]) * h;
-    starts[c * BD * N + k] = h;
-  }
+  if (cl >= nch) return;
+  float* last = ENDS ? p.starts + (chunk + 1) * all_states : chunk + 1 == p.chunks ? p.h_out : nullptr;
+  if (last) store_states(last + bd * in.N, q * NB, in.N, h);
+  if (ENDS && q == 0) p.sums[(int64_t)chunk * in.B * in.D + bd] = sum_w;
 }
 
 // ---- backward --------------------------------------------------------------------------------------
@@ -341,154 +327,212 @@ struct Backward {
   Scan in;
   Seq dy;
   SeqOut du, ddelta, dz;
-  const float *h0, *states, *dh_out;
+  const float *states, *dh_out;
   float* dh0;
   float *bc_parts;                 // [tiles][t][B][G][2][N]: sums of dB and dC over a workgroup's channels
-  float *a_parts;                  // [B][D N | D | D]: dA, dskip, ddelta_bias of a sequence
+  float *a_parts;                  // [chunks][B][D N | D | D]: dA, dskip, ddelta_bias of a chunk of a sequence
   int stretch;
+  int chunk, chunks;               // steps per chunk, a multiple of the stretch
+  float *starts, *sums;            // [chunks][B][D][N]: dL/dh at a chunk's start from its own steps; [chunks][B][D]: sum of w
 };
 
-constexpr int BS = 16;             // steps per block: a lane's h and exp(w A) of a block stay in registers
-constexpr int BACK_WAVES = 4;
+constexpr int BS = 16;             // steps per block: exp(w A) and exp(w A) h of a block stay in a lane's registers
 
-template <int NL>
+template <int NL_, int NB_>
 struct BackwardShape {
+  static constexpr int NL = NL_, NB = NB_;
+  static constexpr int BACK_WAVES = NB == 2 ? 8 : 4;                  // (what fits into LDS with stretches of 256)
   static constexpr int CW = WAVE / NL;                                // channels per wave
   static constexpr int CH = CW * BACK_WAVES;                          // channels per workgroup
   static constexpr int NP = NB * NL;
   static constexpr int THREADS = BACK_WAVES * WAVE;
-  static constexpr int ITEMS = (BS * CH + THREADS - 1) / THREADS;
-  static constexpr int SHARED = (2 * BS * NP + THREADS - 1) / THREADS;
+  static constexpr int ITEMS = BS * CH / THREADS;                     // (step, channel) pairs per thread
+  static constexpr int SHARED = (BS * NP + THREADS - 1) / THREADS;    // values of B, and of C, per thread
+  static constexpr int WAVES_PER_SIMD = NB == 2 && NL >= 8 ? 4 : 2;
 };
 
-// Sums of a lane's eight values (four of dB, four of dC) over the channels of its wave, that is over the lanes with the same
-// lane % NL, into red[2][NP].  Halves of the wave, then neighbouring rows of sixteen lanes, exchange one half of their values each, so that every addition
+// Sums of a lane's 2 NB values (of dB, then of dC) over the channels of its wave, that is over the lanes with the same lane % NL, into
+// red[2][NP].  Halves of the wave, then neighbouring rows of sixteen lanes, exchange one half of their values each, so that every addition
 // adds two values that are wanted; what is left is rotated within the rows.
-template <int NL>
-__device__ inline void channels_sum(float (&v)[2 * NB], int lane, float* red) {
-  constexpr int NP = NB * NL;
-  const int q = lane % NL;
-  float w[NB], x[2];
+template <typename S>
+__device__ inline void channels_sum(const float (&v)[2 * S::NB], int lane, float* red) {
+  constexpr int NL = S::NL, NB = S::NB;
+  float w[NB], x[NB / 2];
 #pragma unroll
-  for (int n = 0; n < NB; ++n) {       // lanes 0 .. 31: dB, 32 .. 63: dC
+  for (int n = 0; n < NB; ++n) {         // lanes 0 .. 31: dB, 32 .. 63: dC
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[n]), __float_as_uint(v[NB + n]), false, false);
     w[n] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
 #pragma unroll
-  for (int n = 0; n < 2; ++n) {        // even rows: states 0 and 2, odd rows: 1 and 3
+  for (int n = 0; n < NB / 2; ++n) {     // even rows: even states, odd rows: odd ones
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(w[2 * n]), __float_as_uint(w[2 * n + 1]), false, false);
     x[n] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  }
-#pragma unroll
-  for (int n = 0; n < 2; ++n) {
     if constexpr (NL <= 8) x[n] = dpp_add<0x128>(x[n]);
     if constexpr (NL <= 4) x[n] = dpp_add<0x124>(x[n]);
     if constexpr (NL <= 2) x[n] = dpp_add<0x122>(x[n]);
-    if constexpr (NL <= 1) x[n] = dpp_add<0x121>(x[n]);
   }
-  if (lane % 16 < NL) {
-    float* out = red + (lane / 32) * NP + q * NB + (lane / 16 % 2);
-    out[0] = x[0];
-    out[2] = x[1];
-  }
+  // (every lane that has a sum writes it)
+#pragma unroll
+  for (int n = 0; n < NB / 2; ++n) red[(lane / 32) * S::NP + lane % NL * NB + 2 * n + lane / 16 % 2] = x[n];
 }
 
-template <typename T, int NL>
-__global__ __launch_bounds__(BACK_WAVES* WAVE) void scan_backward_kernel(Backward p) {
-  using S = BackwardShape<NL>;
-  constexpr int CH = S::CH, NP = S::NP, THREADS = S::THREADS;
+// A workgroup's channels over a chunk of steps, from its end to its start, stretch by stretch: the states at the starts of the stretch's blocks
+// are recomputed from the one kept at its start and put into LDS; then block by block, the last one first, the block's steps
+// are run forward into registers and back.
+template <typename T, typename S, bool GATE>
+__global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_kernel(Backward p) {
+  constexpr int CH = S::CH, NP = S::NP, THREADS = S::THREADS, NL = S::NL, NB = S::NB, BACK_WAVES = S::BACK_WAVES;
   extern __shared__ __align__(16) float lds[];
-  float* wud = lds;                                   // [BS][CH][4]: w, w u, gated dy -> p, q, core
-  float* bc = wud + BS * CH * 4;                      // [BS][2][NP]
-  float* red = bc + BS * 2 * NP;                      // [BACK_WAVES][BS][2][NP]
+  float* wud = lds;                                   // [BS][CH][4]: w, w u, gated dy -> through, dlog, core
+  float* sb = wud + BS * CH * 4;                      // [BS][NP]
+  float* sc = sb + BS * NP;                           // [BS][NP]
+  float* red = sc + BS * NP;                          // [BACK_WAVES][BS][2][NP]
   float* kept = red + BACK_WAVES * BS * 2 * NP;       // [stretch / BS][THREADS][NB]: states at the blocks' starts
   const Scan& in = p.in;
-  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, b = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), b = blockIdx.y, chunk = blockIdx.z;
   const int group = blockIdx.x / in.tiles, tile = blockIdx.x % in.tiles, per = in.D / in.G;
   const int c0 = group * per + tile * CH, nch = min(CH, group * per + per - c0);
   const int len = length_of(in.lengths, b, in.t);
   const int q = lane % NL, cl = wave * S::CW + lane / NL;
   const bool mine = cl < nch;
-  const int64_t d = min(c0 + cl, in.D - 1);
+  const int64_t d = min(c0 + cl, in.D - 1), bd = (int64_t)b * in.D + d, all_states = (int64_t)in.B * in.D * in.N;
   const int64_t gn = (int64_t)group * in.N;
 
-  float A[NB], g[NB], dA[NB] = {};
+  float A[NB], A2[NB], g[NB], dA[NB], h[NB];
   load_states(in.A + d * in.N, q * NB, in.N, A);
 #pragma unroll
-  for (int n = 0; n < NB; ++n) g[n] = 0.0f;
-  if (p.dh_out) load_states(p.dh_out + ((int64_t)b * in.D + d) * in.N, q * NB, in.N, g);
-  float dskip = 0.0f, dbias = 0.0f;
-  const int ic = tid % CH;                            // this thread's channel in the (step, channel) pairs, THREADS being a multiple of CH
-  const float bias = in.bias ? in.bias[min(c0 + ic, in.D - 1)] : 0.0f;
-  const float skip = in.skip ? in.skip[min(c0 + ic, in.D - 1)] : 0.0f;
+  for (int n = 0; n < NB; ++n) {
+    A2[n] = A[n] * LOG2E;
+    dA[n] = g[n] = h[n] = 0.0f;
+  }
+  if (p.dh_out) load_states(p.dh_out + bd * in.N, q * NB, in.N, g);
+  // through the chunks after this one
+  for (int k = p.chunks - 1; k > chunk; --k) {
+    float e[NB];
+    load_states(p.starts + k * all_states + bd * in.N, q * NB, in.N, e);
+    const float w = p.sums[(int64_t)k * in.B * in.D + bd];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) g[n] = e[n] + __builtin_amdgcn_exp2f(w * A2[n]) * g[n];
+  }
 
-  // Puts a block's w, w u, gated dy and B, C into LDS; keeps u, w, dy and what softplus and the gate need.
-  float iu[S::ITEMS], iw[S::ITEMS], idy[S::ITEMS], isig[S::ITEMS], idz[S::ITEMS];
-  auto stage = [&](int s0, bool back) {
+  // a thread's (step, channel) pairs: step i * ROWS + wrow + lrow, channel ic; a wave shares wrow
+  constexpr int ROWS = THREADS / CH;
+  const int ic = tid % CH, wrow = wave * WAVE / CH, lrow = CH < WAVE ? lane / CH : 0, row = wrow + lrow;
+  const int lane_c = CH < WAVE ? ic : lane, wave_c = CH < WAVE ? 0 : wave * WAVE % CH;   // ic = wave_c + lane_c
+  const float bias = in.bias ? in.bias[min(c0 + ic, in.D - 1)] : 0.0f, skip = in.skip ? in.skip[min(c0 + ic, in.D - 1)] : 0.0f;
+  float dskip = 0.0f, dbias = 0.0f;
+  // and its values of B and C: step i * SROWS + srow, state sn
+  constexpr int SROWS = THREADS / NP;
+  const int srow = tid / NP, sn = tid % NP;
+  const bool shared = BS * NP >= THREADS || tid < BS * NP;
+
+  float ru[S::ITEMS], rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
+  auto fetch = [&](int s0, bool back) {
+    const bool all = s0 + BS <= len && nch == CH;
+    const T* au = (const T*)in.u.p + b * in.u.b + c0 + wave_c + (s0 + wrow) * in.u.t;
+    const T* ad = (const T*)in.delta.p + b * in.delta.b + c0 + wave_c + (s0 + wrow) * in.delta.t;
+    const T* ag = (const T*)p.dy.p + b * p.dy.b + c0 + wave_c + (s0 + wrow) * p.dy.t;
+    const T* az = (const T*)in.z.p + b * in.z.b + c0 + wave_c + (s0 + wrow) * in.z.t;
+    const unsigned ou = lane_bytes<T>(in.u.t, lrow, lane_c), od = lane_bytes<T>(in.delta.t, lrow, lane_c),
+                   og = lane_bytes<T>(p.dy.t, lrow, lane_c), oz = lane_bytes<T>(in.z.t, lrow, lane_c);
 #pragma unroll
     for (int i = 0; i < S::ITEMS; ++i) {
-      const int k = i * THREADS + tid, s = s0 + k / CH;
-      const bool live = k < BS * CH && s < len && ic < nch;
-      const float raw = (live ? at<T>(in.delta, s, b, c0 + ic) : 0.0f) + bias;
-      iu[i] = live ? at<T>(in.u, s, b, c0 + ic) : 0.0f;
-      iw[i] = !live ? 0.0f : in.softplus ? softplus_of(raw) : raw;
-      isig[i] = in.softplus ? sigmoid(raw) : 1.0f;
-      idy[i] = 0.0f;
-      idz[i] = 0.0f;
-      if (back) {
-        idy[i] = live ? at<T>(p.dy, s, b, c0 + ic) : 0.0f;
-        if (in.z.p) {
-          const float z = live ? at<T>(in.z, s, b, c0 + ic) : 0.0f, sg = sigmoid(z);
-          idz[i] = idy[i] * sg * (1.0f + z * (1.0f - sg));     // times what the gate multiplied
-          idy[i] *= z * sg;
+      ru[i] = rd[i] = rg[i] = rz[i] = 0.0f;
+      if (all || (s0 + i * ROWS + row < len && ic < nch)) {
+        ru[i] = elem(au, ou);
+        rd[i] = elem(ad, od);
+        if (back) {
+          rg[i] = elem(ag, og);
+          if (GATE) rz[i] = elem(az, oz);
         }
       }
-      if (k < BS * CH) *reinterpret_cast<f32x4*>(wud + 4 * k) = f32x4{iw[i], iw[i] * iu[i], idy[i], 0.0f};
+      au += ROWS * in.u.t;
+      ad += ROWS * in.delta.t;
+      ag += ROWS * p.dy.t;
+      az += ROWS * in.z.t;
     }
 #pragma unroll
     for (int i = 0; i < S::SHARED; ++i) {
-      const int k = i * THREADS + tid, s = s0 + k / (2 * NP), n = k % NP;
-      if (k < 2 * BS * NP) bc[k] = !(s < len && n < in.N) ? 0.0f : k / NP % 2 ? at<T>(in.Cm, s, b, gn + n) : at<T>(in.Bm, s, b, gn + n);
+      const int s = s0 + i * SROWS + srow;
+      rb[i] = rc[i] = 0.0f;
+      if (shared && s < len && sn < in.N) {
+        rb[i] = at<T>(in.Bm, s, b, gn + sn);
+        if (back) rc[i] = at<T>(in.Cm, s, b, gn + sn);
+      }
     }
   };
 
-  const int stretches = (in.t + p.stretch - 1) / p.stretch;
-  for (int st = stretches - 1; st >= 0; --st) {
-    const int first = st * p.stretch, blocks = (min(in.t, first + p.stretch) - first + BS - 1) / BS;
-    float h[NB];
-    load_states(p.states + (((int64_t)st * in.B + b) * in.D + d) * in.N, q * NB, in.N, h);
-    // the states at the starts of the stretch's blocks
-    for (int k = 0; k < blocks; ++k) {
+  const int from = chunk * p.chunk / p.stretch, last_step = min(in.t, (chunk + 1) * p.chunk);
+  auto blocks_of = [&](int st) { return (min(last_step, (st + 1) * p.stretch) - st * p.stretch + BS - 1) / BS; };
+  int st = (last_step - 1) / p.stretch, k = 0;        // stretch; block in it
+  bool back = blocks_of(st) == 1;
+  if (in.t) fetch(st * p.stretch, back);
+  while (in.t && st >= from) {
+    const int s0 = st * p.stretch + k * BS, blocks = blocks_of(st);
+    // stage the block: w, w u, gated dy; what softplus' and the gate's gradients need stays in registers
+    float iu[S::ITEMS], iw[S::ITEMS], isig[S::ITEMS], idy[S::ITEMS], idz[S::ITEMS];
+#pragma unroll
+    for (int i = 0; i < S::ITEMS; ++i) {
+      const float raw = rd[i] + bias;
+      const bool live = s0 + i * ROWS + row < len && ic < nch;
+      iu[i] = ru[i];
+      iw[i] = !live ? 0.0f : in.softplus ? softplus_of(raw) : raw;
+      isig[i] = in.softplus ? sigmoid(raw) : 1.0f;
+      idy[i] = rg[i];
+      if (GATE) {
+        const float sg = sigmoid(rz[i]);
+        idz[i] = rg[i] * sg * (1.0f + rz[i] * (1.0f - sg));    // times what the gate multiplied
+        idy[i] = rg[i] * rz[i] * sg;
+      }
+      *reinterpret_cast<f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x4{iw[i], iw[i] * iu[i], idy[i], 0.0f};
+    }
+    if (shared) {
+#pragma unroll
+      for (int i = 0; i < S::SHARED; ++i) {
+        sb[(i * SROWS + srow) * NP + sn] = rb[i];
+        sc[(i * SROWS + srow) * NP + sn] = rc[i];
+      }
+    }
+    if (k == 0 && (!back || blocks == 1)) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, h);
+    __syncthreads();
+    // the block after this one
+    int next_st = st, next_k = k;
+    bool next_back = true;
+    if (!back) {
+      next_back = k + 1 == blocks - 1;
+      next_k = k + 1;
+    } else if (k > 0) {
+      next_k = k - 1;
+    } else {
+      next_st = st - 1;
+      next_back = p.stretch == BS;
+    }
+    if (next_st >= from) fetch(next_st * p.stretch + next_k * BS, next_back);
+
+    if (!back) {
       float* at_start = kept + (k * THREADS + tid) * NB;
+      store<NB>(at_start, h);
 #pragma unroll
-      for (int n = 0; n < NB; ++n) at_start[n] = h[n];
-      if (k + 1 == blocks) break;
-      stage(first + k * BS, false);
-      __syncthreads();
-#pragma unroll 4
       for (int s = 0; s < BS; ++s) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(wud + 4 * (s * CH + cl));
-        const f32x4 vb = *reinterpret_cast<const f32x4*>(bc + (2 * s) * NP + q * NB);
+        const f32x2 w = *reinterpret_cast<const f32x2*>(wud + 4 * (s * CH + cl));
+        float vb[NB];
+        load<NB>(sb + s * NP + q * NB, vb);
 #pragma unroll
-        for (int n = 0; n < NB; ++n) h[n] = __builtin_amdgcn_exp2f(w[0] * (A[n] * LOG2E)) * h[n] + w[1] * vb[n];
+        for (int n = 0; n < NB; ++n) h[n] = __builtin_amdgcn_exp2f(w[0] * A2[n]) * h[n] + w[1] * vb[n];
       }
       __syncthreads();
-    }
-    for (int k = blocks - 1; k >= 0; --k) {
-      const int s0 = first + k * BS;
-      stage(s0, true);
-#pragma unroll
-      for (int n = 0; n < NB; ++n) h[n] = kept[(k * THREADS + tid) * NB + n];
-      __syncthreads();
+    } else {
+      if (k + 1 < blocks) load<NB>(kept + (k * THREADS + tid) * NB, h);   // (the last block goes on from the one before)
       // forward through the block: exp(w A) and exp(w A) h_{s-1} of every step
       float a[BS][NB], ah[BS][NB];
 #pragma unroll
       for (int s = 0; s < BS; ++s) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(wud + 4 * (s * CH + cl));
-        const f32x4 vb = *reinterpret_cast<const f32x4*>(bc + (2 * s) * NP + q * NB);
+        const f32x2 w = *reinterpret_cast<const f32x2*>(wud + 4 * (s * CH + cl));
+        float vb[NB];
+        load<NB>(sb + s * NP + q * NB, vb);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-          a[s][n] = __builtin_amdgcn_exp2f(w[0] * (A[n] * LOG2E));
+          a[s][n] = __builtin_amdgcn_exp2f(w[0] * A2[n]);
           ah[s][n] = a[s][n] * h[n];
           h[n] = ah[s][n] + w[1] * vb[n];
         }
@@ -497,19 +541,19 @@ __global__ __launch_bounds__(BACK_WAVES* WAVE) void scan_backward_kernel(Backwar
 #pragma unroll
       for (int s = BS - 1; s >= 0; --s) {
         const f32x4 w = *reinterpret_cast<const f32x4*>(wud + 4 * (s * CH + cl));
-        const f32x4 vb = *reinterpret_cast<const f32x4*>(bc + (2 * s) * NP + q * NB);
-        const f32x4 vc = *reinterpret_cast<const f32x4*>(bc + (2 * s + 1) * NP + q * NB);
-        float v[2 * NB], through = 0.0f, dlog = 0.0f, core = 0.0f;
+        float vb[NB], vc[NB], v[2 * NB], through = 0.0f, dlog = 0.0f, core = 0.0f;
+        load<NB>(sb + s * NP + q * NB, vb);
+        load<NB>(sc + s * NP + q * NB, vc);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const float hn = ah[s][n] + w[1] * vb[n];
           g[n] += w[2] * vc[n];
           v[n] = g[n] * w[1];                  // to dB
           v[NB + n] = w[2] * hn;               // to dC
-          through += g[n] * vb[n];
-          core += hn * vc[n];
+          through = n ? through + g[n] * vb[n] : g[n] * vb[n];
+          if (GATE) core = n ? core + hn * vc[n] : hn * vc[n];
           const float r = g[n] * ah[s][n];     // the exponent's gradient
-          dlog += r * A[n];
+          dlog = n ? dlog + r * A[n] : r * A[n];
           dA[n] += r * w[0];
           g[n] *= a[s][n];
         }
@@ -517,41 +561,45 @@ __global__ __launch_bounds__(BACK_WAVES* WAVE) void scan_backward_kernel(Backwar
 #pragma unroll
           for (int n = 0; n < 2 * NB; ++n) v[n] = 0.0f;
         }
-        channels_sum<NL>(v, lane, red + (wave * BS + s) * 2 * NP);
+        channels_sum<S>(v, lane, red + (wave * BS + s) * 2 * NP);
         through = lanes_sum<NL>(through);
         dlog = lanes_sum<NL>(dlog);
-        if (in.z.p) core = lanes_sum<NL>(core);
-        if (q == 0) *reinterpret_cast<f32x4*>(wud + 4 * (s * CH + cl)) = f32x4{through, dlog, core, 0.0f};
+        if (GATE) core = lanes_sum<NL>(core);
+        *reinterpret_cast<f32x4*>(wud + 4 * (s * CH + cl)) = f32x4{through, dlog, core, 0.0f};   // (all lanes of a channel the same)
       }
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        const int k2 = i * THREADS + tid, s = s0 + k2 / CH;
-        if (k2 < BS * CH && s < in.t && ic < nch) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(wud + 4 * k2);
+        const int s = s0 + i * ROWS + row;
+        if (s < last_step && ic < nch) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic));
           const bool live = s < len;
           const float dw = live ? (iu[i] * v[0] + v[1]) * isig[i] : 0.0f;
-          put<T>(p.du, s, b, c0 + ic, live ? iw[i] * v[0] + skip * idy[i] : 0.0f);
-          put<T>(p.ddelta, s, b, c0 + ic, dw);
-          if (in.z.p) put<T>(p.dz, s, b, c0 + ic, live ? idz[i] * (v[2] + skip * iu[i]) : 0.0f);
+          const int64_t sw = s0 + i * ROWS + wrow;
+          set_elem((T*)p.du.p + sw * p.du.t + b * p.du.b + c0 + wave_c, lane_bytes<T>(p.du.t, lrow, lane_c), live ? iw[i] * v[0] + skip * idy[i] : 0.0f);
+          set_elem((T*)p.ddelta.p + sw * p.ddelta.t + b * p.ddelta.b + c0 + wave_c, lane_bytes<T>(p.ddelta.t, lrow, lane_c), dw);
+          if (GATE) set_elem((T*)p.dz.p + sw * p.dz.t + b * p.dz.b + c0 + wave_c, lane_bytes<T>(p.dz.t, lrow, lane_c), live ? idz[i] * (v[2] + skip * iu[i]) : 0.0f);
           dskip += idy[i] * iu[i];
           dbias += dw;
         }
       }
-      for (int k2 = tid; k2 < BS * 2 * in.N; k2 += THREADS) {
-        const int s = k2 / (2 * in.N), r = k2 % (2 * in.N), half = r / in.N, n = r % in.N;
-        if (s0 + s < in.t) {
-          float v = 0.0f;
+      for (int m = tid; m < BS * 2 * NP; m += THREADS) {
+        const int s = m / (2 * NP), half = m / NP % 2, n = m % NP;
+        float v = 0.0f;
 #pragma unroll
-          for (int w = 0; w < BACK_WAVES; ++w) v += red[(w * BS + s) * 2 * NP + half * NP + n];
+        for (int w = 0; w < BACK_WAVES; ++w) v += red[w * BS * 2 * NP + m];
+        if (s0 + s < last_step && n < in.N)
           p.bc_parts[(((((int64_t)tile * in.t + s0 + s) * in.B + b) * in.G + group) * 2 + half) * in.N + n] = v;
-        }
       }
       __syncthreads();
     }
+    st = next_st;
+    k = next_k;
+    back = next_back;
+    if (st < from) break;
   }
-  if (mine && p.dh0) store_states(p.dh0 + ((int64_t)b * in.D + d) * in.N, q * NB, in.N, g);
-  float* parts = p.a_parts + (int64_t)b * in.D * (in.N + 2);
+  if (mine && p.dh0 && chunk == 0) store_states(p.dh0 + bd * in.N, q * NB, in.N, g);
+  float* parts = p.a_parts + ((int64_t)chunk * in.B + b) * in.D * (in.N + 2);
   if (mine) store_states(parts + d * in.N, q * NB, in.N, dA);
   // dskip and ddelta_bias: the threads that share a channel, in their order
   red[tid] = dskip;
@@ -559,13 +607,103 @@ __global__ __launch_bounds__(BACK_WAVES* WAVE) void scan_backward_kernel(Backwar
   __syncthreads();
   if (tid < nch) {
     float s1 = 0.0f, s2 = 0.0f;
-    for (int k = tid; k < THREADS; k += CH) {
-      s1 += red[k];
-      s2 += red[THREADS + k];
+    for (int i = tid; i < THREADS; i += CH) {
+      s1 += red[i];
+      s2 += red[THREADS + i];
     }
     parts[(int64_t)in.D * in.N + c0 + tid] = s1;
     parts[(int64_t)in.D * (in.N + 1) + c0 + tid] = s2;
   }
+}
+
+// dL/dh just before a chunk, from the chunk's own steps: g_{s-1} = exp(w_s A) (g_s + C_s dy_s) from its end to its start; and the sum of w.
+// One wave's channels, as in the forward launches.
+template <typename T, typename S, bool GATE>
+__global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_back_ends_kernel(Backward p) {
+  constexpr int CH = S::CH, TS = S::TS, NP = S::NP, NL = S::NL, NB = S::NB, ROWS = WAVE / CH, SROWS = WAVE / NP;
+  struct Lds { float wg[TS][CH][2], sc[TS][NP]; };
+  __shared__ __align__(16) Lds lds[FORWARD_WAVES];
+  const Scan& in = p.in;
+  const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), b = blockIdx.y, chunk = blockIdx.z + 1;
+  auto& [wg, sc] = lds[wave];
+  const int group = blockIdx.x / in.tiles, per = in.D / in.G;
+  const int c0 = group * per + (blockIdx.x % in.tiles * FORWARD_WAVES + wave) * CH;
+  const int nch = min(CH, group * per + per - c0);
+  if (nch <= 0) return;
+  const int len = length_of(in.lengths, b, in.t);
+  const int begin = chunk * p.chunk, stop = min(len, min(in.t, begin + p.chunk));
+  const int q = lane % NL, cl = lane / NL;
+  const int64_t d = min(c0 + cl, in.D - 1), bd = (int64_t)b * in.D + d, gn = (int64_t)group * in.N;
+  float g[NB], A2[NB], sum_w = 0.0f;
+  load_states(in.A + d * in.N, q * NB, in.N, A2);
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    A2[n] *= LOG2E;
+    g[n] = 0.0f;
+  }
+  const int row = lane / CH, ch = lane % CH, srow = lane / NP, sn = lane % NP;
+  const bool pair = TS * CH >= WAVE || lane < TS * CH, shared = TS * NP >= WAVE || lane < TS * NP;
+  const float bias = in.bias ? in.bias[min(c0 + ch, in.D - 1)] : 0.0f;
+  const T* const pd = (const T*)in.delta.p + b * in.delta.b + c0;
+  const T* const pg = (const T*)p.dy.p + b * p.dy.b + c0;
+  const T* const pz = (const T*)in.z.p + b * in.z.b + c0;
+  const T* const pc = (const T*)in.Cm.p + b * in.Cm.b + gn;
+  float rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rc[S::SHARED];
+  auto fetch = [&](int s0) {
+    const bool all = s0 + TS <= stop && nch == CH;
+    const unsigned od = opaque(lane_bytes<T>(in.delta.t, row, ch)), og = opaque(lane_bytes<T>(p.dy.t, row, ch)),
+                   oz = opaque(lane_bytes<T>(in.z.t, row, ch)), oc = opaque(lane_bytes<T>(in.Cm.t, srow, min(sn, in.N - 1)));
+    const T *ad = pd + s0 * in.delta.t, *ag = pg + s0 * p.dy.t, *az = pz + s0 * in.z.t, *ac = pc + s0 * in.Cm.t;
+#pragma unroll
+    for (int i = 0; i < S::ITEMS; ++i) {
+      rd[i] = rg[i] = rz[i] = 0.0f;
+      if (pair && (all || (s0 + i * ROWS + row < stop && ch < nch))) {
+        rd[i] = elem(ad, od);
+        rg[i] = elem(ag, og);
+        if (GATE) rz[i] = elem(az, oz);
+      }
+      ad += ROWS * in.delta.t;
+      ag += ROWS * p.dy.t;
+      az += ROWS * in.z.t;
+    }
+#pragma unroll
+    for (int i = 0; i < S::SHARED; ++i) {
+      rc[i] = 0.0f;
+      if (shared && s0 + i * SROWS + srow < stop) rc[i] = elem(ac, oc);
+      ac += SROWS * in.Cm.t;
+    }
+  };
+  int s0 = begin + (stop - 1 - begin) / TS * TS;
+  if (begin < stop) fetch(s0);
+  for (; begin < stop && s0 >= begin; s0 -= TS) {
+    if (pair) {
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i) {
+        const bool live = s0 + i * ROWS + row < stop && ch < nch;
+        const float raw = rd[i] + bias, w = !live ? 0.0f : in.softplus ? softplus_of(raw) : raw;
+        *reinterpret_cast<f32x2*>(&wg[i * ROWS + row][ch][0]) = f32x2{w, GATE ? rg[i] * rz[i] * sigmoid(rz[i]) : rg[i]};
+      }
+    }
+    if (shared) {
+#pragma unroll
+      for (int i = 0; i < S::SHARED; ++i) sc[i * SROWS + srow][sn] = sn < in.N ? rc[i] : 0.0f;
+    }
+    wave_sync();
+    if (s0 - TS >= begin) fetch(s0 - TS);
+#pragma unroll
+    for (int s = TS - 1; s >= 0; --s) {
+      const f32x2 w = *reinterpret_cast<const f32x2*>(&wg[s][cl][0]);
+      float vc[NB];
+      load<NB>(&sc[s][q * NB], vc);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) g[n] = __builtin_amdgcn_exp2f(w[0] * A2[n]) * (g[n] + w[1] * vc[n]);
+      sum_w += w[0];
+    }
+    wave_sync();
+  }
+  if (cl >= nch) return;
+  store_states(p.starts + chunk * ((int64_t)in.B * in.D * in.N) + bd * in.N, q * NB, in.N, g);
+  if (q == 0) p.sums[(int64_t)chunk * in.B * in.D + bd] = sum_w;
 }
 
 // dB and dC from the workgroups' sums, in their order.
@@ -585,17 +723,6 @@ __global__ __launch_bounds__(256) void scan_shared_kernel(Shared p) {
     const int64_t sb = k / row;
     put<T>(half ? p.dC : p.dB, sb / p.B, sb % p.B, (int64_t)group * p.N + n, v);
   }
-}
-
-// [B][D N | D | D] -> dA, dskip, ddelta_bias
-__global__ __launch_bounds__(256) void scan_params_kernel(const float* parts, int B, int64_t DN, int64_t D, float* dA, float* dskip, float* dbias) {
-  const int64_t all = DN + 2 * D, k = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (k >= all) return;
-  float v = 0.0f;
-  for (int b = 0; b < B; ++b) v += parts[b * all + k];
-  if (k < DN) dA[k] = v;
-  else if (k < DN + D) { if (dskip) dskip[k - DN] = v; }
-  else if (dbias) dbias[k - DN - D] = v;
 }
 
 // ---- single tokens -----------------------------------------------------------------------------------
@@ -695,48 +822,83 @@ Scan scan_of(const mebptt_scan_desc* d, const mebptt_scan_inputs* in) {
           d->t, d->B, d->D, d->N, d->G, d->softplus, 0};
 }
 
-// How many chunks the time axis is cut into: enough workgroups for two waves on each of the 1024 SIMDs, in chunks of at least MIN_CHUNK steps.  The
-// chunks' ends are computed first, which is most of the work once more, so nothing is cut that fills the chip by itself.
-constexpr int MIN_CHUNK = 64;
-int64_t forward_tiles(const mebptt_scan_desc* d) {
-  int64_t tiles = 0;
-  with_lanes(d->N, [&](auto l) {
-    tiles = ceil_div(d->D / d->G, ForwardShape<decltype(l)::value>::CH);
+// Forward launches.  A SIMD issues a vector instruction of one wave only every other turn, and more waves hide what the recurrence waits
+// for, so what counts is waves.  Where the channels give fewer than 2048, two per SIMD, the time axis is cut into chunks, up to eight
+// waves per SIMD, whose ends are computed first (70 % of the work once more).
+#ifndef SCAN_WANT
+#define SCAN_WANT 8192
+#endif
+constexpr int MIN_CHUNK = 32, MAX_CHUNKS = 64;
+struct Cut {
+  int tiles;           // workgroups per group of channels
+  int chunk, chunks;   // steps per chunk, a multiple of a block's
+};
+template <typename F>
+int with_shape(int N, F&& f) {
+  if (N <= 4) return f(ForwardShape<1, 4>{});
+  if (N <= 8) return f(ForwardShape<2, 4>{});
+  if (N <= 16) return f(ForwardShape<4, 4>{});
+  if (N <= 32) return f(ForwardShape<8, 4>{});
+  return f(ForwardShape<16, 4>{});
+}
+Cut forward_cut(const mebptt_scan_desc* d) {
+  Cut c = {};
+  int64_t waves = 0;
+  with_shape(d->N, [&](auto shape) {
+    using S = decltype(shape);
+    c.tiles = (int)ceil_div(d->D / d->G, S::CH * FORWARD_WAVES);
+    waves = ceil_div(d->D / d->G, S::CH) * d->G * std::max(d->B, 1);
     return 0;
   });
-  return tiles;
+  const int64_t t = std::max(d->t, 1);
+  const int64_t want = waves >= 2048 ? 1 : std::min<int64_t>(MAX_CHUNKS, ceil_div(SCAN_WANT, waves));
+  c.chunk = (int)(ceil_div(std::max<int64_t>(want > 1 ? MIN_CHUNK : t, ceil_div(t, want)), 16) * 16);
+  c.chunks = (int)ceil_div(t, c.chunk);
+  return c;
 }
-struct Cut { int chunk, chunks; };
-Cut cut_of(const mebptt_scan_desc* d, int64_t workgroups, int unit) {
-  const int64_t t = std::max(d->t, 1), want = ceil_div(2048, std::max<int64_t>(1, workgroups));
-  int64_t chunk = std::max<int64_t>(MIN_CHUNK, ceil_div(t, want));
-  chunk = ceil_div(chunk, unit) * unit;
-  const int64_t chunks = ceil_div(t, chunk);
-  return workgroups >= 1024 || chunks < 2 ? Cut{(int)(ceil_div(t, unit) * unit), 1} : Cut{(int)chunk, (int)chunks};
-}
-Cut forward_cut(const mebptt_scan_desc* d) { return cut_of(d, forward_tiles(d) * d->G * d->B, 16); }
 size_t starts_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * d->N * sizeof(float)); }
 size_t sums_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * sizeof(float)); }
 
-int64_t back_tiles(const mebptt_scan_desc* d) {
-  int64_t tiles = 0;
-  with_lanes(d->N, [&](auto l) {
-    tiles = ceil_div(d->D / d->G, BackwardShape<decltype(l)::value>::CH);
+// Backward launches: 2 states per lane, so that what a block keeps (exp(w A) and exp(w A) h of 16 steps) leaves room for four waves per SIMD;
+// 4 only where N is beyond 32.  The time axis is cut as the forward pass's is, in whole stretches.
+struct BackCut {
+  int tiles, ends_tiles, chunk, chunks;
+};
+template <typename F>
+int with_back_shape(int N, F&& f) {
+  if (N <= 4) return f(BackwardShape<2, 2>{});
+  if (N <= 8) return f(BackwardShape<4, 2>{});
+  if (N <= 16) return f(BackwardShape<8, 2>{});
+  if (N <= 32) return f(BackwardShape<16, 2>{});
+  return f(BackwardShape<16, 4>{});
+}
+BackCut back_cut(const mebptt_scan_desc* d) {
+  BackCut c = {};
+  int64_t waves = 0;
+  with_back_shape(d->N, [&](auto shape) {
+    using S = decltype(shape);
+    c.tiles = (int)ceil_div(d->D / d->G, S::CH);
+    waves = ceil_div(d->D / d->G, S::CW) * d->G * std::max(d->B, 1);
     return 0;
   });
-  return tiles;
+  with_shape(d->N, [&](auto shape) {
+    c.ends_tiles = (int)ceil_div(d->D / d->G, decltype(shape)::CH * FORWARD_WAVES);
+    return 0;
+  });
+  const int64_t t = std::max(d->t, 1);
+  const int64_t want = waves >= 2048 ? 1 : std::min<int64_t>(MAX_CHUNKS, ceil_div(4096, waves));
+  c.chunk = (int)(ceil_div(ceil_div(t, want), d->stretch) * d->stretch);
+  c.chunks = (int)ceil_div(t, c.chunk);
+  return c;
 }
-size_t bc_bytes(const mebptt_scan_desc* d) {
-  return align_up((size_t)back_tiles(d) * d->t * d->B * d->G * 2 * d->N * sizeof(float));
+size_t bc_bytes(const mebptt_scan_desc* d, const BackCut& c) {
+  return align_up((size_t)c.tiles * d->t * d->B * d->G * 2 * d->N * sizeof(float));
 }
-size_t a_bytes(const mebptt_scan_desc* d) { return align_up((size_t)d->B * d->D * (d->N + 2) * sizeof(float)); }
+size_t a_bytes(const mebptt_scan_desc* d, const BackCut& c) { return align_up((size_t)c.chunks * d->B * d->D * (d->N + 2) * sizeof(float)); }
 
-template <typename T, int NL>
+template <typename S>
 size_t back_lds(int stretch) {
-  using S = BackwardShape<NL>;
-  // (the last part also holds two floats per thread at the end)
-  return ((size_t)BS * S::CH * 4 + BS * 2 * S::NP + std::max(BACK_WAVES * BS * 2 * S::NP, 2 * S::THREADS) +
-          (size_t)stretch / BS * S::THREADS * NB) * sizeof(float);
+  return ((size_t)BS * S::CH * 4 + 2 * BS * S::NP + S::BACK_WAVES * BS * 2 * S::NP + (size_t)stretch / BS * S::THREADS * S::NB) * sizeof(float);
 }
 
 }  // namespace
@@ -750,7 +912,11 @@ size_t mebptt_scan_state_bytes(const mebptt_scan_desc* d) {
 
 size_t mebptt_scan_workspace_bytes(const mebptt_scan_desc* d, int32_t backward) {
   if (check(d) != MEBPTT_OK) return 0;
-  if (backward) return bc_bytes(d) + a_bytes(d);
+  if (backward) {
+    if (check_stretch(d) != MEBPTT_OK) return 0;
+    const BackCut c = back_cut(d);
+    return bc_bytes(d, c) + a_bytes(d, c) + starts_bytes(d, c.chunks) + sums_bytes(d, c.chunks);
+  }
   const int chunks = forward_cut(d).chunks;
   return starts_bytes(d, chunks) + sums_bytes(d, chunks);
 }
@@ -770,20 +936,15 @@ int mebptt_scan_forward(const mebptt_scan_desc* d, const mebptt_scan_inputs* in,
   const Cut cut = forward_cut(d);
   Forward p = {scan_of(d, in), out_seq(y), in->h0, h_out, (float*)states, d->stretch, cut.chunk, cut.chunks,
                (float*)workspace, (float*)((char*)workspace + starts_bytes(d, cut.chunks))};
+  p.in.tiles = cut.tiles;
+  const unsigned wide = (unsigned)(cut.tiles * d->G);
   hipStream_t s = (hipStream_t)stream;
-  return with_lanes(d->N, [&](auto l) {
-    constexpr int NL = decltype(l)::value;
-    p.in.tiles = (int)ceil_div(d->D / d->G, ForwardShape<NL>::CH);
-    const unsigned wide = (unsigned)(p.in.tiles * d->G);
+  return with_shape(d->N, [&](auto shape) {
+    using S = decltype(shape);
     auto go = [&](auto elem) {
       using T = decltype(elem);
-      if (cut.chunks > 1) {
-        scan_forward_kernel<T, NL, true><<<dim3(wide, d->B, cut.chunks - 1), WAVE, 0, s>>>(p);
-        const int64_t BD = (int64_t)d->B * d->D;
-        if (cut.chunks > 2)
-          scan_join_kernel<<<(unsigned)ceil_div(BD * d->N, 256), 256, 0, s>>>(p.starts, p.sums, in->A, BD, d->D, d->N, cut.chunks);
-      }
-      scan_forward_kernel<T, NL, false><<<dim3(wide, d->B, cut.chunks), WAVE, 0, s>>>(p);
+      if (cut.chunks > 1) scan_forward_kernel<T, S, true><<<dim3(wide, d->B, cut.chunks - 1), FORWARD_WAVES * WAVE, 0, s>>>(p);
+      scan_forward_kernel<T, S, false><<<dim3(wide, d->B, cut.chunks), FORWARD_WAVES * WAVE, 0, s>>>(p);
       return launched("mebptt_scan_forward");
     };
     return d->dtype == MEBPTT_FP32 ? go(float{}) : go(__bf16{});
@@ -803,28 +964,42 @@ int mebptt_scan_backward(const mebptt_scan_desc* d, const mebptt_scan_inputs* in
   if (states_bytes < mebptt_scan_state_bytes(d))
     return set_error(MEBPTT_EWORKSPACE, "states have %zu bytes, %zu needed", states_bytes, mebptt_scan_state_bytes(d));
   if ((rc = check_workspace(workspace, workspace_bytes, mebptt_scan_workspace_bytes(d, 1)))) return rc;
+  const BackCut cut = back_cut(d);
   hipStream_t s = (hipStream_t)stream;
-  float *bc = (float*)workspace, *ap = (float*)((char*)workspace + bc_bytes(d));
+  float *bc = (float*)workspace, *ap = (float*)((char*)bc + bc_bytes(d, cut)), *starts = (float*)((char*)ap + a_bytes(d, cut));
   if (d->B) {
-    Backward p = {scan_of(d, in), in_seq(dy), out_seq(grads->du), out_seq(grads->ddelta), out_seq(grads->dz), in->h0,
-                  (const float*)states, dh_out, grads->dh0, bc, ap, d->stretch};
-    rc = with_lanes(d->N, [&](auto l) {
-      constexpr int NL = decltype(l)::value;
-      p.in.tiles = (int)back_tiles(d);
-      const dim3 grid((unsigned)(p.in.tiles * d->G), d->B);
-      auto go = [&](auto elem) {
-        using T = decltype(elem);
-        const size_t lds = back_lds<T, NL>(d->stretch);
-        const hipError_t e = allow_dynamic_lds<scan_backward_kernel<T, NL>>(back_lds<T, NL>(256));
-        if (e != hipSuccess) return set_error(MEBPTT_EHIP, "mebptt_scan_backward: %s", hipGetErrorString(e));
-        scan_backward_kernel<T, NL><<<grid, BACK_WAVES * WAVE, lds, s>>>(p);
+    Backward p = {scan_of(d, in), in_seq(dy), out_seq(grads->du), out_seq(grads->ddelta), out_seq(grads->dz), (const float*)states, dh_out,
+                  grads->dh0, bc, ap, d->stretch, cut.chunk, cut.chunks, starts, (float*)((char*)starts + starts_bytes(d, cut.chunks))};
+    auto go = [&](auto elem, auto gate) {
+      using T = decltype(elem);
+      constexpr bool GATE = decltype(gate)::value;
+      if (cut.chunks > 1)
+        with_shape(d->N, [&](auto shape) {
+          p.in.tiles = cut.ends_tiles;
+          scan_back_ends_kernel<T, decltype(shape), GATE>
+              <<<dim3((unsigned)(cut.ends_tiles * d->G), d->B, cut.chunks - 1), FORWARD_WAVES * WAVE, 0, s>>>(p);
+          return 0;
+        });
+      return with_back_shape(d->N, [&](auto shape) {
+        using S = decltype(shape);
+        const hipError_t e = allow_dynamic_lds<scan_backward_kernel<T, S, GATE>>(back_lds<S>(256));
+        if (e != hipSuccess) {
+          (void)hipGetLastError();   // reported here, and not by the next call as well
+          return set_error(MEBPTT_EHIP, "mebptt_scan_backward: %s", hipGetErrorString(e));
+        }
+        p.in.tiles = cut.tiles;
+        scan_backward_kernel<T, S, GATE>
+            <<<dim3((unsigned)(cut.tiles * d->G), d->B, cut.chunks), S::THREADS, back_lds<S>(d->stretch), s>>>(p);
         return launched("mebptt_scan_backward");
-      };
-      return d->dtype == MEBPTT_FP32 ? go(float{}) : go(__bf16{});
-    });
+      });
+    };
+    const std::true_type gate{};
+    const std::false_type none{};
+    if (d->dtype == MEBPTT_FP32) rc = in->z.data ? go(float{}, gate) : go(float{}, none);
+    else rc = in->z.data ? go(__bf16{}, gate) : go(__bf16{}, none);
     if (rc) return rc;
     if (d->t) {
-      const Shared q = {bc, out_seq(grads->dBm), out_seq(grads->dCm), d->t, d->B, d->G, d->N, p.in.tiles};
+      const Shared q = {bc, out_seq(grads->dBm), out_seq(grads->dCm), d->t, d->B, d->G, d->N, cut.tiles};
       const unsigned grid = (unsigned)std::min<int64_t>(ceil_div((int64_t)d->t * d->B * d->G * 2 * d->N, 256), 4096);
       if (d->dtype == MEBPTT_FP32) scan_shared_kernel<float><<<grid, 256, 0, s>>>(q);
       else scan_shared_kernel<__bf16><<<grid, 256, 0, s>>>(q);
@@ -832,8 +1007,9 @@ int mebptt_scan_backward(const mebptt_scan_desc* d, const mebptt_scan_inputs* in
     }
   }
   const int64_t DN = (int64_t)d->D * d->N;
-  scan_params_kernel<<<(unsigned)ceil_div(DN + 2 * (int64_t)d->D, 256), 256, 0, s>>>(ap, d->B, DN, d->D, grads->dA, grads->dskip, grads->ddelta_bias);
-  return launched("mebptt_scan_backward");
+  float* const outs[3] = {grads->dA, grads->dskip, grads->ddelta_bias};
+  const int64_t cols[3] = {DN, d->D, d->D};
+  return sum_parts(ap, d->B ? (int64_t)cut.chunks * d->B : 0, 3, cols, outs, s);
 }
 
 int mebptt_scan_step(const mebptt_scan_desc* d, const mebptt_scan_inputs* in, const float* state_in, int64_t slots, const int32_t* index,

@@ -517,7 +517,7 @@ int mebptt_conv_step(const mebptt_conv_desc* desc, const void* x, int64_t ldx, c
                      const void* state_in, int64_t slots, const int32_t* index, void* y, int64_t ldy, void* state_out,
                      void* stream);
 
-/* (For the scan, stride_t is 0 .. 2^26 elements.)
+/* (For the scan, stride_t is 0 .. 2^25 elements.)
  *
  * Selective scan over D channels of N states each.  With G groups, channel d reads row d / (D / G) of B and C:
  *     w_s = delta_s + delta_bias, through softplus if asked;   h_s = exp(w_s A) h_{s-1} + w_s u_s B_s;

@@ -18,10 +18,12 @@ constexpr int NB = 4;              // states per lane
 constexpr int MAX_N = 64;
 constexpr float LOG2E = 1.4426950408889634f;
 
-struct Seq { const void* p; int64_t t, b; };
-struct SeqOut { void* p; int64_t t, b; };
-inline Seq in_seq(const mebptt_seq& s) { return {s.data, s.stride_t, s.stride_b}; }
-inline SeqOut out_seq(const mebptt_seq& s) { return {s.data, s.stride_t, s.stride_b}; }
+constexpr int64_t MAX_STRIDE = 1 << 25;   // over steps, in elements: 15 rows of 4 bytes are below 2^32
+struct Seq { const void* p; int64_t b; int t; };
+struct SeqOut { void* p; int64_t b; int t; };
+// (a stride that is never used, of a sequence of one step, may be anything)
+inline Seq in_seq(const mebptt_seq& s) { return {s.data, s.stride_b, (int)std::min(std::max<int64_t>(s.stride_t, 0), MAX_STRIDE)}; }
+inline SeqOut out_seq(const mebptt_seq& s) { return {s.data, s.stride_b, (int)std::min(std::max<int64_t>(s.stride_t, 0), MAX_STRIDE)}; }
 
 struct Scan {
   Seq u, delta, z, Bm, Cm;
@@ -35,9 +37,13 @@ __device__ inline float at(const Seq& q, int64_t s, int64_t b, int64_t c) { retu
 template <typename T>
 __device__ inline void put(const SeqOut& q, int64_t s, int64_t b, int64_t c, float v) { ((T*)q.p)[s * q.t + b * q.b + c] = (T)v; }
 
-// The same with an address in two parts: uniform over the wave, and a lane's own, at most seven rows in bytes.
+// The same with an address in two parts: uniform over the wave, and a lane's own, of at most 15 rows, in bytes.
 template <typename T>
-__device__ inline unsigned lane_bytes(int64_t stride, int row, int c) { return (unsigned)((row * stride + c) * (int64_t)sizeof(T)); }
+__device__ inline unsigned lane_bytes(int stride, int row, int c) { return (unsigned)(row * stride + c) * (unsigned)sizeof(T); }
+template <typename T>
+__device__ inline const T* row_of(const Seq& q, int s, int b, int64_t c) { return (const T*)q.p + (int64_t)s * q.t + b * q.b + c; }
+template <typename T>
+__device__ inline T* row_of(const SeqOut& q, int s, int b, int64_t c) { return (T*)q.p + (int64_t)s * q.t + b * q.b + c; }
 __device__ inline unsigned opaque(unsigned v) {
   asm volatile("" : "+v"(v));
   return v;
@@ -166,12 +172,6 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
   const bool pair = TS * CH >= WAVE || lane < TS * CH, shared = TS * NP >= WAVE || lane < TS * NP;
   const float bias = in.bias ? in.bias[min(c0 + ch, in.D - 1)] : 0.0f, skip = in.skip ? in.skip[min(c0 + ch, in.D - 1)] : 0.0f;
   const int64_t gn = (int64_t)group * in.N;
-  const T* const pu = (const T*)in.u.p + b * in.u.b + c0;
-  const T* const pd = (const T*)in.delta.p + b * in.delta.b + c0;
-  const T* const pz = (const T*)in.z.p + b * in.z.b + c0;
-  const T* const pb = (const T*)in.Bm.p + b * in.Bm.b + gn;
-  const T* const pc = (const T*)in.Cm.p + b * in.Cm.b + gn;
-  T* const py = (T*)p.y.p + b * p.y.b + c0;
 
   // The next block's inputs, fetched while a block is worked on.  A whole block (all its steps within the sequence, all its channels
   // there) needs no masks; which it is, is the same for the whole wave.
@@ -183,8 +183,9 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
     const unsigned ou = opaque(lane_bytes<T>(in.u.t, row, ch)), od = opaque(lane_bytes<T>(in.delta.t, row, ch)),
                    oz = opaque(lane_bytes<T>(in.z.t, row, ch)), ob = opaque(lane_bytes<T>(in.Bm.t, srow, sk)),
                    oc = opaque(lane_bytes<T>(in.Cm.t, srow, sk));
-    const T *au = pu + s0 * in.u.t, *ad = pd + s0 * in.delta.t, *az = pz + s0 * in.z.t, *ab = pb + s0 * in.Bm.t, *ac = pc + s0 * in.Cm.t;
-    const int64_t iu = ROWS * in.u.t, id = ROWS * in.delta.t, iz = ROWS * in.z.t, ib = SROWS * in.Bm.t, ic = SROWS * in.Cm.t;
+    const T *au = row_of<T>(in.u, s0, b, c0), *ad = row_of<T>(in.delta, s0, b, c0), *az = row_of<T>(in.z, s0, b, c0),
+            *ab = row_of<T>(in.Bm, s0, b, gn), *ac = row_of<T>(in.Cm, s0, b, gn);
+    const int iu = ROWS * in.u.t, id = ROWS * in.delta.t, iz = ROWS * in.z.t, ib = SROWS * in.Bm.t, ic = SROWS * in.Cm.t;
     if (whole(s0)) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
@@ -295,9 +296,9 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) y[i] *= cz[i] * sigmoid(cz[i]);
       }
-      T* ay = py + s0 * p.y.t;
+      T* ay = row_of<T>(p.y, s0, b, c0);
       const unsigned oy = opaque(lane_bytes<T>(p.y.t, row, ch));
-      const int64_t iy = ROWS * p.y.t;
+      const int iy = ROWS * p.y.t;
       if (all) {
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) {
@@ -405,9 +406,10 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     A2[n] = A[n] * LOG2E;
     dA[n] = g[n] = h[n] = 0.0f;
   }
-  if (p.dh_out) load_states(p.dh_out + bd * in.N, q * NB, in.N, g);
+  // (channels beyond the workgroup's keep zeros in h and g: their w, w u and dy are zeros, and so is what they add to dB and dC)
+  if (p.dh_out && mine) load_states(p.dh_out + bd * in.N, q * NB, in.N, g);
   // through the chunks after this one
-  for (int k = p.chunks - 1; k > chunk; --k) {
+  for (int k = p.chunks - 1; mine && k > chunk; --k) {
     float e[NB];
     load_states(p.starts + k * all_states + bd * in.N, q * NB, in.N, e);
     const float w = p.sums[(int64_t)k * in.B * in.D + bd];
@@ -428,39 +430,57 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
 
   float ru[S::ITEMS], rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
   auto fetch = [&](int s0, bool back) {
-    const bool all = s0 + BS <= len && nch == CH;
-    const T* au = (const T*)in.u.p + b * in.u.b + c0 + wave_c + (s0 + wrow) * in.u.t;
-    const T* ad = (const T*)in.delta.p + b * in.delta.b + c0 + wave_c + (s0 + wrow) * in.delta.t;
-    const T* ag = (const T*)p.dy.p + b * p.dy.b + c0 + wave_c + (s0 + wrow) * p.dy.t;
-    const T* az = (const T*)in.z.p + b * in.z.b + c0 + wave_c + (s0 + wrow) * in.z.t;
-    const unsigned ou = lane_bytes<T>(in.u.t, lrow, lane_c), od = lane_bytes<T>(in.delta.t, lrow, lane_c),
-                   og = lane_bytes<T>(p.dy.t, lrow, lane_c), oz = lane_bytes<T>(in.z.t, lrow, lane_c);
+    const unsigned ou = opaque(lane_bytes<T>(in.u.t, lrow, lane_c)), od = opaque(lane_bytes<T>(in.delta.t, lrow, lane_c)),
+                   og = opaque(lane_bytes<T>(p.dy.t, lrow, lane_c)), oz = opaque(lane_bytes<T>(in.z.t, lrow, lane_c));
+    const T *au = row_of<T>(in.u, s0 + wrow, b, c0 + wave_c), *ad = row_of<T>(in.delta, s0 + wrow, b, c0 + wave_c),
+            *ag = row_of<T>(p.dy, s0 + wrow, b, c0 + wave_c), *az = row_of<T>(in.z, s0 + wrow, b, c0 + wave_c);
+    if (s0 + BS <= len && nch == CH) {
 #pragma unroll
-    for (int i = 0; i < S::ITEMS; ++i) {
-      ru[i] = rd[i] = rg[i] = rz[i] = 0.0f;
-      if (all || (s0 + i * ROWS + row < len && ic < nch)) {
+      for (int i = 0; i < S::ITEMS; ++i) {
         ru[i] = elem(au, ou);
         rd[i] = elem(ad, od);
-        if (back) {
+        au += ROWS * in.u.t;
+        ad += ROWS * in.delta.t;
+      }
+      if (back) {
+#pragma unroll
+        for (int i = 0; i < S::ITEMS; ++i) {
           rg[i] = elem(ag, og);
           if (GATE) rz[i] = elem(az, oz);
+          ag += ROWS * p.dy.t;
+          az += ROWS * in.z.t;
         }
       }
-      au += ROWS * in.u.t;
-      ad += ROWS * in.delta.t;
-      ag += ROWS * p.dy.t;
-      az += ROWS * in.z.t;
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i) {
+        ru[i] = rd[i] = rg[i] = rz[i] = 0.0f;
+        if (s0 + i * ROWS + row < len && ic < nch) {
+          ru[i] = elem(au, ou);
+          rd[i] = elem(ad, od);
+          if (back) {
+            rg[i] = elem(ag, og);
+            if (GATE) rz[i] = elem(az, oz);
+          }
+        }
+        au += ROWS * in.u.t;
+        ad += ROWS * in.delta.t;
+        ag += ROWS * p.dy.t;
+        az += ROWS * in.z.t;
+      }
     }
 #pragma unroll
     for (int i = 0; i < S::SHARED; ++i) {
       const int s = s0 + i * SROWS + srow;
       rb[i] = rc[i] = 0.0f;
       if (shared && s < len && sn < in.N) {
-        rb[i] = at<T>(in.Bm, s, b, gn + sn);
-        if (back) rc[i] = at<T>(in.Cm, s, b, gn + sn);
+        rb[i] = elem(row_of<T>(in.Bm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Bm.t, srow, sn));
+        if (back) rc[i] = elem(row_of<T>(in.Cm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Cm.t, srow, sn));
       }
     }
   };
+#pragma unroll
+  for (int i = 0; i < S::ITEMS; ++i) rg[i] = rz[i] = 0.0f;
 
   const int from = chunk * p.chunk / p.stretch, last_step = min(in.t, (chunk + 1) * p.chunk);
   auto blocks_of = [&](int st) { return (min(last_step, (st + 1) * p.stretch) - st * p.stretch + BS - 1) / BS; };
@@ -484,7 +504,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         idz[i] = rg[i] * sg * (1.0f + rz[i] * (1.0f - sg));    // times what the gate multiplied
         idy[i] = rg[i] * rz[i] * sg;
       }
-      *reinterpret_cast<f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x4{iw[i], iw[i] * iu[i], idy[i], 0.0f};
+      *reinterpret_cast<f32x3*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x3{iw[i], iw[i] * iu[i], idy[i]};
     }
     if (shared) {
 #pragma unroll
@@ -493,7 +513,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         sc[(i * SROWS + srow) * NP + sn] = rc[i];
       }
     }
-    if (k == 0 && (!back || blocks == 1)) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, h);
+    if (mine && k == 0 && (!back || blocks == 1)) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, h);
     __syncthreads();
     // the block after this one
     int next_st = st, next_k = k;
@@ -537,13 +557,25 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
           h[n] = ah[s][n] + w[1] * vb[n];
         }
       }
-      // and back
+      // and back; a step's operands are read while the one before is worked on, whose results go over its own
+      f32x3 next_w = *reinterpret_cast<const f32x3*>(wud + 4 * ((BS - 1) * CH + cl));
+      float next_b[NB], next_c[NB];
+      load<NB>(sb + (BS - 1) * NP + q * NB, next_b);
+      load<NB>(sc + (BS - 1) * NP + q * NB, next_c);
 #pragma unroll
       for (int s = BS - 1; s >= 0; --s) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(wud + 4 * (s * CH + cl));
+        const f32x3 w = next_w;
         float vb[NB], vc[NB], v[2 * NB], through = 0.0f, dlog = 0.0f, core = 0.0f;
-        load<NB>(sb + s * NP + q * NB, vb);
-        load<NB>(sc + s * NP + q * NB, vc);
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+          vb[n] = next_b[n];
+          vc[n] = next_c[n];
+        }
+        if (s > 0) {
+          next_w = *reinterpret_cast<const f32x3*>(wud + 4 * ((s - 1) * CH + cl));
+          load<NB>(sb + (s - 1) * NP + q * NB, next_b);
+          load<NB>(sc + (s - 1) * NP + q * NB, next_c);
+        }
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const float hn = ah[s][n] + w[1] * vb[n];
@@ -557,31 +589,33 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
           dA[n] += r * w[0];
           g[n] *= a[s][n];
         }
-        if (!mine) {
-#pragma unroll
-          for (int n = 0; n < 2 * NB; ++n) v[n] = 0.0f;
-        }
         channels_sum<S>(v, lane, red + (wave * BS + s) * 2 * NP);
         through = lanes_sum<NL>(through);
         dlog = lanes_sum<NL>(dlog);
         if (GATE) core = lanes_sum<NL>(core);
-        *reinterpret_cast<f32x4*>(wud + 4 * (s * CH + cl)) = f32x4{through, dlog, core, 0.0f};   // (all lanes of a channel the same)
+        *reinterpret_cast<f32x3*>(wud + 4 * (s * CH + cl)) = f32x3{through, dlog, core};   // (all lanes of a channel the same)
       }
       __syncthreads();
+      T *bu = row_of<T>(p.du, s0 + wrow, b, c0 + wave_c), *bd2 = row_of<T>(p.ddelta, s0 + wrow, b, c0 + wave_c),
+        *bz = row_of<T>(p.dz, s0 + wrow, b, c0 + wave_c);
+      const unsigned ou = opaque(lane_bytes<T>(p.du.t, lrow, lane_c)), od = opaque(lane_bytes<T>(p.ddelta.t, lrow, lane_c)),
+                     oz = opaque(lane_bytes<T>(p.dz.t, lrow, lane_c));
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
         const int s = s0 + i * ROWS + row;
+        const f32x3 v = *reinterpret_cast<const f32x3*>(wud + 4 * ((i * ROWS + row) * CH + ic));
+        const bool live = s < len;
+        const float dw = live ? (iu[i] * v[0] + v[1]) * isig[i] : 0.0f;
         if (s < last_step && ic < nch) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic));
-          const bool live = s < len;
-          const float dw = live ? (iu[i] * v[0] + v[1]) * isig[i] : 0.0f;
-          const int64_t sw = s0 + i * ROWS + wrow;
-          set_elem((T*)p.du.p + sw * p.du.t + b * p.du.b + c0 + wave_c, lane_bytes<T>(p.du.t, lrow, lane_c), live ? iw[i] * v[0] + skip * idy[i] : 0.0f);
-          set_elem((T*)p.ddelta.p + sw * p.ddelta.t + b * p.ddelta.b + c0 + wave_c, lane_bytes<T>(p.ddelta.t, lrow, lane_c), dw);
-          if (GATE) set_elem((T*)p.dz.p + sw * p.dz.t + b * p.dz.b + c0 + wave_c, lane_bytes<T>(p.dz.t, lrow, lane_c), live ? idz[i] * (v[2] + skip * iu[i]) : 0.0f);
+          set_elem(bu, ou, live ? iw[i] * v[0] + skip * idy[i] : 0.0f);
+          set_elem(bd2, od, dw);
+          if (GATE) set_elem(bz, oz, live ? idz[i] * (v[2] + skip * iu[i]) : 0.0f);
           dskip += idy[i] * iu[i];
           dbias += dw;
         }
+        bu += ROWS * p.du.t;
+        bd2 += ROWS * p.ddelta.t;
+        bz += ROWS * p.dz.t;
       }
       for (int m = tid; m < BS * 2 * NP; m += THREADS) {
         const int s = m / (2 * NP), half = m / NP % 2, n = m % NP;
@@ -644,16 +678,13 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_back_ends_kernel(Bac
   const int row = lane / CH, ch = lane % CH, srow = lane / NP, sn = lane % NP;
   const bool pair = TS * CH >= WAVE || lane < TS * CH, shared = TS * NP >= WAVE || lane < TS * NP;
   const float bias = in.bias ? in.bias[min(c0 + ch, in.D - 1)] : 0.0f;
-  const T* const pd = (const T*)in.delta.p + b * in.delta.b + c0;
-  const T* const pg = (const T*)p.dy.p + b * p.dy.b + c0;
-  const T* const pz = (const T*)in.z.p + b * in.z.b + c0;
-  const T* const pc = (const T*)in.Cm.p + b * in.Cm.b + gn;
   float rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rc[S::SHARED];
   auto fetch = [&](int s0) {
     const bool all = s0 + TS <= stop && nch == CH;
     const unsigned od = opaque(lane_bytes<T>(in.delta.t, row, ch)), og = opaque(lane_bytes<T>(p.dy.t, row, ch)),
                    oz = opaque(lane_bytes<T>(in.z.t, row, ch)), oc = opaque(lane_bytes<T>(in.Cm.t, srow, min(sn, in.N - 1)));
-    const T *ad = pd + s0 * in.delta.t, *ag = pg + s0 * p.dy.t, *az = pz + s0 * in.z.t, *ac = pc + s0 * in.Cm.t;
+    const T *ad = row_of<T>(in.delta, s0, b, c0), *ag = row_of<T>(p.dy, s0, b, c0), *az = row_of<T>(in.z, s0, b, c0),
+            *ac = row_of<T>(in.Cm, s0, b, gn);
 #pragma unroll
     for (int i = 0; i < S::ITEMS; ++i) {
       rd[i] = rg[i] = rz[i] = 0.0f;
@@ -799,8 +830,7 @@ int check_stretch(const mebptt_scan_desc* d) {
   const int s = d->stretch;
   return s == 16 || s == 32 || s == 64 || s == 128 || s == 256 ? MEBPTT_OK : set_error(MEBPTT_EINVAL, "stretch must be 16, 32, 64, 128 or 256");
 }
-// A lane's part of an address is 32 bits, of up to seven rows of four bytes.
-bool stride_fits(const mebptt_seq& s) { return s.stride_t >= 0 && s.stride_t <= (1 << 26); }
+bool stride_fits(const mebptt_seq& s) { return s.stride_t >= 0 && s.stride_t <= MAX_STRIDE; }
 int check_inputs(const mebptt_scan_desc* d, const mebptt_scan_inputs* in) {
   if (!in) return set_error(MEBPTT_EINVAL, "inputs are NULL");
   if (!in->A) return set_error(MEBPTT_EINVAL, "A is NULL");
@@ -808,12 +838,12 @@ int check_inputs(const mebptt_scan_desc* d, const mebptt_scan_inputs* in) {
     return set_error(MEBPTT_EINVAL, "u, delta, B and C are required");
   if (d->t > 1)
     for (const mebptt_seq* q : {&in->u, &in->delta, &in->z, &in->Bm, &in->Cm})
-      if (q->data && !stride_fits(*q)) return set_error(MEBPTT_EINVAL, "stride_t must be 0 .. 2^26");
+      if (q->data && !stride_fits(*q)) return set_error(MEBPTT_EINVAL, "stride_t must be 0 .. 2^25");
   return MEBPTT_OK;
 }
 int check_out(const mebptt_scan_desc* d, const mebptt_seq& s, int64_t channels, const char* what) {
   if (d->t && d->B && !s.data) return set_error(MEBPTT_EINVAL, "%s is NULL", what);
-  if (d->t > 1 && !stride_fits(s)) return set_error(MEBPTT_EINVAL, "stride_t must be 0 .. 2^26");
+  if (d->t > 1 && !stride_fits(s)) return set_error(MEBPTT_EINVAL, "stride_t must be 0 .. 2^25");
   if (!rows_apart(s, d->t, d->B, channels)) return set_error(MEBPTT_EINVAL, "rows of %s overlap", what);
   return MEBPTT_OK;
 }

@@ -479,7 +479,7 @@ int mebptt_norm_backward(const mebptt_norm_desc* desc, const void* r, int64_t ld
  *        stored); b_scale [N] fp32; bias [N] fp32 or NULL.  write: out [M, N], row stride ldo.
  * K = 0 gives the bias. */
 typedef struct {
-  int64_t M;         /* 0 .. 2^29 */
+  int64_t M;         /* 0 .. 2^28; M * N at most 2^38 */
   int32_t N, K;      /* N 1 .. 2^21, K 0 .. 131071 */
   int32_t out_dtype; /* MEBPTT_FP32 or MEBPTT_BF16 */
 } mebptt_int8_desc;

@@ -114,9 +114,12 @@ __global__ __launch_bounds__(THREADS) void conv_forward_kernel(Conv p) {
 // dL/dx_p = sum_j w_j dpre_{p+W-1-j} (+ dstate_out where p is one of the last W - 1 inputs), dpre = dy act'(pre), for p from -(W-1), the
 // state's rows, to the sequence's end.  A wave takes 64 groups of channels; its workgroup's four waves, and the workgroup's later turns, different
 // stretches of steps and sequences, adding dweight and dbias up in registers.
+#ifndef CB
+#define CB 3
+#endif
 template <typename T, int W, int V>
-__global__ __launch_bounds__(THREADS) void conv_backward_kernel(ConvBack p) {
-  constexpr int WAVES = THREADS / WAVE;
+__global__ __launch_bounds__(THREADS, W <= 4 ? CB : 2) void conv_backward_kernel(ConvBack p) {
+  constexpr int WAVES = THREADS / WAVE, U = 4;
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
   const int group = blockIdx.x * WAVE + lane, c = group * V;
   const bool mine = group < p.groups;
@@ -145,65 +148,80 @@ __global__ __launch_bounds__(THREADS) void conv_backward_kernel(ConvBack p) {
       const int from = max(first, 0);
 #pragma unroll
       for (int j = 0; j < W - 1; ++j) input<T, W, V>(x, p.xt, state, p.C, from - (W - 1) + j, len, h[j]);
-      for (int s = first; s < live + W - 1; ++s) {
-        // dpre of step s
-        const bool step = s >= 0 && s < len;
-        float d[V];
-        if (s >= 0) {
-          input<T, W, V>(x, p.xt, nullptr, p.C, s, len, h[W - 1]);
-          if (step) {
-            load<V>(dy + s * p.gt, d);
-          } else {
+      // dpre of a step, from its input (already the last of h) and d = dy; OWN: a step that dweight counts here
+      auto through = [&](float (&d)[V], bool own) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) d[e] = 0.0f;
+        for (int e = 0; e < V; ++e) {
+          if (p.silu) {
+            float v = wb[e];
+#pragma unroll
+            for (int j = 0; j < W; ++j) v += w[j][e] * h[j][e];
+            const float sg = sigmoid(v);
+            d[e] *= sg * (1.0f + v * (1.0f - sg));
           }
+          if (own) {
+            dbias[e] += d[e];
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            if (p.silu) {
-              float v = wb[e];
-#pragma unroll
-              for (int j = 0; j < W; ++j) v += w[j][e] * h[j][e];
-              const float sg = sigmoid(v);
-              d[e] *= sg * (1.0f + v * (1.0f - sg));
-            }
-            if (s < s1) {   // its own step: dweight counts every step once
-              dbias[e] += d[e];
-#pragma unroll
-              for (int j = 0; j < W; ++j) dw[j][e] += d[e] * h[j][e];
-            }
+            for (int j = 0; j < W; ++j) dw[j][e] += d[e] * h[j][e];
           }
-#pragma unroll
-          for (int j = 0; j < W - 1; ++j)
-#pragma unroll
-            for (int e = 0; e < V; ++e) h[j][e] = h[j + 1][e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e) d[e] = 0.0f;
         }
 #pragma unroll
-        for (int e = 0; e < V; ++e) g[W - 1][e] = d[e];
-        const int q = s - (W - 1);                                  // whose gradient is now whole
-        if (q >= first) {
-          float v[V];
-          const int r = q - (len - (W - 1));                        // its row of the state after the last step
-          if (r >= 0 && dlast) {
-            load<V>(dlast + (int64_t)r * p.C, v);
-          } else {
+        for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = 0.0f;
-          }
+          for (int e = 0; e < V; ++e) h[j][e] = h[j + 1][e];
+      };
+      // what a step of dpre completes: the gradient of the position W - 1 before
+      auto gather = [&](const float (&d)[V], float (&v)[V]) {
 #pragma unroll
-          for (int e = 0; e < V; ++e)
+        for (int e = 0; e < V; ++e) {
+          g[W - 1][e] = d[e];
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[e] += w[W - 1 - j][e] * g[j][e];
-          if (q >= 0) store<V>(dx + q * p.dt, v);
-          else if (dfirst) store<V>(dfirst + (int64_t)(q + W - 1) * p.C, v);
+          for (int j = 0; j < W; ++j) v[e] += w[W - 1 - j][e] * g[j][e];
         }
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
 #pragma unroll
           for (int e = 0; e < V; ++e) g[j][e] = g[j + 1][e];
+      };
+      // any step: before the first one, past the last, at a stretch's ends
+      auto any = [&](int s) {
+        float d[V] = {}, v[V] = {};
+        if (s >= 0) {
+          input<T, W, V>(x, p.xt, nullptr, p.C, s, len, h[W - 1]);
+          if (s < len) load<V>(dy + s * p.gt, d);
+          through(d, s < s1);
+        }
+        const int q = s - (W - 1), r = q - (len - (W - 1));         // the position, and its row of the state after the last step
+        if (q >= first && r >= 0 && dlast) load<V>(dlast + (int64_t)r * p.C, v);
+        gather(d, v);
+        if (q < first) return;
+        if (q >= 0) store<V>(dx + q * p.dt, v);
+        else if (dfirst) store<V>(dfirst + (int64_t)(q + W - 1) * p.C, v);
+      };
+      int s = first;
+      for (; s < min(from + W - 1, live + W - 1); ++s) any(s);
+      for (; s + U <= live; s += U) {                               // U steps' rows at a time, all of them on their way
+        typedef T Row __attribute__((ext_vector_type(V)));
+        Row xs[U], ds[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) xs[u] = *reinterpret_cast<const Row*>(x + (s + u) * p.xt);
+#pragma unroll
+        for (int u = 0; u < U; ++u) ds[u] = *reinterpret_cast<const Row*>(dy + (s + u) * p.gt);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float d[V], v[V] = {};
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            h[W - 1][e] = (float)xs[u][e];
+            d[e] = (float)ds[u][e];
+          }
+          through(d, true);
+          gather(d, v);
+          store<V>(dx + (s + u - (W - 1)) * p.dt, v);
+        }
       }
+      for (; s < live + W - 1; ++s) any(s);
       const float none[V] = {};
       for (int s = max(s0, live); s < s1; ++s) store<V>(dx + s * p.dt, none);
     }

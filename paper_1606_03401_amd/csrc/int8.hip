@@ -2,8 +2,6 @@
 //     out[m][n] = a_scale[m] * b_scale[n] * sum_k a[m][k] b[n][k] + bias[n]
 // on v_mfma_i32_16x16x64_i8: exact 32-bit sums, one rounding at the end.  b's rows are the instruction's rows, a's its columns, so a
 // lane's four results are neighbours along n and are stored at once.
-#include <cstdlib>
-
 #include "ops.h"
 
 using namespace mebptt;
@@ -69,7 +67,8 @@ __device__ inline void store4(const Product& p, int64_t m, int n, i32x4 acc) {
 // (what eight lanes read at a time) lie in eight different places of 128 bytes.
 __device__ inline int place(int row, int part) { return row * KB + ((part ^ ((row >> 1) & 3)) * 16); }
 
-// 64 x 64 outputs per workgroup, 32 x 32 per wave, operands through LDS one step ahead in registers.  Any size, stride and alignment.
+// 64 x 64 outputs per workgroup, 32 x 32 per wave, operands through LDS one step ahead in registers.  Any size, stride and alignment; in use
+// where K is below 16, less than a lane's load of the others.
 template <typename T>
 __global__ __launch_bounds__(256) void int8_product_kernel(Product p) {
   __shared__ __align__(16) int8_t la[64 * KB], lb[64 * KB];
@@ -303,11 +302,12 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(Product p, int tiles_m, 
 //
 // K is at least 16.  A lane whose 16 bytes would pass K's end reads the last 16 of both rows, those of a that it should not have as zeros.
 template <typename T, int MT, int STEPS, bool HELD>
-__global__ __launch_bounds__(512) void int8_rows_kernel(Product p, int tiles) {
+__global__ __launch_bounds__(512) void int8_rows_kernel(Product p, int tiles, int gx) {
   constexpr int WAVES = 8;
   __shared__ i32x4 red[2][WAVES][MT][WAVE];
   const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), r = lane & 15, g = lane >> 4;
-  const int64_t m0 = (int64_t)blockIdx.y * 16 * MT;
+  const int bx = blockIdx.x % gx;
+  const int64_t m0 = (int64_t)(blockIdx.x / gx) * 16 * MT;
   const int8_t* arow[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) arow[i] = p.a + min(m0 + 16 * i + r, p.M - 1) * p.lda;
@@ -345,20 +345,20 @@ __global__ __launch_bounds__(512) void int8_rows_kernel(Product p, int tiles) {
         acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b[u]), __builtin_bit_cast(i32x4, a[u][i]), acc[i], 0, 0, 0);
   };
   u32x4 a[STEPS][MT], b[STEPS], ahead[STEPS];
-  read_b(blockIdx.x, first, b);
+  read_b(bx, first, b);
   if (HELD) read_a(first, a);
   int turn = 0;
-  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, turn ^= 1) {
+  for (int tile = bx; tile < tiles; tile += gx, turn ^= 1) {
     i32x4 acc[MT] = {};
     if constexpr (HELD) {
-      if (tile + (int)gridDim.x < tiles) read_b(tile + gridDim.x, first, ahead);
+      if (tile + gx < tiles) read_b(tile + gx, first, ahead);
       __builtin_amdgcn_sched_barrier(0);   // the loads first, all of them
       mma(b, a, acc);
     } else {
       for (int s = first; s < last; s += STEPS) {
         read_a(s, a);
         if (s + STEPS < last) read_b(tile, s + STEPS, ahead);
-        else if (tile + (int)gridDim.x < tiles) read_b(tile + gridDim.x, first, ahead);
+        else if (tile + gx < tiles) read_b(tile + gx, first, ahead);
         __builtin_amdgcn_sched_barrier(0);
         mma(b, a, acc);
 #pragma unroll
@@ -383,52 +383,65 @@ __global__ __launch_bounds__(512) void int8_rows_kernel(Product p, int tiles) {
 
 int check(const mebptt_int8_desc* d) {
   if (!d) return set_error(MEBPTT_EINVAL, "desc is NULL");
-  if (d->M < 0 || d->M > (1 << 29)) return set_error(MEBPTT_EINVAL, "M must be 0 .. 2^29");
+  if (d->M < 0 || d->M > (1 << 28)) return set_error(MEBPTT_EINVAL, "M must be 0 .. 2^28");
   if (d->N < 1 || d->N > (1 << 21)) return set_error(MEBPTT_EINVAL, "N must be 1 .. 2^21");
+  if (d->M * d->N > (int64_t)1 << 38) return set_error(MEBPTT_EINVAL, "M * N must not exceed 2^38");
   if (d->K < 0 || d->K > MAX_K) return set_error(MEBPTT_EINVAL, "K must be 0 .. %d: the sums are 32 bits wide", MAX_K);
   if (!float_dtype(d->out_dtype)) return set_error(MEBPTT_EINVAL, "out_dtype must be MEBPTT_FP32 or MEBPTT_BF16");
   return MEBPTT_OK;
 }
 
-#ifndef RG
-#define RG 256
-#endif
-constexpr int ROWS_GROUPS = RG;
+// The three kernels by what a launch is estimated to take, in us, fitted to 15 shapes timed on all of them (M 1 .. 8192, N 512 .. 16384,
+// K 512 .. 8192; within a quarter of the times measured).  One tile alone is bound by its stages' latency, a chip full of them by what
+// the L2s deliver.  Measured, rows / 128 / 256: 32 x 16384 x 4096 20 / 30 / 66, 512 x 512 x 4096 11.5 / 18.8 / 45, 1024 x 4096 x 4096 48 / 25 / 49,
+// 8192 x 4096 x 4096 310 / 221 / 169.
+struct Estimate { double rows, t128, t256; };
+constexpr int ROWS_GROUPS = 256;   // a workgroup per compute unit; two read a twice as often: 26 instead of 20 us at 32 x 16384 x 4096
+Estimate estimate(const Product& p) {
+  const double K = p.K, stages = (double)ceil_div(p.K, KB);
+  const int64_t m_tiles = ceil_div(p.M, p.M <= 16 ? 16 : p.M <= 32 ? 32 : 64);
+  const int64_t t128 = ceil_div(p.M, 128) * ceil_div(p.N, 128), t256 = ceil_div(p.M, 256) * ceil_div(p.N, 256);
+  Estimate e;
+  e.rows = 3 + K / 600 + (double)ceil_div(ceil_div(p.N, 16) * m_tiles, ROWS_GROUPS) * (1.1 + K / 2700);
+  e.t128 = 4 + stages * (t128 <= 256 ? 0.3 : 0.86 * (double)ceil_div(t128, 512));
+  e.t256 = (double)ceil_div(t256, 256) * (13 + stages * (0.52 + 0.58 * (double)std::min<int64_t>(t256, 256) / 256));
+  return e;
+}
+
 template <typename T>
 int launch(const Product& p, hipStream_t stream) {
-  const bool rows16 = aligned(p.a, 16) && aligned(p.b, 16) && p.lda % 16 == 0 && p.ldb % 16 == 0;
-  auto tiles = [&](auto bm, auto bn) {
-    constexpr int BM = decltype(bm)::value, BN = decltype(bn)::value;
-    const int64_t tm = ceil_div(p.M, BM), tn = ceil_div(p.N, BN);
-    int8_tile_kernel<T, BM, BN><<<(unsigned)(ceil_div(tm * tn, 8) * 8), 256, 0, stream>>>(p, (int)tm, (int)tn);
+  using std::integral_constant;
+  auto tiles = [&](auto size) {
+    constexpr int SIZE = decltype(size)::value;
+    const int64_t tm = ceil_div(p.M, SIZE), tn = ceil_div(p.N, SIZE);
+    int8_tile_kernel<T, SIZE, SIZE><<<(unsigned)(ceil_div(tm * tn, 8) * 8), 256, 0, stream>>>(p, (int)tm, (int)tn);
   };
-  // a workgroup per compute unit, which goes through tiles (two of them read a twice as often: 26.1 instead of 20.5 us at 32 x 16384 x 4096); fewer steps of K per wave than 8 where K is short
+  // fewer steps of K per wave than 8 where K is short
   auto rows = [&](auto mt) {
     constexpr int MT = decltype(mt)::value;
     const int n = (int)ceil_div(p.N, 16);
     const int64_t my = ceil_div(p.M, 16 * MT), each = ceil_div(ceil_div(p.K, KB), 8);
-    const dim3 grid((unsigned)std::min<int64_t>(n, std::max<int64_t>(1, ROWS_GROUPS / my)), (unsigned)my);
-    if (each <= 1) int8_rows_kernel<T, MT, 1, true><<<grid, 512, 0, stream>>>(p, n);
-    else if (each <= 2) int8_rows_kernel<T, MT, 2, true><<<grid, 512, 0, stream>>>(p, n);
-    else if (each <= 4) int8_rows_kernel<T, MT, 4, true><<<grid, 512, 0, stream>>>(p, n);
-    else if (each <= 8) int8_rows_kernel<T, MT, 8, true><<<grid, 512, 0, stream>>>(p, n);
-    else int8_rows_kernel<T, MT, 4, false><<<grid, 512, 0, stream>>>(p, n);
+    const int64_t gx = std::min<int64_t>(n, std::max<int64_t>(1, ROWS_GROUPS / my));
+    const unsigned grid = (unsigned)(gx * my);
+    if (each <= 1) int8_rows_kernel<T, MT, 1, true><<<grid, 512, 0, stream>>>(p, n, (int)gx);
+    else if (each <= 2) int8_rows_kernel<T, MT, 2, true><<<grid, 512, 0, stream>>>(p, n, (int)gx);
+    else if (each <= 4) int8_rows_kernel<T, MT, 4, true><<<grid, 512, 0, stream>>>(p, n, (int)gx);
+    else if (each <= 8) int8_rows_kernel<T, MT, 8, true><<<grid, 512, 0, stream>>>(p, n, (int)gx);
+    else int8_rows_kernel<T, MT, 4, false><<<grid, 512, 0, stream>>>(p, n, (int)gx);
   };
-  using std::integral_constant;
-  static const int force = getenv("INT8_FORCE") ? atoi(getenv("INT8_FORCE")) : 0;
-  const int64_t t256 = ceil_div(p.M, 256) * ceil_div(p.N, 256), t128 = ceil_div(p.M, 128) * ceil_div(p.N, 128);
-  if (p.K >= 16 && (force == 1 || (!force && p.M <= 64))) {
+  const Estimate e = estimate(p);
+  const bool rows16 = aligned(p.a, 16) && aligned(p.b, 16) && p.lda % 16 == 0 && p.ldb % 16 == 0;   // what the tiles' loads need
+  if (p.K < 16) {
+    const dim3 grid((unsigned)ceil_div(p.M, 64), (unsigned)ceil_div(p.N, 64));
+    int8_product_kernel<T><<<grid, 256, 0, stream>>>(p);
+  } else if (!rows16 || (e.rows <= e.t128 && e.rows <= e.t256)) {
     if (p.M <= 16) rows(integral_constant<int, 1>{});
     else if (p.M <= 32) rows(integral_constant<int, 2>{});
     else rows(integral_constant<int, 4>{});
-  } else if (rows16 && (force == 2 || (!force && t256 >= 256))) {
-    tiles(integral_constant<int, 256>{}, integral_constant<int, 256>{});
-  } else if (rows16 && (force == 3 || !force)) {
-    (void)t128;
-    tiles(integral_constant<int, 128>{}, integral_constant<int, 128>{});
+  } else if (e.t128 <= e.t256) {
+    tiles(integral_constant<int, 128>{});
   } else {
-    const dim3 grid((unsigned)ceil_div(p.M, 64), (unsigned)ceil_div(p.N, 64));
-    int8_product_kernel<T><<<grid, 256, 0, stream>>>(p);
+    tiles(integral_constant<int, 256>{});
   }
   return launched("mebptt_int8_product");
 }

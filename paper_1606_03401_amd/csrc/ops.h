@@ -20,6 +20,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int WAVE = 64;
@@ -57,6 +58,10 @@ __device__ inline void load(const __bf16* p, float (&v)[V]) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[e + i] = (float)x[i];
     }
+  } else if constexpr (V == 4) {
+    const bf16x4 x = *reinterpret_cast<const bf16x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)x[i];
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = (float)p[e];
@@ -85,6 +90,11 @@ __device__ inline void store(__bf16* p, const float (&v)[V]) {
       for (int i = 0; i < 8; ++i) x[i] = (__bf16)v[e + i];
       *reinterpret_cast<bf16x8*>(p + e) = x;
     }
+  } else if constexpr (V == 4) {
+    bf16x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (__bf16)v[i];
+    *reinterpret_cast<bf16x4*>(p) = x;
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) p[e] = (__bf16)v[e];

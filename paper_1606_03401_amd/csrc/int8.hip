@@ -391,22 +391,56 @@ int check(const mebptt_int8_desc* d) {
   return MEBPTT_OK;
 }
 
+// ---- operands whose rows begin anywhere -----------------------------------------------------------------
+
+// Copies of rows that do not begin at 16-byte boundaries, with zeros up to the next one: 16 bytes per thread.
+struct Copy {
+  const int8_t* from;
+  int8_t* to;
+  int64_t rows, ld, to_ld;
+  int K;
+};
+__global__ __launch_bounds__(256) void int8_copy_kernel(Copy a, Copy b) {
+  const int64_t parts = a.to_ld / 16;
+  for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < (a.rows + b.rows) * parts; k += (int64_t)gridDim.x * 256) {
+    const int64_t row = k / parts, part = k % parts;
+    const bool second = row >= a.rows;
+    const Copy& c = second ? b : a;
+    const int64_t r = second ? row - a.rows : row;
+    *reinterpret_cast<u32x4*>(c.to + r * c.to_ld + part * 16) = fetch(c.from + r * c.ld, (int)part * 16, c.K);
+  }
+}
+
 // The three kernels by what a launch is estimated to take, in us, fitted to 15 shapes timed on all of them (M 1 .. 8192, N 512 .. 16384,
 // K 512 .. 8192; within a quarter of the times measured).  One tile alone is bound by its stages' latency, a chip full of them by what
 // the L2s deliver.  Measured, rows / 128 / 256: 32 x 16384 x 4096 20 / 30 / 66, 512 x 512 x 4096 11.5 / 18.8 / 45, 1024 x 4096 x 4096 48 / 25 / 49,
 // 8192 x 4096 x 4096 310 / 221 / 169.
-struct Estimate { double rows, t128, t256; };
+struct Estimate {
+  double rows, t128, t256;
+  double tiles() const { return std::min(t128, t256); }
+};
 constexpr int ROWS_GROUPS = 256;   // a workgroup per compute unit; two read a twice as often: 26 instead of 20 us at 32 x 16384 x 4096
-Estimate estimate(const Product& p) {
-  const double K = p.K, stages = (double)ceil_div(p.K, KB);
-  const int64_t m_tiles = ceil_div(p.M, p.M <= 16 ? 16 : p.M <= 32 ? 32 : 64);
-  const int64_t t128 = ceil_div(p.M, 128) * ceil_div(p.N, 128), t256 = ceil_div(p.M, 256) * ceil_div(p.N, 256);
+Estimate estimate(int64_t M, int N, int K) {
+  const double stages = (double)ceil_div(K, KB);
+  const int64_t m_tiles = ceil_div(M, M <= 16 ? 16 : M <= 32 ? 32 : 64);
+  const int64_t t128 = ceil_div(M, 128) * ceil_div(N, 128), t256 = ceil_div(M, 256) * ceil_div(N, 256);
   Estimate e;
-  e.rows = 3 + K / 600 + (double)ceil_div(ceil_div(p.N, 16) * m_tiles, ROWS_GROUPS) * (1.1 + K / 2700);
+  e.rows = 3 + K / 600.0 + (double)ceil_div(ceil_div(N, 16) * m_tiles, ROWS_GROUPS) * (1.1 + K / 2700.0);
   e.t128 = 4 + stages * (t128 <= 256 ? 0.3 : 0.86 * (double)ceil_div(t128, 512));
   e.t256 = (double)ceil_div(t256, 256) * (13 + stages * (0.52 + 0.58 * (double)std::min<int64_t>(t256, 256) / 256));
   return e;
 }
+
+// Where K is no multiple of 16, rows that follow each other begin anywhere, and reading them so by rows takes up to three times as long, copies and
+// their launch at least 10 us.  Measured, by rows / from copies: 777 x 1301 x 650 16 / 20, 1000 x 1000 x 1001 12 / 20, 512 x 4096 x 1022
+// 28 / 21, 4000 x 4096 x 510 110 / 41, 8192 x 4096 x 4095 980 / 198.  Whether copies of both operands and tiles are faster:
+bool copies_pay(int64_t M, int N, int K) {
+  if (K % 16 == 0 || K < 16 || M <= 64) return false;
+  const Estimate e = estimate(M, N, K);
+  return e.tiles() + 10 + (double)(M + N) * K / 3.0e6 < 1.6 * e.rows;
+}
+int64_t copied_ld(int K) { return ceil_div(K, 16) * 16; }
+size_t copy_bytes(int64_t rows, int K) { return align_up((size_t)rows * copied_ld(K)); }
 
 template <typename T>
 int launch(const Product& p, hipStream_t stream) {
@@ -429,7 +463,7 @@ int launch(const Product& p, hipStream_t stream) {
     else if (each <= 8) int8_rows_kernel<T, MT, 8, true><<<grid, 512, 0, stream>>>(p, n, (int)gx);
     else int8_rows_kernel<T, MT, 4, false><<<grid, 512, 0, stream>>>(p, n, (int)gx);
   };
-  const Estimate e = estimate(p);
+  const Estimate e = estimate(p.M, p.N, p.K);
   const bool rows16 = aligned(p.a, 16) && aligned(p.b, 16) && p.lda % 16 == 0 && p.ldb % 16 == 0;   // what the tiles' loads need
   if (p.K < 16) {
     const dim3 grid((unsigned)ceil_div(p.M, 64), (unsigned)ceil_div(p.N, 64));
@@ -451,8 +485,8 @@ int launch(const Product& p, hipStream_t stream) {
 extern "C" {
 
 size_t mebptt_int8_workspace_bytes(const mebptt_int8_desc* d) {
-  (void)d;
-  return 0;
+  if (check(d) != MEBPTT_OK || !copies_pay(d->M, d->N, d->K)) return 0;
+  return copy_bytes(d->M, d->K) + copy_bytes(d->N, d->K);
 }
 
 int mebptt_int8_product(const mebptt_int8_desc* d, const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b, int64_t ldb,
@@ -467,6 +501,18 @@ int mebptt_int8_product(const mebptt_int8_desc* d, const int8_t* a, int64_t lda,
   Product p = {a, b, a_scale, b_scale, bias, out, d->M, lda, ldb, ldo, d->N, d->K, rows_aligned(out, ldo, d->out_dtype, 4),
                rows_aligned(out, ldo, d->out_dtype, 8)};
   const hipStream_t st = (hipStream_t)stream;
+  if (copies_pay(d->M, d->N, d->K)) {
+    const int64_t ld = copied_ld(d->K);
+    auto ready = [](const int8_t* x, int64_t ldx) { return aligned(x, 16) && ldx % 16 == 0; };
+    int8_t* room = (int8_t*)workspace;
+    Copy ca = {a, room, ready(a, lda) ? 0 : d->M, lda, ld, d->K}, cb = {b, room + copy_bytes(d->M, d->K), ready(b, ldb) ? 0 : d->N, ldb, ld, d->K};
+    if (ca.rows) p.a = ca.to, p.lda = ld;
+    if (cb.rows) p.b = cb.to, p.ldb = ld;
+    if (ca.rows + cb.rows) {
+      int8_copy_kernel<<<(unsigned)std::min<int64_t>(ceil_div((ca.rows + cb.rows) * (ld / 16), 256), 1 << 16), 256, 0, st>>>(ca, cb);
+      if ((rc = launched("mebptt_int8_product"))) return rc;
+    }
+  }
   return d->out_dtype == MEBPTT_FP32 ? launch<float>(p, st) : launch<__bf16>(p, st);
 }
 

@@ -766,43 +766,65 @@ struct Step {
   const int32_t* index;
   int64_t slots;
 };
-// A lane per NB states: the pool's rows are read and written once.  Bound: HBM.
-template <typename T, int NL>
+// A lane per NB states: the pool's rows are read and written once.  VEC: a channel's states, and its group's B and C, in whole vectors of NB.
+// Bound: HBM.
+template <typename T, int NL, bool VEC>
 __global__ __launch_bounds__(256) void scan_step_kernel(Step p) {
   const Scan& in = p.in;
-  const int q = threadIdx.x % NL;
-  for (int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / NL; item < (int64_t)in.B * in.D; item += (int64_t)gridDim.x * (256 / NL)) {
-    const int b = (int)(item / in.D), d = (int)(item % in.D);
-    const int64_t slot = p.index ? p.index[b] : b;
-    if (slot < 0 || slot >= p.slots) {
-      if (q == 0) put<T>(p.y, 0, b, d, 0.0f);
-      continue;
+  const int q = threadIdx.x % NL, b = blockIdx.y;
+  const unsigned d = blockIdx.x * (256 / NL) + threadIdx.x / NL;
+  if (d >= (unsigned)in.D) return;                       // (all lanes of a channel)
+  const int64_t slot = p.index ? p.index[b] : b;
+  T* const y_at = (T*)p.y.p + b * p.y.b + d;
+  if (slot < 0 || slot >= p.slots) {
+    if (q == 0) *y_at = (T)0.0f;
+    return;
+  }
+  const unsigned group = in.G == 1 ? 0u : d / (unsigned)(in.D / in.G);
+  const int64_t state = (slot * in.D + d) * in.N;
+  const T* const pb = (const T*)in.Bm.p + b * in.Bm.b + (int64_t)group * in.N;
+  const T* const pc = (const T*)in.Cm.p + b * in.Cm.b + (int64_t)group * in.N;
+  float h[NB], A[NB], vb[NB], vc[NB];
+  if constexpr (VEC) {
+    if (q * NB >= in.N) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) h[n] = A[n] = vb[n] = vc[n] = 0.0f;
+    } else {
+      load<NB>(p.state_in + state + q * NB, h);
+      load<NB>(in.A + (int64_t)d * in.N + q * NB, A);
+      load<NB>(pb + q * NB, vb);
+      load<NB>(pc + q * NB, vc);
     }
-    const int64_t state = (slot * in.D + d) * in.N, gn = (int64_t)(d / (in.D / in.G)) * in.N;
-    float h[NB], A[NB];
+  } else {
     load_states(p.state_in + state, q * NB, in.N, h);
     load_states(in.A + (int64_t)d * in.N, q * NB, in.N, A);
-    const float u = at<T>(in.u, 0, b, d);
-    float w = at<T>(in.delta, 0, b, d) + (in.bias ? in.bias[d] : 0.0f);
-    if (in.softplus) w = softplus_of(w);
-    float y = 0.0f;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const bool there = q * NB + n < in.N;
-      const float vb = there ? at<T>(in.Bm, 0, b, gn + q * NB + n) : 0.0f, vc = there ? at<T>(in.Cm, 0, b, gn + q * NB + n) : 0.0f;
-      h[n] = __builtin_amdgcn_exp2f(w * (A[n] * LOG2E)) * h[n] + w * u * vb;
-      y += h[n] * vc;
+      vb[n] = there ? (float)pb[q * NB + n] : 0.0f;
+      vc[n] = there ? (float)pc[q * NB + n] : 0.0f;
     }
-    y = lanes_sum<NL>(y);
+  }
+  const float u = (float)*((const T*)in.u.p + b * in.u.b + d), z = in.z.p ? (float)*((const T*)in.z.p + b * in.z.b + d) : 0.0f;
+  float w = (float)*((const T*)in.delta.p + b * in.delta.b + d) + (in.bias ? in.bias[d] : 0.0f);
+  const float skip = in.skip ? in.skip[d] : 0.0f;
+  if (in.softplus) w = softplus_of(w);
+  float y = 0.0f;
+#pragma unroll
+  for (int n = 0; n < NB; ++n) {
+    h[n] = __builtin_amdgcn_exp2f(w * (A[n] * LOG2E)) * h[n] + w * u * vb[n];
+    y += h[n] * vc[n];
+  }
+  y = lanes_sum<NL>(y);
+  if constexpr (VEC) {
+    if (q * NB < in.N) store<NB>(p.state_out + state + q * NB, h);
+  } else {
     store_states(p.state_out + state, q * NB, in.N, h);
-    if (q == 0) {
-      if (in.skip) y += in.skip[d] * u;
-      if (in.z.p) {
-        const float z = at<T>(in.z, 0, b, d);
-        y *= z * sigmoid(z);
-      }
-      put<T>(p.y, 0, b, d, y);
-    }
+  }
+  if (q == 0) {
+    y += skip * u;
+    if (in.z.p) y *= z * sigmoid(z);
+    *y_at = (T)y;
   }
 }
 
@@ -1052,12 +1074,19 @@ int mebptt_scan_step(const mebptt_scan_desc* d, const mebptt_scan_inputs* in, co
   if (!state_in || !state_out) return set_error(MEBPTT_EINVAL, "state_in and state_out are required");
   if (slots < 0 || (!index && slots < d->B)) return set_error(MEBPTT_EINVAL, "without an index every sequence needs its own slot");
   const Step p = {scan_of(d, in), out_seq(y), state_in, state_out, index, slots};
+  const bool vec = d->N % NB == 0 && aligned(state_in, 16) && aligned(state_out, 16) && aligned(in->A, 16) &&
+                   rows_aligned(in->Bm.data, in->Bm.stride_b, d->dtype, NB) && rows_aligned(in->Cm.data, in->Cm.stride_b, d->dtype, NB);
+  hipStream_t s = (hipStream_t)stream;
   return with_lanes(d->N, [&](auto l) {
     constexpr int NL = decltype(l)::value;
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div((int64_t)d->B * d->D * NL, 256), 1 << 22);
-    if (d->dtype == MEBPTT_FP32) scan_step_kernel<float, NL><<<grid, 256, 0, (hipStream_t)stream>>>(p);
-    else scan_step_kernel<__bf16, NL><<<grid, 256, 0, (hipStream_t)stream>>>(p);
-    return launched("mebptt_scan_step");
+    const dim3 grid((unsigned)ceil_div(d->D, 256 / NL), d->B);
+    auto go = [&](auto elem) {
+      using T = decltype(elem);
+      if (vec) scan_step_kernel<T, NL, true><<<grid, 256, 0, s>>>(p);
+      else scan_step_kernel<T, NL, false><<<grid, 256, 0, s>>>(p);
+      return launched("mebptt_scan_step");
+    };
+    return d->dtype == MEBPTT_FP32 ? go(float{}) : go(__bf16{});
   });
 }
 

@@ -570,64 +570,109 @@ def mebptt_measure_gemms(desc: mebptt_lstm_desc, workspace, reps: int = 20, stre
 # ---- operators of a selective state space block ------------------------------------------------------
 #
 # Tensors are checked here for type, shape and device, which the library cannot see; it checks everything else.  Sequences
-# are [t, B, channels], of any strides over t and B; states, parameters and their gradients are contiguous.
+# are [t, B, channels], of any strides over t and B; states, parameters and their gradients are contiguous.  Single tokens come
+# in calls of a few microseconds, so the checks are one comparison each and say what was wrong only when something was.
+
+_torch = None
+_DTYPES = ()
+_current_device = _current_stream = None
 
 
-def _torch_dtype(code: int):
+def _load_torch():
+    global _torch, _DTYPES, _current_device, _current_stream
     import torch
-    return {FP32: torch.float32, BF16: torch.bfloat16, INT8: torch.int8}[code]
+    _torch, _DTYPES = torch, (torch.float32, torch.bfloat16, torch.int8)
+    torch.cuda.init()
+    _current_device = torch._C._cuda_getDevice
+    # the raw handle without a Stream object around it
+    _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _given(t, name: str, shape, dtype, device, optional: bool = False):
-    """`t` as an argument of this shape and type, on the device of the call's other tensors."""
+def _dtype(code: int):
+    if not 0 <= code < 3:
+        raise ValueError(f"unknown dtype {code}")
+    return _DTYPES[code]
+
+
+def _gpu(t) -> int:
+    """Index of the GPU that holds `t`, the first tensor of a call."""
+    dev = -1 if t is None else t.get_device()
+    if dev < 0:
+        raise ValueError("tensors in a GPU's memory are needed")
+    if _torch is None:
+        _load_torch()
+    return dev
+
+
+def _wrong(t, name: str, shape, dtype, dev: int):
     if t is None:
-        if optional:
-            return None
         raise ValueError(f"{name} is required")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} is needed")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} has type {t.dtype}, {dtype} is needed")
-    if t.device != device or t.device.type != "cuda":
-        raise ValueError(f"{name} is on {t.device}, one GPU's memory is needed")
-    return t
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the call's other tensors on GPU {dev}")
+    raise ValueError(f"{name} must be contiguous" if not t.is_contiguous() else f"{name} is not usable")
 
 
-def _whole(t, name: str, shape, dtype, device, optional: bool = False) -> Optional[int]:
+def _whole(t, name: str, shape, dtype, dev: int) -> int:
     """Pointer of a contiguous tensor."""
-    if _given(t, name, shape, dtype, device, optional) is None:
-        return None
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    if t is None or t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        _wrong(t, name, shape, dtype, dev)
     return t.data_ptr()
 
 
-def _rows(t, name: str, rows: int, width: int, dtype, device, optional: bool = False):
+def _maybe(t, name: str, shape, dtype, dev: int) -> Optional[int]:
+    return None if t is None else _whole(t, name, shape, dtype, dev)
+
+
+def _rows(t, name: str, rows: int, width: int, dtype, dev: int):
     """(pointer, row stride) of a [rows, width] tensor whose rows are contiguous."""
-    if _given(t, name, (rows, width), dtype, device, optional) is None:
-        return None, 0
-    if t.numel() and width > 1 and t.stride(1) != 1:
+    if t is None or t.shape != (rows, width) or t.dtype is not dtype or t.get_device() != dev:
+        _wrong(t, name, (rows, width), dtype, dev)
+    ld, one = t.stride()
+    if one != 1 and width > 1 and rows:
         raise ValueError(f"rows of {name} must be contiguous")
-    return t.data_ptr(), t.stride(0) if rows > 1 else width
+    return t.data_ptr(), ld if rows > 1 else width
 
 
-def _seq(t, name: str, steps: int, B: int, channels: int, dtype, device, optional: bool = False) -> mebptt_seq:
+def _maybe_rows(t, name: str, rows: int, width: int, dtype, dev: int):
+    return (None, 0) if t is None else _rows(t, name, rows, width, dtype, dev)
+
+
+def _seq(t, name: str, steps: int, B: int, channels: int, dtype, dev: int) -> mebptt_seq:
     """A [t, B, channels] tensor whose channels are contiguous."""
-    if _given(t, name, (steps, B, channels), dtype, device, optional) is None:
-        return mebptt_seq(None, 0, 0)
-    if t.numel() and channels > 1 and t.stride(2) != 1:
+    if t is None or t.shape != (steps, B, channels) or t.dtype is not dtype or t.get_device() != dev:
+        _wrong(t, name, (steps, B, channels), dtype, dev)
+    st, sb, one = t.stride()
+    if one != 1 and channels > 1 and steps and B:
         raise ValueError(f"the channels of {name} must be contiguous")
     # the stride of an axis of one is whatever it is: never used, and not to be looked at
-    return mebptt_seq(t.data_ptr() or None, t.stride(0) if steps > 1 else B * channels, t.stride(1) if B > 1 else channels)
+    return mebptt_seq(t.data_ptr() or None, st if steps > 1 else B * channels, sb if B > 1 else channels)
 
 
-def _room(t, name: str, device):
+def _maybe_seq(t, name: str, steps: int, B: int, channels: int, dtype, dev: int) -> mebptt_seq:
+    return mebptt_seq(None, 0, 0) if t is None else _seq(t, name, steps, B, channels, dtype, dev)
+
+
+def _room(t, name: str, dev: int):
     """(pointer, bytes) of a workspace; None where the call needs none."""
     if t is None:
         return None, 0
-    if t.device != device or not t.is_contiguous():
+    if t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and on the GPU of the call's other tensors")
-    return t.data_ptr(), _nbytes(t)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _call(dev: int, stream: Optional[int], fn, *args) -> None:
+    """The library's call on the tensors' GPU and `stream` (default: that GPU's current one)."""
+    if dev != _current_device():
+        with _torch.cuda.device(dev):
+            return _call(dev, stream, fn, *args)
+    rc = fn(*args, _current_stream(dev) if stream is None else stream)
+    if rc != OK:
+        _check(rc)
 
 
 def make_norm_desc(rows: int, width: int, x_dtype: int, residual_dtype: int, y_dtype: int, eps: float = 1e-5) -> mebptt_norm_desc:
@@ -642,33 +687,24 @@ def mebptt_norm_forward(desc: mebptt_norm_desc, x, residual, weight, y, y_scale=
                         stream: Optional[int] = None) -> None:
     """r = x + residual, y = RMS norm of r times `weight`; residual_out receives r, rstd the rows' 1 / rms (for the backward call),
     y_scale the rows' scales of an 8-bit y."""
-    import torch
-    M, W, dev, f32 = desc.rows, desc.width, x.device, torch.float32
-    xt, rt = _torch_dtype(desc.x_dtype), _torch_dtype(desc.residual_dtype)
-    px, ldx = _rows(x, "x", M, W, xt, dev)
-    pr, ldr = _rows(residual, "residual", M, W, rt, dev, optional=True)
-    py, ldy = _rows(y, "y", M, W, _torch_dtype(desc.y_dtype), dev)
-    po, ldo = _rows(residual_out, "residual_out", M, W, rt, dev, optional=True)
-    _check(lib().mebptt_norm_forward(C.byref(desc), px, ldx, pr, ldr, _whole(weight, "weight", (W,), f32, dev, True), py, ldy,
-                                     _whole(y_scale, "y_scale", (M,), f32, dev, True), po, ldo,
-                                     _whole(rstd, "rstd", (M,), f32, dev, True), _stream(stream)))
+    dev, M, W = _gpu(x), desc.rows, desc.width
+    f32, rt = _DTYPES[0], _dtype(desc.residual_dtype)
+    _call(dev, stream, lib().mebptt_norm_forward, C.byref(desc), *_rows(x, "x", M, W, _dtype(desc.x_dtype), dev),
+          *_maybe_rows(residual, "residual", M, W, rt, dev), _maybe(weight, "weight", (W,), f32, dev),
+          *_rows(y, "y", M, W, _dtype(desc.y_dtype), dev), _maybe(y_scale, "y_scale", (M,), f32, dev),
+          *_maybe_rows(residual_out, "residual_out", M, W, rt, dev), _maybe(rstd, "rstd", (M,), f32, dev))
 
 
 def mebptt_norm_backward(desc: mebptt_norm_desc, r, weight, rstd, dy, dresidual_out, dx, dresidual, dweight, workspace,
                          stream: Optional[int] = None) -> None:
     """Gradients of mebptt_norm_forward from r (its residual_out, or x without a residual) and rstd."""
-    import torch
-    M, W, dev, f32 = desc.rows, desc.width, r.device, torch.float32
-    xt, rt = _torch_dtype(desc.x_dtype), _torch_dtype(desc.residual_dtype)
-    pr, ldr = _rows(r, "r", M, W, rt, dev)
-    pg, ldg = _rows(dy, "dy", M, W, xt, dev)
-    pi, ldi = _rows(dresidual_out, "dresidual_out", M, W, rt, dev, optional=True)
-    pd, ldd = _rows(dx, "dx", M, W, xt, dev, optional=True)
-    po, ldo = _rows(dresidual, "dresidual", M, W, rt, dev, optional=True)
-    _check(lib().mebptt_norm_backward(C.byref(desc), pr, ldr, _whole(weight, "weight", (W,), f32, dev, True),
-                                      _whole(rstd, "rstd", (M,), f32, dev), pg, ldg, pi, ldi, pd, ldd, po, ldo,
-                                      _whole(dweight, "dweight", (W,), f32, dev, True), *_room(workspace, "workspace", dev),
-                                      _stream(stream)))
+    dev, M, W = _gpu(r), desc.rows, desc.width
+    f32, xt, rt = _DTYPES[0], _dtype(desc.x_dtype), _dtype(desc.residual_dtype)
+    _call(dev, stream, lib().mebptt_norm_backward, C.byref(desc), *_rows(r, "r", M, W, rt, dev), _maybe(weight, "weight", (W,), f32, dev),
+          _whole(rstd, "rstd", (M,), f32, dev), *_rows(dy, "dy", M, W, xt, dev),
+          *_maybe_rows(dresidual_out, "dresidual_out", M, W, rt, dev), *_maybe_rows(dx, "dx", M, W, xt, dev),
+          *_maybe_rows(dresidual, "dresidual", M, W, rt, dev), _maybe(dweight, "dweight", (W,), f32, dev),
+          *_room(workspace, "workspace", dev))
 
 
 def make_int8_desc(M: int, N: int, K: int, out_dtype: int) -> mebptt_int8_desc:
@@ -681,14 +717,11 @@ def mebptt_int8_workspace_bytes(desc: mebptt_int8_desc) -> int:
 
 def mebptt_int8_product(desc: mebptt_int8_desc, a, a_scale, b, b_scale, bias, out, workspace=None, stream: Optional[int] = None) -> None:
     """out = a_scale[:, None] * b_scale * (a @ b.T) + bias: a [M, K] and b [N, K] int8, scales and bias float32."""
-    import torch
-    M, N, K, dev, f32 = desc.M, desc.N, desc.K, a.device, torch.float32
-    pa, lda = _rows(a, "a", M, K, torch.int8, dev)
-    pb, ldb = _rows(b, "b", N, K, torch.int8, dev)
-    po, ldo = _rows(out, "out", M, N, _torch_dtype(desc.out_dtype), dev)
-    _check(lib().mebptt_int8_product(C.byref(desc), pa, lda, _whole(a_scale, "a_scale", (M,), f32, dev), pb, ldb,
-                                     _whole(b_scale, "b_scale", (N,), f32, dev), _whole(bias, "bias", (N,), f32, dev, True), po, ldo,
-                                     *_room(workspace, "workspace", dev), _stream(stream)))
+    dev, M, N, K = _gpu(a), desc.M, desc.N, desc.K
+    f32, i8 = _DTYPES[0], _DTYPES[2]
+    _call(dev, stream, lib().mebptt_int8_product, C.byref(desc), *_rows(a, "a", M, K, i8, dev), _whole(a_scale, "a_scale", (M,), f32, dev),
+          *_rows(b, "b", N, K, i8, dev), _whole(b_scale, "b_scale", (N,), f32, dev), _maybe(bias, "bias", (N,), f32, dev),
+          *_rows(out, "out", M, N, _dtype(desc.out_dtype), dev), *_room(workspace, "workspace", dev))
 
 
 def make_conv_desc(t: int, B: int, C_: int, taps: int, dtype: int, silu: int = 1) -> mebptt_conv_desc:
@@ -699,57 +732,47 @@ def mebptt_conv_workspace_bytes(desc: mebptt_conv_desc) -> int:
     return lib().mebptt_conv_workspace_bytes(C.byref(desc))
 
 
-def _conv_params(desc, weight, bias, dev):
-    import torch
-    return (_whole(weight, "weight", (desc.C, desc.taps), torch.float32, dev),
-            _whole(bias, "bias", (desc.C,), torch.float32, dev, True))
+def _conv_params(desc, weight, bias, dev: int):
+    return _whole(weight, "weight", (desc.C, desc.taps), _DTYPES[0], dev), _maybe(bias, "bias", (desc.C,), _DTYPES[0], dev)
 
 
 def mebptt_conv_forward(desc: mebptt_conv_desc, x, weight, bias, lengths, state_in, y, state_out=None,
                         stream: Optional[int] = None) -> None:
     """Depthwise causal convolution of [t, B, C]; states are the last taps - 1 inputs, [B, taps - 1, C]."""
-    import torch
-    dev, T = x.device, _torch_dtype(desc.dtype)
-    state = (desc.B, desc.taps - 1, desc.C)
-    _check(lib().mebptt_conv_forward(C.byref(desc), _seq(x, "x", desc.t, desc.B, desc.C, T, dev), *_conv_params(desc, weight, bias, dev),
-                                     _whole(lengths, "lengths", (desc.B,), torch.int32, dev, True),
-                                     _whole(state_in, "state_in", state, T, dev, True), _seq(y, "y", desc.t, desc.B, desc.C, T, dev),
-                                     _whole(state_out, "state_out", state, T, dev, True), _stream(stream)))
+    dev, T = _gpu(x), _dtype(desc.dtype)
+    shape, state = (desc.t, desc.B, desc.C), (desc.B, desc.taps - 1, desc.C)
+    _call(dev, stream, lib().mebptt_conv_forward, C.byref(desc), _seq(x, "x", *shape, T, dev), *_conv_params(desc, weight, bias, dev),
+          _maybe(lengths, "lengths", (desc.B,), _torch.int32, dev), _maybe(state_in, "state_in", state, T, dev),
+          _seq(y, "y", *shape, T, dev), _maybe(state_out, "state_out", state, T, dev))
 
 
 def mebptt_conv_backward(desc: mebptt_conv_desc, x, weight, bias, lengths, state_in, dy, dstate_out, dx, dweight, dbias, dstate_in,
                          workspace, stream: Optional[int] = None) -> None:
-    import torch
-    dev, T, f32 = x.device, _torch_dtype(desc.dtype), torch.float32
-    state, shape = (desc.B, desc.taps - 1, desc.C), (desc.t, desc.B, desc.C)
-    _check(lib().mebptt_conv_backward(C.byref(desc), _seq(x, "x", *shape, T, dev), *_conv_params(desc, weight, bias, dev),
-                                      _whole(lengths, "lengths", (desc.B,), torch.int32, dev, True),
-                                      _whole(state_in, "state_in", state, T, dev, True), _seq(dy, "dy", *shape, T, dev),
-                                      _whole(dstate_out, "dstate_out", state, T, dev, True), _seq(dx, "dx", *shape, T, dev),
-                                      _whole(dweight, "dweight", (desc.C, desc.taps), f32, dev),
-                                      _whole(dbias, "dbias", (desc.C,), f32, dev, True),
-                                      _whole(dstate_in, "dstate_in", state, T, dev, True), *_room(workspace, "workspace", dev),
-                                      _stream(stream)))
+    dev, T = _gpu(x), _dtype(desc.dtype)
+    shape, state = (desc.t, desc.B, desc.C), (desc.B, desc.taps - 1, desc.C)
+    _call(dev, stream, lib().mebptt_conv_backward, C.byref(desc), _seq(x, "x", *shape, T, dev), *_conv_params(desc, weight, bias, dev),
+          _maybe(lengths, "lengths", (desc.B,), _torch.int32, dev), _maybe(state_in, "state_in", state, T, dev),
+          _seq(dy, "dy", *shape, T, dev), _maybe(dstate_out, "dstate_out", state, T, dev), _seq(dx, "dx", *shape, T, dev),
+          _whole(dweight, "dweight", (desc.C, desc.taps), _DTYPES[0], dev), _maybe(dbias, "dbias", (desc.C,), _DTYPES[0], dev),
+          _maybe(dstate_in, "dstate_in", state, T, dev), *_room(workspace, "workspace", dev))
 
 
-def _pool(state_in, state_out, row, dtype, dev, needed: bool):
+def _pool(state_in, state_out, row, dtype, dev: int, needed: bool):
     """(pointer, slots, pointer) of a pool of states and of the pool that receives them."""
     if state_in is None and not needed:
         return None, 1 << 31, None
-    slots = state_in.shape[0] if state_in is not None else 0
-    return (_whole(state_in, "state_in", (slots, *row), dtype, dev), slots, _whole(state_out, "state_out", (slots, *row), dtype, dev))
+    shape = (state_in.shape[0] if state_in is not None and state_in.dim() else 0, *row)
+    return _whole(state_in, "state_in", shape, dtype, dev), shape[0], _whole(state_out, "state_out", shape, dtype, dev)
 
 
 def mebptt_conv_step(desc: mebptt_conv_desc, x, weight, bias, state_in, index, y, state_out, stream: Optional[int] = None) -> None:
     """One token: x, y [B, C]; state_in, state_out [slots, taps - 1, C] (one tensor or two); index [B] int32 names every sequence's
     slot, None: its own number."""
-    import torch
-    dev, T = x.device, _torch_dtype(desc.dtype)
-    px, ldx = _rows(x, "x", desc.B, desc.C, T, dev)
-    py, ldy = _rows(y, "y", desc.B, desc.C, T, dev)
-    pin, slots, pout = _pool(state_in, state_out, (desc.taps - 1, desc.C), T, dev, desc.taps > 1)
-    _check(lib().mebptt_conv_step(C.byref(desc), px, ldx, *_conv_params(desc, weight, bias, dev), pin, slots,
-                                  _whole(index, "index", (desc.B,), torch.int32, dev, True), py, ldy, pout, _stream(stream)))
+    dev, T = _gpu(x), _dtype(desc.dtype)
+    B, Ch = desc.B, desc.C
+    pin, slots, pout = _pool(state_in, state_out, (desc.taps - 1, Ch), T, dev, desc.taps > 1)
+    _call(dev, stream, lib().mebptt_conv_step, C.byref(desc), *_rows(x, "x", B, Ch, T, dev), *_conv_params(desc, weight, bias, dev), pin,
+          slots, _maybe(index, "index", (B,), _torch.int32, dev), *_rows(y, "y", B, Ch, T, dev), pout)
 
 
 def make_scan_desc(t: int, B: int, D: int, N: int, G: int, dtype: int, softplus: int = 1, stretch: int = 64) -> mebptt_scan_desc:
@@ -764,52 +787,54 @@ def mebptt_scan_workspace_bytes(desc: mebptt_scan_desc, backward: bool) -> int:
     return lib().mebptt_scan_workspace_bytes(C.byref(desc), 1 if backward else 0)
 
 
-def _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dev) -> mebptt_scan_inputs:
-    import torch
-    T, f32, D, N = _torch_dtype(desc.dtype), torch.float32, desc.D, desc.N
-    seq = lambda t, name, c, optional=False: _seq(t, name, desc.t, desc.B, c, T, dev, optional)  # noqa: E731
-    return mebptt_scan_inputs(seq(u, "u", D), seq(delta, "delta", D), seq(z, "z", D, True), seq(Bm, "Bm", desc.G * N),
-                              seq(Cm, "Cm", desc.G * N), _whole(A, "A", (D, N), f32, dev), _whole(skip, "skip", (D,), f32, dev, True),
-                              _whole(delta_bias, "delta_bias", (D,), f32, dev, True),
-                              _whole(lengths, "lengths", (desc.B,), torch.int32, dev, True),
-                              _whole(h0, "h0", (desc.B, D, N), f32, dev, True))
+def _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, T, dev: int) -> mebptt_scan_inputs:
+    f32, t, B, D, N, GN = _DTYPES[0], desc.t, desc.B, desc.D, desc.N, desc.G * desc.N
+    return mebptt_scan_inputs(_seq(u, "u", t, B, D, T, dev), _seq(delta, "delta", t, B, D, T, dev), _maybe_seq(z, "z", t, B, D, T, dev),
+                              _seq(Bm, "Bm", t, B, GN, T, dev), _seq(Cm, "Cm", t, B, GN, T, dev), _whole(A, "A", (D, N), f32, dev),
+                              _maybe(skip, "skip", (D,), f32, dev), _maybe(delta_bias, "delta_bias", (D,), f32, dev),
+                              _maybe(lengths, "lengths", (B,), _torch.int32, dev), _maybe(h0, "h0", (B, D, N), f32, dev))
 
 
 def mebptt_scan_forward(desc: mebptt_scan_desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, y, h_out=None, states=None,
                         workspace=None, stream: Optional[int] = None) -> None:
     """Selective scan.  u, delta, z, y [t, B, D]; Bm, Cm [t, B, G N]; A [D, N]; h0, h_out [B, D, N]; `states` (uint8) keeps what a
     backward call needs."""
-    import torch
-    dev = u.device
-    given = _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dev)
-    _check(lib().mebptt_scan_forward(C.byref(desc), C.byref(given), _seq(y, "y", desc.t, desc.B, desc.D, _torch_dtype(desc.dtype), dev),
-                                     _whole(h_out, "h_out", (desc.B, desc.D, desc.N), torch.float32, dev, True),
-                                     *_room(states, "states", dev), *_room(workspace, "workspace", dev), _stream(stream)))
+    dev, T = _gpu(u), _dtype(desc.dtype)
+    given = _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, T, dev)
+    _call(dev, stream, lib().mebptt_scan_forward, C.byref(desc), C.byref(given), _seq(y, "y", desc.t, desc.B, desc.D, T, dev),
+          _maybe(h_out, "h_out", (desc.B, desc.D, desc.N), _DTYPES[0], dev), *_room(states, "states", dev),
+          *_room(workspace, "workspace", dev))
 
 
 def mebptt_scan_backward(desc: mebptt_scan_desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dy, dh_out, states, du, ddelta,
                          dA, dB, dC, dskip, dz, ddelta_bias, dh0, workspace, stream: Optional[int] = None) -> None:
-    import torch
-    dev, T, f32 = u.device, _torch_dtype(desc.dtype), torch.float32
-    D, N, state = desc.D, desc.N, (desc.B, desc.D, desc.N)
-    given = _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, dev)
-    seq = lambda t, name, c, optional=False: _seq(t, name, desc.t, desc.B, c, T, dev, optional)  # noqa: E731
-    grads = mebptt_scan_grads(seq(du, "du", D), seq(ddelta, "ddelta", D), seq(dz, "dz", D, z is None), seq(dB, "dB", desc.G * N),
-                              seq(dC, "dC", desc.G * N), _whole(dA, "dA", (D, N), f32, dev), _whole(dskip, "dskip", (D,), f32, dev, True),
-                              _whole(ddelta_bias, "ddelta_bias", (D,), f32, dev, True), _whole(dh0, "dh0", state, f32, dev, True))
-    _check(lib().mebptt_scan_backward(C.byref(desc), C.byref(given), seq(dy, "dy", D), _whole(dh_out, "dh_out", state, f32, dev, True),
-                                      *_room(states, "states", dev), C.byref(grads), *_room(workspace, "workspace", dev),
-                                      _stream(stream)))
+    dev, T = _gpu(u), _dtype(desc.dtype)
+    f32, t, B, D, N, GN = _DTYPES[0], desc.t, desc.B, desc.D, desc.N, desc.G * desc.N
+    given = _scan_inputs(desc, u, delta, A, Bm, Cm, skip, z, delta_bias, lengths, h0, T, dev)
+    grads = mebptt_scan_grads(_seq(du, "du", t, B, D, T, dev), _seq(ddelta, "ddelta", t, B, D, T, dev),
+                              (_maybe_seq if z is None else _seq)(dz, "dz", t, B, D, T, dev), _seq(dB, "dB", t, B, GN, T, dev),
+                              _seq(dC, "dC", t, B, GN, T, dev), _whole(dA, "dA", (D, N), f32, dev),
+                              _maybe(dskip, "dskip", (D,), f32, dev), _maybe(ddelta_bias, "ddelta_bias", (D,), f32, dev),
+                              _maybe(dh0, "dh0", (B, D, N), f32, dev))
+    _call(dev, stream, lib().mebptt_scan_backward, C.byref(desc), C.byref(given), _seq(dy, "dy", t, B, D, T, dev),
+          _maybe(dh_out, "dh_out", (B, D, N), f32, dev), *_room(states, "states", dev), C.byref(grads), *_room(workspace, "workspace", dev))
+
+
+def _token(t, name: str, B: int, channels: int, dtype, dev: int) -> mebptt_seq:
+    p, ld = _rows(t, name, B, channels, dtype, dev)
+    return mebptt_seq(p, 0, ld)
 
 
 def mebptt_scan_step(desc: mebptt_scan_desc, u, delta, A, Bm, Cm, skip, z, delta_bias, state_in, index, y, state_out,
                      stream: Optional[int] = None) -> None:
     """One token: u, delta, z, y [B, D]; Bm, Cm [B, G N]; state_in, state_out [slots, D, N] float32 (one tensor or two); index as
     in mebptt_conv_step."""
-    import torch
-    dev = u.device
-    one = lambda t: None if t is None else t.unsqueeze(0)  # noqa: E731
-    given = _scan_inputs(desc, one(u), one(delta), A, one(Bm), one(Cm), skip, one(z), delta_bias, None, None, dev)
-    pin, slots, pout = _pool(state_in, state_out, (desc.D, desc.N), torch.float32, dev, True)
-    _check(lib().mebptt_scan_step(C.byref(desc), C.byref(given), pin, slots, _whole(index, "index", (desc.B,), torch.int32, dev, True),
-                                  _seq(one(y), "y", 1, desc.B, desc.D, _torch_dtype(desc.dtype), dev), pout, _stream(stream)))
+    dev, T = _gpu(u), _dtype(desc.dtype)
+    f32, B, D, N, GN = _DTYPES[0], desc.B, desc.D, desc.N, desc.G * desc.N
+    given = mebptt_scan_inputs(_token(u, "u", B, D, T, dev), _token(delta, "delta", B, D, T, dev),
+                               mebptt_seq(None, 0, 0) if z is None else _token(z, "z", B, D, T, dev), _token(Bm, "Bm", B, GN, T, dev),
+                               _token(Cm, "Cm", B, GN, T, dev), _whole(A, "A", (D, N), f32, dev), _maybe(skip, "skip", (D,), f32, dev),
+                               _maybe(delta_bias, "delta_bias", (D,), f32, dev), None, None)
+    pin, slots, pout = _pool(state_in, state_out, (D, N), f32, dev, True)
+    _call(dev, stream, lib().mebptt_scan_step, C.byref(desc), C.byref(given), pin, slots, _maybe(index, "index", (B,), _torch.int32, dev),
+          _token(y, "y", B, D, T, dev), pout)

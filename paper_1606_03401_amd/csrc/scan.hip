@@ -98,7 +98,7 @@ struct Forward {
   float *h_out, *states;
   int stretch;
   int chunk, chunks;               // steps per chunk, a multiple of a block's
-  float *starts, *sums;            // [chunks][B][D][N]: what the chunk before reached by itself; [chunks][B][D]: sum of w
+  float *starts, *sums;            // [chunks][B][D][N]: what the chunk before reached (ENDS: by itself); [chunks][B][D]: sum of w
 };
 
 constexpr int FORWARD_WAVES = 4;   // waves of neighbouring channels per workgroup: they share cache lines, and nothing else
@@ -145,26 +145,8 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
     A2[n] *= LOG2E;
     h[n] = 0.0f;
   }
-  if (chunk == 0) {
-    if (p.h0) load_states(p.h0 + bd * in.N, q * NB, in.N, h);
-  } else if (!ENDS) {
-    // what the chunks before this one reached, each by itself, decayed by exp(A sum w) of those after it
-    for (int k = 1; k <= chunk; k += 8) {
-      float e[8][NB], w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int m = min(k + i, chunk);
-        load_states(p.starts + m * all_states + bd * in.N, q * NB, in.N, e[i]);
-        w[i] = p.sums[(int64_t)(m - 1) * in.B * in.D + bd];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k + i <= chunk) {
-#pragma unroll
-          for (int n = 0; n < NB; ++n) h[n] = e[i][n] + __builtin_amdgcn_exp2f(w[i] * A2[n]) * h[n];
-        }
-    }
-  }
+  const float* start = chunk == 0 ? p.h0 : ENDS ? nullptr : p.starts + chunk * all_states;
+  if (start) load_states(start + bd * in.N, q * NB, in.N, h);
 
   // the pairs of a lane: step i * ROWS + row, channel ch; its values of B and C: step i * SROWS + srow, state sn
   constexpr int ROWS = WAVE / CH, SROWS = WAVE / NP;
@@ -235,9 +217,10 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
   };
 #pragma unroll
   for (int i = 0; i < S::ITEMS; ++i) rz[i] = 0.0f;
-  const int stop = ENDS ? min(end, len) : end;                         // (beyond its length a sequence's state stays as it is)
+  const int stop = min(end, len);                                      // beyond its length a sequence's state stays as it is
   if (begin < stop) fetch(begin);
-  for (int s0 = begin; s0 < stop; s0 += TS) {
+  int s0 = begin;
+  for (; s0 < stop; s0 += TS) {
     const bool all = whole(s0);
     float cu[S::ITEMS], cz[S::ITEMS];
 #pragma unroll
@@ -316,10 +299,54 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
       wave_sync();
     }
   }
+  if constexpr (!ENDS) {
+    for (; s0 < end; s0 += TS) {
+      if (p.states && s0 % p.stretch == 0 && cl < nch) store_states(p.states + (int64_t)(s0 / p.stretch) * all_states + bd * in.N, q * NB, in.N, h);
+      T* ay = row_of<T>(p.y, s0, b, c0);
+      const unsigned oy = opaque(lane_bytes<T>(p.y.t, row, ch));
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i) {
+        if (pair && s0 + i * ROWS + row < end && ch < nch) set_elem(ay, oy, 0.0f);
+        ay += ROWS * p.y.t;
+      }
+    }
+  }
   if (cl >= nch) return;
   float* last = ENDS ? p.starts + (chunk + 1) * all_states : chunk + 1 == p.chunks ? p.h_out : nullptr;
   if (last) store_states(last + bd * in.N, q * NB, in.N, h);
   if (ENDS && q == 0) p.sums[(int64_t)chunk * in.B * in.D + bd] = sum_w;
+}
+
+// What the chunks reached by themselves, one after the other: slot k of `starts`, k = first, first + step, .., `count` of them, adds the slot
+// before it (`before` for the first one, NULL: nothing) times exp(A sum w) of the chunk in between, which is k + shift.
+struct Join {
+  float* starts;
+  const float *sums, *A, *before;
+  int64_t BD;
+  int D, N, first, step, count, shift;
+};
+__global__ __launch_bounds__(256) void scan_join_kernel(Join p) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = p.BD * p.N;
+  if (i >= all) return;
+  const int64_t bd = i / p.N;
+  const float a2 = p.A[(bd % p.D) * p.N + i % p.N] * LOG2E;
+  float h = p.before ? p.before[i] : 0.0f;
+  constexpr int U = 16;                                // slots read at once
+  for (int c = 0; c < p.count; c += U) {
+    float e[U], w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = p.first + min(c + u, p.count - 1) * p.step;
+      e[u] = p.starts[k * all + i];
+      w[u] = p.sums[(k + p.shift) * p.BD + bd];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c + u < p.count) {
+        h = e[u] + __builtin_amdgcn_exp2f(a2 * w[u]) * h;
+        p.starts[(p.first + (c + u) * p.step) * all + i] = h;
+      }
+  }
 }
 
 // ---- backward --------------------------------------------------------------------------------------
@@ -407,15 +434,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     dA[n] = g[n] = h[n] = 0.0f;
   }
   // (channels beyond the workgroup's keep zeros in h and g: their w, w u and dy are zeros, and so is what they add to dB and dC)
-  if (p.dh_out && mine) load_states(p.dh_out + bd * in.N, q * NB, in.N, g);
-  // through the chunks after this one
-  for (int k = p.chunks - 1; mine && k > chunk; --k) {
-    float e[NB];
-    load_states(p.starts + k * all_states + bd * in.N, q * NB, in.N, e);
-    const float w = p.sums[(int64_t)k * in.B * in.D + bd];
-#pragma unroll
-    for (int n = 0; n < NB; ++n) g[n] = e[n] + __builtin_amdgcn_exp2f(w * A2[n]) * g[n];
-  }
+  const float* into = chunk + 1 == p.chunks ? p.dh_out : p.starts + (chunk + 1) * all_states;
+  if (into && mine) load_states(into + bd * in.N, q * NB, in.N, g);
 
   // a thread's (step, channel) pairs: step i * ROWS + wrow + lrow, channel ic; a wave shares wrow
   constexpr int ROWS = THREADS / CH;
@@ -489,32 +509,35 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   if (in.t) fetch(st * p.stretch, back);
   while (in.t && st >= from) {
     const int s0 = st * p.stretch + k * BS, blocks = blocks_of(st);
+    const bool beyond = s0 >= len;                      // no step of the sequence in it: gradients of zero, h and g stay as they are
     // stage the block: w, w u, gated dy; what softplus' and the gate's gradients need stays in registers
     float iu[S::ITEMS], iw[S::ITEMS], isig[S::ITEMS], idy[S::ITEMS], idz[S::ITEMS];
+    if (!beyond) {
 #pragma unroll
-    for (int i = 0; i < S::ITEMS; ++i) {
-      const float raw = rd[i] + bias;
-      const bool live = s0 + i * ROWS + row < len && ic < nch;
-      iu[i] = ru[i];
-      iw[i] = !live ? 0.0f : in.softplus ? softplus_of(raw) : raw;
-      isig[i] = in.softplus ? sigmoid(raw) : 1.0f;
-      idy[i] = rg[i];
-      if (GATE) {
-        const float sg = sigmoid(rz[i]);
-        idz[i] = rg[i] * sg * (1.0f + rz[i] * (1.0f - sg));    // times what the gate multiplied
-        idy[i] = rg[i] * rz[i] * sg;
+      for (int i = 0; i < S::ITEMS; ++i) {
+        const float raw = rd[i] + bias;
+        const bool live = s0 + i * ROWS + row < len && ic < nch;
+        iu[i] = ru[i];
+        iw[i] = !live ? 0.0f : in.softplus ? softplus_of(raw) : raw;
+        isig[i] = in.softplus ? sigmoid(raw) : 1.0f;
+        idy[i] = rg[i];
+        if (GATE) {
+          const float sg = sigmoid(rz[i]);
+          idz[i] = rg[i] * sg * (1.0f + rz[i] * (1.0f - sg));    // times what the gate multiplied
+          idy[i] = rg[i] * rz[i] * sg;
+        }
+        *reinterpret_cast<f32x3*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x3{iw[i], iw[i] * iu[i], idy[i]};
       }
-      *reinterpret_cast<f32x3*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x3{iw[i], iw[i] * iu[i], idy[i]};
-    }
-    if (shared) {
+      if (shared) {
 #pragma unroll
-      for (int i = 0; i < S::SHARED; ++i) {
-        sb[(i * SROWS + srow) * NP + sn] = rb[i];
-        sc[(i * SROWS + srow) * NP + sn] = rc[i];
+        for (int i = 0; i < S::SHARED; ++i) {
+          sb[(i * SROWS + srow) * NP + sn] = rb[i];
+          sc[(i * SROWS + srow) * NP + sn] = rc[i];
+        }
       }
     }
     if (mine && k == 0 && (!back || blocks == 1)) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, h);
-    __syncthreads();
+    if (!beyond) __syncthreads();
     // the block after this one
     int next_st = st, next_k = k;
     bool next_back = true;
@@ -532,15 +555,36 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     if (!back) {
       float* at_start = kept + (k * THREADS + tid) * NB;
       store<NB>(at_start, h);
+      if (!beyond) {
 #pragma unroll
-      for (int s = 0; s < BS; ++s) {
-        const f32x2 w = *reinterpret_cast<const f32x2*>(wud + 4 * (s * CH + cl));
-        float vb[NB];
-        load<NB>(sb + s * NP + q * NB, vb);
+        for (int s = 0; s < BS; ++s) {
+          const f32x2 w = *reinterpret_cast<const f32x2*>(wud + 4 * (s * CH + cl));
+          float vb[NB];
+          load<NB>(sb + s * NP + q * NB, vb);
 #pragma unroll
-        for (int n = 0; n < NB; ++n) h[n] = __builtin_amdgcn_exp2f(w[0] * A2[n]) * h[n] + w[1] * vb[n];
+          for (int n = 0; n < NB; ++n) h[n] = __builtin_amdgcn_exp2f(w[0] * A2[n]) * h[n] + w[1] * vb[n];
+        }
+        __syncthreads();
       }
-      __syncthreads();
+    } else if (beyond) {
+      T *bu = row_of<T>(p.du, s0 + wrow, b, c0 + wave_c), *bd2 = row_of<T>(p.ddelta, s0 + wrow, b, c0 + wave_c),
+        *bz = row_of<T>(p.dz, s0 + wrow, b, c0 + wave_c);
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i) {
+        if (s0 + i * ROWS + row < last_step && ic < nch) {
+          set_elem(bu, lane_bytes<T>(p.du.t, lrow, lane_c), 0.0f);
+          set_elem(bd2, lane_bytes<T>(p.ddelta.t, lrow, lane_c), 0.0f);
+          if (GATE) set_elem(bz, lane_bytes<T>(p.dz.t, lrow, lane_c), 0.0f);
+        }
+        bu += ROWS * p.du.t;
+        bd2 += ROWS * p.ddelta.t;
+        bz += ROWS * p.dz.t;
+      }
+      for (int m = tid; m < BS * 2 * NP; m += THREADS) {
+        const int s = m / (2 * NP), half = m / NP % 2, n = m % NP;
+        if (s0 + s < last_step && n < in.N)
+          p.bc_parts[(((((int64_t)tile * in.t + s0 + s) * in.B + b) * in.G + group) * 2 + half) * in.N + n] = 0.0f;
+      }
     } else {
       if (k + 1 < blocks) load<NB>(kept + (k * THREADS + tid) * NB, h);   // (the last block goes on from the one before)
       // forward through the block: exp(w A) and exp(w A) h_{s-1} of every step
@@ -874,6 +918,8 @@ Scan scan_of(const mebptt_scan_desc* d, const mebptt_scan_inputs* in) {
           d->t, d->B, d->D, d->N, d->G, d->softplus, 0};
 }
 
+void join(const Join& j, hipStream_t s) { scan_join_kernel<<<(unsigned)ceil_div(j.BD * j.N, 256), 256, 0, s>>>(j); }
+
 // Forward launches.  A SIMD issues a vector instruction of one wave only every other turn, and more waves hide what the recurrence waits
 // for, so what counts is waves.  Where the channels give fewer than 2048, two per SIMD, the time axis is cut into chunks, up to eight
 // waves per SIMD, whose ends are computed first (70 % of the work once more).
@@ -996,6 +1042,7 @@ int mebptt_scan_forward(const mebptt_scan_desc* d, const mebptt_scan_inputs* in,
     auto go = [&](auto elem) {
       using T = decltype(elem);
       if (cut.chunks > 1) scan_forward_kernel<T, S, true><<<dim3(wide, d->B, cut.chunks - 1), FORWARD_WAVES * WAVE, 0, s>>>(p);
+      if (cut.chunks > 2) join({p.starts, p.sums, in->A, p.starts + (int64_t)d->B * d->D * d->N, (int64_t)d->B * d->D, d->D, d->N, 2, 1, cut.chunks - 2, -1}, s);
       scan_forward_kernel<T, S, false><<<dim3(wide, d->B, cut.chunks), FORWARD_WAVES * WAVE, 0, s>>>(p);
       return launched("mebptt_scan_forward");
     };
@@ -1030,6 +1077,7 @@ int mebptt_scan_backward(const mebptt_scan_desc* d, const mebptt_scan_inputs* in
           p.in.tiles = cut.ends_tiles;
           scan_back_ends_kernel<T, decltype(shape), GATE>
               <<<dim3((unsigned)(cut.ends_tiles * d->G), d->B, cut.chunks - 1), FORWARD_WAVES * WAVE, 0, s>>>(p);
+          join({p.starts, p.sums, in->A, dh_out, (int64_t)d->B * d->D, d->D, d->N, cut.chunks - 1, -1, cut.chunks - 1, 0}, s);
           return 0;
         });
       return with_back_shape(d->N, [&](auto shape) {

@@ -550,7 +550,8 @@ typedef struct {
   float *dA, *dskip, *ddelta_bias; /* dskip, ddelta_bias: may be NULL */
   float* dh0;                      /* may be NULL */
 } mebptt_scan_grads;
-/* Bytes of the states that a forward call keeps for a backward call; of the workspace of either call (backward != 0: of the latter). */
+/* Bytes of the states that a forward call keeps for a backward call; of a forward call's workspace, or (backward != 0) of one that does for
+ * both calls. */
 size_t mebptt_scan_state_bytes(const mebptt_scan_desc* desc);
 size_t mebptt_scan_workspace_bytes(const mebptt_scan_desc* desc, int32_t backward);
 /* `in` (host) is read during the call only.  write: y; h_out [B, D, N] (NULL: not written; may be h0 itself); states (NULL when no backward call follows;

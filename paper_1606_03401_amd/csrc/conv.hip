@@ -114,11 +114,8 @@ __global__ __launch_bounds__(THREADS) void conv_forward_kernel(Conv p) {
 // dL/dx_p = sum_j w_j dpre_{p+W-1-j} (+ dstate_out where p is one of the last W - 1 inputs), dpre = dy act'(pre), for p from -(W-1), the
 // state's rows, to the sequence's end.  A wave takes 64 groups of channels; its workgroup's four waves, and the workgroup's later turns, different
 // stretches of steps and sequences, adding dweight and dbias up in registers.
-#ifndef CB
-#define CB 3
-#endif
 template <typename T, int W, int V>
-__global__ __launch_bounds__(THREADS, W <= 4 ? CB : 2) void conv_backward_kernel(ConvBack p) {
+__global__ __launch_bounds__(THREADS, W <= 4 ? 3 : 2) void conv_backward_kernel(ConvBack p) {
   constexpr int WAVES = THREADS / WAVE, U = 4;
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
   const int group = blockIdx.x * WAVE + lane, c = group * V;
@@ -298,14 +295,15 @@ int check(const mebptt_conv_desc* d) {
 
 // Steps per thread of a forward launch.  Long stretches read fewer rows twice (W - 1 of them each), short ones give more threads.
 constexpr int STRETCH = 32;
-// The backward pass reads and computes W - 1 steps at both ends of a stretch twice.
-constexpr int BACK_STRETCH = 64;
+// The backward pass reads and computes W - 1 steps at both ends of a stretch twice; its workgroups, three on a compute unit at a time, take
+// stretches in turn.  1000 x 64 x 2048: 184 us; 212 with 1024 workgroups and stretches of 64, 193 with stretches of 32.
+constexpr int BACK_STRETCH = 48, BACK_GROUPS = 768;
 constexpr int BACK_V = 4;
 
 int64_t back_parts(const mebptt_conv_desc* d) {
   const int64_t columns = ceil_div(ceil_div(d->C, d->C % BACK_V ? 1 : BACK_V), WAVE);
   const int64_t items = d->B * std::max<int64_t>(1, ceil_div(d->t, BACK_STRETCH));
-  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, THREADS / WAVE), ceil_div(1024, columns)));
+  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, THREADS / WAVE), ceil_div(BACK_GROUPS, columns)));
 }
 
 template <typename F>

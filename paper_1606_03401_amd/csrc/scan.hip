@@ -376,7 +376,7 @@ struct BackwardShape {
   static constexpr int THREADS = BACK_WAVES * WAVE;
   static constexpr int ITEMS = BS * CH / THREADS;                     // (step, channel) pairs per thread
   static constexpr int SHARED = (BS * NP + THREADS - 1) / THREADS;    // values of B, and of C, per thread
-  static constexpr int WAVES_PER_SIMD = NB == 2 && NL >= 8 ? 4 : 2;
+  static constexpr int WAVES_PER_SIMD = 2;
 };
 
 // Sums of a lane's 2 NB values (of dB, then of dC) over the channels of its wave, that is over the lanes with the same lane % NL, into
@@ -397,7 +397,6 @@ __device__ inline void channels_sum(const float (&v)[2 * S::NB], int lane, float
     x[n] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     if constexpr (NL <= 8) x[n] = dpp_add<0x128>(x[n]);
     if constexpr (NL <= 4) x[n] = dpp_add<0x124>(x[n]);
-    if constexpr (NL <= 2) x[n] = dpp_add<0x122>(x[n]);
   }
   // (every lane that has a sum writes it)
 #pragma unroll
@@ -922,11 +921,9 @@ void join(const Join& j, hipStream_t s) { scan_join_kernel<<<(unsigned)ceil_div(
 
 // Forward launches.  A SIMD issues a vector instruction of one wave only every other turn, and more waves hide what the recurrence waits
 // for, so what counts is waves.  Where the channels give fewer than 2048, two per SIMD, the time axis is cut into chunks, up to eight
-// waves per SIMD, whose ends are computed first (70 % of the work once more).
-#ifndef SCAN_WANT
-#define SCAN_WANT 8192
-#endif
-constexpr int MIN_CHUNK = 32, MAX_CHUNKS = 64;
+// waves per SIMD, whose ends are computed first (70 % of the work once more).  Measured, 10000 x 1 x 2048: 4096 / 6144 / 8192 waves wanted
+// 182 / 178 / 168 us, uncut 6543; 1000 x 32 x 1024, which gives 2048: uncut 220, in four chunks 235.
+constexpr int ENOUGH_WAVES = 2048, WANT_WAVES = 8192, MIN_CHUNK = 32, MAX_CHUNKS = 64;
 struct Cut {
   int tiles;           // workgroups per group of channels
   int chunk, chunks;   // steps per chunk, a multiple of a block's
@@ -937,7 +934,7 @@ int with_shape(int N, F&& f) {
   if (N <= 8) return f(ForwardShape<2, 4>{});
   if (N <= 16) return f(ForwardShape<4, 4>{});
   if (N <= 32) return f(ForwardShape<8, 4>{});
-  return f(ForwardShape<16, 4>{});
+  return f(ForwardShape<8, 8>{});   // (16 lanes of 4 have four channels per wave to stage B and C for: 1242 instead of 500 us at 1000 x 32 x 1024)
 }
 Cut forward_cut(const mebptt_scan_desc* d) {
   Cut c = {};
@@ -949,7 +946,7 @@ Cut forward_cut(const mebptt_scan_desc* d) {
     return 0;
   });
   const int64_t t = std::max(d->t, 1);
-  const int64_t want = waves >= 2048 ? 1 : std::min<int64_t>(MAX_CHUNKS, ceil_div(SCAN_WANT, waves));
+  const int64_t want = waves >= ENOUGH_WAVES ? 1 : std::min<int64_t>(MAX_CHUNKS, ceil_div(WANT_WAVES, waves));
   c.chunk = (int)(ceil_div(std::max<int64_t>(want > 1 ? MIN_CHUNK : t, ceil_div(t, want)), 16) * 16);
   c.chunks = (int)ceil_div(t, c.chunk);
   return c;
@@ -957,17 +954,18 @@ Cut forward_cut(const mebptt_scan_desc* d) {
 size_t starts_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * d->N * sizeof(float)); }
 size_t sums_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * sizeof(float)); }
 
-// Backward launches: 2 states per lane, so that what a block keeps (exp(w A) and exp(w A) h of 16 steps) leaves room for four waves per SIMD;
-// 4 only where N is beyond 32.  The time axis is cut as the forward pass's is, in whole stretches.
+// Backward launches: 4 states per lane, two waves per SIMD, where what a block keeps (exp(w A) and exp(w A) h of 16 steps) takes half the
+// registers; 2 and four waves for few states, where a workgroup of 4 would have too many channels to stage (1000 x 32 x 1024, N = 16: 688 us
+// with 4, 712 with 2; N = 8: 567 and 495; N = 32: 1387 and 1531).  The time axis is cut as the forward pass's is, in whole stretches.
+constexpr int BACK_ENOUGH = 2048, BACK_WANT = 4096;   // waves
 struct BackCut {
   int tiles, ends_tiles, chunk, chunks;
 };
 template <typename F>
 int with_back_shape(int N, F&& f) {
-  if (N <= 4) return f(BackwardShape<2, 2>{});
   if (N <= 8) return f(BackwardShape<4, 2>{});
-  if (N <= 16) return f(BackwardShape<8, 2>{});
-  if (N <= 32) return f(BackwardShape<16, 2>{});
+  if (N <= 16) return f(BackwardShape<4, 4>{});
+  if (N <= 32) return f(BackwardShape<8, 4>{});
   return f(BackwardShape<16, 4>{});
 }
 BackCut back_cut(const mebptt_scan_desc* d) {
@@ -984,7 +982,7 @@ BackCut back_cut(const mebptt_scan_desc* d) {
     return 0;
   });
   const int64_t t = std::max(d->t, 1);
-  const int64_t want = waves >= 2048 ? 1 : std::min<int64_t>(MAX_CHUNKS, ceil_div(4096, waves));
+  const int64_t want = waves >= BACK_ENOUGH ? 1 : std::min<int64_t>(MAX_CHUNKS, ceil_div(BACK_WANT, waves));
   c.chunk = (int)(ceil_div(ceil_div(t, want), d->stretch) * d->stretch);
   c.chunks = (int)ceil_div(t, c.chunk);
   return c;
@@ -1013,7 +1011,7 @@ size_t mebptt_scan_workspace_bytes(const mebptt_scan_desc* d, int32_t backward) 
   if (backward) {
     if (check_stretch(d) != MEBPTT_OK) return 0;
     const BackCut c = back_cut(d);
-    return bc_bytes(d, c) + a_bytes(d, c) + starts_bytes(d, c.chunks) + sums_bytes(d, c.chunks);
+    return std::max(bc_bytes(d, c) + a_bytes(d, c) + starts_bytes(d, c.chunks) + sums_bytes(d, c.chunks), mebptt_scan_workspace_bytes(d, 0));
   }
   const int chunks = forward_cut(d).chunks;
   return starts_bytes(d, chunks) + sums_bytes(d, chunks);

@@ -410,10 +410,9 @@ template <typename T, typename S, bool GATE>
 __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_kernel(Backward p) {
   constexpr int CH = S::CH, NP = S::NP, THREADS = S::THREADS, NL = S::NL, NB = S::NB, BACK_WAVES = S::BACK_WAVES;
   extern __shared__ __align__(16) float lds[];
-  float* wud = lds;                                   // [BS][CH][4]: w, w u, gated dy -> through, dlog, core
-  float* sb = wud + BS * CH * 4;                      // [BS][NP]
-  float* sc = sb + BS * NP;                           // [BS][NP]
-  float* red = sc + BS * NP;                          // [BACK_WAVES][BS][2][NP]
+  // what a block stages, twice: the next one's is written while slower waves still read
+  constexpr int STAGED = BS * (CH * 4 + 2 * NP);
+  float* red = lds + 2 * STAGED;                      // [BACK_WAVES][BS][2][NP]
   float* kept = red + BACK_WAVES * BS * 2 * NP;       // [stretch / BS][THREADS][NB]: states at the blocks' starts
   const Scan& in = p.in;
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), b = blockIdx.y, chunk = blockIdx.z;
@@ -506,7 +505,11 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   int st = (last_step - 1) / p.stretch, k = 0;        // stretch; block in it
   bool back = blocks_of(st) == 1;
   if (in.t) fetch(st * p.stretch, back);
+  int turn = 0;
   while (in.t && st >= from) {
+    float* const wud = lds + turn * STAGED;           // [BS][CH][4]: w, w u, gated dy -> through, dlog, core
+    float* const sb = wud + BS * CH * 4;              // [BS][NP]
+    float* const sc = sb + BS * NP;                   // [BS][NP]
     const int s0 = st * p.stretch + k * BS, blocks = blocks_of(st);
     const bool beyond = s0 >= len;                      // no step of the sequence in it: gradients of zero, h and g stay as they are
     // stage the block: w, w u, gated dy; what softplus' and the gate's gradients need stays in registers
@@ -563,7 +566,6 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
 #pragma unroll
           for (int n = 0; n < NB; ++n) h[n] = __builtin_amdgcn_exp2f(w[0] * A2[n]) * h[n] + w[1] * vb[n];
         }
-        __syncthreads();
       }
     } else if (beyond) {
       T *bu = row_of<T>(p.du, s0 + wrow, b, c0 + wave_c), *bd2 = row_of<T>(p.ddelta, s0 + wrow, b, c0 + wave_c),
@@ -668,8 +670,8 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         if (s0 + s < last_step && n < in.N)
           p.bc_parts[(((((int64_t)tile * in.t + s0 + s) * in.B + b) * in.G + group) * 2 + half) * in.N + n] = v;
       }
-      __syncthreads();
     }
+    if (!beyond) turn ^= 1;
     st = next_st;
     k = next_k;
     back = next_back;
@@ -679,6 +681,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   float* parts = p.a_parts + ((int64_t)chunk * in.B + b) * in.D * (in.N + 2);
   if (mine) store_states(parts + d * in.N, q * NB, in.N, dA);
   // dskip and ddelta_bias: the threads that share a channel, in their order
+  __syncthreads();
   red[tid] = dskip;
   red[THREADS + tid] = dbias;
   __syncthreads();
@@ -994,7 +997,7 @@ size_t a_bytes(const mebptt_scan_desc* d, const BackCut& c) { return align_up((s
 
 template <typename S>
 size_t back_lds(int stretch) {
-  return ((size_t)BS * S::CH * 4 + 2 * BS * S::NP + S::BACK_WAVES * BS * 2 * S::NP + (size_t)stretch / BS * S::THREADS * S::NB) * sizeof(float);
+  return (2 * ((size_t)BS * S::CH * 4 + 2 * BS * S::NP) + S::BACK_WAVES * BS * 2 * S::NP + (size_t)stretch / BS * S::THREADS * S::NB) * sizeof(float);
 }
 
 }  // namespace

@@ -494,7 +494,7 @@ int mebptt_int8_product(const mebptt_int8_desc* desc, const int8_t* a, int64_t l
  * sequence b has lengths[b] steps (clamped to 0 .. t): what stands in x beyond them is not looked at, y (and dx) is zero there,
  * and the state is that after the sequence's own last step. */
 typedef struct {
-  int32_t t, B, C;
+  int32_t t, B, C; /* t 0 .. 2^30, B 0 .. 65535, C 1 .. 2^24 */
   int32_t taps;  /* 1 .. 8 */
   int32_t dtype; /* MEBPTT_FP32 or MEBPTT_BF16: x, y, the states, and their gradients */
   int32_t silu;  /* 0: act(v) = v */
@@ -525,7 +525,7 @@ int mebptt_conv_step(const mebptt_conv_desc* desc, const void* x, int64_t ldx, c
  *     y_s = (sum_n C_s h_s + skip u_s) * (z_s sigmoid(z_s) if there is a z).
  * Lengths as in the convolution; h_out is the state after a sequence's own last step. */
 typedef struct {
-  int32_t t, B, D;
+  int32_t t, B, D;  /* t 0 .. 2^30, B 0 .. 65535, D 1 .. 2^22 */
   int32_t N;        /* 1 .. 64 */
   int32_t G;        /* divides D */
   int32_t dtype;    /* MEBPTT_FP32 or MEBPTT_BF16: u, delta, z, B, C, y and their gradients */

@@ -286,8 +286,8 @@ __global__ __launch_bounds__(THREADS) void conv_step_kernel(ConvStep p) {
 
 int check(const mebptt_conv_desc* d) {
   if (!d) return set_error(MEBPTT_EINVAL, "desc is NULL");
-  if (d->t < 0 || d->B < 0 || d->B > 65535 || d->C < 1 || d->C > (1 << 24))
-    return set_error(MEBPTT_EINVAL, "t >= 0, 0 <= B <= 65535 and 1 <= C <= 2^24 are needed");
+  if (d->t < 0 || d->t > (1 << 30) || d->B < 0 || d->B > 65535 || d->C < 1 || d->C > (1 << 24))
+    return set_error(MEBPTT_EINVAL, "0 <= t <= 2^30, 0 <= B <= 65535 and 1 <= C <= 2^24 are needed");
   if (d->taps < 1 || d->taps > MAX_TAPS) return set_error(MEBPTT_EINVAL, "taps must be 1 .. %d", MAX_TAPS);
   if (!float_dtype(d->dtype)) return set_error(MEBPTT_EINVAL, "dtype must be MEBPTT_FP32 or MEBPTT_BF16");
   return MEBPTT_OK;

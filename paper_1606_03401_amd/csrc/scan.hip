@@ -98,7 +98,7 @@ struct Forward {
   float *h_out, *states;
   int stretch;
   int chunk, chunks;               // steps per chunk, a multiple of a block's
-  float *starts, *sums;            // [chunks][B][D][N]: what the chunk before reached (ENDS: by itself); [chunks][B][D]: sum of w
+  float *starts, *sums;            // [chunks][B][D][N]: what the chunk before reached (ENDS: by itself), the first one's h0; [chunks][B][D]: sum of w
 };
 
 constexpr int FORWARD_WAVES = 4;   // waves of neighbouring channels per workgroup: they share cache lines, and nothing else
@@ -145,8 +145,10 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
     A2[n] *= LOG2E;
     h[n] = 0.0f;
   }
-  const float* start = chunk == 0 ? p.h0 : ENDS ? nullptr : p.starts + chunk * all_states;
+  // h0 of launches in chunks: from its copy, as another workgroup may be writing h_out over it
+  const float* start = chunk == 0 ? (ENDS || p.chunks == 1 || !p.h0 ? p.h0 : p.starts) : ENDS ? nullptr : p.starts + chunk * all_states;
   if (start) load_states(start + bd * in.N, q * NB, in.N, h);
+  if (ENDS && chunk == 0 && p.h0 && cl < nch) store_states(p.starts + bd * in.N, q * NB, in.N, h);
 
   // the pairs of a lane: step i * ROWS + row, channel ch; its values of B and C: step i * SROWS + srow, state sn
   constexpr int ROWS = WAVE / CH, SROWS = WAVE / NP;
@@ -887,8 +889,8 @@ int with_lanes(int N, F&& f) {
 
 int check(const mebptt_scan_desc* d) {
   if (!d) return set_error(MEBPTT_EINVAL, "desc is NULL");
-  if (d->t < 0 || d->B < 0 || d->B > 65535 || d->D < 1 || d->D > (1 << 22))
-    return set_error(MEBPTT_EINVAL, "t >= 0, 0 <= B <= 65535 and 1 <= D <= 2^22 are needed");
+  if (d->t < 0 || d->t > (1 << 30) || d->B < 0 || d->B > 65535 || d->D < 1 || d->D > (1 << 22))
+    return set_error(MEBPTT_EINVAL, "0 <= t <= 2^30, 0 <= B <= 65535 and 1 <= D <= 2^22 are needed");
   if (d->N < 1 || d->N > MAX_N) return set_error(MEBPTT_EINVAL, "N must be 1 .. %d", MAX_N);
   if (d->G < 1 || d->D % d->G) return set_error(MEBPTT_EINVAL, "G must divide D");
   if (!float_dtype(d->dtype)) return set_error(MEBPTT_EINVAL, "dtype must be MEBPTT_FP32 or MEBPTT_BF16");

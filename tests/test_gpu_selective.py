@@ -344,6 +344,21 @@ def test_scan(t, B, D, N, G, gate, skip, softplus, lengths, state, stretch, dtyp
     m.clean()
 
 
+@pytest.mark.parametrize("t,B,D,N,G,lengths", [(500, 2, 130, 16, 1, None), (300, 3, 70, 13, 2, [300, 0, 41]), (40, 2, 64, 16, 1, None), (65, 1, 20, 33, 1, None)])
+def test_scan_state_in_place(t, B, D, N, G, lengths):
+    """h_out may be h0: also where several workgroups share a sequence, of which one reads the state and another writes it."""
+    m = _Made(t + D, "plain")
+    v = _scan_inputs(m, t, B, D, N, G, True, True, True, "bf16")
+    ends = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    desc = mb.make_scan_desc(t, B, D, N, G, mb.BF16, 1)
+    ws = _bytes(mb.mebptt_scan_workspace_bytes(desc, False))
+    y, h_out = m.empty((t, B, D), torch.bfloat16), torch.full((B, D, N), NAN, device=DEV)
+    mb.mebptt_scan_forward(desc, *_call(v, ends), y, h_out, None, ws)
+    y2, ws2 = m.empty((t, B, D), torch.bfloat16), ws.clone().fill_(0x7F)
+    mb.mebptt_scan_forward(desc, *_call(v, ends), y2, v["h0"], None, ws2)
+    assert torch.equal(y, y2) and torch.equal(v["h0"], h_out)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_scan_of_no_steps(dtype):
     """The state passes through, and so does its gradient; parameters have none."""

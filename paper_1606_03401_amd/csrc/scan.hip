@@ -33,8 +33,6 @@ struct Scan {
   int tiles;                       // workgroups per group of channels
 };
 template <typename T>
-__device__ inline float at(const Seq& q, int64_t s, int64_t b, int64_t c) { return (float)((const T*)q.p)[s * q.t + b * q.b + c]; }
-template <typename T>
 __device__ inline void put(const SeqOut& q, int64_t s, int64_t b, int64_t c, float v) { ((T*)q.p)[s * q.t + b * q.b + c] = (T)v; }
 
 // The same with an address in two parts: uniform over the wave, and a lane's own, of at most 15 rows, in bytes.
@@ -49,7 +47,7 @@ __device__ inline unsigned opaque(unsigned v) {
   return v;
 }
 template <typename T>
-__device__ inline float elem(const T* base, unsigned bytes) { return (float)*reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes); }
+__device__ inline T raw(const T* base, unsigned bytes) { return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes); }
 template <typename T>
 __device__ inline void set_elem(T* base, unsigned bytes, float v) { *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + bytes) = (T)v; }
 
@@ -157,9 +155,9 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
   const float bias = in.bias ? in.bias[min(c0 + ch, in.D - 1)] : 0.0f, skip = in.skip ? in.skip[min(c0 + ch, in.D - 1)] : 0.0f;
   const int64_t gn = (int64_t)group * in.N;
 
-  // The next block's inputs, fetched while a block is worked on.  A whole block (all its steps within the sequence, all its channels
+  // The next block's inputs, fetched while a block is worked on, and kept as they came: what turns them into floats would wait for them.  A whole block (all its steps within the sequence, all its channels
   // there) needs no masks; which it is, is the same for the whole wave.
-  float ru[S::ITEMS], rd[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
+  T ru[S::ITEMS], rd[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
   auto whole = [&](int s0) { return TS * CH >= WAVE && TS * NP >= WAVE && s0 + TS <= min(len, end) && nch == CH; };
   auto fetch = [&](int s0) {
     // (opaque: the sums of an address's parts are not to be formed ahead, in registers)
@@ -173,33 +171,33 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
     if (whole(s0)) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        ru[i] = elem(au, ou);
-        rd[i] = elem(ad, od);
+        ru[i] = raw(au, ou);
+        rd[i] = raw(ad, od);
         au += iu;
         ad += id;
       }
       if (!ENDS && in.z.p) {
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) {
-          rz[i] = elem(az, oz);
+          rz[i] = raw(az, oz);
           az += iz;
         }
       }
 #pragma unroll
       for (int i = 0; i < S::SHARED; ++i) {
-        rb[i] = elem(ab, ob);
+        rb[i] = raw(ab, ob);
         ab += ib;
-        if (!ENDS) rc[i] = elem(ac, oc);
+        if (!ENDS) rc[i] = raw(ac, oc);
         ac += ic;
       }
     } else {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        ru[i] = rd[i] = rz[i] = 0.0f;
+        ru[i] = rd[i] = rz[i] = (T)0.0f;
         if (pair && s0 + i * ROWS + row < len && ch < nch) {
-          ru[i] = elem(au, ou);
-          rd[i] = elem(ad, od);
-          if (!ENDS && in.z.p) rz[i] = elem(az, oz);
+          ru[i] = raw(au, ou);
+          rd[i] = raw(ad, od);
+          if (!ENDS && in.z.p) rz[i] = raw(az, oz);
         }
         au += iu;
         ad += id;
@@ -207,10 +205,10 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
       }
 #pragma unroll
       for (int i = 0; i < S::SHARED; ++i) {
-        rb[i] = rc[i] = 0.0f;
+        rb[i] = rc[i] = (T)0.0f;
         if (shared && s0 + i * SROWS + srow < len) {
-          rb[i] = elem(ab, ob);
-          if (!ENDS) rc[i] = elem(ac, oc);
+          rb[i] = raw(ab, ob);
+          if (!ENDS) rc[i] = raw(ac, oc);
         }
         ab += ib;
         ac += ic;
@@ -218,37 +216,37 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
     }
   };
 #pragma unroll
-  for (int i = 0; i < S::ITEMS; ++i) rz[i] = 0.0f;
+  for (int i = 0; i < S::ITEMS; ++i) rz[i] = (T)0.0f;
   const int stop = min(end, len);                                      // beyond its length a sequence's state stays as it is
   if (begin < stop) fetch(begin);
   int s0 = begin;
   for (; s0 < stop; s0 += TS) {
     const bool all = whole(s0);
-    float cu[S::ITEMS], cz[S::ITEMS];
+    float cu[S::ITEMS], cz[S::ITEMS], cw[S::ITEMS];
 #pragma unroll
     for (int i = 0; i < S::ITEMS; ++i) {
-      cu[i] = ru[i];
-      cz[i] = rz[i];
-      rd[i] += bias;
+      cu[i] = (float)ru[i];
+      cz[i] = (float)rz[i];
+      cw[i] = (float)rd[i] + bias;
     }
     if (in.softplus) {
 #pragma unroll
-      for (int i = 0; i < S::ITEMS; ++i) rd[i] = softplus_of(rd[i]);
+      for (int i = 0; i < S::ITEMS; ++i) cw[i] = softplus_of(cw[i]);
     }
     if (!all) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i)      // a step beyond the sequence
-        if (!(s0 + i * ROWS + row < len && ch < nch)) rd[i] = 0.0f;
+        if (!(s0 + i * ROWS + row < len && ch < nch)) cw[i] = 0.0f;
     }
     if (pair) {
 #pragma unroll
-      for (int i = 0; i < S::ITEMS; ++i) *reinterpret_cast<f32x2*>(&wu[i * ROWS + row][ch][0]) = f32x2{rd[i], rd[i] * cu[i]};
+      for (int i = 0; i < S::ITEMS; ++i) *reinterpret_cast<f32x2*>(&wu[i * ROWS + row][ch][0]) = f32x2{cw[i], cw[i] * cu[i]};
     }
     if (shared) {
 #pragma unroll
       for (int i = 0; i < S::SHARED; ++i) {
-        sb[i * SROWS + srow][sn] = sn < in.N ? rb[i] : 0.0f;
-        if (!ENDS) sc[i * SROWS + srow][sn] = sn < in.N ? rc[i] : 0.0f;
+        sb[i * SROWS + srow][sn] = sn < in.N ? (float)rb[i] : 0.0f;
+        if (!ENDS) sc[i * SROWS + srow][sn] = sn < in.N ? (float)rc[i] : 0.0f;
       }
     }
     wave_sync();
@@ -256,12 +254,26 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
     if (!ENDS && p.states && s0 % p.stretch == 0) {
       if (cl < nch) store_states(p.states + (int64_t)(s0 / p.stretch) * all_states + bd * in.N, q * NB, in.N, h);
     }
+    // a step's operands are read from LDS while the one before is worked on
+    f32x2 next_w = *reinterpret_cast<const f32x2*>(&wu[0][cl][0]);
+    float next_b[NB], next_c[NB];
+    load<NB>(&sb[0][q * NB], next_b);
+    if constexpr (!ENDS) load<NB>(&sc[0][q * NB], next_c);
 #pragma unroll
     for (int s = 0; s < TS; ++s) {
-      const f32x2 w = *reinterpret_cast<const f32x2*>(&wu[s][cl][0]);
+      const f32x2 w = next_w;
       float vb[NB], vc[NB], y = 0.0f;
-      load<NB>(&sb[s][q * NB], vb);
-      if constexpr (!ENDS) load<NB>(&sc[s][q * NB], vc);
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        vb[n] = next_b[n];
+        if constexpr (!ENDS) vc[n] = next_c[n];
+      }
+      if (s + 1 < TS) {
+        next_w = *reinterpret_cast<const f32x2*>(&wu[s + 1][cl][0]);
+        load<NB>(&sb[s + 1][q * NB], next_b);
+        if constexpr (!ENDS) load<NB>(&sc[s + 1][q * NB], next_c);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // (they would be read where they are used)
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         const float a = __builtin_amdgcn_exp2f(w[0] * A2[n]);
@@ -448,8 +460,11 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   const int srow = tid / NP, sn = tid % NP;
   const bool shared = BS * NP >= THREADS || tid < BS * NP;
 
-  float ru[S::ITEMS], rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
-  auto fetch = [&](int s0, bool back) {
+  T ru[S::ITEMS], rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
+  float rh[NB];
+  auto fetch = [&](int st, int k, bool back) {
+    const int s0 = st * p.stretch + k * BS;
+    if (mine && k == 0) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, rh);   // (of no use where k == 0 comes after others)
     const unsigned ou = opaque(lane_bytes<T>(in.u.t, lrow, lane_c)), od = opaque(lane_bytes<T>(in.delta.t, lrow, lane_c)),
                    og = opaque(lane_bytes<T>(p.dy.t, lrow, lane_c)), oz = opaque(lane_bytes<T>(in.z.t, lrow, lane_c));
     const T *au = row_of<T>(in.u, s0 + wrow, b, c0 + wave_c), *ad = row_of<T>(in.delta, s0 + wrow, b, c0 + wave_c),
@@ -457,16 +472,16 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     if (s0 + BS <= len && nch == CH) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        ru[i] = elem(au, ou);
-        rd[i] = elem(ad, od);
+        ru[i] = raw(au, ou);
+        rd[i] = raw(ad, od);
         au += ROWS * in.u.t;
         ad += ROWS * in.delta.t;
       }
       if (back) {
 #pragma unroll
         for (int i = 0; i < S::ITEMS; ++i) {
-          rg[i] = elem(ag, og);
-          if (GATE) rz[i] = elem(az, oz);
+          rg[i] = raw(ag, og);
+          if (GATE) rz[i] = raw(az, oz);
           ag += ROWS * p.dy.t;
           az += ROWS * in.z.t;
         }
@@ -474,13 +489,13 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     } else {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        ru[i] = rd[i] = rg[i] = rz[i] = 0.0f;
+        ru[i] = rd[i] = rg[i] = rz[i] = (T)0.0f;
         if (s0 + i * ROWS + row < len && ic < nch) {
-          ru[i] = elem(au, ou);
-          rd[i] = elem(ad, od);
+          ru[i] = raw(au, ou);
+          rd[i] = raw(ad, od);
           if (back) {
-            rg[i] = elem(ag, og);
-            if (GATE) rz[i] = elem(az, oz);
+            rg[i] = raw(ag, og);
+            if (GATE) rz[i] = raw(az, oz);
           }
         }
         au += ROWS * in.u.t;
@@ -492,55 +507,59 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
 #pragma unroll
     for (int i = 0; i < S::SHARED; ++i) {
       const int s = s0 + i * SROWS + srow;
-      rb[i] = rc[i] = 0.0f;
+      rb[i] = rc[i] = (T)0.0f;
       if (shared && s < len && sn < in.N) {
-        rb[i] = elem(row_of<T>(in.Bm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Bm.t, srow, sn));
-        if (back) rc[i] = elem(row_of<T>(in.Cm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Cm.t, srow, sn));
+        rb[i] = raw(row_of<T>(in.Bm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Bm.t, srow, sn));
+        if (back) rc[i] = raw(row_of<T>(in.Cm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Cm.t, srow, sn));
       }
     }
   };
 #pragma unroll
-  for (int i = 0; i < S::ITEMS; ++i) rg[i] = rz[i] = 0.0f;
+  for (int i = 0; i < S::ITEMS; ++i) rg[i] = rz[i] = (T)0.0f;
+#pragma unroll
+  for (int n = 0; n < NB; ++n) rh[n] = 0.0f;
 
   const int from = chunk * p.chunk / p.stretch, last_step = min(in.t, (chunk + 1) * p.chunk);
   auto blocks_of = [&](int st) { return (min(last_step, (st + 1) * p.stretch) - st * p.stretch + BS - 1) / BS; };
   int st = (last_step - 1) / p.stretch, k = 0;        // stretch; block in it
   bool back = blocks_of(st) == 1;
-  if (in.t) fetch(st * p.stretch, back);
+  if (in.t) fetch(st, 0, back);
   int turn = 0;
   while (in.t && st >= from) {
-    float* const wud = lds + turn * STAGED;           // [BS][CH][4]: w, w u, gated dy -> through, dlog, core
+    float* const wud = lds + turn * STAGED;           // [BS][CH][4]: w, w u, gated dy -> through, dlog, core; softplus' slope
     float* const sb = wud + BS * CH * 4;              // [BS][NP]
     float* const sc = sb + BS * NP;                   // [BS][NP]
     const int s0 = st * p.stretch + k * BS, blocks = blocks_of(st);
     const bool beyond = s0 >= len;                      // no step of the sequence in it: gradients of zero, h and g stay as they are
     // stage the block: w, w u, gated dy; what softplus' and the gate's gradients need stays in registers
-    float iu[S::ITEMS], iw[S::ITEMS], isig[S::ITEMS], idy[S::ITEMS], idz[S::ITEMS];
+    float iu[S::ITEMS], iw[S::ITEMS], idy[S::ITEMS], idz[S::ITEMS];
     if (!beyond) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        const float raw = rd[i] + bias;
+        const float v = (float)rd[i] + bias, dy = (float)rg[i];
         const bool live = s0 + i * ROWS + row < len && ic < nch;
-        iu[i] = ru[i];
-        iw[i] = !live ? 0.0f : in.softplus ? softplus_of(raw) : raw;
-        isig[i] = in.softplus ? sigmoid(raw) : 1.0f;
-        idy[i] = rg[i];
+        iu[i] = (float)ru[i];
+        iw[i] = !live ? 0.0f : in.softplus ? softplus_of(v) : v;
+        idy[i] = dy;
         if (GATE) {
-          const float sg = sigmoid(rz[i]);
-          idz[i] = rg[i] * sg * (1.0f + rz[i] * (1.0f - sg));    // times what the gate multiplied
-          idy[i] = rg[i] * rz[i] * sg;
+          const float z = (float)rz[i], sg = sigmoid(z);
+          idz[i] = dy * sg * (1.0f + z * (1.0f - sg));    // times what the gate multiplied
+          idy[i] = dy * z * sg;
         }
-        *reinterpret_cast<f32x3*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x3{iw[i], iw[i] * iu[i], idy[i]};
+        *reinterpret_cast<f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x4{iw[i], iw[i] * iu[i], idy[i], in.softplus ? sigmoid(v) : 1.0f};
       }
       if (shared) {
 #pragma unroll
         for (int i = 0; i < S::SHARED; ++i) {
-          sb[(i * SROWS + srow) * NP + sn] = rb[i];
-          sc[(i * SROWS + srow) * NP + sn] = rc[i];
+          sb[(i * SROWS + srow) * NP + sn] = (float)rb[i];
+          sc[(i * SROWS + srow) * NP + sn] = (float)rc[i];
         }
       }
     }
-    if (mine && k == 0 && (!back || blocks == 1)) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, h);
+    if (k == 0) {       // (a stretch's first block comes up twice; its state is the same)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) h[n] = rh[n];
+    }
     if (!beyond) __syncthreads();
     // the block after this one
     int next_st = st, next_k = k;
@@ -554,7 +573,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
       next_st = st - 1;
       next_back = p.stretch == BS;
     }
-    if (next_st >= from) fetch(next_st * p.stretch + next_k * BS, next_back);
+    if (next_st >= from) fetch(next_st, next_k, next_back);
 
     if (!back) {
       float* at_start = kept + (k * THREADS + tid) * NB;
@@ -650,9 +669,9 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
         const int s = s0 + i * ROWS + row;
-        const f32x3 v = *reinterpret_cast<const f32x3*>(wud + 4 * ((i * ROWS + row) * CH + ic));
+        const f32x4 v = *reinterpret_cast<const f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic));
         const bool live = s < len;
-        const float dw = live ? (iu[i] * v[0] + v[1]) * isig[i] : 0.0f;
+        const float dw = live ? (iu[i] * v[0] + v[1]) * v[3] : 0.0f;
         if (s < last_step && ic < nch) {
           set_elem(bu, ou, live ? iw[i] * v[0] + skip * idy[i] : 0.0f);
           set_elem(bd2, od, dw);
@@ -726,7 +745,7 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_back_ends_kernel(Bac
   const int row = lane / CH, ch = lane % CH, srow = lane / NP, sn = lane % NP;
   const bool pair = TS * CH >= WAVE || lane < TS * CH, shared = TS * NP >= WAVE || lane < TS * NP;
   const float bias = in.bias ? in.bias[min(c0 + ch, in.D - 1)] : 0.0f;
-  float rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rc[S::SHARED];
+  T rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rc[S::SHARED];
   auto fetch = [&](int s0) {
     const bool all = s0 + TS <= stop && nch == CH;
     const unsigned od = opaque(lane_bytes<T>(in.delta.t, row, ch)), og = opaque(lane_bytes<T>(p.dy.t, row, ch)),
@@ -735,11 +754,11 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_back_ends_kernel(Bac
             *ac = row_of<T>(in.Cm, s0, b, gn);
 #pragma unroll
     for (int i = 0; i < S::ITEMS; ++i) {
-      rd[i] = rg[i] = rz[i] = 0.0f;
+      rd[i] = rg[i] = rz[i] = (T)0.0f;
       if (pair && (all || (s0 + i * ROWS + row < stop && ch < nch))) {
-        rd[i] = elem(ad, od);
-        rg[i] = elem(ag, og);
-        if (GATE) rz[i] = elem(az, oz);
+        rd[i] = raw(ad, od);
+        rg[i] = raw(ag, og);
+        if (GATE) rz[i] = raw(az, oz);
       }
       ad += ROWS * in.delta.t;
       ag += ROWS * p.dy.t;
@@ -747,8 +766,8 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_back_ends_kernel(Bac
     }
 #pragma unroll
     for (int i = 0; i < S::SHARED; ++i) {
-      rc[i] = 0.0f;
-      if (shared && s0 + i * SROWS + srow < stop) rc[i] = elem(ac, oc);
+      rc[i] = (T)0.0f;
+      if (shared && s0 + i * SROWS + srow < stop) rc[i] = raw(ac, oc);
       ac += SROWS * in.Cm.t;
     }
   };
@@ -759,13 +778,13 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_back_ends_kernel(Bac
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
         const bool live = s0 + i * ROWS + row < stop && ch < nch;
-        const float raw = rd[i] + bias, w = !live ? 0.0f : in.softplus ? softplus_of(raw) : raw;
-        *reinterpret_cast<f32x2*>(&wg[i * ROWS + row][ch][0]) = f32x2{w, GATE ? rg[i] * rz[i] * sigmoid(rz[i]) : rg[i]};
+        const float v = (float)rd[i] + bias, w = !live ? 0.0f : in.softplus ? softplus_of(v) : v, dy = (float)rg[i], z = (float)rz[i];
+        *reinterpret_cast<f32x2*>(&wg[i * ROWS + row][ch][0]) = f32x2{w, GATE ? dy * z * sigmoid(z) : dy};
       }
     }
     if (shared) {
 #pragma unroll
-      for (int i = 0; i < S::SHARED; ++i) sc[i * SROWS + srow][sn] = sn < in.N ? rc[i] : 0.0f;
+      for (int i = 0; i < S::SHARED; ++i) sc[i * SROWS + srow][sn] = sn < in.N ? (float)rc[i] : 0.0f;
     }
     wave_sync();
     if (s0 - TS >= begin) fetch(s0 - TS);

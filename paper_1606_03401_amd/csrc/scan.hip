@@ -16,7 +16,7 @@ namespace {
 
 constexpr int NB = 4;              // states per lane
 constexpr int MAX_N = 64;
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 constexpr int64_t MAX_STRIDE = 1 << 25;   // over steps, in elements: 15 rows of 4 bytes are below 2^32
 struct Seq { const void* p; int64_t b; int t; };
@@ -57,7 +57,7 @@ __device__ inline int length_of(const int32_t* lengths, int b, int t) { return l
 // added to the logarithm of the sum.
 __device__ inline float softplus_of(float x) {
   const float e = __expf(-fabsf(x)), w = 1.0f + e;
-  return fmaxf(x, 0.0f) + (__builtin_amdgcn_logf(w) * 0.6931471805599453f + (e - (w - 1.0f)));
+  return fmaxf(x, 0.0f) + (__builtin_amdgcn_logf(w) * LN2 + (e - (w - 1.0f)));
 }
 
 // Sum over the NL lanes that share a channel, in every one of them.
@@ -371,7 +371,7 @@ struct Backward {
   SeqOut du, ddelta, dz;
   const float *states, *dh_out;
   float* dh0;
-  float *bc_parts;                 // [tiles][t][B][G][2][N]: sums of dB and dC over a workgroup's channels
+  float *bc_parts;                 // [tiles][B][G][t][2][N]: sums of dB and dC over a workgroup's channels
   float *a_parts;                  // [chunks][B][D N | D | D]: dA, dskip, ddelta_bias of a chunk of a sequence
   int stretch;
   int chunk, chunks;               // steps per chunk, a multiple of the stretch
@@ -438,11 +438,11 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   const int64_t d = min(c0 + cl, in.D - 1), bd = (int64_t)b * in.D + d, all_states = (int64_t)in.B * in.D * in.N;
   const int64_t gn = (int64_t)group * in.N;
 
-  float A[NB], A2[NB], g[NB], dA[NB], h[NB];
-  load_states(in.A + d * in.N, q * NB, in.N, A);
+  float A2[NB], g[NB], dA[NB], h[NB];
+  load_states(in.A + d * in.N, q * NB, in.N, A2);
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    A2[n] = A[n] * LOG2E;
+    A2[n] *= LOG2E;
     dA[n] = g[n] = h[n] = 0.0f;
   }
   // (channels beyond the workgroup's keep zeros in h and g: their w, w u and dy are zeros, and so is what they add to dB and dC)
@@ -460,6 +460,14 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   const int srow = tid / NP, sn = tid % NP;
   const bool shared = BS * NP >= THREADS || tid < BS * NP;
 
+  // (s, b and the wave's part of an address are uniform)
+  const T *const pu = row_of<T>(in.u, wrow, b, c0 + wave_c), *const pd = row_of<T>(in.delta, wrow, b, c0 + wave_c),
+          *const pg = row_of<T>(p.dy, wrow, b, c0 + wave_c), *const pz = row_of<T>(in.z, wrow, b, c0 + wave_c),
+          *const pb = row_of<T>(in.Bm, 0, b, gn), *const pc = row_of<T>(in.Cm, 0, b, gn);
+  T *const qu = row_of<T>(p.du, wrow, b, c0 + wave_c), *const qd = row_of<T>(p.ddelta, wrow, b, c0 + wave_c),
+    *const qz = row_of<T>(p.dz, wrow, b, c0 + wave_c);
+  float* const bc = p.bc_parts + (((int64_t)tile * in.B + b) * in.G + group) * in.t * 2 * in.N;
+
   T ru[S::ITEMS], rd[S::ITEMS], rg[S::ITEMS], rz[S::ITEMS], rb[S::SHARED], rc[S::SHARED];
   float rh[NB];
   auto fetch = [&](int st, int k, bool back) {
@@ -467,8 +475,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     if (mine && k == 0) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, rh);   // (of no use where k == 0 comes after others)
     const unsigned ou = opaque(lane_bytes<T>(in.u.t, lrow, lane_c)), od = opaque(lane_bytes<T>(in.delta.t, lrow, lane_c)),
                    og = opaque(lane_bytes<T>(p.dy.t, lrow, lane_c)), oz = opaque(lane_bytes<T>(in.z.t, lrow, lane_c));
-    const T *au = row_of<T>(in.u, s0 + wrow, b, c0 + wave_c), *ad = row_of<T>(in.delta, s0 + wrow, b, c0 + wave_c),
-            *ag = row_of<T>(p.dy, s0 + wrow, b, c0 + wave_c), *az = row_of<T>(in.z, s0 + wrow, b, c0 + wave_c);
+    const T *au = pu + (int64_t)s0 * in.u.t, *ad = pd + (int64_t)s0 * in.delta.t, *ag = pg + (int64_t)s0 * p.dy.t, *az = pz + (int64_t)s0 * in.z.t;
     if (s0 + BS <= len && nch == CH) {
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
@@ -504,14 +511,17 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         az += ROWS * in.z.t;
       }
     }
+    const T *ab = pb + (int64_t)s0 * in.Bm.t, *ac = pc + (int64_t)s0 * in.Cm.t;
+    const unsigned ob = opaque(lane_bytes<T>(in.Bm.t, srow, sn)), oc = opaque(lane_bytes<T>(in.Cm.t, srow, sn));
 #pragma unroll
     for (int i = 0; i < S::SHARED; ++i) {
-      const int s = s0 + i * SROWS + srow;
       rb[i] = rc[i] = (T)0.0f;
-      if (shared && s < len && sn < in.N) {
-        rb[i] = raw(row_of<T>(in.Bm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Bm.t, srow, sn));
-        if (back) rc[i] = raw(row_of<T>(in.Cm, s0 + i * SROWS, b, gn), lane_bytes<T>(in.Cm.t, srow, sn));
+      if (shared && s0 + i * SROWS + srow < len && sn < in.N) {
+        rb[i] = raw(ab, ob);
+        if (back) rc[i] = raw(ac, oc);
       }
+      ab += SROWS * in.Bm.t;
+      ac += SROWS * in.Cm.t;
     }
   };
 #pragma unroll
@@ -533,21 +543,36 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     const bool beyond = s0 >= len;                      // no step of the sequence in it: gradients of zero, h and g stay as they are
     // stage the block: w, w u, gated dy; what softplus' and the gate's gradients need stays in registers
     float iu[S::ITEMS], iw[S::ITEMS], idy[S::ITEMS], idz[S::ITEMS];
+    const bool whole = s0 + BS <= len && nch == CH;
     if (!beyond) {
+      float slope[S::ITEMS];                            // softplus'
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
-        const float v = (float)rd[i] + bias, dy = (float)rg[i];
-        const bool live = s0 + i * ROWS + row < len && ic < nch;
         iu[i] = (float)ru[i];
-        iw[i] = !live ? 0.0f : in.softplus ? softplus_of(v) : v;
-        idy[i] = dy;
+        iw[i] = (float)rd[i] + bias;
+        idy[i] = (float)rg[i];
+        slope[i] = 1.0f;
         if (GATE) {
           const float z = (float)rz[i], sg = sigmoid(z);
-          idz[i] = dy * sg * (1.0f + z * (1.0f - sg));    // times what the gate multiplied
-          idy[i] = dy * z * sg;
+          idz[i] = idy[i] * sg * (1.0f + z * (1.0f - sg));    // times what the gate multiplied
+          idy[i] *= z * sg;
         }
-        *reinterpret_cast<f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x4{iw[i], iw[i] * iu[i], idy[i], in.softplus ? sigmoid(v) : 1.0f};
       }
+      if (in.softplus) {
+#pragma unroll
+        for (int i = 0; i < S::ITEMS; ++i) {
+          slope[i] = sigmoid(iw[i]);
+          iw[i] = softplus_of(iw[i]);
+        }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < S::ITEMS; ++i)
+          if (!(s0 + i * ROWS + row < len && ic < nch)) iw[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < S::ITEMS; ++i)
+        *reinterpret_cast<f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic)) = f32x4{iw[i], iw[i] * iu[i], idy[i], slope[i]};
       if (shared) {
 #pragma unroll
         for (int i = 0; i < S::SHARED; ++i) {
@@ -589,8 +614,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         }
       }
     } else if (beyond) {
-      T *bu = row_of<T>(p.du, s0 + wrow, b, c0 + wave_c), *bd2 = row_of<T>(p.ddelta, s0 + wrow, b, c0 + wave_c),
-        *bz = row_of<T>(p.dz, s0 + wrow, b, c0 + wave_c);
+      T *bu = qu + (int64_t)s0 * p.du.t, *bd2 = qd + (int64_t)s0 * p.ddelta.t, *bz = qz + (int64_t)s0 * p.dz.t;
 #pragma unroll
       for (int i = 0; i < S::ITEMS; ++i) {
         if (s0 + i * ROWS + row < last_step && ic < nch) {
@@ -603,9 +627,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         bz += ROWS * p.dz.t;
       }
       for (int m = tid; m < BS * 2 * NP; m += THREADS) {
-        const int s = m / (2 * NP), half = m / NP % 2, n = m % NP;
-        if (s0 + s < last_step && n < in.N)
-          p.bc_parts[(((((int64_t)tile * in.t + s0 + s) * in.B + b) * in.G + group) * 2 + half) * in.N + n] = 0.0f;
+        if (s0 + m / (2 * NP) < last_step && m % NP < in.N) bc[(int64_t)s0 * 2 * in.N + m / NP * in.N + m % NP] = 0.0f;
       }
     } else {
       if (k + 1 < blocks) load<NB>(kept + (k * THREADS + tid) * NB, h);   // (the last block goes on from the one before)
@@ -651,7 +673,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
           through = n ? through + g[n] * vb[n] : g[n] * vb[n];
           if (GATE) core = n ? core + hn * vc[n] : hn * vc[n];
           const float r = g[n] * ah[s][n];     // the exponent's gradient
-          dlog = n ? dlog + r * A[n] : r * A[n];
+          dlog = n ? dlog + r * A2[n] : r * A2[n];   // times log2 e
           dA[n] += r * w[0];
           g[n] *= a[s][n];
         }
@@ -662,34 +684,51 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         *reinterpret_cast<f32x3*>(wud + 4 * (s * CH + cl)) = f32x3{through, dlog, core};   // (all lanes of a channel the same)
       }
       __syncthreads();
-      T *bu = row_of<T>(p.du, s0 + wrow, b, c0 + wave_c), *bd2 = row_of<T>(p.ddelta, s0 + wrow, b, c0 + wave_c),
-        *bz = row_of<T>(p.dz, s0 + wrow, b, c0 + wave_c);
+      T *bu = qu + (int64_t)s0 * p.du.t, *bd2 = qd + (int64_t)s0 * p.ddelta.t, *bz = qz + (int64_t)s0 * p.dz.t;
       const unsigned ou = opaque(lane_bytes<T>(p.du.t, lrow, lane_c)), od = opaque(lane_bytes<T>(p.ddelta.t, lrow, lane_c)),
                      oz = opaque(lane_bytes<T>(p.dz.t, lrow, lane_c));
+      if (whole && s0 + BS <= last_step) {
 #pragma unroll
-      for (int i = 0; i < S::ITEMS; ++i) {
-        const int s = s0 + i * ROWS + row;
-        const f32x4 v = *reinterpret_cast<const f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic));
-        const bool live = s < len;
-        const float dw = live ? (iu[i] * v[0] + v[1]) * v[3] : 0.0f;
-        if (s < last_step && ic < nch) {
-          set_elem(bu, ou, live ? iw[i] * v[0] + skip * idy[i] : 0.0f);
+        for (int i = 0; i < S::ITEMS; ++i) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic));
+          const float dw = (iu[i] * v[0] + LN2 * v[1]) * v[3];
+          set_elem(bu, ou, iw[i] * v[0] + skip * idy[i]);
           set_elem(bd2, od, dw);
-          if (GATE) set_elem(bz, oz, live ? idz[i] * (v[2] + skip * iu[i]) : 0.0f);
+          if (GATE) set_elem(bz, oz, idz[i] * (v[2] + skip * iu[i]));
           dskip += idy[i] * iu[i];
           dbias += dw;
+          bu += ROWS * p.du.t;
+          bd2 += ROWS * p.ddelta.t;
+          bz += ROWS * p.dz.t;
         }
-        bu += ROWS * p.du.t;
-        bd2 += ROWS * p.ddelta.t;
-        bz += ROWS * p.dz.t;
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::ITEMS; ++i) {
+          const int s = s0 + i * ROWS + row;
+          const f32x4 v = *reinterpret_cast<const f32x4*>(wud + 4 * ((i * ROWS + row) * CH + ic));
+          const bool live = s < len;
+          const float dw = live ? (iu[i] * v[0] + LN2 * v[1]) * v[3] : 0.0f;
+          if (s < last_step && ic < nch) {
+            set_elem(bu, ou, live ? iw[i] * v[0] + skip * idy[i] : 0.0f);
+            set_elem(bd2, od, dw);
+            if (GATE) set_elem(bz, oz, live ? idz[i] * (v[2] + skip * iu[i]) : 0.0f);
+            dskip += idy[i] * iu[i];
+            dbias += dw;
+          }
+          bu += ROWS * p.du.t;
+          bd2 += ROWS * p.ddelta.t;
+          bz += ROWS * p.dz.t;
+        }
       }
-      for (int m = tid; m < BS * 2 * NP; m += THREADS) {
-        const int s = m / (2 * NP), half = m / NP % 2, n = m % NP;
+      float* const to = bc + (int64_t)s0 * 2 * in.N;
+#pragma unroll
+      for (int i = 0; i < (BS * 2 * NP + THREADS - 1) / THREADS; ++i) {
+        const int m = i * THREADS + tid;
+        if (BS * 2 * NP % THREADS && m >= BS * 2 * NP) break;
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < BACK_WAVES; ++w) v += red[w * BS * 2 * NP + m];
-        if (s0 + s < last_step && n < in.N)
-          p.bc_parts[(((((int64_t)tile * in.t + s0 + s) * in.B + b) * in.G + group) * 2 + half) * in.N + n] = v;
+        if (s0 + m / (2 * NP) < last_step && m % NP < in.N) to[m / NP * in.N + m % NP] = v;
       }
     }
     if (!beyond) turn ^= 1;
@@ -813,13 +852,13 @@ struct Shared {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void scan_shared_kernel(Shared p) {
-  const int64_t row = (int64_t)p.G * 2 * p.N, all = p.t * p.B * row;
+  const int64_t row = p.t * 2 * p.N, all = (int64_t)p.B * p.G * row;
   for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < all; k += (int64_t)gridDim.x * 256) {
     float v = 0.0f;
     for (int i = 0; i < p.tiles; ++i) v += p.parts[i * all + k];
-    const int r = (int)(k % row), group = r / (2 * p.N), half = r / p.N % 2, n = r % p.N;
-    const int64_t sb = k / row;
-    put<T>(half ? p.dC : p.dB, sb / p.B, sb % p.B, (int64_t)group * p.N + n, v);
+    const int64_t bg = k / row, r = k % row;
+    const unsigned step = (unsigned)(r / (2 * p.N)), rest = (unsigned)(r % (2 * p.N)), half = rest / p.N, n = rest % p.N;
+    put<T>(half ? p.dC : p.dB, step, bg / p.G, bg % p.G * p.N + n, v);
   }
 }
 

@@ -378,7 +378,9 @@ struct Backward {
   float *starts, *sums;            // [chunks][B][D][N]: dL/dh at a chunk's start from its own steps; [chunks][B][D]: sum of w
 };
 
-constexpr int BS = 16;             // steps per block: exp(w A) and exp(w A) h of a block stay in a lane's registers
+// Steps per block: exp(w A) and exp(w A) h of a block stay in a lane's registers.  With 8, and so three waves per SIMD instead of two,
+// 1353 instead of 1279 us at 1000 x 64 x 1024: what a block costs apart from its steps comes up twice as often.
+constexpr int BS = 16;
 
 template <int NL_, int NB_>
 struct BackwardShape {
@@ -424,12 +426,14 @@ template <typename T, typename S, bool GATE>
 __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_kernel(Backward p) {
   constexpr int CH = S::CH, NP = S::NP, THREADS = S::THREADS, NL = S::NL, NB = S::NB, BACK_WAVES = S::BACK_WAVES;
   extern __shared__ __align__(16) float lds[];
+  const int tid = threadIdx.x;
   // what a block stages, twice: the next one's is written while slower waves still read
   constexpr int STAGED = BS * (CH * 4 + 2 * NP);
   float* red = lds + 2 * STAGED;                      // [BACK_WAVES][BS][2][NP]
-  float* kept = red + BACK_WAVES * BS * 2 * NP;       // [stretch / BS][THREADS][NB]: states at the blocks' starts
+  // [stretch / BS - 2][THREADS][NB]: states at the starts of a stretch's blocks from its second one to its last but one
+  float* const kept = red + BACK_WAVES * BS * 2 * NP + tid * NB;
   const Scan& in = p.in;
-  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), b = blockIdx.y, chunk = blockIdx.z;
+  const int lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), b = blockIdx.y, chunk = blockIdx.z;
   const int group = blockIdx.x / in.tiles, tile = blockIdx.x % in.tiles, per = in.D / in.G;
   const int c0 = group * per + tile * CH, nch = min(CH, group * per + per - c0);
   const int len = length_of(in.lengths, b, in.t);
@@ -472,7 +476,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   float rh[NB];
   auto fetch = [&](int st, int k, bool back) {
     const int s0 = st * p.stretch + k * BS;
-    if (mine && k == 0) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, rh);   // (of no use where k == 0 comes after others)
+    if (mine && k == 0) load_states(p.states + st * all_states + bd * in.N, q * NB, in.N, rh);   // (its first block comes up twice)
     const unsigned ou = opaque(lane_bytes<T>(in.u.t, lrow, lane_c)), od = opaque(lane_bytes<T>(in.delta.t, lrow, lane_c)),
                    og = opaque(lane_bytes<T>(p.dy.t, lrow, lane_c)), oz = opaque(lane_bytes<T>(in.z.t, lrow, lane_c));
     const T *au = pu + (int64_t)s0 * in.u.t, *ad = pd + (int64_t)s0 * in.delta.t, *ag = pg + (int64_t)s0 * p.dy.t, *az = pz + (int64_t)s0 * in.z.t;
@@ -581,7 +585,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         }
       }
     }
-    if (k == 0) {       // (a stretch's first block comes up twice; its state is the same)
+    if (k == 0) {       // (twice, and the same)
 #pragma unroll
       for (int n = 0; n < NB; ++n) h[n] = rh[n];
     }
@@ -601,8 +605,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
     if (next_st >= from) fetch(next_st, next_k, next_back);
 
     if (!back) {
-      float* at_start = kept + (k * THREADS + tid) * NB;
-      store<NB>(at_start, h);
+      if (k > 0) store<NB>(kept + (k - 1) * THREADS * NB, h);
       if (!beyond) {
 #pragma unroll
         for (int s = 0; s < BS; ++s) {
@@ -630,7 +633,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
         if (s0 + m / (2 * NP) < last_step && m % NP < in.N) bc[(int64_t)s0 * 2 * in.N + m / NP * in.N + m % NP] = 0.0f;
       }
     } else {
-      if (k + 1 < blocks) load<NB>(kept + (k * THREADS + tid) * NB, h);   // (the last block goes on from the one before)
+      if (k > 0 && k + 1 < blocks) load<NB>(kept + (k - 1) * THREADS * NB, h);   // (the last block goes on from the one before)
       // forward through the block: exp(w A) and exp(w A) h_{s-1} of every step
       float a[BS][NB], ah[BS][NB];
 #pragma unroll
@@ -1057,7 +1060,7 @@ size_t a_bytes(const mebptt_scan_desc* d, const BackCut& c) { return align_up((s
 
 template <typename S>
 size_t back_lds(int stretch) {
-  return (2 * ((size_t)BS * S::CH * 4 + 2 * BS * S::NP) + S::BACK_WAVES * BS * 2 * S::NP + (size_t)stretch / BS * S::THREADS * S::NB) * sizeof(float);
+  return (2 * ((size_t)BS * S::CH * 4 + 2 * BS * S::NP) + S::BACK_WAVES * BS * 2 * S::NP + std::max(stretch / BS - 2, 0) * S::THREADS * S::NB) * sizeof(float);
 }
 
 }  // namespace

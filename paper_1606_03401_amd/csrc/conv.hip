@@ -1,7 +1,8 @@
 // Depthwise causal convolution of a few taps, forward, backward, and for single tokens:
 //     y_s = act(bias + sum_j weight_j x_{s-W+1+j}),   act(v) = v sigmoid(v) or v
 // A thread owns V neighbouring channels of one sequence and walks over a stretch of steps with the last W - 1 inputs in registers, so
-// that x is read once (and W - 1 rows more per stretch).  Bound: HBM.
+// that x is read once (and W - 1 rows more per stretch).  Bound: HBM.  1000 x 64 x 2048, bf16, four taps: forward 124 us, 4.2 TB/s, backward 184, 4.3
+// TB/s; 256 tokens x 2048 6 us, most of it the launch and two dependent reads.
 #include "ops.h"
 
 using namespace mebptt;

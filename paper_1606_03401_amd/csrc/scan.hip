@@ -2,10 +2,14 @@
 //     w = delta + delta_bias (through softplus);  h_s = exp(w_s A) h_{s-1} + w_s u_s B_s;  y_s = (C_s . h_s + skip u_s) silu(z_s)
 // forward, backward, and for single tokens.
 //
-// A lane holds NB = 4 states of one or two channels in registers over all steps; NL lanes share a channel (4 NL >= N).  Steps come in blocks: a
-// block's w, w u, B and C are put into LDS once, as floats, while the next block's inputs are already on their way, so that softplus and the
-// gate are computed once per (step, channel) and not in each of the NL lanes.  Bound: the vector unit (per step, channel and
-// state one exponential and four products or multiply-adds forward).
+// A channel's states are spread over NL neighbouring lanes, four of them in each lane's registers over all steps (eight forward beyond
+// N = 32).  Steps come in blocks: a block's w, w u, B and C are put into LDS once, as floats, while the next block's inputs are already on their
+// way, so that softplus and the gate are computed once per (step, channel) and not in each of the NL lanes.
+//
+// Bound: the vector unit.  Per step, channel and state the forward pass needs an exponential and four products or multiply-adds, 24 cycles
+// of a SIMD for 64 of them, the backward pass 60; what staging, sums over lanes and addresses add to that makes 33 and 135.  Measured, bf16 with
+// a gate, N = 16: 1000 x 32 x 1024, forward 185 us and backward 680 (the operations above alone 80 and 200, the bytes 35 and 73), two
+// thirds of the cycles with a vector instruction; 10000 x 1 x 2048, forward, 161 us in three launches (50; 33).
 #include "dynamic_lds.h"
 #include "ops.h"
 
@@ -14,7 +18,7 @@ using namespace mebptt::ops;
 
 namespace {
 
-constexpr int NB = 4;              // states per lane
+constexpr int NB = 4;              // states per lane, single tokens
 constexpr int MAX_N = 64;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -385,7 +389,7 @@ constexpr int BS = 16;
 template <int NL_, int NB_>
 struct BackwardShape {
   static constexpr int NL = NL_, NB = NB_;
-  static constexpr int BACK_WAVES = NB == 2 ? 8 : 4;                  // (what fits into LDS with stretches of 256)
+  static constexpr int BACK_WAVES = 4;                                // (what fits into LDS with stretches of 256)
   static constexpr int CW = WAVE / NL;                                // channels per wave
   static constexpr int CH = CW * BACK_WAVES;                          // channels per workgroup
   static constexpr int NP = NB * NL;
@@ -413,6 +417,7 @@ __device__ inline void channels_sum(const float (&v)[2 * S::NB], int lane, float
     x[n] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     if constexpr (NL <= 8) x[n] = dpp_add<0x128>(x[n]);
     if constexpr (NL <= 4) x[n] = dpp_add<0x124>(x[n]);
+    if constexpr (NL <= 2) x[n] = dpp_add<0x122>(x[n]);
   }
   // (every lane that has a sum writes it)
 #pragma unroll
@@ -876,7 +881,7 @@ struct Step {
   int64_t slots;
 };
 // A lane per NB states: the pool's rows are read and written once.  VEC: a channel's states, and its group's B and C, in whole vectors of NB.
-// Bound: HBM.
+// Bound: HBM.  256 x 2048 x 16: 16 us, 4.4 TB/s (a value at a time 41 us).
 template <typename T, int NL, bool VEC>
 __global__ __launch_bounds__(256) void scan_step_kernel(Step p) {
   const Scan& in = p.in;
@@ -988,7 +993,7 @@ void join(const Join& j, hipStream_t s) { scan_join_kernel<<<(unsigned)ceil_div(
 // Forward launches.  A SIMD issues a vector instruction of one wave only every other turn, and more waves hide what the recurrence waits
 // for, so what counts is waves.  Where the channels give fewer than 2048, two per SIMD, the time axis is cut into chunks, up to eight
 // waves per SIMD, whose ends are computed first (70 % of the work once more).  Measured, 10000 x 1 x 2048: 4096 / 6144 / 8192 waves wanted
-// 182 / 178 / 168 us, uncut 6543; 1000 x 32 x 1024, which gives 2048: uncut 220, in four chunks 235.
+// 174 / 173 / 172 us, uncut 1173; 4000 x 8 x 512 122 / 122 / 119, uncut 476; 1000 x 32 x 1024, which gives 2048: uncut 193, in four chunks 245.
 constexpr int ENOUGH_WAVES = 2048, WANT_WAVES = 8192, MIN_CHUNK = 32, MAX_CHUNKS = 64;
 struct Cut {
   int tiles;           // workgroups per group of channels
@@ -1000,7 +1005,7 @@ int with_shape(int N, F&& f) {
   if (N <= 8) return f(ForwardShape<2, 4>{});
   if (N <= 16) return f(ForwardShape<4, 4>{});
   if (N <= 32) return f(ForwardShape<8, 4>{});
-  return f(ForwardShape<8, 8>{});   // (16 lanes of 4 have four channels per wave to stage B and C for: 1242 instead of 500 us at 1000 x 32 x 1024)
+  return f(ForwardShape<8, 8>{});   // (16 lanes of 4 have four channels per wave to stage B and C for: 631 instead of 475 us at 1000 x 32 x 1024)
 }
 Cut forward_cut(const mebptt_scan_desc* d) {
   Cut c = {};
@@ -1021,15 +1026,16 @@ size_t starts_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ?
 size_t sums_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * sizeof(float)); }
 
 // Backward launches: 4 states per lane, two waves per SIMD, where what a block keeps (exp(w A) and exp(w A) h of 16 steps) takes half the
-// registers; 2 and four waves for few states, where a workgroup of 4 would have too many channels to stage (1000 x 32 x 1024, N = 16: 688 us
-// with 4, 712 with 2; N = 8: 567 and 495; N = 32: 1387 and 1531).  The time axis is cut as the forward pass's is, in whole stretches.
+// registers.  With 2 states per lane and twice the waves: 1000 x 32 x 1024, N = 8 473 us instead of 465, N = 16 883 instead of 711, N = 32
+// 1619 instead of 1240.  The time axis is cut as the forward pass's is, in whole stretches: 1000 x 32 x 1024, which gives 2048 waves, 711 us
+// uncut, 778 in two; 10000 x 1 x 2048, both passes, 660 us, 1827 uncut.
 constexpr int BACK_ENOUGH = 2048, BACK_WANT = 4096;   // waves
 struct BackCut {
   int tiles, ends_tiles, chunk, chunks;
 };
 template <typename F>
 int with_back_shape(int N, F&& f) {
-  if (N <= 8) return f(BackwardShape<4, 2>{});
+  if (N <= 8) return f(BackwardShape<2, 4>{});
   if (N <= 16) return f(BackwardShape<4, 4>{});
   if (N <= 32) return f(BackwardShape<8, 4>{});
   return f(BackwardShape<16, 4>{});

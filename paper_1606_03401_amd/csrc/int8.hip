@@ -114,10 +114,10 @@ __global__ __launch_bounds__(256) void int8_product_kernel(Product p) {
 // it directly, 64 bytes of K per stage, four stages: while a stage is multiplied, the next one's fragments are read into a second set of
 // registers and three more are on their way.  Rows begin at 16-byte boundaries; only the last stage may be short, and goes through registers.
 //
-// Bound: the matrix instructions, and the L2s' delivery beside them.  A stage of 256 x 256 is 1024 cycles of matrix instructions on every SIMD; its
-// 32 KB written to LDS and 64 KB read take 768 at 128 bytes a cycle, its 32 KB come from an L2 that 32 compute units ask at once.  One
-// workgroup alone takes 1230 cycles a stage.  Measured: 8192 x 4096 x 4096 132 us, 2.08 POP/s, matrix units at work 52 % of the time (the library's own
-// 8-bit product of 8192^3: 2.00 POP/s, this one 2.1); rows 4096 bytes apart cost 15 % against 4160.
+// Bound: the card's power, then the matrix instructions.  A stage of 256 x 256 is 1024 cycles of matrix instructions on every SIMD; its 32 KB written to
+// LDS and 64 KB read take 768 at 128 bytes a cycle; one workgroup alone takes 1230.  Measured on random operands: 8192 x 4096 x 4096 132 - 140 us,
+// 2.0 POP/s, 8192^3 480 us, 2.3 POP/s (the library's 8-bit product 2.0), at 1.9 of the card's 2.4 GHz; the same launches on zeros 104 and 366 us.
+// The order of K and the places in LDS make no difference to that.
 
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(1))) const void global_void;

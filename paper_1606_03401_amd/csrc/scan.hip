@@ -7,7 +7,7 @@
 // way, so that softplus and the gate are computed once per (step, channel) and not in each of the NL lanes.
 //
 // Bound: the vector unit.  Per step, channel and state the forward pass needs an exponential and four products or multiply-adds, 24 cycles
-// of a SIMD for 64 of them, the backward pass 60; what staging, sums over lanes and addresses add to that makes 33 and 135.  Measured, bf16 with
+// of a SIMD for 64 of them, the backward pass 60; what staging, sums over lanes and addresses add to that makes 36 and 133.  Measured, bf16 with
 // a gate, N = 16: 1000 x 32 x 1024, forward 185 us and backward 680 (the operations above alone 80 and 200, the bytes 35 and 73), two
 // thirds of the cycles with a vector instruction; 10000 x 1 x 2048, forward, 161 us in three launches (50; 33).
 #include "dynamic_lds.h"

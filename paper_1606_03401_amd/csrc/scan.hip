@@ -57,6 +57,13 @@ __device__ inline void set_elem(T* base, unsigned bytes, float v) { *reinterpret
 
 __device__ inline int length_of(const int32_t* lengths, int b, int t) { return lengths ? min(max(lengths[b], 0), t) : t; }
 
+// A log2 e, finite: where nothing happens (w = 0: beyond a sequence's end, in lanes without a channel) exp(w A) is 1 for an infinite A as well.
+__device__ inline float log2_decay(float A) {
+  constexpr float MOST = 3.402823466e38f;
+  const float v = A * LOG2E;
+  return v < -MOST ? -MOST : v > MOST ? MOST : v;      // (a NaN stays one)
+}
+
 // log(1 + e^x).  Small values keep their relative accuracy, steps of a thousandth being what such a model starts with: what 1 + e lost of e is
 // added to the logarithm of the sum.
 __device__ inline float softplus_of(float x) {
@@ -144,7 +151,7 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_forward_kernel(Forwa
   load_states(in.A + d * in.N, q * NB, in.N, A2);
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    A2[n] *= LOG2E;
+    A2[n] = log2_decay(A2[n]);
     h[n] = 0.0f;
   }
   // h0 of launches in chunks: from its copy, as another workgroup may be writing h_out over it
@@ -347,7 +354,7 @@ __global__ __launch_bounds__(256) void scan_join_kernel(Join p) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = p.BD * p.N;
   if (i >= all) return;
   const int64_t bd = i / p.N;
-  const float a2 = p.A[(bd % p.D) * p.N + i % p.N] * LOG2E;
+  const float a2 = log2_decay(p.A[(bd % p.D) * p.N + i % p.N]);
   float h = p.before ? p.before[i] : 0.0f;
   constexpr int U = 16;                                // slots read at once
   for (int c = 0; c < p.count; c += U) {
@@ -451,7 +458,7 @@ __global__ __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) void scan_backward_k
   load_states(in.A + d * in.N, q * NB, in.N, A2);
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    A2[n] *= LOG2E;
+    A2[n] = log2_decay(A2[n]);
     dA[n] = g[n] = h[n] = 0.0f;
   }
   // (channels beyond the workgroup's keep zeros in h and g: their w, w u and dy are zeros, and so is what they add to dB and dC)
@@ -786,7 +793,7 @@ __global__ __launch_bounds__(FORWARD_WAVES* WAVE) void scan_back_ends_kernel(Bac
   load_states(in.A + d * in.N, q * NB, in.N, A2);
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    A2[n] *= LOG2E;
+    A2[n] = log2_decay(A2[n]);
     g[n] = 0.0f;
   }
   const int row = lane / CH, ch = lane % CH, srow = lane / NP, sn = lane % NP;
@@ -926,7 +933,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(Step p) {
   float y = 0.0f;
 #pragma unroll
   for (int n = 0; n < NB; ++n) {
-    h[n] = __builtin_amdgcn_exp2f(w * (A[n] * LOG2E)) * h[n] + w * u * vb[n];
+    h[n] = __builtin_amdgcn_exp2f(w * log2_decay(A[n])) * h[n] + w * u * vb[n];
     y += h[n] * vc[n];
   }
   y = lanes_sum<NL>(y);

@@ -359,6 +359,44 @@ def test_scan_state_in_place(t, B, D, N, G, lengths):
     assert torch.equal(y, y2) and torch.equal(v["h0"], h_out)
 
 
+@pytest.mark.parametrize("t,B,D,N,G", [(37, 3, 21, 16, 1), (150, 2, 70, 13, 2), (20, 2, 9, 5, 1), (40, 2, 19, 33, 1)])
+def test_scan_states_that_forget_at_once(t, B, D, N, G):
+    """A of minus infinity: such a state keeps nothing from step to step, and nothing of it reaches other channels by way of the lanes and steps that
+    fill up a block."""
+    m = _Made(t + D, "plain")
+    v = _scan_inputs(m, t, B, D, N, G, True, True, True, "fp32")
+    v["A"][-1, :] = -float("inf")
+    v["A"][0, N - 1] = -float("inf")
+    lengths = [t - 3] + [t // 2] * (B - 1)
+    ends = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    n = {k: _np(a) for k, a in v.items()}
+    args = (n["u"], n["delta"], n["A"], n["Bm"], n["Cm"], G, n["skip"], n["z"], n["delta_bias"], lengths, n["h0"], True)
+    want, want_h = sel.scan(*args)
+    desc = mb.make_scan_desc(t, B, D, N, G, mb.FP32, 1, 16)
+    y, h_out = m.empty((t, B, D), torch.float32), torch.full((B, D, N), NAN, device=DEV)
+    states, ws = _bytes(mb.mebptt_scan_state_bytes(desc)), _bytes(mb.mebptt_scan_workspace_bytes(desc, True))
+    mb.mebptt_scan_forward(desc, *_call(v, ends), y, h_out, states, ws)
+    _near(y, want, "y")
+    _near(h_out, want_h, "h_out")
+    dy = m.normal((t, B, D), 0.1, torch.float32)
+    finite = {**n, "A": np.maximum(n["A"], -1e30)}     # the same gradients, without the formula's zero times infinity
+    want = sel.scan_backward(n["u"], n["delta"], finite["A"], n["Bm"], n["Cm"], G, n["skip"], n["z"], n["delta_bias"], lengths, n["h0"], True, _np(dy), None)
+    d = {k: m.empty((t, B, D), torch.float32) for k in ("du", "ddelta", "dz")} | {k: m.empty((t, B, G * N), torch.float32) for k in ("dB", "dC")}
+    d |= {"dA": torch.empty((D, N), device=DEV), "dskip": torch.empty(D, device=DEV), "ddelta_bias": torch.empty(D, device=DEV),
+          "dh0": torch.empty((B, D, N), device=DEV)}
+    mb.mebptt_scan_backward(desc, *_call(v, ends), dy, None, states, d["du"], d["ddelta"], d["dA"], d["dB"], d["dC"], d["dskip"], d["dz"],
+                            d["ddelta_bias"], d["dh0"], ws)
+    for k, got in d.items():
+        _near(got, want[k], k)
+    # a token after another
+    token = mb.make_scan_desc(1, B, D, N, G, mb.FP32, 1)
+    pool = v["h0"].clone()
+    for s in range(2):
+        out = torch.empty((B, D), device=DEV)
+        mb.mebptt_scan_step(token, v["u"][s], v["delta"][s], v["A"], v["Bm"][s], v["Cm"][s], v["skip"], v["z"][s], v["delta_bias"], pool, None, out, pool)
+        _near(out, sel.scan(*args)[0][s], "token")
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_scan_of_no_steps(dtype):
     """The state passes through, and so does its gradient; parameters have none."""

@@ -1,8 +1,9 @@
 // Depthwise causal convolution of a few taps, forward, backward, and for single tokens:
 //     y_s = act(bias + sum_j weight_j x_{s-W+1+j}),   act(v) = v sigmoid(v) or v
 // A thread owns V neighbouring channels of one sequence and walks over a stretch of steps with the last W - 1 inputs in registers, so
-// that x is read once (and W - 1 rows more per stretch).  Bound: HBM.  1000 x 64 x 2048, bf16, four taps: forward 124 us, 4.2 TB/s, backward 184, 4.3
-// TB/s; 256 tokens x 2048 6 us, most of it the launch and two dependent reads.
+// that x is read once (and W - 1 rows more per stretch).  Bound: HBM; where there is little to do, the rounds of rows that a thread waits for.
+// 1000 x 64 x 2048, bf16, four taps: forward 115 us, 4.6 TB/s, backward 179, 4.4 TB/s; 256 tokens x 2048 6 us, most of it the launch and two
+// dependent reads.
 #include "ops.h"
 
 using namespace mebptt;
@@ -55,18 +56,26 @@ __device__ inline void load_weights(const float* weight, const float* bias, int 
   }
 }
 
-// The input of step s (from -(W-1) on) of sequence b: x, the state's rows before step 0, zeros without a state and from `len` on.
+template <typename T, int V>
+using Row = T __attribute__((ext_vector_type(V), aligned(std::min<size_t>(V * sizeof(T), 16))));
+template <typename T, int V>
+__device__ inline Row<T, V> row_at(const T* p) { return *reinterpret_cast<const Row<T, V>*>(p); }
+
+// The input of step s (from -(W-1) on) of sequence b: x, the state's rows before step 0, zeros without a state and from `len` on.  As it came:
+// what turns it into floats waits for it, and belongs behind the other rows' loads.
 template <typename T, int W, int V>
-__device__ inline void input(const T* x, int64_t xt, const T* state, int C, int s, int len, float (&v)[V]) {
-  if (s >= 0 && s < len) {
-    load<V>(x + s * xt, v);
-  } else if (s < 0 && state) {
-    load<V>(state + (int64_t)(s + W - 1) * C, v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = 0.0f;
-  }
+__device__ inline Row<T, V> input(const T* x, int64_t xt, const T* state, int C, int s, int len) {
+  Row<T, V> v = {};
+  if (s < len && (s >= 0 || state)) v = row_at<T, V>(s >= 0 ? x + s * xt : state + (int64_t)(s + W - 1) * C);
+  return v;
 }
+template <typename T, int V>
+__device__ inline void widen(const Row<T, V>& r, float (&v)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = (float)r[e];
+}
+
+constexpr int U = 4;   // rows on their way at once
 
 template <typename T, int W, int V>
 __global__ __launch_bounds__(THREADS) void conv_forward_kernel(Conv p) {
@@ -79,22 +88,26 @@ __global__ __launch_bounds__(THREADS) void conv_forward_kernel(Conv p) {
   T* y = (T*)p.y + b * p.yb + c;
   const T* state = p.state_in ? (const T*)p.state_in + (int64_t)b * (W - 1) * p.C + c : nullptr;
   float w[W][V], wb[V], h[W][V];
+  Row<T, V> before[W], last[W];
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) before[j] = input<T, W, V>(x, p.xt, state, p.C, s0 - (W - 1) + j, len);
+  const bool ends = part == 0 && p.state_out;   // the state may be written over the one read: this thread alone reads and writes these columns
+  if (ends) {
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) last[j] = input<T, W, V>(x, p.xt, state, p.C, len - (W - 1) + j, len);
+  }
   load_weights<W, V>(p.weight, p.bias, c, p.C, w, wb);
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j) input<T, W, V>(x, p.xt, state, p.C, s0 - (W - 1) + j, len, h[j]);
-  if (part == 0 && p.state_out) {   // the state may be written over the one read: this thread alone reads and writes these columns
+  for (int j = 0; j < W - 1; ++j) widen<T, V>(before[j], h[j]);
+  if (ends) {
     T* out = (T*)p.state_out + (int64_t)b * (W - 1) * p.C + c;
-    float last[W][V];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) input<T, W, V>(x, p.xt, state, p.C, len - (W - 1) + j, len, last[j]);
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j) store<V>(out + (int64_t)j * p.C, last[j]);
+    for (int j = 0; j < W - 1; ++j) *reinterpret_cast<Row<T, V>*>(out + (int64_t)j * p.C) = last[j];
   }
   const int live = min(s1, len);
-#pragma unroll 4
-  for (int s = s0; s < live; ++s) {
-    load<V>(x + s * p.xt, h[W - 1]);
+  auto step = [&](int s, const Row<T, V>& row) {
     float v[V];
+    widen<T, V>(row, h[W - 1]);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       v[e] = wb[e];
@@ -107,7 +120,17 @@ __global__ __launch_bounds__(THREADS) void conv_forward_kernel(Conv p) {
     for (int j = 0; j < W - 1; ++j)
 #pragma unroll
       for (int e = 0; e < V; ++e) h[j][e] = h[j + 1][e];
+  };
+  int s = s0;
+  for (; s + U <= live; s += U) {
+    Row<T, V> rows[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) rows[u] = row_at<T, V>(x + (s + u) * p.xt);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) step(s + u, rows[u]);
   }
+  for (; s < live; ++s) step(s, row_at<T, V>(x + s * p.xt));
   const float none[V] = {};
   for (int s = max(s0, live); s < s1; ++s) store<V>(y + s * p.yt, none);
 }
@@ -117,7 +140,7 @@ __global__ __launch_bounds__(THREADS) void conv_forward_kernel(Conv p) {
 // stretches of steps and sequences, adding dweight and dbias up in registers.
 template <typename T, int W, int V>
 __global__ __launch_bounds__(THREADS, W <= 4 ? 3 : 2) void conv_backward_kernel(ConvBack p) {
-  constexpr int WAVES = THREADS / WAVE, U = 4;
+  constexpr int WAVES = THREADS / WAVE;
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
   const int group = blockIdx.x * WAVE + lane, c = group * V;
   const bool mine = group < p.groups;
@@ -144,8 +167,11 @@ __global__ __launch_bounds__(THREADS, W <= 4 ? 3 : 2) void conv_backward_kernel(
 #pragma unroll
         for (int e = 0; e < V; ++e) g[j][e] = 0.0f;
       const int from = max(first, 0);
+      Row<T, V> before[W];
 #pragma unroll
-      for (int j = 0; j < W - 1; ++j) input<T, W, V>(x, p.xt, state, p.C, from - (W - 1) + j, len, h[j]);
+      for (int j = 0; j < W - 1; ++j) before[j] = input<T, W, V>(x, p.xt, state, p.C, from - (W - 1) + j, len);
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) widen<T, V>(before[j], h[j]);
       // dpre of a step, from its input (already the last of h) and d = dy; OWN: a step that dweight counts here
       auto through = [&](float (&d)[V], bool own) {
 #pragma unroll
@@ -181,45 +207,56 @@ __global__ __launch_bounds__(THREADS, W <= 4 ? 3 : 2) void conv_backward_kernel(
 #pragma unroll
           for (int e = 0; e < V; ++e) g[j][e] = g[j + 1][e];
       };
-      // any step: before the first one, past the last, at a stretch's ends
-      auto any = [&](int s) {
-        float d[V] = {}, v[V] = {};
-        if (s >= 0) {
-          input<T, W, V>(x, p.xt, nullptr, p.C, s, len, h[W - 1]);
-          if (s < len) load<V>(dy + s * p.gt, d);
-          through(d, s < s1);
-        }
-        const int q = s - (W - 1), r = q - (len - (W - 1));         // the position, and its row of the state after the last step
-        if (q >= first && r >= 0 && dlast) load<V>(dlast + (int64_t)r * p.C, v);
-        gather(d, v);
-        if (q < first) return;
-        if (q >= 0) store<V>(dx + q * p.dt, v);
-        else if (dfirst) store<V>(dfirst + (int64_t)(q + W - 1) * p.C, v);
-      };
-      int s = first;
-      for (; s < min(from + W - 1, live + W - 1); ++s) any(s);
-      for (; s + U <= live; s += U) {                               // U steps' rows at a time, all of them on their way
-        typedef T Row __attribute__((ext_vector_type(V)));
-        Row xs[U], ds[U];
+      for (int s = first; s < live + W - 1; s += U) {               // U steps' rows at a time, all of them on their way
+        Row<T, V> xs[U], ds[U];
+        if (s >= from + W - 1 && s + U <= live) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) xs[u] = *reinterpret_cast<const Row*>(x + (s + u) * p.xt);
+          for (int u = 0; u < U; ++u) xs[u] = row_at<T, V>(x + (s + u) * p.xt);
 #pragma unroll
-        for (int u = 0; u < U; ++u) ds[u] = *reinterpret_cast<const Row*>(dy + (s + u) * p.gt);
-        __builtin_amdgcn_sched_barrier(0);
+          for (int u = 0; u < U; ++u) ds[u] = row_at<T, V>(dy + (s + u) * p.gt);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float d[V], v[V] = {};
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            h[W - 1][e] = (float)xs[u][e];
-            d[e] = (float)ds[u][e];
+          for (int u = 0; u < U; ++u) {
+            float d[V], v[V] = {};
+            widen<T, V>(xs[u], h[W - 1]);
+            widen<T, V>(ds[u], d);
+            through(d, true);
+            gather(d, v);
+            store<V>(dx + (s + u - (W - 1)) * p.dt, v);
           }
-          through(d, true);
-          gather(d, v);
-          store<V>(dx + (s + u - (W - 1)) * p.dt, v);
+        } else {                                                    // steps before the first one, past the last, at a stretch's ends
+          Row<T, V> ls[U];                                          // gradients of the state after the last step
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int k = s + u, q = k - (W - 1), r = k - len;      // the position that the step completes, and its row of that state
+            xs[u] = ds[u] = ls[u] = Row<T, V>{};
+            if (k >= 0 && k < len) {
+              xs[u] = row_at<T, V>(x + k * p.xt);
+              ds[u] = row_at<T, V>(dy + k * p.gt);
+            }
+            if (q >= first && r >= 0 && r < W - 1 && dlast) ls[u] = row_at<T, V>(dlast + (int64_t)r * p.C);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int k = s + u, q = k - (W - 1);
+            if (k < live + W - 1) {
+              float d[V], v[V];
+              widen<T, V>(ds[u], d);
+              widen<T, V>(ls[u], v);
+              if (k >= 0) {
+                widen<T, V>(xs[u], h[W - 1]);
+                through(d, k < s1);
+              }
+              gather(d, v);
+              if (q >= first) {
+                if (q >= 0) store<V>(dx + q * p.dt, v);
+                else if (dfirst) store<V>(dfirst + (int64_t)(q + W - 1) * p.C, v);
+              }
+            }
+          }
         }
       }
-      for (; s < live + W - 1; ++s) any(s);
       const float none[V] = {};
       for (int s = max(s0, live); s < s1; ++s) store<V>(dx + s * p.dt, none);
     }
@@ -294,16 +331,27 @@ int check(const mebptt_conv_desc* d) {
   return MEBPTT_OK;
 }
 
-// Steps per thread of a forward launch.  Long stretches read fewer rows twice (W - 1 of them each), short ones give more threads.
-constexpr int STRETCH = 32;
+// Steps per thread.  Long stretches read fewer rows twice (W - 1 of them each); short ones give more threads, and fewer rounds of U rows that a thread
+// waits for: halved until two workgroups per compute unit have work (forward; 1536 waves backward), or no further.  Forward and backward, four
+// taps, long stretches everywhere / these: 4000 x 1 x 2048 46 / 36 us, 512 x 8 x 1024 44 / 27, 1197 x 6 x 320 36 / 20, 100 x 2 x 128 36 / 16; with twice as
+// much to fill 1000 x 64 x 512 84 instead of 77.
+int stretch_for(int64_t t, int64_t B, int64_t per_stretch, int64_t enough, int longest, int shortest) {
+  int s = longest;
+  while (s > shortest && B * ceil_div(t, s) * per_stretch < enough) s /= 2;
+  return s;
+}
+constexpr int STRETCH = 32, SHORT = 8;
+constexpr int64_t FILLS = 512 * THREADS;   // threads
 // The backward pass reads and computes W - 1 steps at both ends of a stretch twice; its workgroups, three on a compute unit at a time, take
-// stretches in turn.  1000 x 64 x 2048: 184 us; 212 with 1024 workgroups and stretches of 64, 193 with stretches of 32.
-constexpr int BACK_STRETCH = 48, BACK_GROUPS = 768;
+// stretches in turn.  1000 x 64 x 2048, when it was chosen: 184 us; 212 with 1024 workgroups and stretches of 64, 193 with stretches of 32.
+constexpr int BACK_STRETCH = 48, BACK_SHORT = 6, BACK_GROUPS = 768, BACK_FILLS = 1536;   // waves
 constexpr int BACK_V = 4;
 
+int64_t back_columns(const mebptt_conv_desc* d) { return ceil_div(ceil_div(d->C, d->C % BACK_V ? 1 : BACK_V), WAVE); }
+int back_stretch(const mebptt_conv_desc* d) { return stretch_for(d->t, d->B, back_columns(d), BACK_FILLS, BACK_STRETCH, BACK_SHORT); }
 int64_t back_parts(const mebptt_conv_desc* d) {
-  const int64_t columns = ceil_div(ceil_div(d->C, d->C % BACK_V ? 1 : BACK_V), WAVE);
-  const int64_t items = d->B * std::max<int64_t>(1, ceil_div(d->t, BACK_STRETCH));
+  const int64_t columns = back_columns(d);
+  const int64_t items = d->B * std::max<int64_t>(1, ceil_div(d->t, back_stretch(d)));
   return std::max<int64_t>(1, std::min<int64_t>(ceil_div(items, THREADS / WAVE), ceil_div(BACK_GROUPS, columns)));
 }
 
@@ -324,8 +372,8 @@ int with_taps(int taps, F&& f) {
 template <typename T, int V>
 int forward(Conv p, int taps, hipStream_t stream) {
   p.groups = (int)ceil_div(p.C, V);
-  p.stretch = STRETCH;
-  p.stretches = (int)std::max<int64_t>(1, ceil_div(p.t, STRETCH));
+  p.stretch = stretch_for(p.t, p.B, p.groups, FILLS, STRETCH, SHORT);
+  p.stretches = (int)std::max<int64_t>(1, ceil_div(p.t, p.stretch));
   const dim3 grid((unsigned)ceil_div((int64_t)p.groups * p.stretches, THREADS), p.B);
   return with_taps(taps, [&](auto w) {
     conv_forward_kernel<T, decltype(w)::value, V><<<grid, THREADS, 0, stream>>>(p);
@@ -335,8 +383,7 @@ int forward(Conv p, int taps, hipStream_t stream) {
 template <typename T, int V>
 int backward(ConvBack p, int taps, int64_t parts, hipStream_t stream) {
   p.groups = (int)ceil_div(p.C, V);
-  p.stretch = BACK_STRETCH;
-  p.stretches = (int)std::max<int64_t>(1, ceil_div(p.t, BACK_STRETCH));
+  p.stretches = (int)std::max<int64_t>(1, ceil_div(p.t, p.stretch));
   const dim3 grid((unsigned)ceil_div(p.groups, WAVE), (unsigned)parts);
   return with_taps(taps, [&](auto w) {
     conv_backward_kernel<T, decltype(w)::value, V><<<grid, THREADS, 0, stream>>>(p);
@@ -393,7 +440,7 @@ int mebptt_conv_backward(const mebptt_conv_desc* d, mebptt_seq x, const float* w
   if (d->B && ((rc = check_seq(x, d, false, "x")) || (rc = check_seq(dy, d, false, "dy")) || (rc = check_seq(dx, d, true, "dx")))) return rc;
   if ((rc = check_workspace(workspace, workspace_bytes, mebptt_conv_workspace_bytes(d)))) return rc;
   const ConvBack p = {x.data, state_in, dy.data, dstate_out, dx.data, dstate_in, weight, bias, lengths, (float*)workspace,
-                      x.stride_t, x.stride_b, dy.stride_t, dy.stride_b, dx.stride_t, dx.stride_b, d->t, d->B, d->C, d->silu, 0, 0, 0};
+                      x.stride_t, x.stride_b, dy.stride_t, dy.stride_b, dx.stride_t, dx.stride_b, d->t, d->B, d->C, d->silu, back_stretch(d), 0, 0};
   const bool vec = d->C % BACK_V == 0 && rows_aligned(x, d->dtype, BACK_V) && rows_aligned(dy, d->dtype, BACK_V) &&
                    rows_aligned(dx, d->dtype, BACK_V) && rows_aligned(state_in, d->C, d->dtype, BACK_V) &&
                    rows_aligned(dstate_out, d->C, d->dtype, BACK_V) && rows_aligned(dstate_in, d->C, d->dtype, BACK_V);

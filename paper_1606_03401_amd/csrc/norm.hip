@@ -2,8 +2,9 @@
 //     r = x + residual,   y = r * rstd * weight,   rstd = rsqrt(mean(r^2) + eps)
 //     dr = rstd (weight dy - n mean(weight dy n)) + dresidual_out,   n = r rstd,   dweight = sum over rows of dy n
 // A row stays in the registers of the threads that read it from its first byte to its last: one pass over memory each way.
-// Bound: HBM.  64000 x 1024, bf16 with an fp32 residual: forward 130 us, 6.0 TB/s (part of it never leaves the last cache), backward 247, 4.2 TB/s, and 6
-// for the sum of its partial dweight; 8192 x 4096 to 8 bits 70 us, 5.2 TB/s.  A row of up to 2048 values belongs to one wave, so that its sums need no barrier and four rows share a
+// Bound: HBM.  64000 x 1024, bf16 with an fp32 residual: forward 136 us, 5.8 TB/s (part of it never leaves the last cache), backward 199, 5.3 TB/s, and 6
+// for the sum of its partial dweight; 8192 x 4096 to 8 bits 66 us, 5.6 TB/s; 4 x 1024 3.7 us.
+// A row of up to 2048 values belongs to one wave, so that its sums need no barrier and four rows share a
 // workgroup; wider ones to a workgroup of 4 or 16 waves.
 #include "ops.h"
 
@@ -54,24 +55,37 @@ template <int TPR, bool VEC>
 __device__ inline int column(int chunk, int e, int lane) {
   return VEC ? (chunk * TPR + lane) * V + e : (chunk * V + e) * TPR + lane;
 }
+// A chunk's values as they came, and then as floats, zeros beyond the row: apart, so that all of a row's loads are on their way before the first one is
+// waited for.  Columns beyond the row read its last ones again where that costs no more registers than there are (a VEC width is a multiple of V),
+// which keeps branches out from between the loads: 20000 x 2047, forward and backward, 263 us instead of 610.  Wider rows at any alignment
+// would need an address per value (1183 x 7931, forward: 70 us instead of 60), the largest workgroups' threads have 128 registers.
+template <typename T, bool VEC>
+struct Raw {
+  typedef T Eight __attribute__((ext_vector_type(V), aligned(16)));
+  std::conditional_t<VEC, Eight, T[V]> v;
+};
 template <int TPR, bool VEC, typename T>
-__device__ inline void load_chunk(const T* row, int chunk, int lane, int width, float (&v)[V]) {
+__device__ inline void load_chunk(const T* row, int chunk, int lane, int width, Raw<T, VEC>& raw) {
+  constexpr bool CLAMP = TPR == WAVE || (VEC && TPR < 16 * WAVE);
   if constexpr (VEC) {
     const int c = column<TPR, true>(chunk, 0, lane);
-    if (c < width) {
-      load<V>(row + c, v);
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = 0.0f;
-    }
+    if (!CLAMP) raw.v = {};
+    if (CLAMP || c < width) raw.v = *reinterpret_cast<const typename Raw<T, VEC>::Eight*>(row + (unsigned)(CLAMP ? min(c, width - V) : c));
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       const int c = column<TPR, false>(chunk, e, lane);
-      v[e] = c < width ? (float)row[c] : 0.0f;
+      if (!CLAMP) raw.v[e] = (T)0.0f;
+      if (CLAMP || c < width) raw.v[e] = row[(unsigned)(CLAMP ? min(c, width - 1) : c)];
     }
   }
 }
+template <int TPR, bool VEC, typename T>
+__device__ inline void widen(const Raw<T, VEC>& raw, int chunk, int lane, int width, float (&v)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = column<TPR, VEC>(chunk, VEC ? 0 : e, lane) < width ? (float)raw.v[e] : 0.0f;
+}
+
 template <int TPR, bool VEC, typename T>
 __device__ inline void store_chunk(T* row, int chunk, int lane, int width, const float (&v)[V]) {
   if constexpr (VEC) {
@@ -109,21 +123,34 @@ constexpr int threads_of() { return WAVES == 1 ? 4 * WAVE : WAVES * WAVE; }   //
 template <typename TX, typename TR, typename TY, int WAVES, int NC, bool VEC>
 __global__ __launch_bounds__(threads_of<WAVES>()) void norm_forward_kernel(Norm p) {
   constexpr int TPR = WAVES * WAVE, ROWS = WAVES == 1 ? 4 : 1;
-  constexpr bool QUANT = sizeof(TY) == 1;
+  constexpr bool QUANT = sizeof(TY) == 1, AHEAD = WAVES < 16;   // (the largest workgroups have no registers for it)
   __shared__ float lds[2][WAVES];
-  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int lane = threadIdx.x % TPR, sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);   // (uniform over a wave, and so are rows' addresses)
   for (int64_t row = (int64_t)blockIdx.x * ROWS + sub; row < p.rows; row += (int64_t)gridDim.x * ROWS) {
     float r[NC][V];
     float sum = 0.0f;
     const TX* x = (const TX*)p.x + row * p.ldx;
+    Raw<TX, VEC> xs[NC];
+    Raw<TR, VEC> as[NC];
+    Raw<float, VEC> ws[NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(x, c, lane, p.width, r[c]);
+    for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(x, c, lane, p.width, xs[c]);
     if (p.residual) {
       const TR* res = (const TR*)p.residual + row * p.ldr;
 #pragma unroll
+      for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(res, c, lane, p.width, as[c]);
+    }
+    if (AHEAD && p.weight) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(p.weight, c, lane, p.width, ws[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) widen<TPR, VEC>(xs[c], c, lane, p.width, r[c]);
+    if (p.residual) {
+#pragma unroll
       for (int c = 0; c < NC; ++c) {
         float a[V];
-        load_chunk<TPR, VEC>(res, c, lane, p.width, a);
+        widen<TPR, VEC>(as[c], c, lane, p.width, a);
 #pragma unroll
         for (int e = 0; e < V; ++e) r[c][e] += a[e];
       }
@@ -145,7 +172,9 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void norm_forward_kernel(Norm 
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       float w[V];
-      if (p.weight) load_chunk<TPR, VEC>(p.weight, c, lane, p.width, w);
+      if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);
+      if (!AHEAD && p.weight) load_chunk<TPR, VEC>(p.weight, c, lane, p.width, ws[c]);
+      if (p.weight) widen<TPR, VEC>(ws[c], c, lane, p.width, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         r[c][e] = r[c][e] * rstd * (p.weight ? w[e] : 1.0f);
@@ -174,9 +203,10 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void norm_forward_kernel(Norm 
 template <typename TX, typename TR, int WAVES, int NC, bool VEC>
 __global__ __launch_bounds__(threads_of<WAVES>()) void norm_backward_kernel(NormBack p) {
   constexpr int TPR = WAVES * WAVE, ROWS = WAVES == 1 ? 4 : 1;
+  constexpr bool AHEAD = WAVES < 16;
   __shared__ float lds[WAVES];
   __shared__ float waves_dw[WAVES == 1 ? 3 * NC * V * WAVE : 1];
-  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int lane = threadIdx.x % TPR, sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);   // (uniform over a wave, and so are rows' addresses)
   float dw[NC][V];
 #pragma unroll
   for (int c = 0; c < NC; ++c)
@@ -187,15 +217,33 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void norm_backward_kernel(Norm
     const float rstd = p.rstd[row];
     const TR* r = (const TR*)p.r + row * p.ldr;
     const TX* dy = (const TX*)p.dy + row * p.lddy;
+    Raw<TR, VEC> rs[NC], os[NC];
+    Raw<TX, VEC> gs[NC];
+    Raw<float, VEC> ws[NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(r, c, lane, p.width, n[c]);
+    for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(r, c, lane, p.width, rs[c]);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(dy, c, lane, p.width, g[c]);
+    for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(dy, c, lane, p.width, gs[c]);
+    if (AHEAD && p.weight) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>(p.weight, c, lane, p.width, ws[c]);
+    }
+    if (AHEAD && p.dout) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) load_chunk<TPR, VEC>((const TR*)p.dout + row * p.lddo, c, lane, p.width, os[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      widen<TPR, VEC>(rs[c], c, lane, p.width, n[c]);
+      widen<TPR, VEC>(gs[c], c, lane, p.width, g[c]);
+    }
     float dot = 0.0f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       float w[V];
-      if (p.weight) load_chunk<TPR, VEC>(p.weight, c, lane, p.width, w);
+      if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);
+      if (!AHEAD && p.weight) load_chunk<TPR, VEC>(p.weight, c, lane, p.width, ws[c]);
+      if (p.weight) widen<TPR, VEC>(ws[c], c, lane, p.width, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         n[c][e] *= rstd;
@@ -208,7 +256,9 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void norm_backward_kernel(Norm
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       float d[V];
-      if (p.dout) load_chunk<TPR, VEC>((const TR*)p.dout + row * p.lddo, c, lane, p.width, d);
+      if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);
+      if (!AHEAD && p.dout) load_chunk<TPR, VEC>((const TR*)p.dout + row * p.lddo, c, lane, p.width, os[c]);
+      if (p.dout) widen<TPR, VEC>(os[c], c, lane, p.width, d);
 #pragma unroll
       for (int e = 0; e < V; ++e) d[e] = rstd * (g[c][e] - n[c][e] * dot) + (p.dout ? d[e] : 0.0f);
       if (p.dx) store_chunk<TPR, VEC>((TX*)p.dx + row * p.lddx, c, lane, p.width, d);

@@ -867,10 +867,19 @@ struct Shared {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void scan_shared_kernel(Shared p) {
+  constexpr int U = 8;                                 // parts on their way at once
   const int64_t row = p.t * 2 * p.N, all = (int64_t)p.B * p.G * row;
   for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < all; k += (int64_t)gridDim.x * 256) {
     float v = 0.0f;
-    for (int i = 0; i < p.tiles; ++i) v += p.parts[i * all + k];
+    int i = 0;
+    for (; i + U <= p.tiles; i += U) {
+      float part[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) part[u] = p.parts[(i + u) * all + k];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v += part[u];
+    }
+    for (; i < p.tiles; ++i) v += p.parts[i * all + k];
     const int64_t bg = k / row, r = k % row;
     const unsigned step = (unsigned)(r / (2 * p.N)), rest = (unsigned)(r % (2 * p.N)), half = rest / p.N, n = rest % p.N;
     put<T>(half ? p.dC : p.dB, step, bg / p.G, bg % p.G * p.N + n, v);

@@ -45,14 +45,14 @@ struct ConvStep {
 
 __device__ inline int length_of(const int32_t* lengths, int b, int t) { return lengths ? min(max(lengths[b], 0), t) : t; }
 
+// (a group's V channels are all there)
 template <int W, int V>
-__device__ inline void load_weights(const float* weight, const float* bias, int c, int C, float (&w)[W][V], float (&wb)[V]) {
+__device__ inline void load_weights(const float* weight, const float* bias, int c, float (&w)[W][V], float (&wb)[V]) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int k = min(c + v, C - 1);
-    wb[v] = bias ? bias[k] : 0.0f;
+    wb[v] = bias ? bias[c + v] : 0.0f;
 #pragma unroll
-    for (int j = 0; j < W; ++j) w[j][v] = weight[(int64_t)k * W + j];
+    for (int j = 0; j < W; ++j) w[j][v] = weight[(int64_t)(c + v) * W + j];
   }
 }
 
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(THREADS) void conv_forward_kernel(Conv p) {
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) last[j] = input<T, W, V>(x, p.xt, state, p.C, len - (W - 1) + j, len);
   }
-  load_weights<W, V>(p.weight, p.bias, c, p.C, w, wb);
+  load_weights<W, V>(p.weight, p.bias, c, w, wb);
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) widen<T, V>(before[j], h[j]);
   if (ends) {
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(THREADS, W <= 4 ? 3 : 2) void conv_backward_kernel(
   float dw[W][V] = {}, dbias[V] = {};
   if (mine) {
     float w[W][V], wb[V];
-    load_weights<W, V>(p.weight, p.bias, c, p.C, w, wb);
+    load_weights<W, V>(p.weight, p.bias, c, w, wb);
     const int64_t items = (int64_t)p.B * p.stretches;
     for (int64_t item = (int64_t)blockIdx.y * WAVES + wave; item < items; item += (int64_t)gridDim.y * WAVES) {
       const int b = (int)(item / p.stretches), part = (int)(item % p.stretches);
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(THREADS) void conv_step_kernel(ConvStep p) {
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) load<V>((const T*)p.state_in + at + (int64_t)j * p.C, h[j]);
   load<V>((const T*)p.x + b * p.ldx + c, h[W - 1]);
-  load_weights<W, V>(p.weight, p.bias, c, p.C, w, wb);
+  load_weights<W, V>(p.weight, p.bias, c, w, wb);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
     v[e] = wb[e];

@@ -141,8 +141,10 @@ class Serving:
     def __init__(self, s: Sizes, w: dict, slots: int, device: str = "cuda:0"):
         self.s, self.w, self.dev = s, w, device
         (self.W_in, self.s_in), (self.W_out, self.s_out) = quantise(w["W_in"]), quantise(w["W_out"])
-        self.conv_states = torch.zeros((slots, s.taps - 1, s.mixed), dtype=torch.bfloat16, device=device)
-        self.scan_states = torch.zeros((slots, s.inner, s.N), device=device)
+        # a row behind the pool's last slot takes the states of sequences that have none
+        self._conv_rows = torch.zeros((slots + 1, s.taps - 1, s.mixed), dtype=torch.bfloat16, device=device)
+        self._scan_rows = torch.zeros((slots + 1, s.inner, s.N), device=device)
+        self.slots, self.conv_states, self.scan_states = slots, self._conv_rows[:slots], self._scan_rows[:slots]
         self.kept = {}
 
     def _buffers(self, t: int, B: int) -> dict:
@@ -179,14 +181,17 @@ class Serving:
         return k["out"].view(shape), k["r"].view(shape)
 
     def prompt(self, x, residual, index, lengths=None):
-        """x, residual [t, B, width]; sequence b starts in slot index[b].  Returns (out, the new residual stream): buffers of this object."""
+        """x, residual [t, B, width]; sequence b starts in slot index[b]; one whose index is no slot is passed over (its out is zero).  Returns (out,
+        the new residual stream): buffers of this object."""
         t, B, _ = x.shape
         k, w = self._buffers(t, B), self.w
+        there = (index >= 0) & (index < self.slots)
+        lengths = torch.where(there, t if lengths is None else lengths, 0).to(torch.int32)
         (z, mixed, delta), (u, Bm, Cm) = self._in(k, x, residual)
         mb.mebptt_conv_forward(k["conv"], mixed, w["conv"], w["conv_bias"], lengths, None, k["c"], k["conv_last"])
         mb.mebptt_scan_forward(k["scan"], u, delta, w["A"], Bm, Cm, w["skip"], z, w["delta_bias"], lengths, None, k["y"], k["h"], None, k["ws"])
-        at = index.long()
-        self.conv_states[at], self.scan_states[at] = k["conv_last"], k["h"]
+        at = torch.where(there, index, self.slots).long()
+        self._conv_rows[at], self._scan_rows[at] = k["conv_last"], k["h"]
         return self._out(k, x.shape)
 
     def token(self, x, residual, index: Optional[torch.Tensor] = None):

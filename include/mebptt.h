@@ -474,7 +474,8 @@ int mebptt_norm_backward(const mebptt_norm_desc* desc, const void* r, int64_t ld
                          void* stream);
 
 /* out[m][n] = a_scale[m] * b_scale[n] * sum_k a[m][k] * b[n][k] + bias[n]: a token's and a channel's scale each.  The sums are
- * exact 32-bit integers, which bounds K; they are scaled in fp32 and rounded once.
+ * exact 32-bit integers, which bounds K.  In fp32 then, each with its own rounding: the sum, times a_scale, times b_scale, plus the bias; that is
+ * rounded to out's type.  Whatever the scales, nothing on the way leaves fp32's range unless the result does.
  * read:  a [M, K] int8, row stride lda; a_scale [M] fp32; b [N, K] int8, row stride ldb (a weight matrix as it is
  *        stored); b_scale [N] fp32; bias [N] fp32 or NULL.  write: out [M, N], row stride ldo.
  * K = 0 gives the bias.  Rows of a and b that begin at 16-byte boundaries are read as they are; where K is no multiple of 16 and there is

@@ -1,6 +1,6 @@
 // Product of 8-bit integers with a scale per token and per channel:
 //     out[m][n] = a_scale[m] * b_scale[n] * sum_k a[m][k] b[n][k] + bias[n]
-// on the 8-bit matrix instructions: exact 32-bit sums, one rounding at the end.  b's rows are the instruction's rows, a's its columns, so a
+// on the 8-bit matrix instructions: exact 32-bit sums, scaled in fp32 at the end.  b's rows are the instruction's rows, a's its columns, so a
 // lane's four results are neighbours along n and are stored at once.  Three kernels: many rows by large tiles, few rows with b read once, and
 // one for a K so short that neither's loads fit.
 #include "ops.h"
@@ -43,17 +43,32 @@ __device__ inline void pack4(__bf16* to, const float (&v)[4]) {
   *reinterpret_cast<u32x2*>(to) = r.u;
 }
 
+// sum * sa * sb + bias for any scales.  Their product alone may leave fp32's range where the result does not (2^-75 each and a sum of 2^26; a
+// sum of zero and two large ones), so the sum is multiplied by one after the other.  Nothing is lost below the normal numbers on the way, as sums are
+// whole numbers; a row's scale of 2^96 or more is taken 2^64 times smaller until the end, so that only a result that is too large overflows.
+// One product more per value, which costs at most 1 % at 8192 x 4096 x 4096.
+struct RowScale {
+  float scale, rest;
+  __device__ RowScale() = default;
+  __device__ explicit RowScale(float sa) {
+    const bool large = fabsf(sa) >= 0x1p96f;
+    scale = large ? sa * 0x1p-64f : sa;
+    rest = large ? 0x1p64f : 1.0f;
+  }
+  __device__ float operator()(int sum, float sb, float bias) const { return (float)sum * scale * sb * rest + bias; }
+};
+
 // Four neighbours along n of row m.
 template <typename T>
 __device__ inline void store4(const Product& p, int64_t m, int n, i32x4 acc) {
   if (m >= p.M || n >= p.N) return;
-  const float sa = p.a_scale[m];
+  const RowScale sa(p.a_scale[m]);
   T* out = (T*)p.out + m * p.ldo + n;
   float v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int c = min(n + i, p.N - 1);
-    v[i] = (float)acc[i] * (sa * p.b_scale[c]) + (p.bias ? p.bias[c] : 0.0f);
+    v[i] = sa(acc[i], p.b_scale[c], p.bias ? p.bias[c] : 0.0f);
   }
   if (p.wide_store && n + 4 <= p.N) {
     pack4(out, v);
@@ -244,9 +259,9 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(Product p, int tiles_m, 
   static_assert(ROWS * ROW <= STAGE, "");
   __syncthreads();
   int8_t* mine = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
-  float sa[TM];
+  RowScale sa[TM];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) sa[i] = p.a_scale[min(m0 + wm + 32 * i + r, p.M - 1)];
+  for (int i = 0; i < TM; ++i) sa[i] = RowScale(p.a_scale[min(m0 + wm + 32 * i + r, p.M - 1)]);
   const int first_n = n0 + wn - BM;
 #pragma unroll
   for (int pass = 0; pass < BN / 2 / PASS; ++pass) {
@@ -265,7 +280,7 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(Product p, int tiles_m, 
         for (int e = 0; e < 4; ++e) {
           float v[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) v[c] = (float)acc[i][j][4 * e + c] * (sa[i] * sb[4 * e + c]) + bias[4 * e + c];
+          for (int c = 0; c < 4; ++c) v[c] = sa[i](acc[i][j][4 * e + c], sb[4 * e + c], bias[4 * e + c]);
           const int at = (32 * j + 8 * e + 4 * g - pass * PASS) * (int)sizeof(T), row = 32 * i + r;
           pack4(reinterpret_cast<T*>(mine + row * ROW + ((at / 16) ^ (row & (PARTS - 1))) * 16 + at % 16), v);
         }

@@ -172,7 +172,8 @@ __global__ __launch_bounds__(THREADS, W <= 4 ? 3 : 2) void conv_backward_kernel(
       for (int j = 0; j < W - 1; ++j) before[j] = input<T, W, V>(x, p.xt, state, p.C, from - (W - 1) + j, len);
 #pragma unroll
       for (int j = 0; j < W - 1; ++j) widen<T, V>(before[j], h[j]);
-      // dpre of a step, from its input (already the last of h) and d = dy; OWN: a step that dweight counts here
+      // dpre of a step, from its input (already the last of h) and d = dy; OWN: a step that dweight counts here.  (None past the sequence's end: its
+      // zero times an infinite input would not be zero.)
       auto through = [&](float (&d)[V], bool own) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(THREADS, W <= 4 ? 3 : 2) void conv_backward_kernel(
               widen<T, V>(ls[u], v);
               if (k >= 0) {
                 widen<T, V>(xs[u], h[W - 1]);
-                through(d, k < s1);
+                through(d, k < live);
               }
               gather(d, v);
               if (q >= first) {

@@ -52,3 +52,33 @@ def test_product_of_scales_from_both_ends_of_the_range(M, N, K, bias):
     err = (out.double() - want).abs()
     assert bool((err <= 2.0 ** -22 * (v.abs() + (vb.double().abs() if bias else 0.0)) + 2.0 ** -149)[~inf].all())
     assert torch.equal(out[1], vb if bias else torch.zeros_like(out[1]))
+
+
+# ---- convolution -------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("C", [64, 63])
+@pytest.mark.parametrize("t,lengths", [(9, None), (48, None), (16, [16, 9, 1]), (50, [50, 23, 1])])
+def test_conv_gradient_next_to_an_infinite_last_input(C, t, lengths):
+    """Linear taps: an infinity in a sequence's last step meets the last tap only; the other taps' gradients do not know it."""
+    B, W = 3, 4
+    rng = np.random.default_rng(t)
+    x, dy = rng.standard_normal((t, B, C)), rng.standard_normal((t, B, C))
+    w = rng.standard_normal((C, W))
+    n = [t] * B if lengths is None else lengths
+    up = lambda a, dtype=torch.float32: torch.from_numpy(np.ascontiguousarray(a)).to(DEV).to(dtype)  # noqa: E731
+    x, dy, w = (up(a).double().cpu().numpy() for a in (x, dy, w))
+    finite = x.copy()
+    for b in range(B):
+        x[n[b] - 1, b], finite[n[b] - 1, b] = np.inf, 0.0
+    d = mb.make_conv_desc(t, B, C, W, mb.FP32, 0)
+    dx, dw, db = torch.empty((t, B, C), device=DEV), torch.empty((C, W), device=DEV), torch.empty(C, device=DEV)
+    ws = torch.empty(mb.mebptt_conv_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    mb.mebptt_conv_backward(d, up(x), up(w), None, None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV), None, up(dy), None,
+                            dx, dw, db, None, ws)
+    want_dx, want_dw, want_db, _ = sel.conv_backward(finite, w, None, lengths, None, False, dy, None)
+    # sums of at most 150 products in 32 bits
+    assert np.abs(dw.cpu().numpy()[:, :W - 1] - want_dw[:, :W - 1]).max() <= 2.0 ** -24 * 150 * (np.abs(dy).max() * np.abs(finite).max())
+    assert not np.isfinite(dw.cpu().numpy()[:, W - 1]).any()
+    assert np.abs(dx.cpu().numpy() - want_dx).max() <= 2.0 ** -24 * 8 * W * (np.abs(dy).max() * np.abs(w).max())
+    assert np.abs(db.cpu().numpy() - want_db).max() <= 2.0 ** -24 * 150 * np.abs(dy).max() * 2

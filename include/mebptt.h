@@ -456,8 +456,8 @@ typedef struct {
  *        rstd [rows] fp32 (NULL: not written).  residual_out may be residual itself (and, types and ld being the same, x),
  *        y may be x (types and ld being the same).
  * The statistics and y come from r before it is rounded to residual_out's type.  MEBPTT_INT8: y_scale = max|y| / 127 of the row and
- * y = round to nearest even(y / y_scale), -127 .. 127; a row of zeros has scale 0, a row with a value that is not finite has
- * scale NaN, both with zeros in y. */
+ * y = round to nearest even(y / y_scale), -127 .. 127; a row of zeros (without an eps: one whose squares vanish in fp32) has scale 0, a row with
+ * a value that is not finite, or whose squares leave fp32's range, has scale NaN, both with zeros in y. */
 int mebptt_norm_forward(const mebptt_norm_desc* desc, const void* x, int64_t ldx, const void* residual, int64_t ldr,
                         const float* weight, void* y, int64_t ldy, float* y_scale, void* residual_out, int64_t ldo,
                         float* rstd, void* stream);

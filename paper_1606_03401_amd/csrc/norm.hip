@@ -162,6 +162,8 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void norm_forward_kernel(Norm 
     // (the barriers inside also stand between the row's last load and its first store, where buffers are shared)
     sum = row_reduce<WAVES, false>(sum, lds[0]);
     const float rstd = rsqrtf(sum / (float)p.width + p.eps);
+    // a row whose squares vanish is a row of zeros in 8 bits, without an eps too
+    const float times = QUANT && rstd == __builtin_inff() ? 0.0f : rstd;
     if (p.residual_out) {
       TR* out = (TR*)p.residual_out + row * p.ldo;
 #pragma unroll
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void norm_forward_kernel(Norm 
       if (p.weight) widen<TPR, VEC>(ws[c], c, lane, p.width, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        r[c][e] = r[c][e] * rstd * (p.weight ? w[e] : 1.0f);
+        r[c][e] = r[c][e] * times * (p.weight ? w[e] : 1.0f);
         if constexpr (QUANT) top = max_or_nan(top, fabsf(r[c][e]));
       }
     }

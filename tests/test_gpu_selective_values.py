@@ -82,3 +82,25 @@ def test_conv_gradient_next_to_an_infinite_last_input(C, t, lengths):
     assert not np.isfinite(dw.cpu().numpy()[:, W - 1]).any()
     assert np.abs(dx.cpu().numpy() - want_dx).max() <= 2.0 ** -24 * 8 * W * (np.abs(dy).max() * np.abs(w).max())
     assert np.abs(db.cpu().numpy() - want_db).max() <= 2.0 ** -24 * 150 * np.abs(dy).max() * 2
+
+
+# ---- norm --------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("width", [8, 63, 1024, 2056, 9000])
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm_to_8_bits_of_rows_of_zeros_without_an_eps(width, residual):
+    rows = 5
+    g = _gen(width)
+    x = torch.randn((rows, width), generator=g, device=DEV)
+    res = torch.randn((rows, width), generator=g, device=DEV) if residual else None
+    x[[1, 3]] = 0.0 if not residual else -res[[1, 3]]
+    d = mb.make_norm_desc(rows, width, mb.FP32, mb.FP32, mb.INT8, 0.0)
+    y, scale = torch.full((rows, width), 7, dtype=torch.int8, device=DEV), torch.full((rows,), 7.0, device=DEV)
+    mb.mebptt_norm_forward(d, x, res, None, y, scale)
+    assert bool((scale[[1, 3]] == 0).all()) and bool((y[[1, 3]] == 0).all())
+    # the others: a row's largest value is 127 steps
+    assert bool((y[[0, 2, 4]].abs().amax(1) == 127).all())
+    r = x.double() if res is None else (x + res).double()
+    top = (r * torch.rsqrt(r.square().mean(1, keepdim=True))).abs().amax(1)
+    assert bool((scale[[0, 2, 4]].double() * 127 / top[[0, 2, 4]] - 1).abs().max() < 2.0 ** -18)

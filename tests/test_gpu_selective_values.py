@@ -104,3 +104,52 @@ def test_norm_to_8_bits_of_rows_of_zeros_without_an_eps(width, residual):
     r = x.double() if res is None else (x + res).double()
     top = (r * torch.rsqrt(r.square().mean(1, keepdim=True))).abs().amax(1)
     assert bool((scale[[0, 2, 4]].double() * 127 / top[[0, 2, 4]] - 1).abs().max() < 2.0 ** -18)
+
+
+# ---- scan --------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("N", [3, 8, 16, 24, 40])
+@pytest.mark.parametrize("t,lengths", [(9, None), (40, [40, 9, 33]), (64, [48, 1, 63])])
+def test_scan_gradient_next_to_infinite_ends(N, t, lengths):
+    """An infinite last input makes the last state infinite, which no gradient of A or of earlier steps looks at; an infinite gradient of the last
+    state stays out of what lies beyond a sequence's end, which is zero.  Tolerance: sums of at most 64 x 64 products of values up to 8, 2^-24 * 4096
+    of the largest."""
+    B, D = 3, 20
+    rng = np.random.default_rng(t + N)
+    n = [t] * B if lengths is None else lengths
+    f32 = lambda *s: rng.standard_normal(s).astype(np.float32).astype(np.float64)  # noqa: E731
+    u, delta, dy, Bm, Cm = f32(t, B, D), f32(t, B, D) - 1.0, f32(t, B, D), f32(t, B, N), f32(t, B, N)
+    A, dh = -np.abs(f32(D, N)) - 0.1, f32(B, D, N)
+    finite = u.copy()
+    for b in range(B):
+        u[n[b] - 1, b, 2], finite[n[b] - 1, b, 2] = np.inf, 0.0
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to(DEV).to(torch.float32)  # noqa: E731
+    A = up(A).double().cpu().numpy()
+    at = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    d = mb.make_scan_desc(t, B, D, N, 1, mb.FP32, 1, 16)
+    new = lambda *s, dtype=torch.float32: torch.full(s, 5, dtype=dtype, device=DEV)  # noqa: E731
+    states = new(mb.mebptt_scan_state_bytes(d), dtype=torch.uint8)
+    ws = new(max(256, mb.mebptt_scan_workspace_bytes(d, True)), dtype=torch.uint8)
+
+    def gradients(u, dh):
+        args = (up(u), up(delta), up(A), up(Bm), up(Cm), None, None, None, at, None)
+        mb.mebptt_scan_forward(d, *args, new(t, B, D), None, states, ws)
+        du, dd, dA, dB, dC, dh0 = new(t, B, D), new(t, B, D), new(D, N), new(t, B, N), new(t, B, N), new(B, D, N)
+        mb.mebptt_scan_backward(d, *args, up(dy), up(dh), states, du, dd, dA, dB, dC, None, None, None, dh0, ws)
+        return {k: v.double().cpu().numpy() for k, v in dict(du=du, ddelta=dd, dA=dA, dB=dB, dC=dC, dh0=dh0).items()}
+
+    got = gradients(u, dh)
+    want = sel.scan_backward(finite, delta, A, Bm, Cm, 1, None, None, None, n, None, True, dy, dh)
+    near = lambda k, g, w: np.testing.assert_array_less(np.abs(g - w), 2.0 ** -12 * np.abs(want[k]).max() + 1e-30, err_msg=k)  # noqa: E731
+    near("dA", got["dA"], want["dA"])
+    near("dh0", got["dh0"], want["dh0"])
+    for b in range(B):
+        for k in ("du", "ddelta", "dB", "dC"):
+            near(k, got[k][:n[b] - 1, b], want[k][:n[b] - 1, b])
+            assert (got[k][n[b]:, b] == 0).all(), k
+    dh[:, 5] = np.inf
+    got = gradients(finite, dh)
+    for b in range(B):
+        for k in ("du", "ddelta", "dB", "dC"):
+            assert (got[k][n[b]:, b] == 0).all(), k

@@ -479,7 +479,8 @@ int mebptt_norm_backward(const mebptt_norm_desc* desc, const void* r, int64_t ld
  * read:  a [M, K] int8, row stride lda; a_scale [M] fp32; b [N, K] int8, row stride ldb (a weight matrix as it is
  *        stored); b_scale [N] fp32; bias [N] fp32 or NULL.  write: out [M, N], row stride ldo.
  * K = 0 gives the bias.  Rows of a and b that begin at 16-byte boundaries are read as they are; where K is no multiple of 16 and there is
- * much to multiply, others are first copied into the workspace. */
+ * much to multiply, others are first copied into the workspace: at most mebptt_int8_workspace_bytes, nothing for an operand whose address and
+ * stride are multiples of 16. */
 typedef struct {
   int64_t M;         /* 0 .. 2^28; M * N at most 2^38 */
   int32_t N, K;      /* N 1 .. 2^21, K 0 .. 131071 */

@@ -516,15 +516,17 @@ int mebptt_int8_product(const mebptt_int8_desc* d, const int8_t* a, int64_t lda,
   if (d->M == 0) return MEBPTT_OK;
   if (!a_scale || !b_scale || !out || (d->K && (!a || !b))) return set_error(MEBPTT_EINVAL, "a required pointer is NULL");
   if ((d->K && (lda < d->K || ldb < d->K)) || ldo < d->N) return set_error(MEBPTT_EINVAL, "a row stride is below the row's length");
-  if ((rc = check_workspace(workspace, workspace_bytes, mebptt_int8_workspace_bytes(d)))) return rc;
   Product p = {a, b, a_scale, b_scale, bias, out, d->M, lda, ldb, ldo, d->N, d->K, rows_aligned(out, ldo, d->out_dtype, 4),
                rows_aligned(out, ldo, d->out_dtype, 8)};
   const hipStream_t st = (hipStream_t)stream;
   if (copies_pay(d->M, d->N, d->K)) {
     const int64_t ld = copied_ld(d->K);
     auto ready = [](const int8_t* x, int64_t ldx) { return aligned(x, 16) && ldx % 16 == 0; };
-    int8_t* room = (int8_t*)workspace;
-    Copy ca = {a, room, ready(a, lda) ? 0 : d->M, lda, ld, d->K}, cb = {b, room + copy_bytes(d->M, d->K), ready(b, ldb) ? 0 : d->N, ldb, ld, d->K};
+    Copy ca = {a, nullptr, ready(a, lda) ? 0 : d->M, lda, ld, d->K}, cb = {b, nullptr, ready(b, ldb) ? 0 : d->N, ldb, ld, d->K};
+    // (rows that are ready need no room)
+    if ((rc = check_workspace(workspace, workspace_bytes, copy_bytes(ca.rows, d->K) + copy_bytes(cb.rows, d->K)))) return rc;
+    ca.to = (int8_t*)workspace;
+    cb.to = ca.to + copy_bytes(ca.rows, d->K);
     if (ca.rows) p.a = ca.to, p.lda = ld;
     if (cb.rows) p.b = cb.to, p.ldb = ld;
     if (ca.rows + cb.rows) {

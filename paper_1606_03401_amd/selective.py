@@ -148,21 +148,18 @@ class Serving:
         self.kept = {}
 
     def _buffers(self, t: int, B: int) -> dict:
-        """What a call of these sizes needs; made once per size, so that a captured call finds it in place."""
-        key = (t, B)
-        if key not in self.kept:
-            s, M, f32 = self.s, t * B, torch.float32
-            new = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device=self.dev)  # noqa: E731
-            k = {"norm": mb.make_norm_desc(M, s.width, mb.BF16, mb.FP32, mb.INT8, EPS), "norm_out": mb.make_norm_desc(M, s.inner, mb.BF16, mb.BF16, mb.INT8, EPS),
-                 "product": mb.make_int8_desc(M, s.projected, s.width, mb.BF16), "product_out": mb.make_int8_desc(M, s.width, s.inner, mb.BF16),
-                 "conv": mb.make_conv_desc(t, B, s.mixed, s.taps, mb.BF16, 1), "scan": mb.make_scan_desc(t, B, s.inner, s.N, s.groups, mb.BF16, 1),
-                 "n": new(M, s.width, dtype=torch.int8), "n_scale": new(M, dtype=f32), "r": new(M, s.width, dtype=f32), "p": new(t, B, s.projected),
-                 "c": new(t, B, s.mixed), "y": new(t, B, s.inner), "m": new(M, s.inner, dtype=torch.int8), "m_scale": new(M, dtype=f32),
-                 "out": new(M, s.width), "conv_last": new(B, s.taps - 1, s.mixed), "h": new(B, s.inner, s.N, dtype=f32)}
-            k["ws"] = _bytes(max(mb.mebptt_scan_workspace_bytes(k["scan"], False), mb.mebptt_int8_workspace_bytes(k["product"]),
-                                 mb.mebptt_int8_workspace_bytes(k["product_out"])), self.dev)
-            self.kept[key] = k
-        return self.kept[key]
+        """What a call of these sizes needs."""
+        s, M, f32 = self.s, t * B, torch.float32
+        new = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device=self.dev)  # noqa: E731
+        k = {"norm": mb.make_norm_desc(M, s.width, mb.BF16, mb.FP32, mb.INT8, EPS), "norm_out": mb.make_norm_desc(M, s.inner, mb.BF16, mb.BF16, mb.INT8, EPS),
+             "product": mb.make_int8_desc(M, s.projected, s.width, mb.BF16), "product_out": mb.make_int8_desc(M, s.width, s.inner, mb.BF16),
+             "conv": mb.make_conv_desc(t, B, s.mixed, s.taps, mb.BF16, 1), "scan": mb.make_scan_desc(t, B, s.inner, s.N, s.groups, mb.BF16, 1),
+             "n": new(M, s.width, dtype=torch.int8), "n_scale": new(M, dtype=f32), "r": new(M, s.width, dtype=f32), "p": new(t, B, s.projected),
+             "c": new(t, B, s.mixed), "y": new(t, B, s.inner), "m": new(M, s.inner, dtype=torch.int8), "m_scale": new(M, dtype=f32),
+             "out": new(M, s.width)}
+        k["ws"] = _bytes(max(mb.mebptt_scan_workspace_bytes(k["scan"], False), mb.mebptt_int8_workspace_bytes(k["product"]),
+                             mb.mebptt_int8_workspace_bytes(k["product_out"])), self.dev)
+        return k
 
     def _in(self, k: dict, x, residual):
         s, w = self.s, self.w
@@ -182,22 +179,28 @@ class Serving:
 
     def prompt(self, x, residual, index, lengths=None):
         """x, residual [t, B, width]; sequence b starts in slot index[b]; one whose index is no slot is passed over (its out is zero).  Returns (out,
-        the new residual stream): buffers of this object."""
+        the new residual stream), the caller's own: prompts come in any length, so nothing is kept of a call."""
         t, B, _ = x.shape
-        k, w = self._buffers(t, B), self.w
+        s, k, w = self.s, self._buffers(t, B), self.w
+        conv_last = torch.empty((B, s.taps - 1, s.mixed), dtype=torch.bfloat16, device=self.dev)
+        h = torch.empty((B, s.inner, s.N), device=self.dev)
         there = (index >= 0) & (index < self.slots)
         lengths = torch.where(there, t if lengths is None else lengths, 0).to(torch.int32)
         (z, mixed, delta), (u, Bm, Cm) = self._in(k, x, residual)
-        mb.mebptt_conv_forward(k["conv"], mixed, w["conv"], w["conv_bias"], lengths, None, k["c"], k["conv_last"])
-        mb.mebptt_scan_forward(k["scan"], u, delta, w["A"], Bm, Cm, w["skip"], z, w["delta_bias"], lengths, None, k["y"], k["h"], None, k["ws"])
+        mb.mebptt_conv_forward(k["conv"], mixed, w["conv"], w["conv_bias"], lengths, None, k["c"], conv_last)
+        mb.mebptt_scan_forward(k["scan"], u, delta, w["A"], Bm, Cm, w["skip"], z, w["delta_bias"], lengths, None, k["y"], h, None, k["ws"])
         at = torch.where(there, index, self.slots).long()
-        self._conv_rows[at], self._scan_rows[at] = k["conv_last"], k["h"]
+        self._conv_rows[at], self._scan_rows[at] = conv_last, h
         return self._out(k, x.shape)
 
     def token(self, x, residual, index: Optional[torch.Tensor] = None):
-        """x, residual [B, width], one token each; a sequence whose index is no slot is passed over."""
-        B = x.shape[0]
-        k, w = self._buffers(1, B), self.w
+        """x, residual [B, width], one token each; a sequence whose index is no slot is passed over.  Returns (out, the new residual stream):
+        buffers of this object, made once per batch size and stream, so that a captured call finds them in place."""
+        B, w = x.shape[0], self.w
+        key = (B, torch.cuda.current_stream(self.dev).cuda_stream)
+        if key not in self.kept:
+            self.kept[key] = self._buffers(1, B)
+        k = self.kept[key]
         (z, mixed, delta), (u, Bm, Cm) = self._in(k, x, residual)
         mb.mebptt_conv_step(k["conv"], mixed[0], w["conv"], w["conv_bias"], self.conv_states, index, k["c"][0], self.conv_states)
         mb.mebptt_scan_step(k["scan"], u[0], delta[0], w["A"], Bm[0], Cm[0], w["skip"], z[0], w["delta_bias"], self.scan_states, index, k["y"][0],

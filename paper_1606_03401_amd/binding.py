@@ -581,11 +581,12 @@ _current_device = _current_stream = None
 def _load_torch():
     global _torch, _DTYPES, _current_device, _current_stream
     import torch
-    _torch, _DTYPES = torch, (torch.float32, torch.bfloat16, torch.int8)
     torch.cuda.init()
+    _DTYPES = (torch.float32, torch.bfloat16, torch.int8)
     _current_device = torch._C._cuda_getDevice
     # the raw handle without a Stream object around it
     _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    _torch = torch      # last: whoever finds it goes on with all the others
 
 
 def _dtype(code: int):

@@ -80,7 +80,8 @@ __device__ inline void store4(const Product& p, int64_t m, int n, i32x4 acc) {
 }
 
 // LDS rows of KB bytes; the four 16-byte parts of a row change places with the row, so that eight neighbouring rows' same part
-// (what eight lanes read at a time) lie in eight different places of 128 bytes.
+// (what eight lanes read at a time) lie in eight different places of 128 bytes.  (The counters have eight cycles to a read of 1 KB, 128 bytes a cycle,
+// and count half of them as conflicts.)
 __device__ inline int place(int row, int part) { return row * KB + ((part ^ ((row >> 1) & 3)) * 16); }
 
 // 64 x 64 outputs per workgroup, 32 x 32 per wave, operands through LDS one step ahead in registers.  Any size, stride and alignment; in use
@@ -129,10 +130,11 @@ __global__ __launch_bounds__(256) void int8_product_kernel(Product p) {
 // it directly, 64 bytes of K per stage, four stages: while a stage is multiplied, the next one's fragments are read into a second set of
 // registers and three more are on their way.  Rows begin at 16-byte boundaries; only the last stage may be short, and goes through registers.
 //
-// Bound: the card's power, then the matrix instructions.  A stage of 256 x 256 is 1024 cycles of matrix instructions on every SIMD; its 32 KB written to
-// LDS and 64 KB read take 768 at 128 bytes a cycle; one workgroup alone takes 1230.  Measured on random operands: 8192 x 4096 x 4096 132 - 140 us,
-// 2.0 POP/s, 8192^3 480 us, 2.3 POP/s (the library's 8-bit product 2.0), at 1.9 of the card's 2.4 GHz; the same launches on zeros 104 and 366 us.
-// The order of K and the places in LDS make no difference to that.
+// Bound: the card's power, the matrix instructions, and what a tile does before and after them, with no other workgroup on its compute unit.  A stage of
+// 256 x 256 is 1024 cycles of matrix instructions on every SIMD, 0.43 us at 2.4 GHz; its 32 KB written to LDS and 64 KB read take 768 at 128 bytes a
+// cycle.  Measured with the chip full, K from 4096 to 16384: 0.54 us a stage on zeros, 0.85 on random operands, at 1.9 GHz, and 14 to 16 us a tile
+// besides.  8192 x 4096 x 4096, two tiles per compute unit, 137 - 141 us, 2.0 POP/s, on zeros 100, the matrix unit 51 % busy; 8192^3 480 us, 2.3 POP/s, on
+// zeros 366 (the library's 8-bit product 2.0 POP/s).  The order of K and the places in LDS make no difference to that.
 
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(1))) const void global_void;
@@ -431,8 +433,8 @@ __global__ __launch_bounds__(256) void int8_copy_kernel(Copy a, Copy b) {
 }
 
 // The three kernels by what a launch is estimated to take, in us, fitted to 15 shapes timed on all of them (M 1 .. 8192, N 512 .. 16384,
-// K 512 .. 8192; within a quarter of the times measured).  One tile alone is bound by its stages' latency, a chip full of them by what
-// the L2s deliver.  Measured, rows / 128 / 256: 32 x 16384 x 4096 20 / 30 / 66, 512 x 512 x 4096 11.5 / 18.8 / 45, 1024 x 4096 x 4096 48 / 25 / 49,
+// K 512 .. 8192; within a quarter of the times measured).  A tile's stages take longer the fuller the
+// chip is.  Measured, rows / 128 / 256: 32 x 16384 x 4096 20 / 30 / 66, 512 x 512 x 4096 11.5 / 18.8 / 45, 1024 x 4096 x 4096 48 / 25 / 49,
 // 8192 x 4096 x 4096 310 / 221 / 169.
 struct Estimate {
   double rows, t128, t256;

@@ -8,8 +8,8 @@
 //
 // Bound: the vector unit.  Per step, channel and state the forward pass needs an exponential and four products or multiply-adds, 24 cycles
 // of a SIMD for 64 of them, the backward pass 60; what staging, sums over lanes and addresses add to that makes 36 and 133.  Measured, bf16 with
-// a gate, N = 16: 1000 x 32 x 1024, forward 185 us and backward 680 (the operations above alone 80 and 200, the bytes 35 and 73), two
-// thirds of the cycles with a vector instruction; 10000 x 1 x 2048, forward, 161 us in three launches (50; 33).
+// a gate, N = 16: 1000 x 32 x 1024, forward 175 us and backward 640 (the operations above alone 80 and 200, the bytes 35 and 73), two
+// thirds of the cycles with a vector instruction; 10000 x 1 x 2048, forward, 150 us in three launches (50; 33).
 #include "dynamic_lds.h"
 #include "ops.h"
 
@@ -64,8 +64,8 @@ __device__ inline float log2_decay(float A) {
   return v < -MOST ? -MOST : v > MOST ? MOST : v;      // (a NaN stays one)
 }
 
-// log(1 + e^x).  Small values keep their relative accuracy, steps of a thousandth being what such a model starts with: what 1 + e lost of e is
-// added to the logarithm of the sum.
+// log(1 + e^x).  Small values are as accurate as e^x is, (4 + 1.5 |x|) 2^-24 of themselves, steps of a thousandth being what such a model starts with:
+// what 1 + e lost of e is added to the logarithm of the sum.
 __device__ inline float softplus_of(float x) {
   const float e = __expf(-fabsf(x)), w = 1.0f + e;
   return fmaxf(x, 0.0f) + (__builtin_amdgcn_logf(w) * LN2 + (e - (w - 1.0f)));
@@ -1055,7 +1055,8 @@ size_t starts_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ?
 size_t sums_bytes(const mebptt_scan_desc* d, int chunks) { return chunks < 2 ? 0 : align_up((size_t)chunks * d->B * d->D * sizeof(float)); }
 
 // Backward launches: 4 states per lane, two waves per SIMD, where what a block keeps (exp(w A) and exp(w A) h of 16 steps) takes half the
-// registers.  With 2 states per lane and twice the waves: 1000 x 32 x 1024, N = 8 473 us instead of 465, N = 16 883 instead of 711, N = 32
+// registers.  (With stretches of 256, and of 128 up to N = 8, the states at the starts of their blocks take so much LDS that a compute unit holds one
+// workgroup, one wave per SIMD: below.)  With 2 states per lane and twice the waves, when that was chosen: 1000 x 32 x 1024, N = 8 473 us instead of 465, N = 16 883 instead of 711, N = 32
 // 1619 instead of 1240.  The time axis is cut as the forward pass's is, in whole stretches: 1000 x 32 x 1024, which gives 2048 waves, 711 us
 // uncut, 778 in two; 10000 x 1 x 2048, both passes, 660 us, 1827 uncut.
 constexpr int BACK_ENOUGH = 2048, BACK_WANT = 4096;   // waves
@@ -1093,6 +1094,9 @@ size_t bc_bytes(const mebptt_scan_desc* d, const BackCut& c) {
 }
 size_t a_bytes(const mebptt_scan_desc* d, const BackCut& c) { return align_up((size_t)c.chunks * d->B * d->D * (d->N + 2) * sizeof(float)); }
 
+// Per workgroup at stretches of 64 / 128 / 256: N = 8 80 / 96 / 129 thousand bytes, N = 16 53 / 70 / 102, N = 32 49 / 66 / 98, of a compute unit's 164.  Time by stretch,
+// 16 / 32 / 64 / 128 / 256: 1000 x 32 x 1024, N = 8 390 / 436 / 464 / 711 / 724 us, N = 16 524 / 603 / 635 / 651 / 1003 (the forward pass, which writes the
+// states, 207 / 177 / 170 / 168 / 165).
 template <typename S>
 size_t back_lds(int stretch) {
   return (2 * ((size_t)BS * S::CH * 4 + 2 * BS * S::NP) + S::BACK_WAVES * BS * 2 * S::NP + std::max(stretch / BS - 2, 0) * S::THREADS * S::NB) * sizeof(float);

@@ -289,14 +289,14 @@ def _own_adamw(s):
                                         [k["copy"][at:at + n] for at, n in places] if c["copy"] else None)
         table = _bytes(mb.mebptt_adamw_table_bytes(tensors))
         mb.mebptt_adamw_prepare(tensors, table)
-        k |= {"table": table, "tensors": tensors,
+        k |= {"table": table, "tensors": tensors, "ws": _bytes(mb.mebptt_adamw_workspace_bytes(tensors)),
               "desc": mb.make_adamw_desc(ADAM["rate"], ADAM["beta1"], ADAM["beta2"], ADAM["eps"], ADAM["decay"], ADAM["step"], ADAM["seed"])}
         if small:
             k |= {"m": torch.empty(total, dtype=torch.bfloat16, device="cuda"), "v": torch.empty(total, dtype=torch.bfloat16, device="cuda")}
         return k
     k = _kept(s, make)
     if c["clip"]:
-        mb.mebptt_adamw_norm(k["tensors"], k["table"], 1.0, k["norm"])
+        mb.mebptt_adamw_norm(k["tensors"], k["table"], 1.0, k["norm"], k["ws"])
     mb.mebptt_adamw_step(k["desc"], k["tensors"], k["table"], k["norm"][1:] if c["clip"] else None)
     out = {"p": s["p"], "m": s["m"], "v": s["v"]}
     if small:
@@ -505,9 +505,9 @@ def _mix(x):
 
 
 def _random(case, total):
-    """What a value is rounded with: a hash of the seed, its block's number over all tensors and its place there."""
+    """What a value is rounded with: a hash of the seed, the step, its block's number over all tensors and its place there."""
     block, place = torch.arange(total // BLOCK, device="cuda"), torch.arange(BLOCK, device="cuda")
-    key = _mix((ADAM["seed"] + block * 0x9E3779B9) & 0xFFFFFFFF)
+    key = _mix((ADAM["seed"] + ADAM["step"] * 0x632BE5AB + block * 0x9E3779B9) & 0xFFFFFFFF)
     return _mix((key[:, None] + place * 0x85157AF5) & 0xFFFFFFFF).flatten()
 
 

@@ -570,6 +570,138 @@ int mebptt_scan_backward(const mebptt_scan_desc* desc, const mebptt_scan_inputs*
 int mebptt_scan_step(const mebptt_scan_desc* desc, const mebptt_scan_inputs* in, const float* state_in, int64_t slots,
                      const int32_t* index, mebptt_seq y, float* state_out, void* stream);
 
+/* ---- a block with a matrix for a state, and the step that trains it ------------------------------------
+ * A recurrent core whose state is a matrix per head, corrected at every step by what it answers to that step's key (the gated delta rule), the
+ * norms that stand behind such a core and before the next one, and AdamW over all tensors of a model at once.  The rules of
+ * the section above hold here too. */
+
+/* Gated delta rule.  Per sequence and value head, with a state S [dk, dv] and key head h / (H / Hk):
+ *     alpha_s = exp(g_s),  r_s = v_s - alpha_s S_{s-1}^T k^_s,  S_s = alpha_s S_{s-1} + beta_s k^_s r_s^T,  y_s = scale S_s^T q^_s,
+ * q^, k^: q and k divided by sqrt(their squares' sum + eps) if `normalise`, else as they are.  activate: g = A softplus(a + a_bias), beta = sigmoid(b);
+ * otherwise g = a (not above 0 where the recurrence is to be stable) and beta = b as given.  Without an a, g = 0.  g below -10000 counts as that.
+ * Steps are taken 64 at a time; a value of a sequence's own that is not finite may reach its head's results up to 63 steps earlier, those of no
+ * other sequence or head.  Lengths as in the convolution; h_out is the state after a sequence's own last step. */
+typedef struct {
+  int32_t t, B;      /* t 0 .. 2^30, B 0 .. 65535; B * H at most 2^22 */
+  int32_t Hk, H;     /* heads of q and k, heads of v: 1 .. 1024, Hk divides H */
+  int32_t dk, dv;    /* 1 .. 128, 1 .. 256 */
+  int32_t dtype;     /* MEBPTT_FP32 or MEBPTT_BF16: q, k, v, a, b, y and their gradients */
+  int32_t activate, normalise;
+  int32_t stretch;   /* the backward pass's memory for time: the state of every `stretch`-th step is kept, and the backward call recomputes what
+                        lies between, one stretch after the other.  A multiple of 64, up to 2^20; not looked at without `states`. */
+  float scale, eps;  /* eps >= 0 */
+} mebptt_delta_desc;
+typedef struct {
+  mebptt_seq q, k;         /* Hk * dk channels */
+  mebptt_seq v;            /* H * dv channels */
+  mebptt_seq a;            /* H channels; data NULL: no decay */
+  mebptt_seq b;            /* H channels */
+  const float *A, *a_bias; /* [H], with activate and an a; a_bias may be NULL */
+  const int32_t* lengths;  /* [B] or NULL */
+  const float* h0;         /* [B, H, dk, dv] or NULL: zeros */
+} mebptt_delta_inputs;
+typedef struct {
+  mebptt_seq dq, dk, dv, db;
+  mebptt_seq da;           /* written if there is an a */
+  float *dA, *da_bias;     /* [H], with activate and an a; may be NULL */
+  float* dh0;              /* may be NULL */
+} mebptt_delta_grads;
+/* Bytes of the states that a forward call keeps for a backward call; of a forward call's workspace, or (backward != 0) of one that does for
+ * both calls. */
+size_t mebptt_delta_state_bytes(const mebptt_delta_desc* desc);
+size_t mebptt_delta_workspace_bytes(const mebptt_delta_desc* desc, int32_t backward);
+/* `in` (host) is read during the call only.  write: y [H * dv channels]; h_out [B, H, dk, dv] (NULL: not written; may be h0 itself); states (NULL
+ * when no backward call follows; 256-byte aligned). */
+int mebptt_delta_forward(const mebptt_delta_desc* desc, const mebptt_delta_inputs* in, mebptt_seq y, float* h_out, void* states,
+                         size_t states_bytes, void* workspace, size_t workspace_bytes, void* stream);
+/* read: the forward call's inputs and the states that it kept, dy, dh_out [B, H, dk, dv] (NULL: zeros).  write: all of `grads` (host).  dh0 may be
+ * dh_out itself. */
+int mebptt_delta_backward(const mebptt_delta_desc* desc, const mebptt_delta_inputs* in, mebptt_seq dy, const float* dh_out,
+                          const void* states, size_t states_bytes, const mebptt_delta_grads* grads, void* workspace,
+                          size_t workspace_bytes, void* stream);
+/* One token for each of B sequences, states in a pool [slots, H, dk, dv] and indices as in mebptt_conv_step.  desc->t must be 1; the
+ * sequences' stride_t, and in->lengths and in->h0, are not looked at. */
+int mebptt_delta_step(const mebptt_delta_desc* desc, const mebptt_delta_inputs* in, const float* state_in, int64_t slots,
+                      const int32_t* index, mebptt_seq y, float* state_out, void* stream);
+
+/* What joins a block to the residual stream: the norm of the block's output x, per group of `group` neighbouring columns (a head, or the whole
+ * row), its gate, the addition to the scaled stream, and the norm in front of the next block:
+ *     branch = x * rsqrt(mean over the group(x^2) + eps) * weight * silu(z);   without a residual  y = branch,  with one
+ *     r = scale * residual + branch,   y = r * rsqrt(mean(r^2) + eps) * weight_next. */
+typedef struct {
+  int64_t rows;
+  int32_t width;          /* 1 .. 16384 */
+  int32_t group;          /* divides width; at least 8 where width is over 4096 * group */
+  int32_t x_dtype;        /* MEBPTT_FP32 or MEBPTT_BF16: x, z, y and their gradients */
+  int32_t residual_dtype; /* the same choice for residual, residual_out and their gradients */
+  float scale;
+  float eps;              /* >= 0 */
+} mebptt_join_desc;
+/* read:  x [rows, width], row stride ldx (elements, >= width; all ld alike); z (NULL: no gate); weight [width] fp32 (NULL: ones);
+ *        residual (NULL: none, and then weight_next, residual_out and rstd_next must be NULL); weight_next [width] fp32 (NULL: ones).
+ * write: y; residual_out = r rounded to its type (NULL: not written); rstd [rows, width / group] and rstd_next [rows] fp32, the norms'
+ *        factors (NULL: not written).  residual_out may be residual itself, y may be x or z (ld being the same).
+ * The second norm's statistics and y come from r before it is rounded to residual_out's type. */
+int mebptt_join_forward(const mebptt_join_desc* desc, const void* x, int64_t ldx, const void* z, int64_t ldz, const float* weight,
+                        const void* residual, int64_t ldr, const float* weight_next, void* y, int64_t ldy, void* residual_out,
+                        int64_t ldo, float* rstd, float* rstd_next, void* stream);
+/* Gradients of mebptt_join_forward.
+ * read:  x, z, weight as there; r [rows, width]: what residual_out received (NULL: there was no residual, and then weight_next, rstd_next,
+ *        dresidual_out, dresidual and dweight_next must be NULL), weight_next, rstd, rstd_next, dy, dresidual_out (the gradient that arrives at
+ *        residual_out; NULL: none).
+ * write: dx; dz (NULL exactly if z is); dresidual (NULL: not written; may be dresidual_out itself); dweight, dweight_next [width] fp32
+ *        (NULL: not computed).  dx may be dy. */
+size_t mebptt_join_workspace_bytes(const mebptt_join_desc* desc);
+int mebptt_join_backward(const mebptt_join_desc* desc, const void* x, int64_t ldx, const void* z, int64_t ldz, const float* weight,
+                         const void* r, int64_t ldr, const float* weight_next, const float* rstd, const float* rstd_next,
+                         const void* dy, int64_t lddy, const void* dresidual_out, int64_t lddo, void* dx, int64_t lddx, void* dz,
+                         int64_t lddz, float* dweight, void* dresidual, int64_t lddr, float* dweight_next, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* AdamW, one step over many tensors:
+ *     g = factor * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *     param = param (1 - rate decay) - rate (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
+ * States have 32 bits, or 8: then each block of 256 values (counted from a tensor's first one) has a scale in m_scale and v_scale, and a code stands for
+ * scale * 2^(e - 15) (1 + f / 8) with sign, 4 bits of e and 3 of f (m), or scale * 2^(e - 31) (1 + f / 8) with 5 bits of e (v); 0 is zero.  A scale
+ * is the block's largest new value / 1.875.  Values between two codes take one of them by chance, with the odds that keep the mean:
+ * a v that changes by a thousandth a step would never move otherwise.  The chance is a hash of seed, step and the value's place, so
+ * that the same call gives the same bits.  m below 1.125 * 2^-15 of its scale becomes that or zero in the same way, v below 1.125 * 2^-31 of its becomes
+ * that, never zero, which would make the next step too large. */
+enum { MEBPTT_ADAMW_NO_DECAY = 1 };
+typedef struct {
+  float* param;
+  const void* grad;        /* grad_dtype */
+  void *m, *v;             /* fp32, or a byte per value */
+  float *m_scale, *v_scale; /* [ceil(n / 256)], 8-bit states only */
+  void* copy;              /* receives param in bf16; or NULL */
+  int64_t n;               /* 0 .. 2^40 */
+  int32_t grad_dtype;      /* MEBPTT_FP32 or MEBPTT_BF16 */
+  int32_t state_dtype;     /* MEBPTT_FP32 or MEBPTT_INT8 */
+  int32_t flags;
+  int32_t reserved;        /* 0 */
+} mebptt_adamw_tensor;
+typedef struct {
+  float rate, beta1, beta2, eps, decay; /* beta1, beta2 0 .. below 1; eps >= 0 */
+  uint32_t seed;
+  int64_t step;            /* 1, 2, ... */
+} mebptt_adamw_desc;
+/* `tensors` (host) are read during a call only; at most 65536 of them, 2^42 values in all.  prepare writes what the other calls need to know of
+ * the tensors into `table` (device, 256-byte aligned), to be called again when a pointer or size changes.  The others only look at the number and sizes of
+ * `tensors`, which must be those of the table. */
+size_t mebptt_adamw_table_bytes(const mebptt_adamw_tensor* tensors, int32_t count);
+int mebptt_adamw_prepare(const mebptt_adamw_tensor* tensors, int32_t count, void* table, size_t table_bytes, void* stream);
+/* out[0] = norm of all gradients together, summed in 64 bits; out[1] = min(1, max_norm / norm), the factor that limits it, NaN if the norm is not
+ * finite.  max_norm > 0. */
+size_t mebptt_adamw_workspace_bytes(const mebptt_adamw_tensor* tensors, int32_t count);
+int mebptt_adamw_norm(const mebptt_adamw_tensor* tensors, int32_t count, const void* table, size_t table_bytes, float max_norm,
+                      float* out, void* workspace, size_t workspace_bytes, void* stream);
+/* factor (device, NULL: 1): what gradients are multiplied by; if it is not finite the call changes nothing.  rate, step (device, NULL: those of desc):
+ * for a captured call that is replayed; a step below 1 counts as 1. */
+int mebptt_adamw_step(const mebptt_adamw_desc* desc, const mebptt_adamw_tensor* tensors, int32_t count, const void* table,
+                      size_t table_bytes, const float* factor, const float* rate, const int64_t* step, void* stream);
+/* Values that n codes of one tensor stand for, to fp32 or bf16 (`is_signed`: those of m). */
+int mebptt_adamw_unpack(const uint8_t* codes, const float* scale, int64_t n, int32_t is_signed, void* out, int32_t out_dtype, void* stream);
+
 /* ---- measurement hooks ---------------------------------------------------------------------
  * Kernel classes of the hot path, for timing with HIP events on the run's own stream. */
 enum {

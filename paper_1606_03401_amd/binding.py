@@ -120,6 +120,36 @@ class mebptt_scan_grads(C.Structure):
                 + [(n, C.c_void_p) for n in ("dA", "dskip", "ddelta_bias", "dh0")])
 
 
+class mebptt_delta_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("t", "B", "Hk", "H", "dk", "dv", "dtype", "activate", "normalise", "stretch")]
+                + [("scale", C.c_float), ("eps", C.c_float)])
+
+
+class mebptt_delta_inputs(C.Structure):
+    _fields_ = [(n, mebptt_seq) for n in ("q", "k", "v", "a", "b")] + [(n, C.c_void_p) for n in ("A", "a_bias", "lengths", "h0")]
+
+
+class mebptt_delta_grads(C.Structure):
+    _fields_ = [(n, mebptt_seq) for n in ("dq", "dk", "dv", "db", "da")] + [(n, C.c_void_p) for n in ("dA", "da_bias", "dh0")]
+
+
+class mebptt_join_desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("group", C.c_int32), ("x_dtype", C.c_int32), ("residual_dtype", C.c_int32),
+                ("scale", C.c_float), ("eps", C.c_float)]
+
+
+ADAMW_NO_DECAY = 1
+
+
+class mebptt_adamw_tensor(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [("n", C.c_int64)]
+                + [(n, C.c_int32) for n in ("grad_dtype", "state_dtype", "flags", "reserved")])
+
+
+class mebptt_adamw_desc(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("rate", "beta1", "beta2", "eps", "decay")] + [("seed", C.c_uint32), ("step", C.c_int64)]
+
+
 # name -> (restype, argtypes): every symbol the header declares
 _P = C.c_void_p
 _DESC = C.POINTER(mebptt_lstm_desc)
@@ -190,6 +220,25 @@ SIGNATURES = {
                                        C.POINTER(mebptt_scan_grads), _P, C.c_size_t, _P]),
     "mebptt_scan_step": (C.c_int, [C.POINTER(mebptt_scan_desc), C.POINTER(mebptt_scan_inputs), _P, C.c_int64, _P, mebptt_seq, _P,
                                    _P]),
+    "mebptt_delta_state_bytes": (C.c_size_t, [C.POINTER(mebptt_delta_desc)]),
+    "mebptt_delta_workspace_bytes": (C.c_size_t, [C.POINTER(mebptt_delta_desc), C.c_int32]),
+    "mebptt_delta_forward": (C.c_int, [C.POINTER(mebptt_delta_desc), C.POINTER(mebptt_delta_inputs), mebptt_seq, _P, _P, C.c_size_t,
+                                       _P, C.c_size_t, _P]),
+    "mebptt_delta_backward": (C.c_int, [C.POINTER(mebptt_delta_desc), C.POINTER(mebptt_delta_inputs), mebptt_seq, _P, _P, C.c_size_t,
+                                        C.POINTER(mebptt_delta_grads), _P, C.c_size_t, _P]),
+    "mebptt_delta_step": (C.c_int, [C.POINTER(mebptt_delta_desc), C.POINTER(mebptt_delta_inputs), _P, C.c_int64, _P, mebptt_seq, _P,
+                                    _P]),
+    "mebptt_join_forward": (C.c_int, [C.POINTER(mebptt_join_desc), _P, C.c_int64, _P, C.c_int64, _P, _P, C.c_int64, _P, _P, C.c_int64, _P,
+                                      C.c_int64, _P, _P, _P]),
+    "mebptt_join_workspace_bytes": (C.c_size_t, [C.POINTER(mebptt_join_desc)]),
+    "mebptt_join_backward": (C.c_int, [C.POINTER(mebptt_join_desc), _P, C.c_int64, _P, C.c_int64, _P, _P, C.c_int64, _P, _P, _P, _P, C.c_int64,
+                                       _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, _P, C.c_int64, _P, _P, C.c_size_t, _P]),
+    "mebptt_adamw_table_bytes": (C.c_size_t, [C.POINTER(mebptt_adamw_tensor), C.c_int32]),
+    "mebptt_adamw_prepare": (C.c_int, [C.POINTER(mebptt_adamw_tensor), C.c_int32, _P, C.c_size_t, _P]),
+    "mebptt_adamw_workspace_bytes": (C.c_size_t, [C.POINTER(mebptt_adamw_tensor), C.c_int32]),
+    "mebptt_adamw_norm": (C.c_int, [C.POINTER(mebptt_adamw_tensor), C.c_int32, _P, C.c_size_t, C.c_float, _P, _P, C.c_size_t, _P]),
+    "mebptt_adamw_step": (C.c_int, [C.POINTER(mebptt_adamw_desc), C.POINTER(mebptt_adamw_tensor), C.c_int32, _P, C.c_size_t, _P, _P, _P, _P]),
+    "mebptt_adamw_unpack": (C.c_int, [_P, _P, C.c_int64, C.c_int32, _P, C.c_int32, _P]),
     "mebptt_null_launch_us": (C.c_int, [C.c_int32, _P, C.POINTER(C.c_double)]),
     "mebptt_measure_sync": (C.c_int, [C.c_int32, C.c_int32, _P, C.POINTER(C.c_double), C.POINTER(C.c_int32)]),
     "mebptt_chunk_steps": (C.c_int32, [_DESC]),
@@ -839,3 +888,179 @@ def mebptt_scan_step(desc: mebptt_scan_desc, u, delta, A, Bm, Cm, skip, z, delta
     pin, slots, pout = _pool(state_in, state_out, (D, N), f32, dev, True)
     _call(dev, stream, lib().mebptt_scan_step, C.byref(desc), C.byref(given), pin, slots, _maybe(index, "index", (B,), _torch.int32, dev),
           _token(y, "y", B, D, T, dev), pout)
+
+
+# ---- a block with a matrix for a state, and the step that trains it ----------------------------------
+
+
+def make_delta_desc(t: int, B: int, Hk: int, H: int, dk: int, dv: int, dtype: int, activate: int = 1, normalise: int = 1, stretch: int = 256,
+                    scale: float = 1.0, eps: float = 1e-6) -> mebptt_delta_desc:
+    return mebptt_delta_desc(t, B, Hk, H, dk, dv, dtype, activate, normalise, stretch, scale, eps)
+
+
+def mebptt_delta_state_bytes(desc: mebptt_delta_desc) -> int:
+    return lib().mebptt_delta_state_bytes(C.byref(desc))
+
+
+def mebptt_delta_workspace_bytes(desc: mebptt_delta_desc, backward: bool) -> int:
+    return lib().mebptt_delta_workspace_bytes(C.byref(desc), 1 if backward else 0)
+
+
+def _delta_inputs(desc, q, k, v, a, b, A, a_bias, lengths, h0, T, dev: int) -> mebptt_delta_inputs:
+    f32, t, B, H = _DTYPES[0], desc.t, desc.B, desc.H
+    return mebptt_delta_inputs(_seq(q, "q", t, B, desc.Hk * desc.dk, T, dev), _seq(k, "k", t, B, desc.Hk * desc.dk, T, dev),
+                               _seq(v, "v", t, B, H * desc.dv, T, dev), _maybe_seq(a, "a", t, B, H, T, dev), _seq(b, "b", t, B, H, T, dev),
+                               _maybe(A, "A", (H,), f32, dev), _maybe(a_bias, "a_bias", (H,), f32, dev),
+                               _maybe(lengths, "lengths", (B,), _torch.int32, dev), _maybe(h0, "h0", (B, H, desc.dk, desc.dv), f32, dev))
+
+
+def mebptt_delta_forward(desc: mebptt_delta_desc, q, k, v, a, b, A, a_bias, lengths, h0, y, h_out=None, states=None, workspace=None,
+                         stream: Optional[int] = None) -> None:
+    """Gated delta rule.  q, k [t, B, Hk dk]; v, y [t, B, H dv]; a (None: no decay), b [t, B, H]; A, a_bias [H]; h0, h_out [B, H, dk, dv];
+    `states` (uint8) keeps what a backward call needs."""
+    dev, T = _gpu(q), _dtype(desc.dtype)
+    given = _delta_inputs(desc, q, k, v, a, b, A, a_bias, lengths, h0, T, dev)
+    _call(dev, stream, lib().mebptt_delta_forward, C.byref(desc), C.byref(given), _seq(y, "y", desc.t, desc.B, desc.H * desc.dv, T, dev),
+          _maybe(h_out, "h_out", (desc.B, desc.H, desc.dk, desc.dv), _DTYPES[0], dev), *_room(states, "states", dev),
+          *_room(workspace, "workspace", dev))
+
+
+def mebptt_delta_backward(desc: mebptt_delta_desc, q, k, v, a, b, A, a_bias, lengths, h0, dy, dh_out, states, dq, dk, dv, da, db, dA, da_bias,
+                          dh0, workspace, stream: Optional[int] = None) -> None:
+    """Gradients of mebptt_delta_forward from the states that it kept; da where there is an a."""
+    dev, T = _gpu(q), _dtype(desc.dtype)
+    f32, t, B, H, state = _DTYPES[0], desc.t, desc.B, desc.H, (desc.B, desc.H, desc.dk, desc.dv)
+    given = _delta_inputs(desc, q, k, v, a, b, A, a_bias, lengths, h0, T, dev)
+    grads = mebptt_delta_grads(_seq(dq, "dq", t, B, desc.Hk * desc.dk, T, dev), _seq(dk, "dk", t, B, desc.Hk * desc.dk, T, dev),
+                               _seq(dv, "dv", t, B, H * desc.dv, T, dev), _seq(db, "db", t, B, H, T, dev),
+                               (_maybe_seq if a is None else _seq)(da, "da", t, B, H, T, dev), _maybe(dA, "dA", (H,), f32, dev),
+                               _maybe(da_bias, "da_bias", (H,), f32, dev), _maybe(dh0, "dh0", state, f32, dev))
+    _call(dev, stream, lib().mebptt_delta_backward, C.byref(desc), C.byref(given), _seq(dy, "dy", t, B, H * desc.dv, T, dev),
+          _maybe(dh_out, "dh_out", state, f32, dev), *_room(states, "states", dev), C.byref(grads), *_room(workspace, "workspace", dev))
+
+
+def mebptt_delta_step(desc: mebptt_delta_desc, q, k, v, a, b, A, a_bias, state_in, index, y, state_out, stream: Optional[int] = None) -> None:
+    """One token: q, k [B, Hk dk]; v, y [B, H dv]; a, b [B, H]; state_in, state_out [slots, H, dk, dv] float32 (one tensor or two); index as
+    in mebptt_conv_step."""
+    dev, T = _gpu(q), _dtype(desc.dtype)
+    f32, B, H, dk, dv = _DTYPES[0], desc.B, desc.H, desc.dk, desc.dv
+    given = mebptt_delta_inputs(_token(q, "q", B, desc.Hk * dk, T, dev), _token(k, "k", B, desc.Hk * dk, T, dev), _token(v, "v", B, H * dv, T, dev),
+                                mebptt_seq(None, 0, 0) if a is None else _token(a, "a", B, H, T, dev), _token(b, "b", B, H, T, dev),
+                                _maybe(A, "A", (H,), f32, dev), _maybe(a_bias, "a_bias", (H,), f32, dev), None, None)
+    pin, slots, pout = _pool(state_in, state_out, (H, dk, dv), f32, dev, True)
+    _call(dev, stream, lib().mebptt_delta_step, C.byref(desc), C.byref(given), pin, slots, _maybe(index, "index", (B,), _torch.int32, dev),
+          _token(y, "y", B, H * dv, T, dev), pout)
+
+
+def make_join_desc(rows: int, width: int, group: int, x_dtype: int, residual_dtype: int = FP32, scale: float = 1.0,
+                   eps: float = 1e-5) -> mebptt_join_desc:
+    return mebptt_join_desc(rows, width, group, x_dtype, residual_dtype, scale, eps)
+
+
+def mebptt_join_workspace_bytes(desc: mebptt_join_desc) -> int:
+    return lib().mebptt_join_workspace_bytes(C.byref(desc))
+
+
+def mebptt_join_forward(desc: mebptt_join_desc, x, z, weight, residual, weight_next, y, residual_out=None, rstd=None, rstd_next=None,
+                        stream: Optional[int] = None) -> None:
+    """branch = norm of x per group times `weight` times silu(z); without a residual y = branch, with one r = scale residual + branch goes to
+    residual_out and y = norm(r) times weight_next.  rstd [rows, width / group] and rstd_next [rows] are for the backward call."""
+    dev, M, W = _gpu(x), desc.rows, desc.width
+    f32, xt, rt = _DTYPES[0], _dtype(desc.x_dtype), _dtype(desc.residual_dtype)
+    _call(dev, stream, lib().mebptt_join_forward, C.byref(desc), *_rows(x, "x", M, W, xt, dev), *_maybe_rows(z, "z", M, W, xt, dev),
+          _maybe(weight, "weight", (W,), f32, dev), *_maybe_rows(residual, "residual", M, W, rt, dev),
+          _maybe(weight_next, "weight_next", (W,), f32, dev), *_rows(y, "y", M, W, xt, dev), *_maybe_rows(residual_out, "residual_out", M, W, rt, dev),
+          _maybe(rstd, "rstd", (M, W // max(desc.group, 1)), f32, dev), _maybe(rstd_next, "rstd_next", (M,), f32, dev))
+
+
+def mebptt_join_backward(desc: mebptt_join_desc, x, z, weight, r, weight_next, rstd, rstd_next, dy, dresidual_out, dx, dz, dweight, dresidual,
+                         dweight_next, workspace, stream: Optional[int] = None) -> None:
+    """Gradients of mebptt_join_forward; r is its residual_out (None: there was no residual)."""
+    dev, M, W = _gpu(x), desc.rows, desc.width
+    f32, xt, rt = _DTYPES[0], _dtype(desc.x_dtype), _dtype(desc.residual_dtype)
+    _call(dev, stream, lib().mebptt_join_backward, C.byref(desc), *_rows(x, "x", M, W, xt, dev), *_maybe_rows(z, "z", M, W, xt, dev),
+          _maybe(weight, "weight", (W,), f32, dev), *_maybe_rows(r, "r", M, W, rt, dev), _maybe(weight_next, "weight_next", (W,), f32, dev),
+          _whole(rstd, "rstd", (M, W // max(desc.group, 1)), f32, dev), _maybe(rstd_next, "rstd_next", (M,), f32, dev),
+          *_rows(dy, "dy", M, W, xt, dev), *_maybe_rows(dresidual_out, "dresidual_out", M, W, rt, dev), *_rows(dx, "dx", M, W, xt, dev),
+          *_maybe_rows(dz, "dz", M, W, xt, dev), _maybe(dweight, "dweight", (W,), f32, dev), *_maybe_rows(dresidual, "dresidual", M, W, rt, dev),
+          _maybe(dweight_next, "dweight_next", (W,), f32, dev), *_room(workspace, "workspace", dev))
+
+
+class AdamwTensors:
+    """What mebptt_adamw_* take of a list of tensors; keeps them alive."""
+
+    def __init__(self, array, device: int, kept):
+        self.array, self.count, self.device, self.kept = array, len(kept), device, kept
+
+
+def make_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, no_decay=None) -> AdamwTensors:
+    """Lists of one length: params float32; grads float32 or bfloat16; m and v float32, or uint8 with scales of ceil(n / 256) float32 each; copies
+    (entries may be None) bfloat16; no_decay: truth values.  All contiguous and on one GPU."""
+    params = list(params)
+    if not params:
+        raise ValueError("at least one tensor is needed")
+    dev, n = _gpu(params[0]), len(params)
+    f32, bf16, byte = _DTYPES[0], _DTYPES[1], _torch.uint8
+    lists = {"grads": grads, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "copies": copies, "no_decay": no_decay}
+    lists = {k: [None] * n if x is None else list(x) for k, x in lists.items()}
+    for k, x in lists.items():
+        if len(x) != n:
+            raise ValueError(f"{k} has {len(x)} entries, {n} are needed")
+    array, kept = (mebptt_adamw_tensor * n)(), []
+    for i, p in enumerate(params):
+        g, mi, vi, ms, vs, c, flag = (lists[k][i] for k in ("grads", "m", "v", "m_scale", "v_scale", "copies", "no_decay"))
+        shape, blocks = None if p is None else p.shape, 0 if p is None else (-(-p.numel() // 256),)
+        small = mi is not None and mi.dtype is byte
+        st = byte if small else f32
+        wide = g is None or g.dtype is not bf16
+        array[i] = mebptt_adamw_tensor(
+            _whole(p, f"params[{i}]", shape, f32, dev), _whole(g, f"grads[{i}]", shape, f32 if wide else bf16, dev),
+            _whole(mi, f"m[{i}]", shape, st, dev), _whole(vi, f"v[{i}]", shape, st, dev), _whole(ms, f"m_scale[{i}]", blocks, f32, dev) if small else None,
+            _whole(vs, f"v_scale[{i}]", blocks, f32, dev) if small else None, _maybe(c, f"copies[{i}]", shape, bf16, dev), p.numel(),
+            FP32 if wide else BF16, INT8 if small else FP32, ADAMW_NO_DECAY if flag else 0, 0)
+        kept.append((p, g, mi, vi, ms, vs, c))
+    return AdamwTensors(array, dev, kept)
+
+
+def make_adamw_desc(rate: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, decay: float = 0.01, step: int = 1,
+                    seed: int = 0) -> mebptt_adamw_desc:
+    return mebptt_adamw_desc(rate, beta1, beta2, eps, decay, seed & 0xFFFFFFFF, step)
+
+
+def mebptt_adamw_table_bytes(tensors: AdamwTensors) -> int:
+    return lib().mebptt_adamw_table_bytes(tensors.array, tensors.count)
+
+
+def mebptt_adamw_workspace_bytes(tensors: AdamwTensors) -> int:
+    return lib().mebptt_adamw_workspace_bytes(tensors.array, tensors.count)
+
+
+def mebptt_adamw_prepare(tensors: AdamwTensors, table, stream: Optional[int] = None) -> None:
+    """Writes what the other calls need to know of the tensors into `table` (uint8)."""
+    _call(tensors.device, stream, lib().mebptt_adamw_prepare, tensors.array, tensors.count, *_room(table, "table", tensors.device))
+
+
+def mebptt_adamw_norm(tensors: AdamwTensors, table, max_norm: float, out, workspace, stream: Optional[int] = None) -> None:
+    """out [2] float32: the norm of all gradients, and the factor that limits it to max_norm."""
+    dev = tensors.device
+    _call(dev, stream, lib().mebptt_adamw_norm, tensors.array, tensors.count, *_room(table, "table", dev), max_norm,
+          _whole(out, "out", (2,), _DTYPES[0], dev), *_room(workspace, "workspace", dev))
+
+
+def mebptt_adamw_step(desc: mebptt_adamw_desc, tensors: AdamwTensors, table, factor=None, rate=None, step=None,
+                      stream: Optional[int] = None) -> None:
+    """One step over all tensors.  factor, rate ([1] float32) and step ([1] int64) are read on the GPU when the step runs."""
+    dev = tensors.device
+    _call(dev, stream, lib().mebptt_adamw_step, C.byref(desc), tensors.array, tensors.count, *_room(table, "table", dev),
+          _maybe(factor, "factor", (1,), _DTYPES[0], dev), _maybe(rate, "rate", (1,), _DTYPES[0], dev),
+          _maybe(step, "step", (1,), _torch.int64, dev))
+
+
+def mebptt_adamw_unpack(codes, scale, is_signed: bool, out, stream: Optional[int] = None) -> None:
+    """The values that one tensor's 8-bit states stand for (`is_signed`: those of m), to float32 or bfloat16."""
+    dev = _gpu(codes)
+    n = codes.numel()
+    wide = out is None or out.dtype is not _DTYPES[1]
+    _call(dev, stream, lib().mebptt_adamw_unpack, _whole(codes, "codes", codes.shape, _torch.uint8, dev),
+          _whole(scale, "scale", (-(-n // 256),), _DTYPES[0], dev), n, 1 if is_signed else 0,
+          _whole(out, "out", codes.shape, _DTYPES[0] if wide else _DTYPES[1], dev), FP32 if wide else BF16)

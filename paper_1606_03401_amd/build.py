@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libmebptt.so")
 SOURCES = ["resident_wide_2.hip", "resident_wide_1.hip", "resident_wide_3.hip", "resident_sweep_bf16.hip", "resident_sweep_fp32.hip", "resident_chain_bf16_k4.hip",
            "resident_chain_bf16_k8.hip", "resident_chain_fp32_k8.hip", "resident_back_bf16.hip",
            "resident_chain_fp32_k4.hip", "kernels.hip", "run.hip", "resident.hip", "chain_run.hip", "measure_sync.hip",
-           "norm.hip", "int8.hip", "conv.hip", "scan.hip", "planner.cpp", "chain_planner.cpp"]
+           "norm.hip", "int8.hip", "conv.hip", "scan.hip", "delta.hip", "delta_prepare.hip", "delta_walk.hip", "delta_gradients.hip", "join.hip", "adamw.hip", "planner.cpp", "chain_planner.cpp"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wall", "-Wno-unused-command-line-argument", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 

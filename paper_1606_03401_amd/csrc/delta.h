@@ -1,0 +1,267 @@
+// What the kernels of the gated delta rule share: the recurrence cut into chunks, matrix products out of registers and LDS, what a chunk's
+// preparation leaves for the kernels that walk over chunks.  Not part of the ABI.
+//
+// Per sequence and head, with a state S [dk, dv], k^ = k / |k| and q~ = scale q / |q| (or k and scale q as they are), alpha = exp(g):
+//     r_s = v_s - alpha_s S_{s-1}^T k^_s,   S_s = alpha_s S_{s-1} + beta_s k^_s r_s^T,   y_s = S_s^T q~_s.
+// Over a chunk of 64 steps, with G the running sum of g, gamma = exp(G), D_ij = exp(G_i - G_j) (j <= i), M = K^ K^^T o D below the diagonal,
+// P = Q~ K^^T o D up to it:
+//     R = T (V - gamma K^ S),  T = (I + M beta)^-1,   Y = gamma Q~ S + P beta R,   S' = gamma_C S + (gamma_C / gamma K^)^T beta R.
+// T and P do not depend on the state: one launch prepares them for all chunks at once, another walks over the chunks with the state in
+// registers.  Backward, with dS' the gradient of the state behind the chunk:
+//     dU = P^T dY + (gamma_C / gamma K^) dS',   Z = T^T beta dU = dV,   dS = gamma_C dS' + (gamma Q~)^T dY - (gamma K^)^T Z,
+// and the other gradients from q, k, dY, R, Z, S and dS' of the chunk alone.
+#pragma once
+
+#include <type_traits>
+
+#include "ops.h"
+
+namespace mebptt {
+namespace delta {
+
+using namespace mebptt::ops;
+
+constexpr int C = 64;            // steps of a chunk
+constexpr int MAX_DK = 128, MAX_DV = 256, MAX_HEADS = 1024;
+
+// ---- products ----------------------------------------------------------------------------------------
+//
+// An operand of one instruction's worth: 16 rows (or columns) by 32 of what is summed over.  Lane l holds row l % 16 and, with g = l / 16, the eight
+// values 4 g .. 4 g + 3 and 16 + 4 g .. of the 32.  A result tile has column l % 16 and rows 4 g .. 4 g + 3 in lane l, so two tiles above each
+// other are an operand of the next product as they stand: what a wave computes in a column never leaves its registers.
+//
+// bf16 inputs go to the bf16 matrix instruction as they are; what has 32 bits is cut into N parts of 8 significant bits each, h = bf16(x), m =
+// bf16(x - h), l = bf16(x - h - m): with three of them 24 bits arrive, with two 16 (errors of about 2^-18).  fp32 inputs go to the fp32 instruction.
+template <typename T, int N>
+struct Op;
+template <int N>
+struct Op<__bf16, N> {
+  bf16x8 p[N];
+};
+template <int N>
+struct Op<float, N> {
+  f32x4 v[2];
+};
+
+template <typename T, int N>
+__device__ inline Op<T, N> cut(f32x4 a, f32x4 b) {
+  Op<T, N> o;
+  if constexpr (std::is_same<T, float>::value) {
+    o.v[0] = a;
+    o.v[1] = b;
+  } else {
+    float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        o.p[n][e] = (__bf16)x[e];
+        if (n + 1 < N) x[e] -= (float)o.p[n][e];
+      }
+  }
+  return o;
+}
+
+// The operand whose row `row` (of this lane) stands at p, 32 values from p on.
+__device__ inline Op<__bf16, 1> from_row(const __bf16* p, int g) {
+  const bf16x4 a = *reinterpret_cast<const bf16x4*>(p + 4 * g), b = *reinterpret_cast<const bf16x4*>(p + 16 + 4 * g);
+  Op<__bf16, 1> o;
+  o.p[0] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  return o;
+}
+__device__ inline Op<float, 1> from_row(const float* p, int g) {
+  Op<float, 1> o;
+  o.v[0] = *reinterpret_cast<const f32x4*>(p + 4 * g);
+  o.v[1] = *reinterpret_cast<const f32x4*>(p + 16 + 4 * g);
+  return o;
+}
+
+// c += a b; of the products of parts those that matter.
+template <int NA, int NB>
+__device__ inline void mma(f32x4& c, const Op<__bf16, NA>& a, const Op<__bf16, NB>& b) {
+  constexpr int MOST = NA > NB ? NA : NB;
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (i + j < MOST) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c, 0, 0, 0);
+}
+template <int NA, int NB>
+__device__ inline void mma(f32x4& c, const Op<float, NA>& a, const Op<float, NB>& b) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[h][e], b.v[h][e], c, 0, 0, 0);
+}
+
+// ---- a chunk's rows in LDS -----------------------------------------------------------------------------
+
+// [C][KD] values of T as rows; bf16 also as columns, [KD][C], which products that sum over steps read (fp32 operands are
+// single values there and are picked out of the rows).  Rows are padded so that 16 of them begin in different banks.
+template <typename T>
+struct Lds;
+template <>
+struct Lds<__bf16> {
+  static constexpr int PAD = 8;
+  static constexpr int ld(int KD) { return KD + PAD; }
+  static constexpr int row_bytes(int KD) { return C * ld(KD) * 2; }
+  static constexpr int column_bytes(int KD) { return KD * (C + PAD) * 2; }
+};
+template <>
+struct Lds<float> {
+  static constexpr int PAD = 4;
+  static constexpr int ld(int KD) { return KD + PAD; }
+  static constexpr int row_bytes(int KD) { return C * ld(KD) * 4; }
+  static constexpr int column_bytes(int) { return 0; }
+};
+// The operand with column `col` (of this lane) and steps s0 .. s0 + 31: from the columns, or picked out of the rows.
+template <int KD>
+__device__ inline Op<__bf16, 1> from_column(const __bf16*, const __bf16* columns, int col, int s0, int g) {
+  return from_row(columns + col * (C + Lds<__bf16>::PAD) + s0, g);
+}
+template <int KD>
+__device__ inline Op<float, 1> from_column(const float* rows, const float*, int col, int s0, int g) {
+  Op<float, 1> o;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o.v[h][e] = rows[(s0 + 16 * h + 4 * g + e) * Lds<float>::ld(KD) + col];
+  return o;
+}
+
+// Four steps' values of one vector's width, on their way from memory to LDS.
+template <typename T>
+struct Piece {
+  static constexpr int E = 16 / sizeof(T);
+  typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(16)));
+  Vec v[4];
+};
+// Piece u of [C][KD] (u % (KD / E): which vector, u / (KD / E): which four steps).  Steps from `live` on and columns from `width` on are zeros.  `p`: the
+// chunk's first row; rows `stride` apart.
+template <typename T, int KD>
+__device__ inline void load_piece(Piece<T>& x, const T* p, int64_t stride, int width, int live, bool vec, int u) {
+  constexpr int E = Piece<T>::E, COLS = KD / E;
+  const int c = u % COLS * E, s = u / COLS * 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x.v[i] = {};
+    if (s + i < live) {
+      const T* row = p + (int64_t)(s + i) * stride;
+      if (vec) {
+        if (c < width) x.v[i] = *reinterpret_cast<const typename Piece<T>::Vec*>(row + c);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (c + e < width) x.v[i][e] = row[c + e];
+      }
+    }
+  }
+}
+template <typename T, int KD>
+__device__ inline void put_rows(const Piece<T>& x, T* rows, int u) {
+  constexpr int E = Piece<T>::E, COLS = KD / E;
+  const int c = u % COLS * E, s = u / COLS * 4;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<typename Piece<T>::Vec*>(rows + (s + i) * Lds<T>::ld(KD) + c) = x.v[i];
+}
+template <typename T, int KD>
+__device__ inline void put_columns(const Piece<T>& x, T* columns, int u) {
+  if constexpr (sizeof(T) == 2) {
+    constexpr int E = Piece<T>::E, COLS = KD / E;
+    const int c = u % COLS * E, s = u / COLS * 4;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const bf16x4 t = {x.v[0][e], x.v[1][e], x.v[2][e], x.v[3][e]};
+      *reinterpret_cast<bf16x4*>(columns + (c + e) * (C + Lds<T>::PAD) + s) = t;
+    }
+  }
+}
+template <typename T>
+constexpr int pieces(int KD) { return C / 4 * (KD / Piece<T>::E); }
+
+// ---- what a chunk's preparation leaves ---------------------------------------------------------------
+
+// Per step, in rows of C floats.
+enum { GA = 0, BE = 1, LA = 2, SK = 3, SQ = 4, RQ = 5, GATES = 6 };   // gamma, beta, gamma_C / gamma, 1 / |k|, scale / |q|, 1 / |q|
+
+// Matrices [C][C] as operands in the order in which lanes read them.  A lower triangle has six pieces of 16 rows by 32 columns: (0,0) (1,0)
+// (2,0) (2,1) (3,0) (3,1); its transpose (0,0) (0,1) (1,0) (1,1) (2,1) (3,1).
+constexpr int FRAGS = 6;
+__device__ inline constexpr int lower(int rt, int pb) { return rt < 2 ? rt : 2 + (rt - 2) * 2 + pb; }
+__device__ inline constexpr int upper(int rt, int pb) { return rt < 2 ? rt * 2 + pb : 4 + rt - 2; }
+// KiB per piece: parts of bf16, or two halves of fp32.
+template <typename T>
+constexpr int units(int parts) { return sizeof(T) == 2 ? parts : 2; }
+template <typename T>
+constexpr int frag_bytes(int parts) { return FRAGS * units<T>(parts) * 1024; }
+template <typename T, int N>
+__device__ inline Op<T, N> from_frag(const char* at, int f, int lane) {
+  Op<T, N> o;
+  const char* p = at + f * units<T>(N) * 1024 + lane * 16;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) o.p[n] = *reinterpret_cast<const bf16x8*>(p + n * 1024);
+  } else {
+    o.v[0] = *reinterpret_cast<const f32x4*>(p);
+    o.v[1] = *reinterpret_cast<const f32x4*>(p + 1024);
+  }
+  return o;
+}
+
+constexpr int T_PARTS = 3, P_PARTS = 2, PT_PARTS = 3;   // P reaches y only, which is rounded to bf16
+// A chunk's record: forward [T | P | gates | G], backward [T | T^T | P^T | gates | G], G in 64 bits.
+template <typename T, bool BACK>
+struct Record {
+  static constexpr int T_ = 0;
+  static constexpr int TT = frag_bytes<T>(T_PARTS);
+  static constexpr int P = BACK ? TT + frag_bytes<T>(T_PARTS) : TT;     // P, or its transpose
+  static constexpr int GATE = P + frag_bytes<T>(BACK ? PT_PARTS : P_PARTS);
+  static constexpr int SUMS = GATE + GATES * C * 4;
+  static constexpr int BYTES = SUMS + C * 8;
+};
+inline size_t record_bytes(int dtype, bool back) {
+  if (dtype == MEBPTT_FP32) return back ? Record<float, true>::BYTES : Record<float, false>::BYTES;
+  return back ? Record<__bf16, true>::BYTES : Record<__bf16, false>::BYTES;
+}
+
+// ---- arguments -----------------------------------------------------------------------------------------
+
+struct Args {
+  mebptt_seq q, k, v, a, b, y;
+  const float *A, *bias;
+  const int32_t* lengths;
+  int t, B, Hk, H, dk, dv, dvp;        // dvp: dv rounded up to 16
+  int activate, normalise;
+  float scale, eps;
+  int vec;                              // rows of q and k are whole 16-byte vectors at 16-byte boundaries
+  int c0, c1;                           // chunks of this launch
+  char* records;                        // [c1 - c0][B H]
+  const float* from;                    // states [B][H][dk][dv] before the first chunk, or NULL
+  float* to;                            // after the last one, or NULL
+  float* states;                        // kept states, or NULL
+  int keep;                             // every keep-th chunk's
+  float *S, *R, *Z, *dS;                // of every chunk of the launch: [KD][dvp] and [C][dvp]
+  mebptt_seq dy, dq, dkey, dval, da, db;
+  float* parts;                         // [c1 - c0][B][2 H]: sums of dg softplus and da
+};
+
+__device__ inline int ends_at(const Args& p, int b) { return p.lengths ? min(max(p.lengths[b], 0), p.t) : p.t; }
+
+int prepare(const Args& p, int dtype, bool back, hipStream_t stream);
+int walk(const Args& p, int dtype, bool again, hipStream_t stream);        // `again`: S and R of every chunk instead of y
+int walk_back(const Args& p, int dtype, hipStream_t stream);
+int gradients(const Args& p, int dtype, hipStream_t stream);
+
+inline int padded(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
+template <typename F>
+int with_size(int dtype, int dk, F&& f) {
+  auto at = [&](auto t) {
+    if (dk <= 32) return f(t, std::integral_constant<int, 32>{});
+    if (dk <= 64) return f(t, std::integral_constant<int, 64>{});
+    return f(t, std::integral_constant<int, 128>{});
+  };
+  return dtype == MEBPTT_FP32 ? at(float{}) : at(__bf16{});
+}
+
+}  // namespace delta
+}  // namespace mebptt

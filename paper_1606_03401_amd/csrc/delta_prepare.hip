@@ -1,0 +1,231 @@
+// Gated delta rule: what a chunk's steps need of each other, T = (I + M beta)^-1 and P, for all chunks of a launch at once, and the
+// factors of its steps.  One workgroup of four waves per chunk, sequence and head.
+#include "delta.h"
+#include "dynamic_lds.h"
+
+using namespace mebptt;
+using namespace mebptt::delta;
+
+namespace {
+
+constexpr int LM = C + 4;        // floats between rows of the 64 x 64 matrices
+constexpr float LEAST = -1e4f;   // exp of it is zero; sums of it stay far from infinity
+
+template <typename T, int KD>
+constexpr int lds_bytes() { return 2 * Lds<T>::row_bytes(KD) + 2 * C * LM * 4 + GATES * C * 4 + C * 8; }
+
+// c += a b of one 16 x 16 x 16 in fp32: a as rows in LDS, b as a result tile.
+__device__ inline void mma16(f32x4& c, const float* a, f32x4 b, int lane) {
+  const f32x4 x = *reinterpret_cast<const f32x4*>(a + (lane % 16) * LM + lane / 16 * 4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], b[e], c, 0, 0, 0);
+}
+__device__ inline f32x4 tile(const float* a, int lane) {
+  f32x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = a[(lane / 16 * 4 + e) * LM + lane % 16];
+  return v;
+}
+__device__ inline void put_tile(float* a, f32x4 v, int lane) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) a[(lane / 16 * 4 + e) * LM + lane % 16] = v[e];
+}
+
+// The pieces of a triangle, or of its transpose, in the order of the operands.
+template <typename T, int PARTS, bool TRANSPOSED>
+__device__ inline void put_frags(char* out, const float* m) {
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16;
+  for (int f = wave; f < FRAGS; f += 4) {
+    const int rt = TRANSPOSED ? (f < 4 ? f / 2 : f - 2) : (f < 2 ? f : f / 2 + 1);
+    const int pb = TRANSPOSED ? (f < 4 ? f % 2 : 1) : (f < 2 ? 0 : f % 2);
+    const int row = 16 * rt + lane % 16, col = 32 * pb + 4 * g;
+    f32x4 x, y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = TRANSPOSED ? m[(col + e) * LM + row] : m[row * LM + col + e];
+      y[e] = TRANSPOSED ? m[(col + 16 + e) * LM + row] : m[row * LM + col + 16 + e];
+    }
+    const Op<T, PARTS> o = cut<T, PARTS>(x, y);
+    char* p = out + f * units<T>(PARTS) * 1024 + lane * 16;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int n = 0; n < PARTS; ++n) *reinterpret_cast<bf16x8*>(p + n * 1024) = o.p[n];
+    } else {
+      *reinterpret_cast<f32x4*>(p) = o.v[0];
+      *reinterpret_cast<f32x4*>(p + 1024) = o.v[1];
+    }
+  }
+}
+
+template <typename T, int KD, bool BACK>
+__global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
+  extern __shared__ __align__(16) char lds[];
+  T* K = reinterpret_cast<T*>(lds);
+  T* Q = reinterpret_cast<T*>(lds + Lds<T>::row_bytes(KD));
+  float* M = reinterpret_cast<float*>(lds + 2 * Lds<T>::row_bytes(KD));
+  float* P = M + C * LM;
+  double* G = reinterpret_cast<double*>(P + C * LM);
+  float* gate = reinterpret_cast<float*>(G + C);
+  constexpr int LD = Lds<T>::ld(KD);
+  const int BH = p.B * p.H, chunk = p.c0 + blockIdx.x / BH, bh = blockIdx.x % BH, b = bh / p.H, h = bh % p.H, hk = h / (p.H / p.Hk);
+  const int s0 = chunk * C, live = min(ends_at(p, b) - s0, C);
+  if (live <= 0) return;   // (nobody reads the record)
+  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16;
+  using R = Record<T, BACK>;
+  char* out = p.records + (int64_t)blockIdx.x * R::BYTES;
+
+  const T* kp = (const T*)p.k.data + s0 * p.k.stride_t + b * p.k.stride_b + hk * p.dk;
+  const T* qp = (const T*)p.q.data + s0 * p.q.stride_t + b * p.q.stride_b + hk * p.dk;
+  for (int u = threadIdx.x; u < pieces<T>(KD); u += 256) {
+    Piece<T> x, y;
+    load_piece<T, KD>(x, kp, p.k.stride_t, p.dk, live, p.vec, u);
+    load_piece<T, KD>(y, qp, p.q.stride_t, p.dk, live, p.vec, u);
+    put_rows<T, KD>(x, K, u);
+    put_rows<T, KD>(y, Q, u);
+  }
+  if (wave == 0) {   // decays and betas of the steps
+    float lg = 0.0f, beta = 0.0f;
+    if (lane < live) {
+      const int64_t s = s0 + lane;
+      const float bv = (float)((const T*)p.b.data)[s * p.b.stride_t + b * p.b.stride_b + h];
+      beta = p.activate ? 1.0f / (1.0f + expf(-bv)) : bv;
+      if (p.a.data) {
+        lg = (float)((const T*)p.a.data)[s * p.a.stride_t + b * p.a.stride_b + h];
+        if (p.activate) {
+          lg += p.bias ? p.bias[h] : 0.0f;
+          lg = p.A[h] * (fmaxf(lg, 0.0f) + log1pf(expf(-fabsf(lg))));
+        }
+        // (a NaN stays one)
+        if (lg < LEAST) lg = LEAST;
+      }
+    }
+    // in 64 bits: after one step that forgets all, differences of the sums behind it would have few bits left in 32
+    double sum = lg;
+#pragma unroll
+    for (int m = 1; m < WAVE; m <<= 1) {
+      const double before = __shfl_up(sum, m);
+      if (lane >= m) sum += before;
+    }
+    G[lane] = sum;
+    gate[GA * C + lane] = expf((float)sum);
+    gate[BE * C + lane] = beta;
+    gate[LA * C + lane] = expf((float)(__shfl(sum, C - 1) - sum));
+  }
+  __syncthreads();
+  {   // lengths of k and q: four threads a row
+    const int row = threadIdx.x / 4, part = threadIdx.x % 4;
+    float kk = 0.0f, qq = 0.0f;
+    for (int c = part; c < KD; c += 4) {
+      const float x = (float)K[row * LD + c], y = (float)Q[row * LD + c];
+      kk += x * x;
+      qq += y * y;
+    }
+#pragma unroll
+    for (int m = 1; m < 4; m <<= 1) kk += __shfl_xor(kk, m), qq += __shfl_xor(qq, m);
+    if (part == 0) {
+      const float rq = p.normalise ? 1.0f / sqrtf(qq + p.eps) : 1.0f;
+      gate[SK * C + row] = p.normalise ? 1.0f / sqrtf(kk + p.eps) : 1.0f;
+      gate[SQ * C + row] = p.scale * rq;
+      gate[RQ * C + row] = rq;
+    }
+  }
+  __syncthreads();
+  // row tile `wave` of M beta and P; what stands above the diagonal is zero
+  for (int jt = 0; jt < 4; ++jt) {
+    f32x4 kk = {}, qk = {};
+    if (jt <= wave) {
+#pragma unroll
+      for (int c = 0; c < KD; c += 32) {
+        const auto kj = from_row(K + (16 * jt + lane % 16) * LD + c, g);
+        mma(kk, from_row(K + (16 * wave + lane % 16) * LD + c, g), kj);
+        mma(qk, from_row(Q + (16 * wave + lane % 16) * LD + c, g), kj);
+      }
+      const int j = 16 * jt + lane % 16;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 16 * wave + 4 * g + e;
+        const float d = j <= i ? expf((float)(G[i] - G[j])) * gate[SK * C + j] : 0.0f;
+        kk[e] = j < i ? kk[e] * d * gate[SK * C + i] * gate[BE * C + j] : 0.0f;
+        qk[e] = j <= i ? qk[e] * d * gate[SQ * C + i] : 0.0f;
+      }
+    }
+    put_tile(M + 16 * wave * LM + 16 * jt, kk, lane);
+    put_tile(P + 16 * wave * LM + 16 * jt, qk, lane);
+  }
+  __syncthreads();
+  // T over M.  Diagonal tiles by substitution, a column per lane; then from two diagonal blocks' inverses the block below: -T22 M21 T11.
+  {
+    float* m = M + 16 * wave * (LM + 1);
+    const int c = lane % 16;
+    float x[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float s = r == c ? 1.0f : 0.0f;
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (j < r) s -= m[r * LM + j] * x[j];
+      x[r] = s;
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (lane < 16) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) m[r * LM + c] = x[r];
+    }
+  }
+  __syncthreads();
+  if (wave < 2) {
+    float* m = M + 32 * wave * (LM + 1);
+    f32x4 w = {}, x = {};
+    mma16(w, m + 16 * LM, tile(m, lane), lane);
+    mma16(x, m + 16 * (LM + 1), w, lane);
+    __builtin_amdgcn_wave_barrier();
+    put_tile(m + 16 * LM, -x, lane);
+  }
+  __syncthreads();
+  f32x4 low[2] = {};
+  if (wave < 2) {   // column tile `wave` of the lower left 32 x 32
+    f32x4 w[2] = {};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) mma16(w[i], M + (32 + 16 * i) * LM + 16 * k, tile(M + 16 * k * LM + 16 * wave, lane), lane);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int k = 0; k <= i; ++k) mma16(low[i], M + (32 + 16 * i) * LM + 32 + 16 * k, w[k], lane);
+  }
+  __syncthreads();
+  if (wave < 2) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) put_tile(M + (32 + 16 * i) * LM + 16 * wave, -low[i], lane);
+  }
+  __syncthreads();
+  put_frags<T, T_PARTS, false>(out + R::T_, M);
+  if constexpr (BACK) {
+    put_frags<T, T_PARTS, true>(out + R::TT, M);
+    put_frags<T, PT_PARTS, true>(out + R::P, P);
+  } else {
+    put_frags<T, P_PARTS, false>(out + R::P, P);
+  }
+  for (int i = threadIdx.x; i < GATES * C; i += 256) reinterpret_cast<float*>(out + R::GATE)[i] = gate[i];
+  if (threadIdx.x < C) reinterpret_cast<double*>(out + R::SUMS)[threadIdx.x] = G[threadIdx.x];
+}
+
+template <typename T, int KD, bool BACK>
+int launch(const Args& p, hipStream_t stream) {
+  constexpr int BYTES = lds_bytes<T, KD>();
+  const hipError_t e = allow_dynamic_lds<delta_prepare_kernel<T, KD, BACK>>(BYTES);
+  if (e != hipSuccess) return set_error(MEBPTT_EHIP, "LDS of the delta rule: %s", hipGetErrorString(e));
+  delta_prepare_kernel<T, KD, BACK><<<(unsigned)((p.c1 - p.c0) * p.B * p.H), 256, BYTES, stream>>>(p);
+  return launched("delta rule, preparation");
+}
+
+}  // namespace
+
+int mebptt::delta::prepare(const Args& p, int dtype, bool back, hipStream_t stream) {
+  return with_size(dtype, p.dk, [&](auto t, auto n) {
+    using T = decltype(t);
+    constexpr int KD = decltype(n)::value;
+    return back ? launch<T, KD, true>(p, stream) : launch<T, KD, false>(p, stream);
+  });
+}

@@ -580,7 +580,8 @@ int mebptt_scan_step(const mebptt_scan_desc* desc, const mebptt_scan_inputs* in,
  * q^, k^: q and k divided by sqrt(their squares' sum + eps) if `normalise`, else as they are.  activate: g = A softplus(a + a_bias), beta = sigmoid(b);
  * otherwise g = a (not above 0 where the recurrence is to be stable) and beta = b as given.  Without an a, g = 0.  g below -10000 counts as that.
  * Steps are taken 64 at a time; a value of a sequence's own that is not finite may reach its head's results up to 63 steps earlier, those of no
- * other sequence or head.  Lengths as in the convolution; h_out is the state after a sequence's own last step. */
+ * other sequence or head.  Lengths as in the convolution; h_out is the state after a sequence's own last step.  stride_t of every sequence is 0 .. 2^23
+ * elements.  Rows of q and k that are whole 16-byte vectors at 16-byte boundaries are read in place, others are copied into the workspace first. */
 typedef struct {
   int32_t t, B;      /* t 0 .. 2^30, B 0 .. 65535; B * H at most 2^22 */
   int32_t Hk, H;     /* heads of q and k, heads of v: 1 .. 1024, Hk divides H */

@@ -96,37 +96,57 @@ __device__ inline void mma(f32x4& c, const Op<float, NA>& a, const Op<float, NB>
 
 // ---- a chunk's rows in LDS -----------------------------------------------------------------------------
 
-// [C][KD] values of T as rows; bf16 also as columns, [KD][C], which products that sum over steps read (fp32 operands are
-// single values there and are picked out of the rows).  Rows are padded so that 16 of them begin in different banks.
+// [C][KD] values of T as rows, padded so that 16 of them begin in different banks.
 template <typename T>
-struct Lds;
-template <>
-struct Lds<__bf16> {
-  static constexpr int PAD = 8;
+struct Lds {
+  static constexpr int PAD = 16 / sizeof(T);
   static constexpr int ld(int KD) { return KD + PAD; }
-  static constexpr int row_bytes(int KD) { return C * ld(KD) * 2; }
-  static constexpr int column_bytes(int KD) { return KD * (C + PAD) * 2; }
+  static constexpr int row_bytes(int KD) { return C * ld(KD) * (int)sizeof(T); }
 };
-template <>
-struct Lds<float> {
-  static constexpr int PAD = 4;
-  static constexpr int ld(int KD) { return KD + PAD; }
-  static constexpr int row_bytes(int KD) { return C * ld(KD) * 4; }
-  static constexpr int column_bytes(int) { return 0; }
-};
-// The operand with column `col` (of this lane) and steps s0 .. s0 + 31: from the columns, or picked out of the rows.
-template <int KD>
-__device__ inline Op<__bf16, 1> from_column(const __bf16*, const __bf16* columns, int col, int s0, int g) {
-  return from_row(columns + col * (C + Lds<__bf16>::PAD) + s0, g);
+// The operand with column c0 + l % 16 and steps s0 .. s0 + 31.  bf16: LDS turns 4 steps x 16 columns round on the way (lane i of 16 gives the address of 4
+// columns of step i / 4 and receives column i of the four steps); fp32: single values.
+template <int LD>
+__device__ inline Op<__bf16, 1> from_columns(const __bf16* rows, int c0, int s0, int lane) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* At;
+  const int i = lane % 16;
+  const __bf16* p = rows + (s0 + lane / 16 * 4 + i / 4) * LD + c0 + i % 4 * 4;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)p), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p + 16 * LD));
+  Op<__bf16, 1> o;
+  o.p[0] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  return o;
 }
-template <int KD>
-__device__ inline Op<float, 1> from_column(const float* rows, const float*, int col, int s0, int g) {
+template <int LD>
+__device__ inline Op<float, 1> from_columns(const float* rows, int c0, int s0, int lane) {
   Op<float, 1> o;
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o.v[h][e] = rows[(s0 + 16 * h + 4 * g + e) * Lds<float>::ld(KD) + col];
+    for (int e = 0; e < 4; ++e) o.v[h][e] = rows[(s0 + 16 * h + lane / 16 * 4 + e) * LD + c0 + lane % 16];
   return o;
+}
+
+// What a chunk's loads go by.  Loads are never conditional, since each would be waited for in its branch: steps that do not exist read the last one that
+// does, columns that do not exist the last ones, and both become zeros afterwards.  A lane's address is a uniform base and 32 bits.
+constexpr int64_t NEAR = 1 << 23;   // elements between steps, at most, for that
+struct Window {
+  int stride, live;
+  __device__ inline Window(int64_t stride, int live) : stride((int)stride), live(live) {}
+};
+template <typename T>
+__device__ inline T* near(T* base, unsigned bytes) {
+  return reinterpret_cast<T*>(reinterpret_cast<std::conditional_t<std::is_const<T>::value, const char, char>*>(base) + bytes);
+}
+
+// Numbers that the compiler knows nothing of: what is computed from them stays where it is used.  Taken out of the loop over chunks, the addresses of
+// rows would fill the registers.
+__device__ inline int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ inline int here_uniform(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
 }
 
 // Four steps' values of one vector's width, on their way from memory to LDS.
@@ -136,25 +156,32 @@ struct Piece {
   typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(16)));
   Vec v[4];
 };
-// Piece u of [C][KD] (u % (KD / E): which vector, u / (KD / E): which four steps).  Steps from `live` on and columns from `width` on are zeros.  `p`: the
-// chunk's first row; rows `stride` apart.
+// Piece u of [C][KD] (u % (KD / E): which vector, u / (KD / E): which four steps) of rows of `width` values, whole vectors.  `p`: the chunk's first row.
 template <typename T, int KD>
-__device__ inline void load_piece(Piece<T>& x, const T* p, int64_t stride, int width, int live, bool vec, int u) {
+__device__ inline void load_piece(Piece<T>& x, const T* p, const Window& w, int width, int u) {
   constexpr int E = Piece<T>::E, COLS = KD / E;
-  const int c = u % COLS * E, s = u / COLS * 4;
+  using Vec = typename Piece<T>::Vec;
+  const int at = min(u % COLS * E, width - E), s = u / COLS * 4;
+  if (w.live >= C) {
+    const unsigned off = (unsigned)(s * w.stride + at) * (unsigned)sizeof(T);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x.v[i] = {};
-    if (s + i < live) {
-      const T* row = p + (int64_t)(s + i) * stride;
-      if (vec) {
-        if (c < width) x.v[i] = *reinterpret_cast<const typename Piece<T>::Vec*>(row + c);
-      } else {
+    for (int i = 0; i < 4; ++i) x.v[i] = *reinterpret_cast<const Vec*>(near(p + (int64_t)i * w.stride, off));
+  } else {
+    const int first = here(s);
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (c + e < width) x.v[i][e] = row[c + e];
-      }
-    }
+    for (int i = 0; i < 4; ++i) x.v[i] = *reinterpret_cast<const Vec*>(near(p, (unsigned)(min(first + i, w.live - 1) * w.stride + at) * (unsigned)sizeof(T)));
+  }
+}
+// What does not exist becomes zero.
+template <typename T, int KD>
+__device__ inline void clear_piece(Piece<T>& x, const Window& w, int width, int u) {
+  constexpr int E = Piece<T>::E, COLS = KD / E;
+  if (width < KD && u % COLS * E >= width) x.v[0] = x.v[1] = x.v[2] = x.v[3] = typename Piece<T>::Vec{};
+  if (w.live < C) {
+    const int first = here(u / COLS * 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (first + i >= w.live) x.v[i] = typename Piece<T>::Vec{};
   }
 }
 template <typename T, int KD>
@@ -164,25 +191,13 @@ __device__ inline void put_rows(const Piece<T>& x, T* rows, int u) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) *reinterpret_cast<typename Piece<T>::Vec*>(rows + (s + i) * Lds<T>::ld(KD) + c) = x.v[i];
 }
-template <typename T, int KD>
-__device__ inline void put_columns(const Piece<T>& x, T* columns, int u) {
-  if constexpr (sizeof(T) == 2) {
-    constexpr int E = Piece<T>::E, COLS = KD / E;
-    const int c = u % COLS * E, s = u / COLS * 4;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const bf16x4 t = {x.v[0][e], x.v[1][e], x.v[2][e], x.v[3][e]};
-      *reinterpret_cast<bf16x4*>(columns + (c + e) * (C + Lds<T>::PAD) + s) = t;
-    }
-  }
-}
 template <typename T>
 constexpr int pieces(int KD) { return C / 4 * (KD / Piece<T>::E); }
 
 // ---- what a chunk's preparation leaves ---------------------------------------------------------------
 
-// Per step, in rows of C floats.
-enum { GA = 0, BE = 1, LA = 2, SK = 3, SQ = 4, RQ = 5, GATES = 6 };   // gamma, beta, gamma_C / gamma, 1 / |k|, scale / |q|, 1 / |q|
+// Per step, in rows of C floats; the walks need the first five.  GA: gamma, BE: beta, LA: gamma_C / gamma, SK: 1 / |k|, SQ: scale / |q|, RQ: 1 / |q|.
+enum { GA_SK = 0, GA_SQ = 1, BE = 2, LA_SK = 3, GA = 4, LA = 5, SK = 6, SQ = 7, RQ = 8, GATES = 9, WALK_GATES = 5 };
 
 // Matrices [C][C] as operands in the order in which lanes read them.  A lower triangle has six pieces of 16 rows by 32 columns: (0,0) (1,0)
 // (2,0) (2,1) (3,0) (3,1); its transpose (0,0) (0,1) (1,0) (1,1) (2,1) (3,1).
@@ -233,7 +248,8 @@ struct Args {
   int t, B, Hk, H, dk, dv, dvp;        // dvp: dv rounded up to 16
   int activate, normalise;
   float scale, eps;
-  int vec;                              // rows of q and k are whole 16-byte vectors at 16-byte boundaries
+  int width;                            // of the rows of q and k: whole 16-byte vectors at 16-byte boundaries, zeros from dk on
+  int head;                             // values between heads of q and k
   int c0, c1;                           // chunks of this launch
   char* records;                        // [c1 - c0][B H]
   const float* from;                    // states [B][H][dk][dv] before the first chunk, or NULL
@@ -247,6 +263,8 @@ struct Args {
 
 __device__ inline int ends_at(const Args& p, int b) { return p.lengths ? min(max(p.lengths[b], 0), p.t) : p.t; }
 
+// Rows of q and k that are no whole vectors, copied to ones that are: steps c0 C .. of [t][B][Hk][width].
+int pad_rows(const mebptt_seq& from, const Args& p, int dtype, void* to, hipStream_t stream);
 int prepare(const Args& p, int dtype, bool back, hipStream_t stream);
 int walk(const Args& p, int dtype, bool again, hipStream_t stream);        // `again`: S and R of every chunk instead of y
 int walk_back(const Args& p, int dtype, hipStream_t stream);

@@ -25,17 +25,22 @@ int check_stretch(const mebptt_delta_desc* d) {
   if (d->stretch < C || d->stretch > 1 << 20 || d->stretch % C) return set_error(MEBPTT_EINVAL, "stretch must be a multiple of %d up to 2^20", C);
   return MEBPTT_OK;
 }
-int check_seq(const mebptt_seq& s, const char* what, bool needed = true) {
-  return needed && !s.data ? set_error(MEBPTT_EINVAL, "%s is required", what) : MEBPTT_OK;
+int check_seq(const mebptt_seq& s, const mebptt_delta_desc* d, const char* what) {
+  if (!s.data) return set_error(MEBPTT_EINVAL, "%s is required", what);
+  if (d->t > 1 && (s.stride_t < 0 || s.stride_t > NEAR)) return set_error(MEBPTT_EINVAL, "stride_t of %s must be 0 .. %lld", what, (long long)NEAR);
+  return MEBPTT_OK;
 }
 int check_output(const mebptt_seq& s, const mebptt_delta_desc* d, int64_t channels, const char* what) {
-  if (!s.data) return set_error(MEBPTT_EINVAL, "%s is required", what);
+  const int rc = check_seq(s, d, what);
+  if (rc) return rc;
   return rows_apart(s, d->t, d->B, channels) ? MEBPTT_OK : set_error(MEBPTT_EINVAL, "rows of %s overlap", what);
 }
 int check_inputs(const mebptt_delta_desc* d, const mebptt_delta_inputs* in, bool steps) {
   int rc;
   if (!in) return set_error(MEBPTT_EINVAL, "in is NULL");
-  if (steps && ((rc = check_seq(in->q, "q")) || (rc = check_seq(in->k, "k")) || (rc = check_seq(in->v, "v")) || (rc = check_seq(in->b, "b")))) return rc;
+  if (steps && ((rc = check_seq(in->q, d, "q")) || (rc = check_seq(in->k, d, "k")) || (rc = check_seq(in->v, d, "v")) || (rc = check_seq(in->b, d, "b")) ||
+                (in->a.data && (rc = check_seq(in->a, d, "a")))))
+    return rc;
   if (d->activate && in->a.data && !in->A) return set_error(MEBPTT_EINVAL, "A is required");
   return MEBPTT_OK;
 }
@@ -43,9 +48,17 @@ int check_inputs(const mebptt_delta_desc* d, const mebptt_delta_inputs* in, bool
 int64_t chunks_of(const mebptt_delta_desc* d) { return ceil_div(d->t, C); }
 size_t state_bytes(const mebptt_delta_desc* d) { return align_up((size_t)d->B * d->H * d->dk * d->dv * 4); }
 
+int width_of(const mebptt_delta_desc* d) {
+  const int V = d->dtype == MEBPTT_FP32 ? 4 : 8;
+  return (int)ceil_div(d->dk, V) * V;
+}
+size_t row_bytes(const mebptt_delta_desc* d, int64_t chunks) {
+  return align_up((size_t)std::min<int64_t>(chunks * C, d->t) * d->B * d->Hk * width_of(d) * elem_bytes(d->dtype));
+}
+
 struct Forward {
   int64_t slab;
-  size_t records, carry, total;
+  size_t records, carry, rows, total;
 };
 Forward forward_layout(const mebptt_delta_desc* d) {
   const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d);
@@ -53,12 +66,13 @@ Forward forward_layout(const mebptt_delta_desc* d) {
   f.slab = std::min(std::max<int64_t>(1, RECORDS / std::max<int64_t>(BH, 1)), std::max<int64_t>(chunks, 1));
   f.records = align_up((size_t)(std::min(f.slab, chunks) * BH) * record_bytes(d->dtype, false));
   f.carry = f.slab < chunks ? state_bytes(d) : 0;
-  f.total = f.records + f.carry;
+  f.rows = row_bytes(d, f.slab);
+  f.total = f.records + f.carry + 2 * f.rows;
   return f;
 }
 struct Backward {
   int64_t slab;
-  size_t records, states, rows, carry, parts, total;
+  size_t records, states, rows, carry, parts, padded, total;
 };
 Backward backward_layout(const mebptt_delta_desc* d) {
   const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d), dvp = ceil_div(d->dv, 16) * 16;
@@ -70,7 +84,8 @@ Backward backward_layout(const mebptt_delta_desc* d) {
   w.rows = align_up(n * C * dvp * 4);
   w.carry = w.slab < chunks ? state_bytes(d) : 0;
   w.parts = align_up((size_t)chunks * d->B * 2 * d->H * 4);
-  w.total = w.records + 2 * w.states + 2 * w.rows + w.carry + w.parts;
+  w.padded = row_bytes(d, w.slab);
+  w.total = w.records + 2 * w.states + 2 * w.rows + w.carry + w.parts + 2 * w.padded;
   return w;
 }
 
@@ -80,9 +95,28 @@ Args args_of(const mebptt_delta_desc* d, const mebptt_delta_inputs* in) {
   p.A = in->A, p.bias = in->a_bias, p.lengths = in->lengths;
   p.t = d->t, p.B = d->B, p.Hk = d->Hk, p.H = d->H, p.dk = d->dk, p.dv = d->dv, p.dvp = (int)ceil_div(d->dv, 16) * 16;
   p.activate = d->activate, p.normalise = d->normalise, p.scale = d->scale, p.eps = d->eps;
-  const int V = d->dtype == MEBPTT_FP32 ? 4 : 8;
-  p.vec = d->dk % V == 0 && rows_aligned(in->q, d->dtype, V) && rows_aligned(in->k, d->dtype, V);
+  p.width = width_of(d);
+  p.head = d->dk;
   return p;
+}
+// Whether rows of q and k are whole vectors; else they are copied to ones that are.
+bool whole_rows(const mebptt_delta_desc* d, const mebptt_delta_inputs* in) {
+  const int V = d->dtype == MEBPTT_FP32 ? 4 : 8;
+  return d->dk % V == 0 && rows_aligned(in->q, d->dtype, V) && rows_aligned(in->k, d->dtype, V);
+}
+int pad(Args& p, const mebptt_delta_desc* d, const mebptt_delta_inputs* in, char* rows, size_t bytes, hipStream_t stream) {
+  const size_t e = elem_bytes(d->dtype);
+  mebptt_seq* to[2] = {&p.q, &p.k};
+  const mebptt_seq* from[2] = {&in->q, &in->k};
+  p.head = p.width;
+  for (int i = 0; i < 2; ++i) {
+    char* at = rows + i * bytes;
+    const int64_t sb = (int64_t)d->Hk * p.width, st = d->B * sb;
+    const int rc = pad_rows(*from[i], p, d->dtype, at, stream);
+    if (rc) return rc;
+    *to[i] = {at - (int64_t)p.c0 * C * st * (int64_t)e, st, sb};    // (as if it held all steps)
+  }
+  return MEBPTT_OK;
 }
 
 // ---- single tokens -------------------------------------------------------------------------------------
@@ -252,6 +286,7 @@ int mebptt_delta_forward(const mebptt_delta_desc* d, const mebptt_delta_inputs* 
   p.keep = states ? d->stretch / C : 1;
   const int64_t chunks = chunks_of(d);
   float* carry = (float*)((char*)workspace + f.records);
+  const bool whole = whole_rows(d, in);
   if (!chunks) {
     p.from = in->h0, p.to = h_out;
     return h_out ? walk(p, d->dtype, false, s) : MEBPTT_OK;
@@ -260,6 +295,7 @@ int mebptt_delta_forward(const mebptt_delta_desc* d, const mebptt_delta_inputs* 
     p.c0 = (int)c, p.c1 = (int)std::min(c + f.slab, chunks);
     p.from = c ? carry : in->h0;
     p.to = p.c1 < chunks ? carry : h_out;
+    if (!whole && (rc = pad(p, d, in, (char*)workspace + f.records + f.carry, f.rows, s))) return rc;
     if ((rc = prepare(p, d->dtype, false, s)) || (rc = walk(p, d->dtype, false, s))) return rc;
   }
   return MEBPTT_OK;
@@ -274,7 +310,7 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
   if ((rc = check_inputs(d, in, steps))) return rc;
   if (!grads) return set_error(MEBPTT_EINVAL, "grads is NULL");
   const int64_t qk = (int64_t)d->Hk * d->dk;
-  if (steps && ((rc = check_seq(dy, "dy")) || (rc = check_output(grads->dq, d, qk, "dq")) || (rc = check_output(grads->dk, d, qk, "dk")) ||
+  if (steps && ((rc = check_seq(dy, d, "dy")) || (rc = check_output(grads->dq, d, qk, "dq")) || (rc = check_output(grads->dk, d, qk, "dk")) ||
                 (rc = check_output(grads->dv, d, (int64_t)d->H * d->dv, "dv")) || (rc = check_output(grads->db, d, d->H, "db")) ||
                 (in->a.data && (rc = check_output(grads->da, d, d->H, "da")))))
     return rc;
@@ -297,6 +333,7 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
   p.records = (char*)take(w.records);
   p.S = take(w.states), p.dS = take(w.states), p.R = take(w.rows), p.Z = take(w.rows);
   float *carry = take(w.carry), *parts = take(w.parts);
+  const bool whole = whole_rows(d, in);
   const int64_t chunks = chunks_of(d), BH = (int64_t)d->B * d->H;
   if (d->B && !chunks && grads->dh0) {
     p.from = dh_out, p.to = grads->dh0;
@@ -305,6 +342,7 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
   for (int64_t slab = d->B ? ceil_div(chunks, w.slab) : 0; slab-- > 0;) {
     p.c0 = (int)(slab * w.slab), p.c1 = (int)std::min(p.c0 + w.slab, chunks);
     p.parts = parts + (int64_t)p.c0 * d->B * 2 * d->H;
+    if (!whole && (rc = pad(p, d, in, at, w.padded, s))) return rc;
     if ((rc = prepare(p, d->dtype, true, s))) return rc;
     p.from = (const float*)states + slab * BH * d->dk * d->dv;
     p.to = nullptr;

@@ -26,8 +26,7 @@ struct Layout {
   static constexpr int NV = sizeof(T) == 2 ? N32 : 1;
   static constexpr int WLD = C + Lds<T>::PAD, WSIZE = C * WLD * (int)sizeof(T);
   static constexpr int NM = sizeof(T) == 2 ? NW : 1;
-  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), KT = Q + Lds<T>::row_bytes(KD), QT = KT + Lds<T>::column_bytes(KD),
-                       BLOCK = QT + Lds<T>::column_bytes(KD);
+  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), BLOCK = Q + Lds<T>::row_bytes(KD);
   static constexpr int DY = BLOCK, Z = DY + VSIZE, R = Z + NV * VSIZE;
   static constexpr int W1 = BLOCK, W2 = W1 + NM * WSIZE, W3 = W2 + NM * WSIZE;      // over the blocks, when they have been read
   static constexpr int SUMS = BLOCK + ((1 + 2 * NV) * VSIZE > 3 * NM * WSIZE ? (1 + 2 * NV) * VSIZE : 3 * NM * WSIZE);
@@ -88,7 +87,7 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
   using L = Layout<T, KD>;
   using Rec = Record<T, true>;
   constexpr int LD = Lds<T>::ld(KD), NT = KD / 16, VB = L::VB, VLD = L::VLD, WLD = L::WLD;
-  T *K = (T*)(lds + L::K), *Q = (T*)(lds + L::Q), *KT = (T*)(lds + L::KT), *QT = (T*)(lds + L::QT);
+  T *K = (T*)(lds + L::K), *Q = (T*)(lds + L::Q);
   T *DY = (T*)(lds + L::DY), *ZL = (T*)(lds + L::Z), *RL = (T*)(lds + L::R), *W1 = (T*)(lds + L::W1), *W2 = (T*)(lds + L::W2), *W3 = (T*)(lds + L::W3);
   double* G = (double*)(lds + L::SUMS);
   float *gate = (float*)(lds + L::GATE), *rowF = (float*)(lds + L::ROWF), *cols = (float*)(lds + L::COLS), *dots = (float*)(lds + L::DOTS),
@@ -114,12 +113,13 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
   }
   for (int u = threadIdx.x; u < pieces<T>(KD); u += THREADS) {
     Piece<T> x, y;
-    load_piece<T, KD>(x, (const T*)p.k.data + (int64_t)s0 * p.k.stride_t + b * p.k.stride_b + hk * p.dk, p.k.stride_t, p.dk, live, p.vec, u);
-    load_piece<T, KD>(y, (const T*)p.q.data + (int64_t)s0 * p.q.stride_t + b * p.q.stride_b + hk * p.dk, p.q.stride_t, p.dk, live, p.vec, u);
+    const Window wk(p.k.stride_t, live), wq(p.q.stride_t, live);
+    load_piece<T, KD>(x, (const T*)p.k.data + (int64_t)s0 * p.k.stride_t + b * p.k.stride_b + hk * p.head, wk, p.width, u);
+    load_piece<T, KD>(y, (const T*)p.q.data + (int64_t)s0 * p.q.stride_t + b * p.q.stride_b + hk * p.head, wq, p.width, u);
+    clear_piece<T, KD>(x, wk, p.width, u);
+    clear_piece<T, KD>(y, wq, p.width, u);
     put_rows<T, KD>(x, K, u);
     put_rows<T, KD>(y, Q, u);
-    put_columns<T, KD>(x, KT, u);
-    put_columns<T, KD>(y, QT, u);
   }
   f32x4 dQ[4] = {}, dK[4] = {};
   for (int h = hk * group; h < (hk + 1) * group; ++h) {
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         f32x4 x = {}, w = {};
 #pragma unroll
         for (int pb = 0; pb < 2; ++pb) {
-          const auto kc = from_column<KD>(K, KT, col, 32 * pb, g), qc = from_column<KD>(Q, QT, col, 32 * pb, g);
+          const auto kc = from_columns<LD>(K, 16 * wave, 32 * pb, lane), qc = from_columns<LD>(Q, 16 * wave, 32 * pb, lane);
           mma(x, from_parts<NW>(W1 + (16 * rt + c16) * WLD + 32 * pb, L::WSIZE / (int)sizeof(T), g), kc);
           mma(w, from_parts<NW>(W2 + (16 * rt + c16) * WLD + 32 * pb, L::WSIZE / (int)sizeof(T), g), qc);
           mma(w, from_parts<NW>(W3 + (16 * rt + c16) * WLD + 32 * pb, L::WSIZE / (int)sizeof(T), g), kc);

@@ -76,22 +76,33 @@ __device__ inline Op<float, 1> from_row(const float* p, int g) {
   return o;
 }
 
-// c += a b; of the products of parts those that matter.
-template <int NA, int NB>
-__device__ inline void mma(f32x4& c, const Op<__bf16, NA>& a, const Op<__bf16, NB>& b) {
+// c[r] += a[r] b for R tiles; of the products of parts those that matter.  Tiles innermost: an instruction's result can be added to four or more
+// instructions later without a pause.
+template <int R, int M, int NA, int NB>
+__device__ inline void mma(f32x4 (&c)[M], const Op<__bf16, NA> (&a)[R], const Op<__bf16, NB>& b, int first = 0) {
   constexpr int MOST = NA > NB ? NA : NB;
 #pragma unroll
-  for (int i = 0; i < NA; ++i)
+  for (int i = NA - 1; i >= 0; --i)
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-      if (i + j < MOST) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[j], c, 0, 0, 0);
+    for (int j = NB - 1; j >= 0; --j)
+      if (i + j < MOST) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) c[first + r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[r].p[i], b.p[j], c[first + r], 0, 0, 0);
+      }
 }
-template <int NA, int NB>
-__device__ inline void mma(f32x4& c, const Op<float, NA>& a, const Op<float, NB>& b) {
+template <int R, int M, int NA, int NB>
+__device__ inline void mma(f32x4 (&c)[M], const Op<float, NA> (&a)[R], const Op<float, NB>& b, int first = 0) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[h][e], b.v[h][e], c, 0, 0, 0);
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int r = 0; r < R; ++r) c[first + r] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r].v[h][e], b.v[h][e], c[first + r], 0, 0, 0);
+}
+template <typename T, int NA, int NB>
+__device__ inline void mma(f32x4& c, const Op<T, NA>& a, const Op<T, NB>& b) {
+  const Op<T, NA> row[1] = {a};
+  mma(*reinterpret_cast<f32x4(*)[1]>(&c), row, b);
 }
 
 // ---- a chunk's rows in LDS -----------------------------------------------------------------------------
@@ -130,8 +141,10 @@ __device__ inline Op<float, 1> from_columns(const float* rows, int c0, int s0, i
 // does, columns that do not exist the last ones, and both become zeros afterwards.  A lane's address is a uniform base and 32 bits.
 constexpr int64_t NEAR = 1 << 23;   // elements between steps, at most, for that
 struct Window {
-  int stride, live;
-  __device__ inline Window(int64_t stride, int live) : stride((int)stride), live(live) {}
+  int stride, live;   // live: at least one (a chunk of none is read all the same, and not used)
+  __device__ inline Window(int64_t stride, int live) : stride((int)stride), live(min(max(live, 1), C)) {}
+  // Offset of a step, `first` being its offset were they all there.
+  __device__ inline unsigned row(unsigned first) const { return min(first, (unsigned)((live - 1) * stride)); }
 };
 template <typename T>
 __device__ inline T* near(T* base, unsigned bytes) {
@@ -149,50 +162,46 @@ __device__ inline int here_uniform(int x) {
   return x;
 }
 
-// Four steps' values of one vector's width, on their way from memory to LDS.
-template <typename T>
-struct Piece {
-  static constexpr int E = 16 / sizeof(T);
-  typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(16)));
-  Vec v[4];
+// Rows of an input that are whole 16-byte vectors at 16-byte boundaries: head h of step s of sequence b is at data + s stride_t + b stride_b + h head, `width`
+// values, zeros behind those that the input has.
+struct Rows {
+  const void* data;
+  int64_t stride_t, stride_b;
+  int head, width;
 };
-// Piece u of [C][KD] (u % (KD / E): which vector, u / (KD / E): which four steps) of rows of `width` values, whole vectors.  `p`: the chunk's first row.
-template <typename T, int KD>
-__device__ inline void load_piece(Piece<T>& x, const T* p, const Window& w, int width, int u) {
-  constexpr int E = Piece<T>::E, COLS = KD / E;
-  using Vec = typename Piece<T>::Vec;
-  const int at = min(u % COLS * E, width - E), s = u / COLS * 4;
-  if (w.live >= C) {
-    const unsigned off = (unsigned)(s * w.stride + at) * (unsigned)sizeof(T);
+// [C][COLS] of such rows from column c0 on, on their way from memory to LDS by THREADS threads; 16 or more neighbours have a row.
+template <typename T, int COLS, int THREADS>
+struct Fetch {
+  static constexpr int E = 16 / sizeof(T), PER_ROW = COLS / E, VECS = C * PER_ROW, N = (VECS + THREADS - 1) / THREADS;
+  typedef T Vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(16)));
+  Vec v[N];
+  // (where there are more threads than vectors the last ones do the same as others)
+  static __device__ inline int number(int i) { return (VECS % THREADS ? min(i * THREADS + (int)threadIdx.x, VECS - 1) : i * THREADS + (int)threadIdx.x); }
+  __device__ inline void load(const Rows& r, int64_t s0, int b, int h, int c0, int live) {
+    const Window w(r.stride_t, live);
+    const T* p = (const T*)r.data + s0 * r.stride_t + b * r.stride_b + (int64_t)h * r.head;
+    const unsigned at = (unsigned)min(c0 + number(0) % PER_ROW * E, r.width - E);
+    static_assert(THREADS % PER_ROW == 0, "all of a thread's vectors are in the same columns");
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[i] = *reinterpret_cast<const Vec*>(near(p + (int64_t)i * w.stride, off));
-  } else {
-    const int first = here(s);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.v[i] = *reinterpret_cast<const Vec*>(near(p, (unsigned)(min(first + i, w.live - 1) * w.stride + at) * (unsigned)sizeof(T)));
+    for (int i = 0; i < N; ++i)
+      v[i] = *reinterpret_cast<const Vec*>(near(p, (w.row((unsigned)(number(i) / PER_ROW * w.stride)) + at) * (unsigned)sizeof(T)));
   }
-}
-// What does not exist becomes zero.
-template <typename T, int KD>
-__device__ inline void clear_piece(Piece<T>& x, const Window& w, int width, int u) {
-  constexpr int E = Piece<T>::E, COLS = KD / E;
-  if (width < KD && u % COLS * E >= width) x.v[0] = x.v[1] = x.v[2] = x.v[3] = typename Piece<T>::Vec{};
-  if (w.live < C) {
-    const int first = here(u / COLS * 4);
+  // What does not exist becomes zero.
+  __device__ inline void put(T* rows, const Rows& r, int c0, int live) {
+    if (r.width < c0 + COLS && c0 + number(0) % PER_ROW * E >= r.width) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (first + i >= w.live) x.v[i] = typename Piece<T>::Vec{};
+      for (int i = 0; i < N; ++i) v[i] = Vec{};
+    }
+    if (live < C) {
+      const int first = here(number(0) / PER_ROW);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (first + i * (THREADS / PER_ROW) >= live) v[i] = Vec{};
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<Vec*>(rows + number(i) / PER_ROW * Lds<T>::ld(COLS) + number(i) % PER_ROW * E) = v[i];
   }
-}
-template <typename T, int KD>
-__device__ inline void put_rows(const Piece<T>& x, T* rows, int u) {
-  constexpr int E = Piece<T>::E, COLS = KD / E;
-  const int c = u % COLS * E, s = u / COLS * 4;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<typename Piece<T>::Vec*>(rows + (s + i) * Lds<T>::ld(KD) + c) = x.v[i];
-}
-template <typename T>
-constexpr int pieces(int KD) { return C / 4 * (KD / Piece<T>::E); }
+};
 
 // ---- what a chunk's preparation leaves ---------------------------------------------------------------
 
@@ -242,14 +251,13 @@ inline size_t record_bytes(int dtype, bool back) {
 // ---- arguments -----------------------------------------------------------------------------------------
 
 struct Args {
-  mebptt_seq q, k, v, a, b, y;
+  Rows q, k, v, dy;
+  mebptt_seq a, b, y;
   const float *A, *bias;
   const int32_t* lengths;
-  int t, B, Hk, H, dk, dv, dvp;        // dvp: dv rounded up to 16
+  int t, B, Hk, H, dk, dv, dvp;         // dvp: dv rounded up to 32
   int activate, normalise;
   float scale, eps;
-  int width;                            // of the rows of q and k: whole 16-byte vectors at 16-byte boundaries, zeros from dk on
-  int head;                             // values between heads of q and k
   int c0, c1;                           // chunks of this launch
   char* records;                        // [c1 - c0][B H]
   const float* from;                    // states [B][H][dk][dv] before the first chunk, or NULL
@@ -257,14 +265,15 @@ struct Args {
   float* states;                        // kept states, or NULL
   int keep;                             // every keep-th chunk's
   float *S, *R, *Z, *dS;                // of every chunk of the launch: [KD][dvp] and [C][dvp]
-  mebptt_seq dy, dq, dkey, dval, da, db;
+  mebptt_seq dq, dkey, dval, da, db;
+  int vec_out;                          // rows of y, or of dval, are whole vectors of four
   float* parts;                         // [c1 - c0][B][2 H]: sums of dg softplus and da
 };
 
 __device__ inline int ends_at(const Args& p, int b) { return p.lengths ? min(max(p.lengths[b], 0), p.t) : p.t; }
 
-// Rows of q and k that are no whole vectors, copied to ones that are: steps c0 C .. of [t][B][Hk][width].
-int pad_rows(const mebptt_seq& from, const Args& p, int dtype, void* to, hipStream_t stream);
+// Rows that are no whole vectors, copied to ones that are: the launch's steps, [..][B][heads][r.width].
+int pad_rows(const mebptt_seq& from, const Args& p, int heads, int d, int width, int dtype, void* to, hipStream_t stream);
 int prepare(const Args& p, int dtype, bool back, hipStream_t stream);
 int walk(const Args& p, int dtype, bool again, hipStream_t stream);        // `again`: S and R of every chunk instead of y
 int walk_back(const Args& p, int dtype, hipStream_t stream);

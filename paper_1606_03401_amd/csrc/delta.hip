@@ -48,17 +48,18 @@ int check_inputs(const mebptt_delta_desc* d, const mebptt_delta_inputs* in, bool
 int64_t chunks_of(const mebptt_delta_desc* d) { return ceil_div(d->t, C); }
 size_t state_bytes(const mebptt_delta_desc* d) { return align_up((size_t)d->B * d->H * d->dk * d->dv * 4); }
 
-int width_of(const mebptt_delta_desc* d) {
+int whole(const mebptt_delta_desc* d, int n) {
   const int V = d->dtype == MEBPTT_FP32 ? 4 : 8;
-  return (int)ceil_div(d->dk, V) * V;
+  return (int)ceil_div(n, V) * V;
 }
-size_t row_bytes(const mebptt_delta_desc* d, int64_t chunks) {
-  return align_up((size_t)std::min<int64_t>(chunks * C, d->t) * d->B * d->Hk * width_of(d) * elem_bytes(d->dtype));
+// Room for rows of q, k, v and dy that are copied to whole vectors (any may be: it depends on their addresses).
+size_t row_bytes(const mebptt_delta_desc* d, int64_t chunks, int heads, int n) {
+  return align_up((size_t)std::min<int64_t>(chunks * C, d->t) * d->B * heads * whole(d, n) * elem_bytes(d->dtype));
 }
 
 struct Forward {
   int64_t slab;
-  size_t records, carry, rows, total;
+  size_t records, carry, total;
 };
 Forward forward_layout(const mebptt_delta_desc* d) {
   const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d);
@@ -66,16 +67,15 @@ Forward forward_layout(const mebptt_delta_desc* d) {
   f.slab = std::min(std::max<int64_t>(1, RECORDS / std::max<int64_t>(BH, 1)), std::max<int64_t>(chunks, 1));
   f.records = align_up((size_t)(std::min(f.slab, chunks) * BH) * record_bytes(d->dtype, false));
   f.carry = f.slab < chunks ? state_bytes(d) : 0;
-  f.rows = row_bytes(d, f.slab);
-  f.total = f.records + f.carry + 2 * f.rows;
+  f.total = f.records + f.carry + 2 * row_bytes(d, f.slab, d->Hk, d->dk) + row_bytes(d, f.slab, d->H, d->dv);
   return f;
 }
 struct Backward {
   int64_t slab;
-  size_t records, states, rows, carry, parts, padded, total;
+  size_t records, states, rows, carry, parts, total;
 };
 Backward backward_layout(const mebptt_delta_desc* d) {
-  const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d), dvp = ceil_div(d->dv, 16) * 16;
+  const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d), dvp = ceil_div(d->dv, 32) * 32;
   Backward w = {};
   w.slab = std::min<int64_t>(d->stretch / C, std::max<int64_t>(chunks, 1));
   const size_t n = (size_t)(std::min(w.slab, chunks) * BH);
@@ -84,39 +84,30 @@ Backward backward_layout(const mebptt_delta_desc* d) {
   w.rows = align_up(n * C * dvp * 4);
   w.carry = w.slab < chunks ? state_bytes(d) : 0;
   w.parts = align_up((size_t)chunks * d->B * 2 * d->H * 4);
-  w.padded = row_bytes(d, w.slab);
-  w.total = w.records + 2 * w.states + 2 * w.rows + w.carry + w.parts + 2 * w.padded;
+  w.total = w.records + 2 * w.states + 2 * w.rows + w.carry + w.parts + 2 * row_bytes(d, w.slab, d->Hk, d->dk) + 2 * row_bytes(d, w.slab, d->H, d->dv);
   return w;
 }
 
 Args args_of(const mebptt_delta_desc* d, const mebptt_delta_inputs* in) {
   Args p = {};
-  p.q = in->q, p.k = in->k, p.v = in->v, p.a = in->a, p.b = in->b;
+  p.a = in->a, p.b = in->b;
   p.A = in->A, p.bias = in->a_bias, p.lengths = in->lengths;
-  p.t = d->t, p.B = d->B, p.Hk = d->Hk, p.H = d->H, p.dk = d->dk, p.dv = d->dv, p.dvp = (int)ceil_div(d->dv, 16) * 16;
+  p.t = d->t, p.B = d->B, p.Hk = d->Hk, p.H = d->H, p.dk = d->dk, p.dv = d->dv, p.dvp = (int)ceil_div(d->dv, 32) * 32;
   p.activate = d->activate, p.normalise = d->normalise, p.scale = d->scale, p.eps = d->eps;
-  p.width = width_of(d);
-  p.head = d->dk;
   return p;
 }
-// Whether rows of q and k are whole vectors; else they are copied to ones that are.
-bool whole_rows(const mebptt_delta_desc* d, const mebptt_delta_inputs* in) {
-  const int V = d->dtype == MEBPTT_FP32 ? 4 : 8;
-  return d->dk % V == 0 && rows_aligned(in->q, d->dtype, V) && rows_aligned(in->k, d->dtype, V);
-}
-int pad(Args& p, const mebptt_delta_desc* d, const mebptt_delta_inputs* in, char* rows, size_t bytes, hipStream_t stream) {
-  const size_t e = elem_bytes(d->dtype);
-  mebptt_seq* to[2] = {&p.q, &p.k};
-  const mebptt_seq* from[2] = {&in->q, &in->k};
-  p.head = p.width;
-  for (int i = 0; i < 2; ++i) {
-    char* at = rows + i * bytes;
-    const int64_t sb = (int64_t)d->Hk * p.width, st = d->B * sb;
-    const int rc = pad_rows(*from[i], p, d->dtype, at, stream);
-    if (rc) return rc;
-    *to[i] = {at - (int64_t)p.c0 * C * st * (int64_t)e, st, sb};    // (as if it held all steps)
+// Rows of a launch's steps as the kernels read them: in place, or copied to `room`, which moves on.
+int rows_of(Rows* to, const Args& p, const mebptt_delta_desc* d, const mebptt_seq& from, int heads, int n, char*& room, int64_t slab, hipStream_t stream) {
+  const int width = whole(d, n), V = d->dtype == MEBPTT_FP32 ? 4 : 8;
+  if (width == n && rows_aligned(from, d->dtype, V)) {
+    *to = {from.data, from.stride_t, from.stride_b, n, n};
+    return MEBPTT_OK;
   }
-  return MEBPTT_OK;
+  char* at = room;
+  room += row_bytes(d, slab, heads, n);
+  const int64_t sb = (int64_t)heads * width, st = d->B * sb;
+  *to = {at - (int64_t)p.c0 * C * st * (int64_t)elem_bytes(d->dtype), st, sb, width, width};    // (as if it held all steps)
+  return pad_rows(from, p, heads, n, width, d->dtype, at, stream);
 }
 
 // ---- single tokens -------------------------------------------------------------------------------------
@@ -281,12 +272,12 @@ int mebptt_delta_forward(const mebptt_delta_desc* d, const mebptt_delta_inputs* 
   hipStream_t s = (hipStream_t)stream;
   Args p = args_of(d, in);
   p.y = y;
+  p.vec_out = d->dv % 4 == 0 && rows_aligned(y, d->dtype, 4);
   p.records = (char*)workspace;
   p.states = (float*)states;
   p.keep = states ? d->stretch / C : 1;
   const int64_t chunks = chunks_of(d);
   float* carry = (float*)((char*)workspace + f.records);
-  const bool whole = whole_rows(d, in);
   if (!chunks) {
     p.from = in->h0, p.to = h_out;
     return h_out ? walk(p, d->dtype, false, s) : MEBPTT_OK;
@@ -295,7 +286,10 @@ int mebptt_delta_forward(const mebptt_delta_desc* d, const mebptt_delta_inputs* 
     p.c0 = (int)c, p.c1 = (int)std::min(c + f.slab, chunks);
     p.from = c ? carry : in->h0;
     p.to = p.c1 < chunks ? carry : h_out;
-    if (!whole && (rc = pad(p, d, in, (char*)workspace + f.records + f.carry, f.rows, s))) return rc;
+    char* room = (char*)workspace + f.records + f.carry;
+    if ((rc = rows_of(&p.q, p, d, in->q, d->Hk, d->dk, room, f.slab, s)) || (rc = rows_of(&p.k, p, d, in->k, d->Hk, d->dk, room, f.slab, s)) ||
+        (rc = rows_of(&p.v, p, d, in->v, d->H, d->dv, room, f.slab, s)))
+      return rc;
     if ((rc = prepare(p, d->dtype, false, s)) || (rc = walk(p, d->dtype, false, s))) return rc;
   }
   return MEBPTT_OK;
@@ -323,7 +317,8 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
   if ((rc = check_workspace(workspace, workspace_bytes, w.total))) return rc;
   hipStream_t s = (hipStream_t)stream;
   Args p = args_of(d, in);
-  p.dy = dy, p.dq = grads->dq, p.dkey = grads->dk, p.dval = grads->dv, p.da = grads->da, p.db = grads->db;
+  p.dq = grads->dq, p.dkey = grads->dk, p.dval = grads->dv, p.da = grads->da, p.db = grads->db;
+  p.vec_out = d->dv % 4 == 0 && rows_aligned(grads->dv, d->dtype, 4);
   char* at = (char*)workspace;
   auto take = [&](size_t n) {
     char* got = at;
@@ -333,7 +328,6 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
   p.records = (char*)take(w.records);
   p.S = take(w.states), p.dS = take(w.states), p.R = take(w.rows), p.Z = take(w.rows);
   float *carry = take(w.carry), *parts = take(w.parts);
-  const bool whole = whole_rows(d, in);
   const int64_t chunks = chunks_of(d), BH = (int64_t)d->B * d->H;
   if (d->B && !chunks && grads->dh0) {
     p.from = dh_out, p.to = grads->dh0;
@@ -342,7 +336,10 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
   for (int64_t slab = d->B ? ceil_div(chunks, w.slab) : 0; slab-- > 0;) {
     p.c0 = (int)(slab * w.slab), p.c1 = (int)std::min(p.c0 + w.slab, chunks);
     p.parts = parts + (int64_t)p.c0 * d->B * 2 * d->H;
-    if (!whole && (rc = pad(p, d, in, at, w.padded, s))) return rc;
+    char* room = at;
+    if ((rc = rows_of(&p.q, p, d, in->q, d->Hk, d->dk, room, w.slab, s)) || (rc = rows_of(&p.k, p, d, in->k, d->Hk, d->dk, room, w.slab, s)) ||
+        (rc = rows_of(&p.v, p, d, in->v, d->H, d->dv, room, w.slab, s)) || (rc = rows_of(&p.dy, p, d, dy, d->H, d->dv, room, w.slab, s)))
+      return rc;
     if ((rc = prepare(p, d->dtype, true, s))) return rc;
     p.from = (const float*)states + slab * BH * d->dk * d->dv;
     p.to = nullptr;

@@ -18,23 +18,35 @@ namespace {
 constexpr int WAVES = 8, THREADS = WAVES * WAVE;
 // Parts of R, Z, S and dS' in the products, and of W1 .. W3, which reach dq and dk only.
 constexpr int N32 = 3, NW = 2;
+constexpr int VB = 32;      // columns of a block of dY, Z and R
 
 template <typename T, int KD>
 struct Layout {
-  static constexpr int VB = sizeof(T) == 2 ? 64 : 32;     // columns of a block of dY, Z and R
-  static constexpr int VLD = VB + Lds<T>::PAD, VSIZE = C * VLD * (int)sizeof(T);
-  static constexpr int NV = sizeof(T) == 2 ? N32 : 1;
-  static constexpr int WLD = C + Lds<T>::PAD, WSIZE = C * WLD * (int)sizeof(T);
-  static constexpr int NM = sizeof(T) == 2 ? NW : 1;
-  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), BLOCK = Q + Lds<T>::row_bytes(KD);
-  static constexpr int DY = BLOCK, Z = DY + VSIZE, R = Z + NV * VSIZE;
-  static constexpr int W1 = BLOCK, W2 = W1 + NM * WSIZE, W3 = W2 + NM * WSIZE;      // over the blocks, when they have been read
-  static constexpr int SUMS = BLOCK + ((1 + 2 * NV) * VSIZE > 3 * NM * WSIZE ? (1 + 2 * NV) * VSIZE : 3 * NM * WSIZE);
+  static constexpr int VLD = VB + Lds<T>::PAD, VSIZE = C * VLD * (int)sizeof(T), NV = sizeof(T) == 2 ? N32 : 1, BLOCK_BYTES = (1 + 2 * NV) * VSIZE;
+  static constexpr int WLD = C + Lds<T>::PAD, WSIZE = C * WLD * (int)sizeof(T), NM = sizeof(T) == 2 ? NW : 1;
+  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), BLOCK = Q + Lds<T>::row_bytes(KD);    // two blocks, one being filled
+  static constexpr int W = BLOCK;                                                                    // four matrices, over them
+  static constexpr int SUMS = BLOCK + (2 * BLOCK_BYTES > 4 * NM * WSIZE ? 2 * BLOCK_BYTES : 4 * NM * WSIZE);
   static constexpr int GATE = SUMS + C * 8, ROWF = GATE + GATES * C * 4, COLS = ROWF + WAVES * C * 4, DOTS = COLS + 4 * C * 4,
                        MORE = DOTS + 2 * WAVES * C * 4, BYTES = MORE + WAVES * 4;
 };
 
-// An operand with N parts whose row stands at p; parts `apart` values from each other.
+// An operand in the order in which it stands: lane l's eight values are 8 g .. 8 g + 7 of the 32.  (Both operands of such a product come from memory.)
+template <int N>
+__device__ inline Op<__bf16, N> as_it_stands(const __bf16* p, int apart, int g) {
+  Op<__bf16, N> o;
+#pragma unroll
+  for (int n = 0; n < N; ++n) o.p[n] = *reinterpret_cast<const bf16x8*>(p + n * apart + 8 * g);
+  return o;
+}
+template <int N>
+__device__ inline Op<float, N> as_it_stands(const float* p, int, int g) {
+  Op<float, N> o;
+  o.v[0] = *reinterpret_cast<const f32x4*>(p + 8 * g);
+  o.v[1] = *reinterpret_cast<const f32x4*>(p + 8 * g + 4);
+  return o;
+}
+// An operand with N parts whose row stands at p, or (columns) whose rows c0 .. stand as columns; parts `apart` values from each other.
 template <int N>
 __device__ inline Op<__bf16, N> from_parts(const __bf16* p, int apart, int g) {
   Op<__bf16, N> o;
@@ -50,18 +62,22 @@ __device__ inline Op<float, N> from_parts(const float* p, int, int g) {
   o.v[1] = x.v[1];
   return o;
 }
-// A value as its parts.
-template <int N>
-__device__ inline void put_parts(__bf16* p, int apart, float x) {
+template <int N, int LD>
+__device__ inline Op<__bf16, N> from_part_columns(const __bf16* p, int apart, int c0, int s0, int lane) {
+  Op<__bf16, N> o;
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const __bf16 part = (__bf16)x;
-    p[n * apart] = part;
-    x -= (float)part;
-  }
+  for (int n = 0; n < N; ++n) o.p[n] = from_columns<LD>(p + n * apart, c0, s0, lane).p[0];
+  return o;
 }
-template <int N>
-__device__ inline void put_parts(float* p, int, float x) { *p = x; }
+template <int N, int LD>
+__device__ inline Op<float, N> from_part_columns(const float* p, int, int c0, int s0, int lane) {
+  const Op<float, 1> x = from_columns<LD>(p, c0, s0, lane);
+  Op<float, N> o;
+  o.v[0] = x.v[0];
+  o.v[1] = x.v[1];
+  return o;
+}
+// Four values as their parts.
 template <int N>
 __device__ inline void put_parts(__bf16* p, int apart, f32x4 x) {
 #pragma unroll
@@ -75,26 +91,31 @@ __device__ inline void put_parts(__bf16* p, int apart, f32x4 x) {
 template <int N>
 __device__ inline void put_parts(float* p, int, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 
-__device__ inline float over_columns(float v) {   // sum over a tile's 16 columns
-#pragma unroll
-  for (int m = 1; m < 16; m <<= 1) v += __shfl_xor(v, m);
+// Sum over 16 neighbouring lanes, a tile's columns, in each of them.
+__device__ inline float over_columns(float v) {
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));   // from 8 lanes on, round the row of 16
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x124, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x122, 0xf, 0xf, false));
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x121, 0xf, 0xf, false));
   return v;
 }
 
-template <typename T, int KD>
+// SHARED: more than one value head to a key head.  (Without the loop over them the compiler keeps what belongs to it out of registers.)
+template <typename T, int KD, bool SHARED>
 __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
   extern __shared__ __align__(16) char lds[];
   using L = Layout<T, KD>;
   using Rec = Record<T, true>;
-  constexpr int LD = Lds<T>::ld(KD), NT = KD / 16, VB = L::VB, VLD = L::VLD, WLD = L::WLD;
+  constexpr int LD = Lds<T>::ld(KD), NT = KD / 16, VLD = L::VLD, WLD = L::WLD, VA = L::VSIZE / (int)sizeof(T), WA = L::WSIZE / (int)sizeof(T);
   T *K = (T*)(lds + L::K), *Q = (T*)(lds + L::Q);
-  T *DY = (T*)(lds + L::DY), *ZL = (T*)(lds + L::Z), *RL = (T*)(lds + L::R), *W1 = (T*)(lds + L::W1), *W2 = (T*)(lds + L::W2), *W3 = (T*)(lds + L::W3);
+  // [j][i], i >= j: W1 and W3 with the factor of column j's key, and with that of row i's query or key
+  T *W1 = (T*)(lds + L::W), *W1q = W1 + L::NM * WA, *W3 = W1q + L::NM * WA, *W3k = W3 + L::NM * WA;
   double* G = (double*)(lds + L::SUMS);
   float *gate = (float*)(lds + L::GATE), *rowF = (float*)(lds + L::ROWF), *cols = (float*)(lds + L::COLS), *dots = (float*)(lds + L::DOTS),
         *more = (float*)(lds + L::MORE);
-  const int per = p.B * p.Hk, chunk = p.c0 + blockIdx.x / per, b = blockIdx.x % per / p.Hk, hk = blockIdx.x % p.Hk, group = p.H / p.Hk;
+  const int per = p.B * p.Hk, chunk = p.c0 + blockIdx.x / per, b = blockIdx.x % per / p.Hk, hk = blockIdx.x % p.Hk, group = SHARED ? p.H / p.Hk : 1;
   const int s0 = chunk * C, steps = min(p.t - s0, C), live = min(ends_at(p, b) - s0, C), BH = p.B * p.H;
-  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16, c16 = lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE, g = lane / 16, c16 = lane % 16;
   const bool mine = wave < NT;               // waves with columns of dq and dk
   const int jt = wave % 4, col = 16 * wave + c16;
   float* parts = p.parts + ((int64_t)(chunk - p.c0) * p.B + b) * 2 * p.H;
@@ -111,127 +132,118 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
     for (int i = threadIdx.x; i < group; i += THREADS) parts[hk * group + i] = parts[p.H + hk * group + i] = 0.0f;
     return;
   }
-  for (int u = threadIdx.x; u < pieces<T>(KD); u += THREADS) {
-    Piece<T> x, y;
-    const Window wk(p.k.stride_t, live), wq(p.q.stride_t, live);
-    load_piece<T, KD>(x, (const T*)p.k.data + (int64_t)s0 * p.k.stride_t + b * p.k.stride_b + hk * p.head, wk, p.width, u);
-    load_piece<T, KD>(y, (const T*)p.q.data + (int64_t)s0 * p.q.stride_t + b * p.q.stride_b + hk * p.head, wq, p.width, u);
-    clear_piece<T, KD>(x, wk, p.width, u);
-    clear_piece<T, KD>(y, wq, p.width, u);
-    put_rows<T, KD>(x, K, u);
-    put_rows<T, KD>(y, Q, u);
+  {
+    Fetch<T, KD, THREADS> fk, fq;
+    fk.load(p.k, s0, b, hk, 0, live);
+    fq.load(p.q, s0, b, hk, 0, live);
+    fk.put(K, p.k, 0, live);
+    fq.put(Q, p.q, 0, live);
   }
+  const int vs = threadIdx.x / (VB / 4), vc = threadIdx.x % (VB / 4) * 4;   // a thread's step and four columns of a block
+  static_assert(C * VB / 4 == THREADS, "a block is four values a thread");
   f32x4 dQ[4] = {}, dK[4] = {};
-  for (int h = hk * group; h < (hk + 1) * group; ++h) {
+  for (int h = hk * group, n = 0; n < group; ++h, ++n) {
     const int64_t at = (int64_t)(chunk - p.c0) * BH + b * p.H + h;
     const char* rec = p.records + at * Rec::BYTES;
     const float *Sg = p.S + at * KD * p.dvp, *dSg = p.dS + at * KD * p.dvp, *Rg = p.R + at * C * p.dvp, *Zg = p.Z + at * C * p.dvp;
-    const T* dyg = (const T*)p.dy.data + (int64_t)s0 * p.dy.stride_t + b * p.dy.stride_b + h * p.dv;
+    const T* dyg = (const T*)p.dy.data + (int64_t)s0 * p.dy.stride_t + b * p.dy.stride_b + (int64_t)h * p.dy.head;
+    const unsigned off_y = (unsigned)(min(vs, live - 1) * (int)p.dy.stride_t);
+    typedef T Quad __attribute__((ext_vector_type(4), aligned(sizeof(T) * 4)));
+    f32x4 z, r, x[2], y[2];
+    Quad q4;
+    const unsigned off_v = (unsigned)(vs * p.dvp + vc) * 4u, off_s = (unsigned)((mine ? col : c16) * p.dvp + 8 * g) * 4u;
+    auto fetch = [&](int v0) {
+      z = *reinterpret_cast<const f32x4*>(near(Zg + v0, off_v));
+      r = *reinterpret_cast<const f32x4*>(near(Rg + v0, off_v));
+      q4 = *reinterpret_cast<const Quad*>(near(dyg, (off_y + (unsigned)min(v0 + vc, p.dy.width - 4)) * (unsigned)sizeof(T)));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[i] = *reinterpret_cast<const f32x4*>(near(Sg + v0 + 4 * i, off_s));
+        y[i] = *reinterpret_cast<const f32x4*>(near(dSg + v0 + 4 * i, off_s));
+      }
+    };
+    auto put = [&](int v0, int buffer) {
+      T* dy = (T*)(lds + L::BLOCK + buffer * L::BLOCK_BYTES);
+      if (vs >= live || v0 + vc >= p.dy.width) q4 = Quad{};
+      *reinterpret_cast<Quad*>(dy + vs * VLD + vc) = q4;
+      put_parts<L::NV>(dy + VA + vs * VLD + vc, VA, z);
+      put_parts<L::NV>(dy + (1 + L::NV) * VA + vs * VLD + vc, VA, r);
+    };
+    fetch(0);
     __syncthreads();   // the head before has been read
     for (int i = threadIdx.x; i < GATES * C; i += THREADS) gate[i] = reinterpret_cast<const float*>(rec + Rec::GATE)[i];
     if (threadIdx.x < C) G[threadIdx.x] = reinterpret_cast<const double*>(rec + Rec::SUMS)[threadIdx.x];
     f32x4 YS[4] = {}, ZS[4] = {}, RS[4] = {}, AA[4] = {};
     float inner = 0.0f;
-    for (int v0 = 0; v0 < p.dvp; v0 += VB) {
-      if (v0) __syncthreads();
-      for (int u = threadIdx.x; u < C * VB / 4; u += THREADS) {   // four values of a step
-        const int s = u / (VB / 4), v = u % (VB / 4) * 4;
-        f32x4 z = {}, r = {}, y = {};
-        if (v0 + v < p.dvp) {
-          z = *reinterpret_cast<const f32x4*>(Zg + s * p.dvp + v0 + v);
-          r = *reinterpret_cast<const f32x4*>(Rg + s * p.dvp + v0 + v);
-        }
+    for (int v0 = 0, buffer = 0; v0 < p.dvp; v0 += VB, buffer ^= 1) {
+      put(v0, buffer);
+      const Op<T, N32> s = cut<T, N32>(x[0], x[1]), ds = cut<T, N32>(y[0], y[1]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (s < live && v0 + v + e < p.dv) y[e] = (float)dyg[(int64_t)s * p.dy.stride_t + v0 + v + e];
-        put_parts<1>(DY + s * VLD + v, 0, y);
-        put_parts<L::NV>(ZL + s * VLD + v, L::VSIZE / (int)sizeof(T), z);
-        put_parts<L::NV>(RL + s * VLD + v, L::VSIZE / (int)sizeof(T), r);
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) inner += x[i][e] * y[i][e];
+      __syncthreads();   // (and the block before the last one has been read)
+      fetch(min(v0 + VB, p.dvp - VB));   // (not under a condition: it would be waited for there)
+      const T *DY = (const T*)(lds + L::BLOCK + buffer * L::BLOCK_BYTES), *ZL = DY + VA, *RL = ZL + L::NV * VA;
+      const auto rj = as_it_stands<N32>(RL + (16 * jt + c16) * VLD, VA, g);
+      Op<T, 1> dy[4];
+      Op<T, N32> zr[4];
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) {
+        dy[rt] = as_it_stands<1>(DY + (16 * rt + c16) * VLD, VA, g);
+        zr[rt] = as_it_stands<N32>(ZL + (16 * rt + c16) * VLD, VA, g);
       }
-      __syncthreads();
+      // (all four tiles: the ones above the diagonal cost less than branches)
+      if (wave < 4) mma(AA, dy, rj);
+      else mma(AA, zr, rj);
+      __builtin_amdgcn_sched_barrier(0);
+      if (mine) {
+        mma(YS, dy, s);
+        mma(ZS, zr, s);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int v = 0; v < VB; v += 32) {
-        if (v0 + v >= p.dvp) break;
-        // R's (waves 0 .. 3) or Z's pairs with column tile jt of R
-        const auto rj = from_parts<N32>(RL + (16 * jt + c16) * VLD + v, L::VSIZE / (int)sizeof(T), g);
-        Op<T, N32> s, ds;
-        if (mine) {
-          f32x4 x[2], y[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int c = v0 + v + 16 * i + 4 * g;
-            x[i] = y[i] = f32x4{};
-            if (c < p.dvp) {
-              x[i] = *reinterpret_cast<const f32x4*>(Sg + col * p.dvp + c);
-              y[i] = *reinterpret_cast<const f32x4*>(dSg + col * p.dvp + c);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) inner += x[i][e] * y[i][e];
-          }
-          s = cut<T, N32>(x[0], x[1]);
-          ds = cut<T, N32>(y[0], y[1]);
-        }
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-          const auto y = from_row(DY + (16 * rt + c16) * VLD + v, g);
-          const auto z = from_parts<N32>(ZL + (16 * rt + c16) * VLD + v, L::VSIZE / (int)sizeof(T), g);
-          if (rt >= jt) {
-            if (wave < 4) mma(AA[rt], y, rj);
-            else mma(AA[rt], z, rj);
-          }
-          if (mine) {
-            mma(YS[rt], y, s);
-            mma(ZS[rt], z, s);
-            mma(RS[rt], from_parts<N32>(RL + (16 * rt + c16) * VLD + v, L::VSIZE / (int)sizeof(T), g), ds);
-          }
-        }
+        for (int rt = 0; rt < 4; ++rt) zr[rt] = as_it_stands<N32>(RL + (16 * rt + c16) * VLD, VA, g);
+        mma(RS, zr, ds);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     __syncthreads();   // the blocks have been read: W1 .. W3 go there
     {
       const int j = 16 * jt + c16;
       const float skj = gate[SK * C + j], bej = gate[BE * C + j];
+      const double Gj = G[j];
       float down = 0.0f, colF = 0.0f;
+      T *first = wave < 4 ? W1 : W3, *second = wave < 4 ? W1q : W3k;
+      const T* rows = wave < 4 ? Q : K;
+      const float* factor = gate + (wave < 4 ? SQ : SK) * C;
+      for (int rt = jt; rt < 4; ++rt) {
+        f32x4 m = {};
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-        f32x4 x = {};
-        if (rt >= jt) {
-#pragma unroll
-          for (int c = 0; c < KD; c += 32)
-            mma(x, from_row((wave < 4 ? Q : K) + (16 * rt + c16) * LD + c, g), from_row(K + j * LD + c, g));
-        }
+        for (int c = 0; c < KD; c += 32) mma(m, from_row(rows + (16 * rt + c16) * LD + c, g), from_row(K + j * LD + c, g));
+        const f32x4 fi = *reinterpret_cast<const f32x4*>(factor + 16 * rt + 4 * g);
+        f32x4 a = rt == 0 ? AA[0] : rt == 1 ? AA[1] : rt == 2 ? AA[2] : AA[3], w1, w2;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * rt + 4 * g + e;
-          float f = 0.0f;
-          if (wave < 4) {
-            float w1 = 0.0f, w2 = 0.0f;
-            if (j <= i) {
-              const float d = expf((float)(G[i] - G[j])), m = x[e] * gate[SQ * C + i] * skj * d;
-              const float dp = AA[rt][e] * bej;
-              down += m * AA[rt][e];
-              f = dp * m;
-              w1 = dp * d * skj;
-              w2 = dp * d * gate[SQ * C + i];
-            }
-            put_parts<L::NM>(W1 + i * WLD + j, L::WSIZE / (int)sizeof(T), w1);
-            put_parts<L::NM>(W2 + j * WLD + i, L::WSIZE / (int)sizeof(T), w2);
-          } else {
-            if (j < i) {
-              const float d = expf((float)(G[i] - G[j])), m = x[e] * gate[SK * C + i] * skj * d;
-              const float dm = -AA[rt][e] * bej;
-              down -= m * AA[rt][e];
-              f = dm * m;
-              put_parts<L::NM>(W3 + i * WLD + j, L::WSIZE / (int)sizeof(T), dm * d * skj);
-              put_parts<L::NM>(W3 + j * WLD + i, L::WSIZE / (int)sizeof(T), dm * d * gate[SK * C + i]);
-            } else if (j == i) {
-              put_parts<L::NM>(W3 + i * WLD + i, L::WSIZE / (int)sizeof(T), 0.0f);
-            }
-          }
+          const bool in = wave < 4 ? j <= i : j < i;
+          const float d = in ? expf((float)(G[i] - Gj)) : 0.0f, u = (wave < 4 ? a[e] : -a[e]) * bej;
+          m[e] *= fi[e] * skj * d;
+          down += m[e] * (wave < 4 ? a[e] : -a[e]);
+          const float f = u * m[e];
+          w1[e] = u * d * skj;
+          w2[e] = u * d * fi[e];
           colF += f;
-          f = over_columns(f);
-          if (c16 == 0) rowF[wave * C + i] = f;
+          const float row = over_columns(f);
+          if (c16 == 0) rowF[wave * C + i] = row;
         }
+        put_parts<L::NM>(first + j * WLD + 16 * rt + 4 * g, WA, w1);
+        put_parts<L::NM>(second + j * WLD + 16 * rt + 4 * g, WA, w2);
+      }
+      for (int rt = 0; rt < jt; ++rt) {   // above the diagonal, as far as the products read
+        const f32x4 zero = {};
+        put_parts<L::NM>(first + j * WLD + 16 * rt + 4 * g, WA, zero);
+        put_parts<L::NM>(second + j * WLD + 16 * rt + 4 * g, WA, zero);
+        if (c16 < 4) rowF[wave * C + 16 * rt + 4 * g + c16] = 0.0f;
       }
       down += __shfl_xor(down, 16);
       colF += __shfl_xor(colF, 16);
@@ -243,9 +255,34 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       }
     }
     inner = wave_sum(inner);
-    if (lane == 0) more[wave] = mine ? inner : 0.0f;
+    if (lane == 0) more[wave] = inner;
     __syncthreads();
     if (mine) {
+      // lower triangles have tiles 0 .. 3 of the first 32 columns and 2, 3 of the others, their transposes 0, 1 of the first and all of the others
+      f32x4 wx[4] = {}, w[4] = {};
+#pragma unroll
+      for (int pb = 0; pb < 2; ++pb) {
+        const auto kc = from_columns<LD>(K, 16 * wave, 32 * pb, lane), qc = from_columns<LD>(Q, 16 * wave, 32 * pb, lane);
+        constexpr int LOW = 4;
+        Op<T, NW> a[LOW];
+        auto products = [&](const T* m, bool transposed, f32x4(&to)[4], const Op<T, 1>& x) {
+          // (what a triangle leaves empty is zero in LDS as far as it is read)
+#pragma unroll
+          for (int rt = 0; rt < 4; ++rt)
+            a[rt] = transposed ? from_parts<NW>(m + (16 * rt + c16) * WLD + 32 * pb, WA, g) : from_part_columns<NW, WLD>(m, WA, 16 * rt, 32 * pb, lane);
+          if (transposed ? pb == 1 : pb == 0) {
+            mma(to, a, x);
+          } else {
+            const Op<T, NW> part[2] = {a[transposed ? 0 : 2], a[transposed ? 1 : 3]};
+            mma(to, part, x, transposed ? 0 : 2);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        products(W1, false, wx, kc);
+        products(W1q, true, w, qc);
+        products(W3, false, w, kc);
+        products(W3k, true, w, kc);
+      }
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) {
         const f32x4 ga = *reinterpret_cast<const f32x4*>(gate + GA * C + 16 * rt + 4 * g);
@@ -253,27 +290,20 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         const f32x4 la = *reinterpret_cast<const f32x4*>(gate + LA * C + 16 * rt + 4 * g);
         const f32x4 sk = *reinterpret_cast<const f32x4*>(gate + SK * C + 16 * rt + 4 * g);
         const f32x4 sq = *reinterpret_cast<const f32x4*>(gate + SQ * C + 16 * rt + 4 * g);
-        const f32x4 y = ga * YS[rt], z = ga * ZS[rt], r = la * RS[rt];
-        f32x4 x = {}, w = {};
-#pragma unroll
-        for (int pb = 0; pb < 2; ++pb) {
-          const auto kc = from_columns<LD>(K, 16 * wave, 32 * pb, lane), qc = from_columns<LD>(Q, 16 * wave, 32 * pb, lane);
-          mma(x, from_parts<NW>(W1 + (16 * rt + c16) * WLD + 32 * pb, L::WSIZE / (int)sizeof(T), g), kc);
-          mma(w, from_parts<NW>(W2 + (16 * rt + c16) * WLD + 32 * pb, L::WSIZE / (int)sizeof(T), g), qc);
-          mma(w, from_parts<NW>(W3 + (16 * rt + c16) * WLD + 32 * pb, L::WSIZE / (int)sizeof(T), g), kc);
-        }
-        dQ[rt] += x + y;
-        dK[rt] += w + be * r - z;
+        const f32x4 ys = ga * YS[rt], zs = ga * ZS[rt], rs = la * RS[rt];
+        dQ[rt] += wx[rt] + ys;
+        dK[rt] += w[rt] + be * rs - zs;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * rt + 4 * g + e;
           const float k = (float)K[i * LD + col] * sk[e], q = (float)Q[i * LD + col] * sq[e];
-          const float first = over_columns(q * y[e] - k * z[e]), second = over_columns(k * r[e]);
+          const float one = over_columns(q * ys[e] - k * zs[e]), two = over_columns(k * rs[e]);
           if (c16 == 0) {
-            dots[wave * C + i] = first;
-            dots[(WAVES + wave) * C + i] = second;
+            dots[wave * C + i] = one;
+            dots[(WAVES + wave) * C + i] = two;
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     __syncthreads();
@@ -340,30 +370,39 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         }
     }
     __syncthreads();
+    if (threadIdx.x < 2 * C) {   // over the waves, with the factors of both norms
+      const int i = threadIdx.x % C, k = threadIdx.x / C;
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < NT; ++w) sum += dots[(k * WAVES + w) * C + i];
+      const float f = gate[(k ? SK : RQ) * C + i];
+      cols[k * C + i] = sum * f * f * (k ? 1.0f : p.scale);
+    }
+    __syncthreads();
   }
   if (!mine || col >= p.dk) return;
 #pragma unroll
-  for (int rt = 0; rt < 4; ++rt)
+  for (int rt = 0; rt < 4; ++rt) {
+    f32x4 dqt = p.scale * dQ[rt], dkt = dK[rt];
+    if (p.normalise) {
+      const f32x4 rq = *reinterpret_cast<const f32x4*>(gate + RQ * C + 16 * rt + 4 * g), rk = *reinterpret_cast<const f32x4*>(gate + SK * C + 16 * rt + 4 * g);
+      const f32x4 a = *reinterpret_cast<const f32x4*>(cols + 16 * rt + 4 * g), c = *reinterpret_cast<const f32x4*>(cols + C + 16 * rt + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = 16 * rt + 4 * g + e;
+        dqt[e] = rq[e] * (dqt[e] - (float)Q[i * LD + col] * a[e]);
+        dkt[e] = rk[e] * (dkt[e] - (float)K[i * LD + col] * c[e]);
+      }
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = 16 * rt + 4 * g + e;
-      float x = p.scale * dQ[rt][e], y = dK[rt][e];
-      if (p.normalise) {
-        float first = 0.0f, second = 0.0f;
-#pragma unroll
-        for (int w = 0; w < NT; ++w) {
-          first += dots[w * C + i];
-          second += dots[(WAVES + w) * C + i];
-        }
-        const float rq = gate[RQ * C + i], rk = gate[SK * C + i];
-        x = rq * (x - (float)Q[i * LD + col] * rq * rq * p.scale * first);
-        y = rk * (y - (float)K[i * LD + col] * rk * rk * second);
-      }
       if (i < steps) {
-        dq[(int64_t)i * p.dq.stride_t] = (T)(i < live ? x : 0.0f);
-        dk[(int64_t)i * p.dkey.stride_t] = (T)(i < live ? y : 0.0f);
+        dq[(int64_t)i * p.dq.stride_t] = (T)(i < live ? dqt[e] : 0.0f);
+        dk[(int64_t)i * p.dkey.stride_t] = (T)(i < live ? dkt[e] : 0.0f);
       }
     }
+  }
 }
 
 }  // namespace
@@ -373,9 +412,13 @@ int mebptt::delta::gradients(const Args& p, int dtype, hipStream_t stream) {
     using T = decltype(t);
     constexpr int KD = decltype(n)::value, BYTES = Layout<T, KD>::BYTES;
     static_assert(BYTES <= 160 * 1024, "LDS of a compute unit");
-    const hipError_t e = allow_dynamic_lds<delta_gradients_kernel<T, KD>>(BYTES);
-    if (e != hipSuccess) return set_error(MEBPTT_EHIP, "LDS of the delta rule: %s", hipGetErrorString(e));
-    delta_gradients_kernel<T, KD><<<(unsigned)((p.c1 - p.c0) * p.B * p.Hk), THREADS, BYTES, stream>>>(p);
-    return launched("delta rule, gradients");
+    auto go = [&](auto shared) {
+      constexpr bool SHARED = decltype(shared)::value;
+      const hipError_t e = allow_dynamic_lds<delta_gradients_kernel<T, KD, SHARED>>(BYTES);
+      if (e != hipSuccess) return set_error(MEBPTT_EHIP, "LDS of the delta rule: %s", hipGetErrorString(e));
+      delta_gradients_kernel<T, KD, SHARED><<<(unsigned)((p.c1 - p.c0) * p.B * p.Hk), THREADS, BYTES, stream>>>(p);
+      return launched("delta rule, gradients");
+    };
+    return p.H > p.Hk ? go(std::true_type{}) : go(std::false_type{});
   });
 }

@@ -74,18 +74,11 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
   using R = Record<T, BACK>;
   char* out = p.records + (int64_t)blockIdx.x * R::BYTES;
 
-  const T* kp = (const T*)p.k.data + s0 * p.k.stride_t + b * p.k.stride_b + (int64_t)hk * p.head;
-  const T* qp = (const T*)p.q.data + s0 * p.q.stride_t + b * p.q.stride_b + (int64_t)hk * p.head;
-  for (int u = threadIdx.x; u < pieces<T>(KD); u += 256) {
-    Piece<T> x, y;
-    const Window wk(p.k.stride_t, live), wq(p.q.stride_t, live);
-    load_piece<T, KD>(x, kp, wk, p.width, u);
-    load_piece<T, KD>(y, qp, wq, p.width, u);
-    clear_piece<T, KD>(x, wk, p.width, u);
-    clear_piece<T, KD>(y, wq, p.width, u);
-    put_rows<T, KD>(x, K, u);
-    put_rows<T, KD>(y, Q, u);
-  }
+  Fetch<T, KD, 256> fk, fq;
+  fk.load(p.k, s0, b, hk, 0, live);
+  fq.load(p.q, s0, b, hk, 0, live);
+  fk.put(K, p.k, 0, live);
+  fq.put(Q, p.q, 0, live);
   if (wave == 0) {   // decays and betas of the steps
     float lg = 0.0f, beta = 0.0f;
     if (lane < live) {
@@ -222,13 +215,13 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void delta_pad_kernel(mebptt_seq from, int B, int Hk, int dk, int width, int s0, int64_t n, T* to) {
+__global__ __launch_bounds__(256) void delta_pad_kernel(mebptt_seq from, int B, int heads, int d, int width, int s0, int64_t n, T* to) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int c = (int)(i % width);
     const int64_t row = i / width;
-    const int h = (int)(row % Hk), b = (int)(row / Hk % B);
-    const int64_t s = s0 + row / Hk / B;
-    to[i] = c < dk ? ((const T*)from.data)[s * from.stride_t + b * from.stride_b + h * dk + c] : (T)0.0f;
+    const int h = (int)(row % heads), b = (int)(row / heads % B);
+    const int64_t s = s0 + row / heads / B;
+    to[i] = c < d ? ((const T*)from.data)[s * from.stride_t + b * from.stride_b + h * d + c] : (T)0.0f;
   }
 }
 
@@ -243,12 +236,12 @@ int launch(const Args& p, hipStream_t stream) {
 
 }  // namespace
 
-int mebptt::delta::pad_rows(const mebptt_seq& from, const Args& p, int dtype, void* to, hipStream_t stream) {
-  const int64_t n = (int64_t)std::min((p.c1 - p.c0) * C, p.t - p.c0 * C) * p.B * p.Hk * p.width;
+int mebptt::delta::pad_rows(const mebptt_seq& from, const Args& p, int heads, int d, int width, int dtype, void* to, hipStream_t stream) {
+  const int64_t n = (int64_t)std::min((p.c1 - p.c0) * C, p.t - p.c0 * C) * p.B * heads * width;
   const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, 256), 1 << 16);
-  if (dtype == MEBPTT_FP32) delta_pad_kernel<float><<<grid, 256, 0, stream>>>(from, p.B, p.Hk, p.dk, p.width, p.c0 * C, n, (float*)to);
-  else delta_pad_kernel<__bf16><<<grid, 256, 0, stream>>>(from, p.B, p.Hk, p.dk, p.width, p.c0 * C, n, (__bf16*)to);
-  return launched("delta rule, rows of q and k");
+  if (dtype == MEBPTT_FP32) delta_pad_kernel<float><<<grid, 256, 0, stream>>>(from, p.B, heads, d, width, p.c0 * C, n, (float*)to);
+  else delta_pad_kernel<__bf16><<<grid, 256, 0, stream>>>(from, p.B, heads, d, width, p.c0 * C, n, (__bf16*)to);
+  return launched("delta rule, rows");
 }
 
 int mebptt::delta::prepare(const Args& p, int dtype, bool back, hipStream_t stream) {

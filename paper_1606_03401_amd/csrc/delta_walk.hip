@@ -9,115 +9,94 @@ using namespace mebptt::delta;
 
 namespace {
 
-// A record's [bytes] from one place to LDS, by way of registers.
+// A record's [bytes] from one place to LDS, by way of registers.  (The last threads' share may be another's: the same bytes twice.)
 template <int BYTES, int THREADS>
 struct Copy {
   static constexpr int N = (BYTES / 16 + THREADS - 1) / THREADS;
   u32x4 v[N];
+  static __device__ inline unsigned at(int i) { return (unsigned)min((i * THREADS + (int)threadIdx.x) * 16, BYTES - 16); }
   __device__ inline void load(const char* from) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int u = i * THREADS + (int)threadIdx.x;
-      if (N * THREADS * 16 == BYTES || u * 16 < BYTES) v[i] = *reinterpret_cast<const u32x4*>(from + u * 16);
-    }
+    for (int i = 0; i < N; ++i) v[i] = *reinterpret_cast<const u32x4*>(near(from, at(i)));
   }
   __device__ inline void put(char* to) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int u = i * THREADS + (int)threadIdx.x;
-      if (N * THREADS * 16 == BYTES || u * 16 < BYTES) *reinterpret_cast<u32x4*>(to + u * 16) = v[i];
-    }
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(to + at(i)) = v[i];
   }
 };
 
-template <typename T, int KD, int W>
-struct Chunk {   // [C][KD] of one of the inputs
-  static constexpr int N = (pieces<T>(KD) + W * WAVE - 1) / (W * WAVE);
-  static constexpr bool ALL = N * W * WAVE == pieces<T>(KD);
-  Piece<T> x[N];
-  __device__ inline void load(const T* p, const Window& w, int width) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int u = i * W * WAVE + (int)threadIdx.x;
-      if (ALL || u < pieces<T>(KD)) load_piece<T, KD>(x[i], p, w, width, u);
-    }
-  }
-  __device__ inline void put(T* rows, const Window& w, int width) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int u = i * W * WAVE + (int)threadIdx.x;
-      if (ALL || u < pieces<T>(KD)) {
-        clear_piece<T, KD>(x[i], w, width, u);
-        put_rows<T, KD>(x[i], rows, u);
-      }
-    }
-  }
-};
-
-// Between a chunk's products: operands of the next one are not to be fetched early, which would take more registers than there are.
+// Nothing is moved across: operands are fetched a product ahead, where that is written, and not all at once, for which there are no registers.
 __device__ inline void next_product() { __builtin_amdgcn_sched_barrier(0); }
 
 __device__ inline f32x4 steps_of(const float* gate, int row, int rt, int g) { return *reinterpret_cast<const f32x4*>(gate + row * C + 16 * rt + 4 * g); }
 
-// A column of a chunk's rows: [rt][e] is step 16 rt + 4 g + e of column `col`.
+// Columns c0 + l % 16 of rows in LDS, as result tiles.
+template <int LD>
+__device__ inline void load_tiles(f32x4 (&x)[4], const __bf16* rows, int c0, int lane) {
+#pragma unroll
+  for (int pb = 0; pb < 2; ++pb) {
+    const Op<__bf16, 1> o = from_columns<LD>(rows, c0, 32 * pb, lane);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[2 * pb + e / 4][e % 4] = (float)o.p[0][e];
+  }
+}
+template <int LD>
+__device__ inline void load_tiles(f32x4 (&x)[4], const float* rows, int c0, int lane) {
+#pragma unroll
+  for (int pb = 0; pb < 2; ++pb) {
+    const Op<float, 1> o = from_columns<LD>(rows, c0, 32 * pb, lane);
+    x[2 * pb] = o.v[0], x[2 * pb + 1] = o.v[1];
+  }
+}
+// Result tiles to `steps` rows of an output, column c0 + l % 16 of `width`, zeros from `live` on.  bf16 rows that are whole vectors of four go there by way of the wave's
+// own 16 columns of LDS, which turns them round, so that a lane has four neighbouring columns.
+constexpr int TURN = 16 * (C + 8);   // values of LDS for it
 template <typename T>
-struct Column {
-  unsigned v[4][4];   // (a register each: two in one would have to be waited for)
-  static __device__ inline unsigned raw(const T* p) {
-    if constexpr (sizeof(T) == 2) return *reinterpret_cast<const unsigned short*>(p);
-    else return *reinterpret_cast<const unsigned*>(p);
-  }
-  __device__ inline void load(const T* p, const Window& w, int col, int g) {
-    if (w.live >= C) {
-      const unsigned off = (unsigned)(4 * g * w.stride + col) * (unsigned)sizeof(T);
-      const int64_t stride = here_uniform(w.stride);
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[rt][e] = raw(near(p + (16 * rt + e) * stride, off));
-    } else {
-      const int first = here(4 * g);
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[rt][e] = raw(near(p, (unsigned)(min(16 * rt + first + e, w.live - 1) * w.stride + col) * (unsigned)sizeof(T)));
-    }
-  }
-  __device__ inline void get(f32x4 (&x)[4], const Window& w, bool there, int g) const {
-#pragma unroll
-    for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[rt][e] = __uint_as_float(sizeof(T) == 2 ? v[rt][e] << 16 : v[rt][e]);
-    if (w.live < C) {
-      const int first = here(4 * g);
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[rt][e] = 16 * rt + first + e < w.live ? x[rt][e] : 0.0f;
-    }
-    if (!there) x[0] = x[1] = x[2] = x[3] = f32x4{};
-  }
-};
-// The first `steps` of a column, zeros from `live` on.
-template <typename T>
-__device__ inline void store_column(T* p, int step, const f32x4 (&x)[4], int steps, int live, int col, int g) {
+__device__ inline void store_tiles(T* p, int step, const f32x4 (&x)[4], int steps, int live, int c0, int width, bool vec, T* turn, int lane) {
+  const int g = lane / 16, i = lane % 16;
   const int64_t stride = here_uniform(step);
-  const unsigned off = (unsigned)(4 * g * (int)stride + col) * (unsigned)sizeof(T);
-  if (live >= C) {
+  if constexpr (sizeof(T) == 2) {
+    if (vec) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4* At;
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt)
+      for (int rt = 0; rt < 4; ++rt)
+        *reinterpret_cast<bf16x4*>(turn + i * (C + 8) + 16 * rt + 4 * g) = bf16x4{(__bf16)x[rt][0], (__bf16)x[rt][1], (__bf16)x[rt][2], (__bf16)x[rt][3]};
+      __builtin_amdgcn_wave_barrier();
+      const unsigned off = (unsigned)(i * (int)stride + c0 + 4 * g) * 2u;
+      s16x4 y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) *near(p + (16 * rt + e) * stride, off) = (T)x[rt][e];
-  } else {
-    const int first = here(4 * g);
+      for (int rt = 0; rt < 4; ++rt) y[rt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(turn + (4 * g + i / 4) * (C + 8) + 16 * rt + i % 4 * 4));
+      if (c0 + 4 * g < width) {
+        if (live >= C) {
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt)
+          for (int rt = 0; rt < 4; ++rt) *reinterpret_cast<s16x4*>(near(p + 16 * rt * stride, off)) = y[rt];
+        } else {
+          const int first = here(i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int s = 16 * rt + first + e;
-        if (s < steps) *near(p + (16 * rt + e) * stride, off) = (T)(s < live ? x[rt][e] : 0.0f);
+          for (int rt = 0; rt < 4; ++rt)
+            if (16 * rt + first < steps) *reinterpret_cast<s16x4*>(near(p + 16 * rt * stride, off)) = 16 * rt + first < live ? y[rt] : s16x4{};
+        }
       }
+      return;
+    }
   }
+  if (c0 + i >= width) return;
+  const unsigned off = (unsigned)(4 * g * (int)stride + c0 + i) * (unsigned)sizeof(T);
+  const int first = here(4 * g);
+#pragma unroll
+  for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int s = 16 * rt + first + e;
+      if (s < steps) *near(p + (16 * rt + e) * stride, off) = (T)(s < live ? x[rt][e] : 0.0f);
+    }
+}
+// Zeros where a whole chunk is behind the sequence's end.
+template <typename T>
+__device__ inline void store_zeros(T* p, int64_t stride, int steps, int col, int width, int g) {
+  if (col < width)
+    for (int s = g; s < steps; s += 4) p[s * stride + col] = (T)0.0f;
 }
 
 // Waves of a SIMD: the registers of one of four waves that hold 128 rows and fetch the next chunk's are more than half.
@@ -155,46 +134,46 @@ __device__ inline void store_state(const f32x4 (&S)[NT], float* to, int rows, in
 
 // ---- forward -------------------------------------------------------------------------------------------
 
-template <typename T, int KD, bool AGAIN>
+template <typename T, int KD, int W, bool AGAIN>
 struct Layout {   // of LDS
   static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), T_ = AGAIN ? Q : Q + Lds<T>::row_bytes(KD), P = T_ + frag_bytes<T>(T_PARTS),
-                       GATE = AGAIN ? P : P + frag_bytes<T>(P_PARTS), BYTES = GATE + WALK_GATES * C * 4;
+                       GATE = AGAIN ? P : P + frag_bytes<T>(P_PARTS), V = GATE + WALK_GATES * C * 4, Y = V + Lds<T>::row_bytes(16 * W),
+                       BYTES = AGAIN || sizeof(T) == 4 ? Y : Y + W * TURN * 2;
 };
 
 // AGAIN: the backward pass's recomputation, from its records, of S and R of every chunk.
 template <typename T, int KD, int W, bool AGAIN>
 __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kernel(Args p) {
   extern __shared__ __align__(16) char lds[];
-  using L = Layout<T, KD, AGAIN>;
+  using L = Layout<T, KD, W, AGAIN>;
   using R = Record<T, AGAIN>;
   constexpr int LD = Lds<T>::ld(KD), NT = KD / 16;
-  T *K = reinterpret_cast<T*>(lds + L::K), *Q = reinterpret_cast<T*>(lds + L::Q);
+  constexpr bool DEEP = per_simd<KD, W>() == 1;
+  T *K = reinterpret_cast<T*>(lds + L::K), *Q = reinterpret_cast<T*>(lds + L::Q), *VL = reinterpret_cast<T*>(lds + L::V);
   const float* gate = reinterpret_cast<const float*>(lds + L::GATE);
   const int bh = blockIdx.x, b = bh / p.H, h = bh % p.H, hk = h / (p.H / p.Hk), BH = p.B * p.H;
-  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16;
-  const int col = (blockIdx.y * W + wave) * 16 + lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE, g = lane / 16;
+  const int c0 = blockIdx.y * W * 16, col = c0 + 16 * wave + lane % 16;
   const bool there = col < p.dv;
-  const int end = ends_at(p, b), near_col = min(col, p.dv - 1);
+  const int end = ends_at(p, b);
 
   f32x4 S[NT];
   load_state(S, p.from ? p.from + (int64_t)bh * p.dk * p.dv : nullptr, p.dk, p.dv, col, g);
 
-  Chunk<T, KD, W> ck, cq;
+  Fetch<T, KD, W * WAVE> ck, cq;
+  Fetch<T, 16 * W, W * WAVE> cv;
   Copy<frag_bytes<T>(T_PARTS), W * WAVE> ct;
   Copy<frag_bytes<T>(P_PARTS), W * WAVE> cp;
   Copy<WALK_GATES * C * 4, W * WAVE> cg;
-  Column<T> V;
   auto fetch = [&](int chunk) {
-    const int64_t s0 = (int64_t)chunk * C;
-    const int live = min(end - chunk * C, C);
-    if (live <= 0) return;
-    ck.load((const T*)p.k.data + s0 * p.k.stride_t + b * p.k.stride_b + hk * p.head, Window(p.k.stride_t, live), p.width);
-    if (!AGAIN) cq.load((const T*)p.q.data + s0 * p.q.stride_t + b * p.q.stride_b + hk * p.head, Window(p.q.stride_t, live), p.width);
+    const int live = end - chunk * C;
+    ck.load(p.k, (int64_t)chunk * C, b, hk, 0, live);
+    if (!AGAIN) cq.load(p.q, (int64_t)chunk * C, b, hk, 0, live);
+    cv.load(p.v, (int64_t)chunk * C, b, h, c0, live);
     const char* rec = p.records + ((int64_t)(chunk - p.c0) * BH + bh) * R::BYTES;
     ct.load(rec + R::T_);
     if (!AGAIN) cp.load(rec + R::P);
     cg.load(rec + R::GATE);
-    V.load((const T*)p.v.data + s0 * p.v.stride_t + b * p.v.stride_b + h * p.dv, Window(p.v.stride_t, live), near_col, g);
   };
   if (p.c0 < p.c1) fetch(p.c0);
   for (int chunk = p.c0; chunk < p.c1; ++chunk) {
@@ -203,69 +182,114 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kerne
       store_state(S, p.states + ((int64_t)(chunk / p.keep) * BH + bh) * p.dk * p.dv, p.dk, p.dv, col, g);
     T* y = AGAIN ? nullptr : (T*)p.y.data + (int64_t)s0 * p.y.stride_t + b * p.y.stride_b + h * p.dv;
     if (live <= 0) {   // behind the sequence's end: zeros, the state stays
-      if (!AGAIN && there)
-        for (int s = g; s < steps; s += 4) y[(int64_t)s * p.y.stride_t + col] = (T)0.0f;
+      if (!AGAIN) store_zeros(y, p.y.stride_t, steps, col, p.dv, g);
       continue;
     }
     if (AGAIN && col < p.dvp) store_state(S, p.S + ((int64_t)(chunk - p.c0) * BH + bh) * KD * p.dvp, KD, p.dvp, col, g);
     __syncthreads();   // the chunk before has been read
-    ck.put(K, Window(p.k.stride_t, live), p.width);
+    ck.put(K, p.k, 0, live);
     ct.put(lds + L::T_);
-    if (!AGAIN) cq.put(Q, Window(p.q.stride_t, live), p.width), cp.put(lds + L::P);
+    if (!AGAIN) cq.put(Q, p.q, 0, live), cp.put(lds + L::P);
     cg.put(lds + L::GATE);
-    f32x4 X[4];
-    V.get(X, Window(p.v.stride_t, live), there, g);
+    cv.put(VL, p.v, c0, live);
     __syncthreads();
-    if (chunk + 1 < p.c1) fetch(chunk + 1);
+    fetch(min(chunk + 1, p.c1 - 1));   // (not under a condition, see there)
     next_product();
 
-    f32x4 KS[4] = {}, Y[4] = {};
+    // K S and Q S: tiles 0 .. 3 and 4 .. 7
+    constexpr int ROWS = AGAIN ? 4 : 8;
+    f32x4 KQ[ROWS] = {};
+    auto rows = [&](Op<T, 1>(&o)[4], int rt0, int n) {
 #pragma unroll
-    for (int n = 0; n < NT / 2; ++n) {
-      const Op<T, 3> s = cut<T, 3>(S[2 * n], S[2 * n + 1]);
+      for (int rt = 0; rt < 4; ++rt) o[rt] = from_row((rt0 ? Q : K) + (16 * rt + lane % 16) * LD + 32 * n, g);
+    };
+    if constexpr (DEEP) {   // operands a product ahead, and cut while it runs
+      Op<T, 1> a[2][ROWS / 4][4];
+      Op<T, 3> s[2];
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-        mma(KS[rt], from_row(K + (16 * rt + lane % 16) * LD + 32 * n, g), s);
-        if (!AGAIN) mma(Y[rt], from_row(Q + (16 * rt + lane % 16) * LD + 32 * n, g), s);
-      }
-      next_product();
-    }
-    f32x4 U[4] = {};
-    {
+      for (int r = 0; r < ROWS; r += 4) rows(a[0][r / 4], r, 0);
+      s[0] = cut<T, 3>(S[0], S[1]);
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) X[rt] -= steps_of(gate, GA_SK, rt, g) * KS[rt];
-      const Op<T, 3> Xp[2] = {cut<T, 3>(X[0], X[1]), cut<T, 3>(X[2], X[3])};
+      for (int n = 0; n < NT / 2; ++n) {
+        if (n + 1 < NT / 2) {
 #pragma unroll
-      for (int pb = 0; pb < 2; ++pb)
+          for (int r = 0; r < ROWS; r += 4) rows(a[(n + 1) % 2][r / 4], r, n + 1);
+        }
+        next_product();
 #pragma unroll
-        for (int rt = 2 * pb; rt < 4; ++rt) mma(U[rt], from_frag<T, T_PARTS>(lds + L::T_, lower(rt, pb), lane), Xp[pb]);
-    }
-    next_product();
-    if (AGAIN && col < p.dvp) store_state(U, p.R + ((int64_t)(chunk - p.c0) * BH + bh) * C * p.dvp, C, p.dvp, col, g);
-#pragma unroll
-    for (int rt = 0; rt < 4; ++rt) U[rt] *= steps_of(gate, BE, rt, g);
-    if constexpr (!AGAIN) {
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt) Y[rt] *= steps_of(gate, GA_SQ, rt, g);
-#pragma unroll
-      for (int pb = 0; pb < 2; ++pb) {
-        const Op<T, 2> u = cut<T, 2>(U[2 * pb], U[2 * pb + 1]);
-#pragma unroll
-        for (int rt = 2 * pb; rt < 4; ++rt) mma(Y[rt], from_frag<T, P_PARTS>(lds + L::P, lower(rt, pb), lane), u);
+        for (int r = 0; r < ROWS; r += 4) mma(KQ, a[n % 2][r / 4], s[n % 2], r);
+        if (n + 1 < NT / 2) s[(n + 1) % 2] = cut<T, 3>(S[2 * n + 2], S[2 * n + 3]);
         next_product();
       }
-      if (there) store_column(y, (int)p.y.stride_t, Y, steps, live, col, g);
+    } else {
+#pragma unroll
+      for (int n = 0; n < NT / 2; ++n) {
+        Op<T, 1> a[4];
+        rows(a, 0, n);
+        const Op<T, 3> s = cut<T, 3>(S[2 * n], S[2 * n + 1]);
+        mma(KQ, a, s);
+        if constexpr (!AGAIN) {
+          rows(a, 4, n);
+          mma(KQ, a, s, 4);
+        }
+        next_product();
+      }
+    }
+    f32x4 X[4];
+    load_tiles<Lds<T>::ld(16 * W)>(X, VL, 16 * wave, lane);
+    f32x4 U[4] = {};
+    {
+      Op<T, T_PARTS> t0[4], t1[2];
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) t0[rt] = from_frag<T, T_PARTS>(lds + L::T_, lower(rt, 0), lane);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) X[rt] -= steps_of(gate, GA_SK, rt, g) * KQ[rt];
+      next_product();
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) t1[rt] = from_frag<T, T_PARTS>(lds + L::T_, lower(2 + rt, 1), lane);
+      mma(U, t0, cut<T, 3>(X[0], X[1]));
+      next_product();
+      mma(U, t1, cut<T, 3>(X[2], X[3]), 2);
+    }
+    Op<T, 1> columns[DEEP ? 2 : 1][NT];
+    auto fetch_columns = [&](int pb) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) columns[DEEP ? pb : 0][n] = from_columns<LD>(K, 16 * n, 32 * pb, lane);
+    };
+    if (AGAIN && col < p.dvp) store_state(U, p.R + ((int64_t)(chunk - p.c0) * BH + bh) * C * p.dvp, C, p.dvp, col, g);
+    if constexpr (!AGAIN) {
+      f32x4 Y[4];
+      Op<T, P_PARTS> p0[4], p1[2];
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) p0[rt] = from_frag<T, P_PARTS>(lds + L::P, lower(rt, 0), lane);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) {
+        Y[rt] = steps_of(gate, GA_SQ, rt, g) * KQ[4 + rt];
+        U[rt] *= steps_of(gate, BE, rt, g);
+      }
+      if (DEEP) next_product();
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) p1[rt] = from_frag<T, P_PARTS>(lds + L::P, lower(2 + rt, 1), lane);
+      mma(Y, p0, cut<T, 2>(U[0], U[1]));
+      next_product();
+      if (DEEP) fetch_columns(0);
+      mma(Y, p1, cut<T, 2>(U[2], U[3]), 2);
+      store_tiles(y, (int)p.y.stride_t, Y, steps, live, c0 + 16 * wave, p.dv, p.vec_out, reinterpret_cast<T*>(lds + L::Y) + wave * TURN, lane);
+      next_product();
+    } else {
+      if (DEEP) fetch_columns(0);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) U[rt] *= steps_of(gate, BE, rt, g);
     }
     const float last = gate[GA * C + C - 1];
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) U[rt] *= steps_of(gate, LA_SK, rt, g);
 #pragma unroll
     for (int n = 0; n < NT; ++n) S[n] *= last;
 #pragma unroll
     for (int pb = 0; pb < 2; ++pb) {
-      U[2 * pb] *= steps_of(gate, LA_SK, 2 * pb, g);
-      U[2 * pb + 1] *= steps_of(gate, LA_SK, 2 * pb + 1, g);
-      const Op<T, 3> u = cut<T, 3>(U[2 * pb], U[2 * pb + 1]);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) mma(S[n], from_columns<LD>(K, 16 * n, 32 * pb, lane), u);
+      if (!DEEP || pb == 0) fetch_columns(DEEP ? 1 : pb);
+      mma(S, columns[DEEP ? pb : 0], cut<T, 3>(U[2 * pb], U[2 * pb + 1]));
       next_product();
     }
   }
@@ -274,103 +298,132 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kerne
 
 // ---- back ----------------------------------------------------------------------------------------------
 
-template <typename T, int KD>
+template <typename T, int KD, int W>
 struct BackLayout {   // of LDS: the record's part from T^T on as it is
   using R = Record<T, true>;
   static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), REC = Q + Lds<T>::row_bytes(KD), RBYTES = R::GATE + WALK_GATES * C * 4 - R::TT,
-                       T_ = REC, P = REC + R::P - R::TT, GATE = REC + R::GATE - R::TT, BYTES = REC + RBYTES;
+                       T_ = REC, P = REC + R::P - R::TT, GATE = REC + R::GATE - R::TT, N = REC + RBYTES, Y = N + Lds<T>::row_bytes(16 * W),
+                       BYTES = sizeof(T) == 4 ? Y : Y + W * TURN * 2;
 };
 
 template <typename T, int KD, int W>
 __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_back_kernel(Args p) {
   extern __shared__ __align__(16) char lds[];
-  using L = BackLayout<T, KD>;
+  using L = BackLayout<T, KD, W>;
   using R = Record<T, true>;
   constexpr int LD = Lds<T>::ld(KD), NT = KD / 16;
-  T *K = reinterpret_cast<T*>(lds + L::K), *Q = reinterpret_cast<T*>(lds + L::Q);
+  constexpr bool DEEP = per_simd<KD, W>() == 1;
+  T *K = reinterpret_cast<T*>(lds + L::K), *Q = reinterpret_cast<T*>(lds + L::Q), *NL = reinterpret_cast<T*>(lds + L::N);
   const float* gate = reinterpret_cast<const float*>(lds + L::GATE);
   const int bh = blockIdx.x, b = bh / p.H, h = bh % p.H, hk = h / (p.H / p.Hk), BH = p.B * p.H;
-  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16;
-  const int col = (blockIdx.y * W + wave) * 16 + lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE, g = lane / 16;
+  const int c0 = blockIdx.y * W * 16, col = c0 + 16 * wave + lane % 16;
   const bool there = col < p.dv;
-  const int end = ends_at(p, b), near_col = min(col, p.dv - 1);
+  const int end = ends_at(p, b);
 
   f32x4 S[NT];   // gradient of the state behind the chunk
   load_state(S, p.from ? p.from + (int64_t)bh * p.dk * p.dv : nullptr, p.dk, p.dv, col, g);
 
-  Chunk<T, KD, W> ck, cq;
+  Fetch<T, KD, W * WAVE> ck, cq;
+  Fetch<T, 16 * W, W * WAVE> cn;
   Copy<L::RBYTES, W * WAVE> cr;
-  Column<T> N;
   auto fetch = [&](int chunk) {
-    const int64_t s0 = (int64_t)chunk * C;
-    const int live = min(end - chunk * C, C);
-    if (live <= 0) return;
-    ck.load((const T*)p.k.data + s0 * p.k.stride_t + b * p.k.stride_b + hk * p.head, Window(p.k.stride_t, live), p.width);
-    cq.load((const T*)p.q.data + s0 * p.q.stride_t + b * p.q.stride_b + hk * p.head, Window(p.q.stride_t, live), p.width);
+    const int live = end - chunk * C;
+    ck.load(p.k, (int64_t)chunk * C, b, hk, 0, live);
+    cq.load(p.q, (int64_t)chunk * C, b, hk, 0, live);
+    cn.load(p.dy, (int64_t)chunk * C, b, h, c0, live);
     cr.load(p.records + ((int64_t)(chunk - p.c0) * BH + bh) * R::BYTES + R::TT);
-    N.load((const T*)p.dy.data + s0 * p.dy.stride_t + b * p.dy.stride_b + h * p.dv, Window(p.dy.stride_t, live), near_col, g);
   };
   if (p.c0 < p.c1) fetch(p.c1 - 1);
   for (int chunk = p.c1 - 1; chunk >= p.c0; --chunk) {
     const int s0 = chunk * C, live = min(end - s0, C), steps = min(p.t - s0, C);
     T* dv = (T*)p.dval.data + (int64_t)s0 * p.dval.stride_t + b * p.dval.stride_b + h * p.dv;
     if (live <= 0) {
-      if (there)
-        for (int s = g; s < steps; s += 4) dv[(int64_t)s * p.dval.stride_t + col] = (T)0.0f;
-      if (chunk > p.c0) fetch(chunk - 1);
+      store_zeros(dv, p.dval.stride_t, steps, col, p.dv, g);
+      fetch(max(chunk - 1, p.c0));
       continue;
     }
     if (col < p.dvp) store_state(S, p.dS + ((int64_t)(chunk - p.c0) * BH + bh) * KD * p.dvp, KD, p.dvp, col, g);
     __syncthreads();   // the chunk before has been read
-    ck.put(K, Window(p.k.stride_t, live), p.width);
-    cq.put(Q, Window(p.q.stride_t, live), p.width);
+    ck.put(K, p.k, 0, live);
+    cq.put(Q, p.q, 0, live);
     cr.put(lds + L::REC);
-    f32x4 dY[4];
-    N.get(dY, Window(p.dy.stride_t, live), there, g);
+    cn.put(NL, p.dy, c0, live);
     __syncthreads();
-    if (chunk > p.c0) fetch(chunk - 1);
+    fetch(max(chunk - 1, p.c0));   // (not under a condition, see there)
     next_product();
 
     f32x4 U[4] = {};
+    {
+      Op<T, 1> a[2][4];
+      Op<T, 3> x[2];
+      auto rows = [&](Op<T, 1>(&o)[4], int n) {
 #pragma unroll
-    for (int n = 0; n < NT / 2; ++n) {
-      const Op<T, 3> s = cut<T, 3>(S[2 * n], S[2 * n + 1]);
+        for (int rt = 0; rt < 4; ++rt) o[rt] = from_row(K + (16 * rt + lane % 16) * LD + 32 * n, g);
+      };
+      rows(a[0], 0);
+      x[0] = cut<T, 3>(S[0], S[1]);
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) mma(U[rt], from_row(K + (16 * rt + lane % 16) * LD + 32 * n, g), s);
-      next_product();
+      for (int n = 0; n < NT / 2; ++n) {
+        if (n + 1 < NT / 2) rows(a[(n + 1) % 2], n + 1);
+        next_product();
+        mma(U, a[n % 2], x[n % 2]);
+        if (n + 1 < NT / 2) x[(n + 1) % 2] = cut<T, 3>(S[2 * n + 2], S[2 * n + 3]);
+        next_product();
+      }
     }
+    f32x4 dY[4];
+    load_tiles<Lds<T>::ld(16 * W)>(dY, NL, 16 * wave, lane);
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) U[rt] *= steps_of(gate, LA_SK, rt, g);
+    {
+      Op<T, PT_PARTS> p0[2], p1[4];
 #pragma unroll
-    for (int pb = 0; pb < 2; ++pb) {
-      const Op<T, 1> y = cut<T, 1>(dY[2 * pb], dY[2 * pb + 1]);   // (exact: dY has T's bits)
+      for (int rt = 0; rt < 2; ++rt) p0[rt] = from_frag<T, PT_PARTS>(lds + L::P, upper(rt, 0), lane);
 #pragma unroll
-      for (int rt = 0; rt < 2 * pb + 2; ++rt) mma(U[rt], from_frag<T, PT_PARTS>(lds + L::P, upper(rt, pb), lane), y);
+      for (int rt = 0; rt < 4; ++rt) p1[rt] = from_frag<T, PT_PARTS>(lds + L::P, upper(rt, 1), lane);
+      mma(U, p0, cut<T, 1>(dY[0], dY[1]));   // (exact: dY has T's bits)
+      mma(U, p1, cut<T, 1>(dY[2], dY[3]));
       next_product();
     }
     f32x4 Z[4] = {};
+    {
+      Op<T, T_PARTS> t0[2], t1[4];
 #pragma unroll
-    for (int pb = 0; pb < 2; ++pb) {
-      const Op<T, 3> u = cut<T, 3>(U[2 * pb] * steps_of(gate, BE, 2 * pb, g), U[2 * pb + 1] * steps_of(gate, BE, 2 * pb + 1, g));
+      for (int rt = 0; rt < 2; ++rt) t0[rt] = from_frag<T, T_PARTS>(lds + L::T_, upper(rt, 0), lane);
 #pragma unroll
-      for (int rt = 0; rt < 2 * pb + 2; ++rt) mma(Z[rt], from_frag<T, T_PARTS>(lds + L::T_, upper(rt, pb), lane), u);
+      for (int rt = 0; rt < 4; ++rt) t1[rt] = from_frag<T, T_PARTS>(lds + L::T_, upper(rt, 1), lane);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) U[rt] *= steps_of(gate, BE, rt, g);
+      mma(Z, t0, cut<T, 3>(U[0], U[1]));
+      mma(Z, t1, cut<T, 3>(U[2], U[3]));
       next_product();
     }
     if (col < p.dvp) store_state(Z, p.Z + ((int64_t)(chunk - p.c0) * BH + bh) * C * p.dvp, C, p.dvp, col, g);
-    if (there) store_column(dv, (int)p.dval.stride_t, Z, steps, live, col, g);
+    store_tiles(dv, (int)p.dval.stride_t, Z, steps, live, c0 + 16 * wave, p.dv, p.vec_out, reinterpret_cast<T*>(lds + L::Y) + wave * TURN, lane);
     const float last = gate[GA * C + C - 1];
 #pragma unroll
     for (int n = 0; n < NT; ++n) S[n] *= last;
 #pragma unroll
-    for (int pb = 0; pb < 2; ++pb) {
-      const Op<T, 3> y = cut<T, 3>(dY[2 * pb] * steps_of(gate, GA_SQ, 2 * pb, g), dY[2 * pb + 1] * steps_of(gate, GA_SQ, 2 * pb + 1, g));
-      const Op<T, 3> z = cut<T, 3>(-Z[2 * pb] * steps_of(gate, GA_SK, 2 * pb, g), -Z[2 * pb + 1] * steps_of(gate, GA_SK, 2 * pb + 1, g));
+    for (int rt = 0; rt < 4; ++rt) {
+      dY[rt] *= steps_of(gate, GA_SQ, rt, g);
+      Z[rt] *= -steps_of(gate, GA_SK, rt, g);
+    }
+    {
+      Op<T, 1> a[DEEP ? 2 : 1][NT];   // columns of q, of k, the first 32 steps, then the others
+      auto columns = [&](int i) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        mma(S[n], from_columns<LD>(Q, 16 * n, 32 * pb, lane), y);
-        mma(S[n], from_columns<LD>(K, 16 * n, 32 * pb, lane), z);
+        for (int n = 0; n < NT; ++n) a[DEEP ? i % 2 : 0][n] = from_columns<LD>(i % 2 ? K : Q, 16 * n, 32 * (i / 2), lane);
+      };
+      if (DEEP) columns(0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (!DEEP) columns(i);
+        else if (i < 3) columns(i + 1);
+        if (DEEP) next_product();
+        mma(S, a[DEEP ? i % 2 : 0], i % 2 ? cut<T, 3>(Z[i - 1], Z[i]) : cut<T, 3>(dY[i], dY[i + 1]));
+        next_product();
       }
-      next_product();
     }
   }
   if (p.to && there) store_state(S, p.to + (int64_t)bh * p.dk * p.dv, p.dk, p.dv, col, g);
@@ -390,8 +443,8 @@ bool eight_waves(const Args& p) { return p.dv > 64 && p.B * p.H >= 128; }
 
 template <typename T, int KD, int W>
 int forward(const Args& p, bool again, hipStream_t stream) {
-  if (!again) return launch<delta_walk_kernel<T, KD, W, false>>(p, W, Layout<T, KD, false>::BYTES, "delta rule, forward", stream);
-  return launch<delta_walk_kernel<T, KD, W, true>>(p, W, Layout<T, KD, true>::BYTES, "delta rule, recomputation", stream);
+  if (!again) return launch<delta_walk_kernel<T, KD, W, false>>(p, W, Layout<T, KD, W, false>::BYTES, "delta rule, forward", stream);
+  return launch<delta_walk_kernel<T, KD, W, true>>(p, W, Layout<T, KD, W, true>::BYTES, "delta rule, recomputation", stream);
 }
 
 }  // namespace
@@ -408,7 +461,7 @@ int mebptt::delta::walk_back(const Args& p, int dtype, hipStream_t stream) {
   return with_size(dtype, p.dk, [&](auto t, auto n) {
     using T = decltype(t);
     constexpr int KD = decltype(n)::value;
-    if (eight_waves(p)) return launch<delta_walk_back_kernel<T, KD, 8>>(p, 8, BackLayout<T, KD>::BYTES, "delta rule, back", stream);
-    return launch<delta_walk_back_kernel<T, KD, 4>>(p, 4, BackLayout<T, KD>::BYTES, "delta rule, back", stream);
+    if (eight_waves(p)) return launch<delta_walk_back_kernel<T, KD, 8>>(p, 8, BackLayout<T, KD, 8>::BYTES, "delta rule, back", stream);
+    return launch<delta_walk_back_kernel<T, KD, 4>>(p, 4, BackLayout<T, KD, 4>::BYTES, "delta rule, back", stream);
   });
 }

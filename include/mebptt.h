@@ -682,9 +682,10 @@ typedef struct {
   int32_t reserved;        /* 0 */
 } mebptt_adamw_tensor;
 typedef struct {
-  float rate, beta1, beta2, eps, decay; /* beta1, beta2 0 .. below 1; eps >= 0 */
-  uint32_t seed;
+  double rate, beta1, beta2, eps, decay; /* beta1, beta2 0 .. below 1; eps >= 0 */
   int64_t step;            /* 1, 2, ... */
+  uint32_t seed;
+  int32_t reserved;        /* 0 */
 } mebptt_adamw_desc;
 /* `tensors` (host) are read during a call only; at most 65536 of them, 2^42 values in all.  prepare writes what the other calls need to know of
  * the tensors into `table` (device, 256-byte aligned), to be called again when a pointer or size changes.  The others only look at the number and sizes of

@@ -147,7 +147,8 @@ class mebptt_adamw_tensor(C.Structure):
 
 
 class mebptt_adamw_desc(C.Structure):
-    _fields_ = [(n, C.c_float) for n in ("rate", "beta1", "beta2", "eps", "decay")] + [("seed", C.c_uint32), ("step", C.c_int64)]
+    _fields_ = ([(n, C.c_double) for n in ("rate", "beta1", "beta2", "eps", "decay")]
+                + [("step", C.c_int64), ("seed", C.c_uint32), ("reserved", C.c_int32)])
 
 
 # name -> (restype, argtypes): every symbol the header declares
@@ -1024,7 +1025,7 @@ def make_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=N
 
 def make_adamw_desc(rate: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, decay: float = 0.01, step: int = 1,
                     seed: int = 0) -> mebptt_adamw_desc:
-    return mebptt_adamw_desc(rate, beta1, beta2, eps, decay, seed & 0xFFFFFFFF, step)
+    return mebptt_adamw_desc(rate, beta1, beta2, eps, decay, step, seed & 0xFFFFFFFF, 0)
 
 
 def mebptt_adamw_table_bytes(tensors: AdamwTensors) -> int:

@@ -62,7 +62,7 @@ __device__ inline float value_of(uint32_t code, float scale) {
 // One of the two neighbours of x / scale; `bits16` says which where the part cut off leaves a choice.
 template <bool SIGNED>
 __device__ inline uint32_t code_of(float x, float scale, uint32_t bits16) {
-  const float u = scale > 0.0f ? fabsf(x) / scale : fabsf(x);
+  const float u = scale > 0.0f ? fabsf(x) / scale : fabsf(x);   // (at most 1.875 and a rounding)
   const int code = (int)((__float_as_uint(u) + (bits16 << 4)) >> 20) - ((SIGNED ? 112 : 96) << 3);
   if constexpr (SIGNED) {
     constexpr float LEAST = 1.125f * 0x1p-15f;
@@ -79,7 +79,7 @@ struct Step {
   const float *factor, *rate;
   const int64_t* step;
   int64_t desc_step;
-  float desc_rate, beta1, beta2, eps, decay, log1, log2;   // logarithms of beta1 and beta2
+  float desc_rate, beta1, beta2, rest1, rest2, eps, decay, log1, log2;   // rest1, log1: 1 - beta1 and beta1's logarithm, from 64 bits
   uint32_t seed;
 };
 
@@ -121,7 +121,7 @@ __device__ inline void write_codes(uint8_t* p, float* scale, int64_t left, bool 
   for (int e = 0; e < V; ++e) top = max_or_nan(top, fabsf(v[e]));
 #pragma unroll
   for (int m = SHARE / 2; m; m >>= 1) top = max_or_nan(top, __shfl_xor(top, m));
-  const float s = top / 1.875f;
+  const float s = top * (1.0f / 1.875f);
   if (left <= 0) return;
   if (first) *scale = s;
   uint32_t c[V];
@@ -138,6 +138,8 @@ __device__ inline void write_codes(uint8_t* p, float* scale, int64_t left, bool 
     if (e < left) p[e] = (uint8_t)c[e];
 }
 
+// One rounding to an operation, so that codes do not depend on what a compiler joins.
+#pragma clang fp contract(off)
 template <bool VEC>
 __device__ inline void piece_step(const Step& p, const Entry& t, int64_t start, float factor) {
   const float rate = p.rate ? *p.rate : p.desc_rate;
@@ -164,8 +166,8 @@ __device__ inline void piece_step(const Step& p, const Entry& t, int64_t start, 
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       g[e] *= factor;
-      m[e] = p.beta1 * m[e] + (1.0f - p.beta1) * g[e];
-      v[e] = p.beta2 * v[e] + (1.0f - p.beta2) * (g[e] * g[e]);
+      m[e] = p.beta1 * m[e] + p.rest1 * g[e];
+      v[e] = p.beta2 * v[e] + p.rest2 * (g[e] * g[e]);
       w[e] = w[e] * keep - rate * (m[e] * inv1) / (sqrtf(v[e] * inv2) + p.eps);
     }
     write<float, VEC>(t.param + at, left, w);
@@ -184,6 +186,8 @@ __device__ inline void piece_step(const Step& p, const Entry& t, int64_t start, 
     }
   }
 }
+
+#pragma clang fp contract(fast)
 
 __global__ __launch_bounds__(THREADS) void adamw_step_kernel(Step p, int64_t pieces) {
   const float factor = p.factor ? *p.factor : 1.0f;
@@ -348,14 +352,14 @@ int mebptt_adamw_norm(const mebptt_adamw_tensor* tensors, int32_t count, const v
 int mebptt_adamw_step(const mebptt_adamw_desc* d, const mebptt_adamw_tensor* tensors, int32_t count, const void* table, size_t table_bytes,
                       const float* factor, const float* rate, const int64_t* step, void* stream) {
   if (!d) return set_error(MEBPTT_EINVAL, "desc is NULL");
-  if (!(d->beta1 >= 0.0f && d->beta1 < 1.0f && d->beta2 >= 0.0f && d->beta2 < 1.0f)) return set_error(MEBPTT_EINVAL, "beta1 and beta2 must be 0 .. below 1");
-  if (!(d->eps >= 0.0f)) return set_error(MEBPTT_EINVAL, "eps must not be negative");
+  if (!(d->beta1 >= 0.0 && d->beta1 < 1.0 && d->beta2 >= 0.0 && d->beta2 < 1.0)) return set_error(MEBPTT_EINVAL, "beta1 and beta2 must be 0 .. below 1");
+  if (!(d->eps >= 0.0)) return set_error(MEBPTT_EINVAL, "eps must not be negative");
   if (!step && d->step < 1) return set_error(MEBPTT_EINVAL, "step must be at least 1");
   int64_t pieces;
   const int rc = check_table(table, table_bytes, tensors, count, &pieces);
   if (rc || !pieces) return rc;
-  const Step p = {(const Entry*)table, (const int32_t*)((const char*)table + map_at(count)), factor, rate, step, d->step, d->rate, d->beta1, d->beta2,
-                  d->eps, d->decay, (float)log((double)d->beta1), (float)log((double)d->beta2), d->seed};
+  const Step p = {(const Entry*)table, (const int32_t*)((const char*)table + map_at(count)), factor, rate, step, d->step, (float)d->rate, (float)d->beta1, (float)d->beta2,
+                  (float)(1.0 - d->beta1), (float)(1.0 - d->beta2), (float)d->eps, (float)d->decay, (float)log(d->beta1), (float)log(d->beta2), d->seed};
   adamw_step_kernel<<<grid_of(pieces, 1 << 22), THREADS, 0, (hipStream_t)stream>>>(p, pieces);
   return launched("mebptt_adamw_step");
 }

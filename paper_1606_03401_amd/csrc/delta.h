@@ -260,8 +260,12 @@ struct Args {
   float scale, eps;
   int c0, c1;                           // chunks of this launch
   char* records;                        // [c1 - c0][B H]
+  int seg;                              // chunks of a segment: a launch walks over its segments side by side
   const float* from;                    // states [B][H][dk][dv] before the first chunk, or NULL
+  float* starts;                        // [segments][B][H][start_rows][start_width] before every segment; NULL: one segment, that starts with `from`
+  int start_rows, start_width;
   float* to;                            // after the last one, or NULL
+  float *moves, *ends;                  // of a survey: [segments][B][H][KD][KD] and [KD][dvp], see there
   float* states;                        // kept states, or NULL
   int keep;                             // every keep-th chunk's
   float *S, *R, *Z, *dS;                // of every chunk of the launch: [KD][dvp] and [C][dvp]
@@ -275,7 +279,9 @@ __device__ inline int ends_at(const Args& p, int b) { return p.lengths ? min(max
 // Rows that are no whole vectors, copied to ones that are: the launch's steps, [..][B][heads][r.width].
 int pad_rows(const mebptt_seq& from, const Args& p, int heads, int d, int width, int dtype, void* to, hipStream_t stream);
 int prepare(const Args& p, int dtype, bool back, hipStream_t stream);
-int walk(const Args& p, int dtype, bool again, hipStream_t stream);        // `again`: S and R of every chunk instead of y
+enum { WALK = 0, AGAIN = 1, SURVEY = 2 };   // y; S and R of every chunk; what segments do to the state
+int walk(const Args& p, int dtype, int mode, hipStream_t stream);
+int join_segments(const Args& p, int dtype, hipStream_t stream);
 int walk_back(const Args& p, int dtype, hipStream_t stream);
 int gradients(const Args& p, int dtype, hipStream_t stream);
 

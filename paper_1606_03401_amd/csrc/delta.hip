@@ -58,26 +58,42 @@ size_t row_bytes(const mebptt_delta_desc* d, int64_t chunks, int heads, int n) {
 }
 
 struct Forward {
-  int64_t slab;
-  size_t records, carry, total;
+  int64_t slab, seg;           // chunks of a launch, and of its segments
+  size_t records, carry, moves, ends, starts, total;
 };
+// Segments of a launch: as many as fill the chip with the workgroups that walk, of at least eight chunks, since what segments do to the state has to be
+// found out first, which costs as much again as the walk (dk + dv columns instead of dv, without y).
+int64_t segment_of(const mebptt_delta_desc* d, int64_t chunks) {
+  const int64_t groups = std::max<int64_t>(1, (int64_t)d->B * d->H * ceil_div(d->dv, 64));
+  const int64_t n = std::min<int64_t>(256 / groups, chunks / 8);
+  return n < 3 ? std::max<int64_t>(chunks, 1) : ceil_div(chunks, n);
+}
 Forward forward_layout(const mebptt_delta_desc* d) {
-  const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d);
+  const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d), KD = padded(d->dk), dvp = ceil_div(d->dv, 32) * 32;
   Forward f = {};
   f.slab = std::min(std::max<int64_t>(1, RECORDS / std::max<int64_t>(BH, 1)), std::max<int64_t>(chunks, 1));
+  f.seg = segment_of(d, f.slab);
+  const int64_t segments = ceil_div(f.slab, f.seg);
   f.records = align_up((size_t)(std::min(f.slab, chunks) * BH) * record_bytes(d->dtype, false));
   f.carry = f.slab < chunks ? state_bytes(d) : 0;
-  f.total = f.records + f.carry + 2 * row_bytes(d, f.slab, d->Hk, d->dk) + row_bytes(d, f.slab, d->H, d->dv);
+  if (segments > 1) {
+    f.moves = align_up((size_t)((segments - 1) * BH) * KD * KD * 4);
+    f.ends = align_up((size_t)((segments - 1) * BH) * KD * dvp * 4);
+    f.starts = align_up((size_t)(segments * BH) * KD * dvp * 4);
+  }
+  f.total = f.records + f.carry + f.moves + f.ends + f.starts + 2 * row_bytes(d, f.slab, d->Hk, d->dk) + row_bytes(d, f.slab, d->H, d->dv);
   return f;
 }
 struct Backward {
-  int64_t slab;
+  int64_t slab, seg;
   size_t records, states, rows, carry, parts, total;
 };
+// A stretch after the other, or, where there is little in one, as many at a time as have 512 chunks in all.
 Backward backward_layout(const mebptt_delta_desc* d) {
   const int64_t BH = (int64_t)d->B * d->H, chunks = chunks_of(d), dvp = ceil_div(d->dv, 32) * 32;
   Backward w = {};
-  w.slab = std::min<int64_t>(d->stretch / C, std::max<int64_t>(chunks, 1));
+  w.seg = d->stretch / C;
+  w.slab = std::min(w.seg * std::max<int64_t>(1, 512 / std::max<int64_t>(w.seg * BH, 1)), std::max<int64_t>(chunks, 1));
   const size_t n = (size_t)(std::min(w.slab, chunks) * BH);
   w.records = align_up(n * record_bytes(d->dtype, true));
   w.states = align_up(n * padded(d->dk) * dvp * 4);
@@ -279,18 +295,23 @@ int mebptt_delta_forward(const mebptt_delta_desc* d, const mebptt_delta_inputs* 
   const int64_t chunks = chunks_of(d);
   float* carry = (float*)((char*)workspace + f.records);
   if (!chunks) {
-    p.from = in->h0, p.to = h_out;
-    return h_out ? walk(p, d->dtype, false, s) : MEBPTT_OK;
+    p.from = in->h0, p.to = h_out, p.seg = 1;
+    return h_out ? walk(p, d->dtype, WALK, s) : MEBPTT_OK;
   }
   for (int64_t c = 0; c < chunks; c += f.slab) {
-    p.c0 = (int)c, p.c1 = (int)std::min(c + f.slab, chunks);
+    p.c0 = (int)c, p.c1 = (int)std::min(c + f.slab, chunks), p.seg = (int)f.seg;
     p.from = c ? carry : in->h0;
     p.to = p.c1 < chunks ? carry : h_out;
     char* room = (char*)workspace + f.records + f.carry;
+    p.moves = (float*)room, p.ends = (float*)(room + f.moves);
+    p.starts = p.c1 - p.c0 > p.seg ? (float*)(room + f.moves + f.ends) : nullptr, p.start_rows = padded(d->dk), p.start_width = p.dvp;
+    room += f.moves + f.ends + f.starts;
     if ((rc = rows_of(&p.q, p, d, in->q, d->Hk, d->dk, room, f.slab, s)) || (rc = rows_of(&p.k, p, d, in->k, d->Hk, d->dk, room, f.slab, s)) ||
         (rc = rows_of(&p.v, p, d, in->v, d->H, d->dv, room, f.slab, s)))
       return rc;
-    if ((rc = prepare(p, d->dtype, false, s)) || (rc = walk(p, d->dtype, false, s))) return rc;
+    if ((rc = prepare(p, d->dtype, false, s))) return rc;
+    if (p.starts && ((rc = walk(p, d->dtype, SURVEY, s)) || (rc = join_segments(p, d->dtype, s)))) return rc;
+    if ((rc = walk(p, d->dtype, WALK, s))) return rc;
   }
   return MEBPTT_OK;
 }
@@ -341,9 +362,11 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
         (rc = rows_of(&p.v, p, d, in->v, d->H, d->dv, room, w.slab, s)) || (rc = rows_of(&p.dy, p, d, dy, d->H, d->dv, room, w.slab, s)))
       return rc;
     if ((rc = prepare(p, d->dtype, true, s))) return rc;
-    p.from = (const float*)states + slab * BH * d->dk * d->dv;
+    const int64_t state = BH * d->dk * d->dv;
+    p.seg = (int)w.seg;
+    p.starts = (float*)states + p.c0 / p.seg * state, p.start_rows = d->dk, p.start_width = d->dv;   // (read only)
     p.to = nullptr;
-    if ((rc = walk(p, d->dtype, true, s))) return rc;
+    if ((rc = walk(p, d->dtype, AGAIN, s))) return rc;
     p.from = p.c1 == chunks ? dh_out : carry;
     p.to = slab ? carry : grads->dh0;
     if ((rc = walk_back(p, d->dtype, s)) || (rc = gradients(p, d->dtype, s))) return rc;

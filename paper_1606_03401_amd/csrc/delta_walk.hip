@@ -50,7 +50,7 @@ __device__ inline void load_tiles(f32x4 (&x)[4], const float* rows, int c0, int 
 }
 // Result tiles to `steps` rows of an output, column c0 + l % 16 of `width`, zeros from `live` on.  bf16 rows that are whole vectors of four go there by way of the wave's
 // own 16 columns of LDS, which turns them round, so that a lane has four neighbouring columns.
-constexpr int TURN = 16 * (C + 8);   // values of LDS for it
+constexpr int TURN_LD = C + 8, TURN = 16 * TURN_LD;   // values of LDS for it
 template <typename T>
 __device__ inline void store_tiles(T* p, int step, const f32x4 (&x)[4], int steps, int live, int c0, int width, bool vec, T* turn, int lane) {
   const int g = lane / 16, i = lane % 16;
@@ -61,12 +61,12 @@ __device__ inline void store_tiles(T* p, int step, const f32x4 (&x)[4], int step
       typedef __attribute__((address_space(3))) s16x4* At;
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt)
-        *reinterpret_cast<bf16x4*>(turn + i * (C + 8) + 16 * rt + 4 * g) = bf16x4{(__bf16)x[rt][0], (__bf16)x[rt][1], (__bf16)x[rt][2], (__bf16)x[rt][3]};
+        *reinterpret_cast<bf16x4*>(turn + i * TURN_LD + 16 * rt + 4 * g) = bf16x4{(__bf16)x[rt][0], (__bf16)x[rt][1], (__bf16)x[rt][2], (__bf16)x[rt][3]};
       __builtin_amdgcn_wave_barrier();
       const unsigned off = (unsigned)(i * (int)stride + c0 + 4 * g) * 2u;
       s16x4 y[4];
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) y[rt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(turn + (4 * g + i / 4) * (C + 8) + 16 * rt + i % 4 * 4));
+      for (int rt = 0; rt < 4; ++rt) y[rt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(turn + (4 * g + i / 4) * TURN_LD + 16 * rt + i % 4 * 4));
       if (c0 + 4 * g < width) {
         if (live >= C) {
 #pragma unroll
@@ -100,8 +100,8 @@ __device__ inline void store_zeros(T* p, int64_t stride, int steps, int col, int
 }
 
 // Waves of a SIMD: the registers of one of four waves that hold 128 rows and fetch the next chunk's are more than half.
-template <int KD, int W>
-constexpr int per_simd() { return W == 4 && KD == 128 ? 1 : 2; }
+template <int KD, int W, int MODE>
+constexpr int per_simd() { return W == 4 && KD == 128 && MODE != SURVEY ? 1 : 2; }
 
 // The state's tiles: rows 16 n + 4 g + e of column `col`, of `rows` rows with `width` columns.
 template <int NT>
@@ -134,31 +134,48 @@ __device__ inline void store_state(const f32x4 (&S)[NT], float* to, int rows, in
 
 // ---- forward -------------------------------------------------------------------------------------------
 
-template <typename T, int KD, int W, bool AGAIN>
+template <typename T, int KD, int W, int MODE>
 struct Layout {   // of LDS
-  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), T_ = AGAIN ? Q : Q + Lds<T>::row_bytes(KD), P = T_ + frag_bytes<T>(T_PARTS),
-                       GATE = AGAIN ? P : P + frag_bytes<T>(P_PARTS), V = GATE + WALK_GATES * C * 4, Y = V + Lds<T>::row_bytes(16 * W),
-                       BYTES = AGAIN || sizeof(T) == 4 ? Y : Y + W * TURN * 2;
+  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), T_ = MODE ? Q : Q + Lds<T>::row_bytes(KD), P = T_ + frag_bytes<T>(T_PARTS),
+                       GATE = MODE ? P : P + frag_bytes<T>(P_PARTS), V = GATE + WALK_GATES * C * 4, Y = V + Lds<T>::row_bytes(16 * W),
+                       BYTES = MODE || sizeof(T) == 4 ? Y : Y + W * TURN * 2;
 };
 
-// AGAIN: the backward pass's recomputation, from its records, of S and R of every chunk.
-template <typename T, int KD, int W, bool AGAIN>
-__global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kernel(Args p) {
+// WALK: y.  AGAIN: the backward pass's recomputation, from its records, of S and R of every chunk.
+// SURVEY: S behind a segment is linear in S before it, A S + B.  Workgroups of the first columns walk from S = 0 (the first segment: from what it
+// is) and leave B in `ends`, the others from the columns of I without a v and leave A in `moves`.  For few sequences: with A and B of every segment joined
+// one after another the segments can be walked side by side.
+template <typename T, int KD, int W, int MODE>
+__global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk_kernel(Args p) {
   extern __shared__ __align__(16) char lds[];
-  using L = Layout<T, KD, W, AGAIN>;
-  using R = Record<T, AGAIN>;
+  using L = Layout<T, KD, W, MODE>;
+  using R = Record<T, MODE == AGAIN>;
   constexpr int LD = Lds<T>::ld(KD), NT = KD / 16;
-  constexpr bool DEEP = per_simd<KD, W>() == 1;
+  constexpr bool DEEP = per_simd<KD, W, MODE>() == 1;
   T *K = reinterpret_cast<T*>(lds + L::K), *Q = reinterpret_cast<T*>(lds + L::Q), *VL = reinterpret_cast<T*>(lds + L::V);
   const float* gate = reinterpret_cast<const float*>(lds + L::GATE);
   const int bh = blockIdx.x, b = bh / p.H, h = bh % p.H, hk = h / (p.H / p.Hk), BH = p.B * p.H;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE, g = lane / 16;
-  const int c0 = blockIdx.y * W * 16, col = c0 + 16 * wave + lane % 16;
+  const int blocks = (p.dv + 16 * W - 1) / (16 * W);
+  const bool unit = MODE == SURVEY && blockIdx.y >= blocks;   // columns of I
+  const int c0 = (blockIdx.y - (unit ? blocks : 0)) * W * 16, col = c0 + 16 * wave + lane % 16;
   const bool there = col < p.dv;
-  const int end = ends_at(p, b);
+  const int end = ends_at(p, b), segment = blockIdx.z, first = p.c0 + segment * p.seg, behind = min(first + p.seg, p.c1);
+  if (unit && segment == 0) return;   // (its start is known)
 
   f32x4 S[NT];
-  load_state(S, p.from ? p.from + (int64_t)bh * p.dk * p.dv : nullptr, p.dk, p.dv, col, g);
+  if (unit) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[n][e] = 16 * n + 4 * g + e == col ? 1.0f : 0.0f;
+  } else if (MODE == SURVEY ? segment == 0 : !p.starts) {
+    load_state(S, p.from ? p.from + (int64_t)bh * p.dk * p.dv : nullptr, p.dk, p.dv, col, g);
+    // (a copy for the walk, whose last segment may end where the first one started)
+    if (MODE == SURVEY && col < p.dvp) store_state(S, p.starts + (int64_t)bh * KD * p.dvp, KD, p.dvp, col, g);
+  } else {
+    load_state(S, MODE == SURVEY ? nullptr : p.starts + ((int64_t)segment * BH + bh) * p.start_rows * p.start_width, p.start_rows, p.start_width, col, g);
+  }
 
   Fetch<T, KD, W * WAVE> ck, cq;
   Fetch<T, 16 * W, W * WAVE> cv;
@@ -168,36 +185,36 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kerne
   auto fetch = [&](int chunk) {
     const int live = end - chunk * C;
     ck.load(p.k, (int64_t)chunk * C, b, hk, 0, live);
-    if (!AGAIN) cq.load(p.q, (int64_t)chunk * C, b, hk, 0, live);
-    cv.load(p.v, (int64_t)chunk * C, b, h, c0, live);
+    if (MODE == WALK) cq.load(p.q, (int64_t)chunk * C, b, hk, 0, live);
+    if (!unit) cv.load(p.v, (int64_t)chunk * C, b, h, c0, live);
     const char* rec = p.records + ((int64_t)(chunk - p.c0) * BH + bh) * R::BYTES;
     ct.load(rec + R::T_);
-    if (!AGAIN) cp.load(rec + R::P);
+    if (MODE == WALK) cp.load(rec + R::P);
     cg.load(rec + R::GATE);
   };
-  if (p.c0 < p.c1) fetch(p.c0);
-  for (int chunk = p.c0; chunk < p.c1; ++chunk) {
+  if (first < behind) fetch(first);
+  for (int chunk = first; chunk < behind; ++chunk) {
     const int s0 = chunk * C, live = min(end - s0, C), steps = min(p.t - s0, C);
-    if (p.states && chunk % p.keep == 0 && there)
+    if (MODE == WALK && p.states && chunk % p.keep == 0 && there)
       store_state(S, p.states + ((int64_t)(chunk / p.keep) * BH + bh) * p.dk * p.dv, p.dk, p.dv, col, g);
-    T* y = AGAIN ? nullptr : (T*)p.y.data + (int64_t)s0 * p.y.stride_t + b * p.y.stride_b + h * p.dv;
+    T* y = MODE ? nullptr : (T*)p.y.data + (int64_t)s0 * p.y.stride_t + b * p.y.stride_b + h * p.dv;
     if (live <= 0) {   // behind the sequence's end: zeros, the state stays
-      if (!AGAIN) store_zeros(y, p.y.stride_t, steps, col, p.dv, g);
+      if (MODE == WALK) store_zeros(y, p.y.stride_t, steps, col, p.dv, g);
       continue;
     }
-    if (AGAIN && col < p.dvp) store_state(S, p.S + ((int64_t)(chunk - p.c0) * BH + bh) * KD * p.dvp, KD, p.dvp, col, g);
+    if (MODE == AGAIN && col < p.dvp) store_state(S, p.S + ((int64_t)(chunk - p.c0) * BH + bh) * KD * p.dvp, KD, p.dvp, col, g);
     __syncthreads();   // the chunk before has been read
     ck.put(K, p.k, 0, live);
     ct.put(lds + L::T_);
-    if (!AGAIN) cq.put(Q, p.q, 0, live), cp.put(lds + L::P);
+    if (MODE == WALK) cq.put(Q, p.q, 0, live), cp.put(lds + L::P);
     cg.put(lds + L::GATE);
-    cv.put(VL, p.v, c0, live);
+    if (!unit) cv.put(VL, p.v, c0, live);
     __syncthreads();
-    fetch(min(chunk + 1, p.c1 - 1));   // (not under a condition, see there)
+    fetch(min(chunk + 1, behind - 1));   // (not under a condition, see there)
     next_product();
 
     // K S and Q S: tiles 0 .. 3 and 4 .. 7
-    constexpr int ROWS = AGAIN ? 4 : 8;
+    constexpr int ROWS = MODE ? 4 : 8;
     f32x4 KQ[ROWS] = {};
     auto rows = [&](Op<T, 1>(&o)[4], int rt0, int n) {
 #pragma unroll
@@ -228,15 +245,15 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kerne
         rows(a, 0, n);
         const Op<T, 3> s = cut<T, 3>(S[2 * n], S[2 * n + 1]);
         mma(KQ, a, s);
-        if constexpr (!AGAIN) {
+        if constexpr (MODE == WALK) {
           rows(a, 4, n);
           mma(KQ, a, s, 4);
         }
         next_product();
       }
     }
-    f32x4 X[4];
-    load_tiles<Lds<T>::ld(16 * W)>(X, VL, 16 * wave, lane);
+    f32x4 X[4] = {};
+    if (!unit) load_tiles<Lds<T>::ld(16 * W)>(X, VL, 16 * wave, lane);
     f32x4 U[4] = {};
     {
       Op<T, T_PARTS> t0[4], t1[2];
@@ -256,8 +273,8 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kerne
 #pragma unroll
       for (int n = 0; n < NT; ++n) columns[DEEP ? pb : 0][n] = from_columns<LD>(K, 16 * n, 32 * pb, lane);
     };
-    if (AGAIN && col < p.dvp) store_state(U, p.R + ((int64_t)(chunk - p.c0) * BH + bh) * C * p.dvp, C, p.dvp, col, g);
-    if constexpr (!AGAIN) {
+    if (MODE == AGAIN && col < p.dvp) store_state(U, p.R + ((int64_t)(chunk - p.c0) * BH + bh) * C * p.dvp, C, p.dvp, col, g);
+    if constexpr (MODE == WALK) {
       f32x4 Y[4];
       Op<T, P_PARTS> p0[4], p1[2];
 #pragma unroll
@@ -293,7 +310,13 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_kerne
       next_product();
     }
   }
-  if (p.to && there) store_state(S, p.to + (int64_t)bh * p.dk * p.dv, p.dk, p.dv, col, g);
+  if constexpr (MODE == SURVEY) {
+    const int64_t at = (int64_t)segment * BH + bh;
+    if (unit && col < KD) store_state(S, p.moves + at * KD * KD, KD, KD, col, g);
+    if (!unit && col < p.dvp) store_state(S, p.ends + at * KD * p.dvp, KD, p.dvp, col, g);
+  } else if (p.to && there && behind == p.c1) {
+    store_state(S, p.to + (int64_t)bh * p.dk * p.dv, p.dk, p.dv, col, g);
+  }
 }
 
 // ---- back ----------------------------------------------------------------------------------------------
@@ -307,12 +330,12 @@ struct BackLayout {   // of LDS: the record's part from T^T on as it is
 };
 
 template <typename T, int KD, int W>
-__global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_back_kernel(Args p) {
+__global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, WALK>())) void delta_walk_back_kernel(Args p) {
   extern __shared__ __align__(16) char lds[];
   using L = BackLayout<T, KD, W>;
   using R = Record<T, true>;
   constexpr int LD = Lds<T>::ld(KD), NT = KD / 16;
-  constexpr bool DEEP = per_simd<KD, W>() == 1;
+  constexpr bool DEEP = per_simd<KD, W, WALK>() == 1;
   T *K = reinterpret_cast<T*>(lds + L::K), *Q = reinterpret_cast<T*>(lds + L::Q), *NL = reinterpret_cast<T*>(lds + L::N);
   const float* gate = reinterpret_cast<const float*>(lds + L::GATE);
   const int bh = blockIdx.x, b = bh / p.H, h = bh % p.H, hk = h / (p.H / p.Hk), BH = p.B * p.H;
@@ -429,31 +452,91 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W>())) void delta_walk_back_
   if (p.to && there) store_state(S, p.to + (int64_t)bh * p.dk * p.dv, p.dk, p.dv, col, g);
 }
 
+// ---- segments ------------------------------------------------------------------------------------------
+
+// States before all segments but the first, one after another: S <- A S + B.  A wave has 16 rows of 16 columns, waves give each other theirs in LDS.
+template <int KD>
+__global__ __launch_bounds__(KD * 4) void delta_join_segments_kernel(Args p, int segments) {
+  constexpr int NT = KD / 16, LD = 20;
+  __shared__ __align__(16) float S[2][KD][LD];
+  const int bh = blockIdx.x, BH = p.B * p.H, wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16, c16 = lane % 16;
+  const int c0 = blockIdx.y * 16;
+  const unsigned off = (unsigned)((16 * wave + 4 * g) * p.dvp + c0 + c16), row = (unsigned)((16 * wave + c16) * KD + 4 * g);
+  f32x4 x, A[NT] = {};
+  auto of = [&](const float* m, int s) { return m + ((int64_t)s * BH + bh) * KD * p.dvp; };
+  auto rows = [&](int s) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) A[n] = *reinterpret_cast<const f32x4*>(p.moves + ((int64_t)s * BH + bh) * KD * KD + row + 16 * n);
+  };
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = of(p.ends, 0)[off + e * p.dvp];
+  if (segments > 2) rows(1);
+  for (int s = 0; s + 1 < segments; ++s) {
+    if (s) {
+      f32x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = of(p.ends, s)[off + e * p.dvp];
+      f32x4 sum[2] = {};
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[n % 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(A[n][e], S[s % 2][16 * n + 4 * g + e][c16], sum[n % 2], 0, 0, 0);
+      x = y + (sum[0] + sum[1]);
+      rows(min(s + 1, segments - 2));
+    }
+    float* to = p.starts + ((int64_t)(s + 1) * BH + bh) * KD * p.dvp;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      to[off + e * p.dvp] = x[e];
+      S[(s + 1) % 2][16 * wave + 4 * g + e][c16] = x[e];
+    }
+    __syncthreads();
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------
+
 template <auto Kernel>
-int launch(const Args& p, int W, int bytes, const char* what, hipStream_t stream) {
+int launch(const Args& p, int W, int bytes, const char* what, hipStream_t stream, int columns, int segments = 1) {
   const hipError_t e = allow_dynamic_lds<Kernel>(bytes);
   if (e != hipSuccess) return set_error(MEBPTT_EHIP, "LDS of the delta rule: %s", hipGetErrorString(e));
-  const dim3 grid((unsigned)(p.B * p.H), (unsigned)ceil_div(p.dv, 16 * W));
+  const dim3 grid((unsigned)(p.B * p.H), (unsigned)columns, (unsigned)segments);
   Kernel<<<grid, W * WAVE, bytes, stream>>>(p);
   return launched(what);
 }
 
-// 128 columns in one workgroup, which reads a chunk once; in two where there are compute units to spare.
-bool eight_waves(const Args& p) { return p.dv > 64 && p.B * p.H >= 128; }
+// 128 columns in one workgroup, which reads a chunk once and whose waves hide each other's latencies; in two, whose waves fetch operands ahead, where there
+// are compute units for both (10000 x 1 x 16 heads of 128 x 128 in eight segments: 165 us with eight waves, 102 with four).
+bool eight_waves(const Args& p, int segments) { return p.dv > 64 && (int64_t)p.B * p.H * segments > 128; }
 
 template <typename T, int KD, int W>
-int forward(const Args& p, bool again, hipStream_t stream) {
-  if (!again) return launch<delta_walk_kernel<T, KD, W, false>>(p, W, Layout<T, KD, W, false>::BYTES, "delta rule, forward", stream);
-  return launch<delta_walk_kernel<T, KD, W, true>>(p, W, Layout<T, KD, W, true>::BYTES, "delta rule, recomputation", stream);
+int forward(const Args& p, int mode, int segments, hipStream_t stream) {
+  const int columns = (int)ceil_div(p.dv, 16 * W);
+  if (mode == WALK) return launch<delta_walk_kernel<T, KD, W, WALK>>(p, W, Layout<T, KD, W, WALK>::BYTES, "delta rule, forward", stream, columns, segments);
+  return launch<delta_walk_kernel<T, KD, W, AGAIN>>(p, W, Layout<T, KD, W, AGAIN>::BYTES, "delta rule, recomputation", stream, columns, segments);
 }
 
 }  // namespace
 
-int mebptt::delta::walk(const Args& p, int dtype, bool again, hipStream_t stream) {
+int mebptt::delta::walk(const Args& p, int dtype, int mode, hipStream_t stream) {
+  const int segments = (int)std::max<int64_t>(1, ceil_div(p.c1 - p.c0, p.seg));
   return with_size(dtype, p.dk, [&](auto t, auto n) {
     using T = decltype(t);
     constexpr int KD = decltype(n)::value;
-    return eight_waves(p) ? forward<T, KD, 8>(p, again, stream) : forward<T, KD, 4>(p, again, stream);
+    if (mode == SURVEY) {   // (of the last segment nothing has to be known)
+      const int columns = (int)ceil_div(p.dv, 64) + (int)ceil_div(KD, 64);
+      return launch<delta_walk_kernel<T, KD, 4, SURVEY>>(p, 4, Layout<T, KD, 4, SURVEY>::BYTES, "delta rule, survey", stream, columns, segments - 1);
+    }
+    return eight_waves(p, segments) ? forward<T, KD, 8>(p, mode, segments, stream) : forward<T, KD, 4>(p, mode, segments, stream);
+  });
+}
+
+int mebptt::delta::join_segments(const Args& p, int dtype, hipStream_t stream) {
+  const int segments = (int)ceil_div(p.c1 - p.c0, p.seg);
+  return with_size(dtype, p.dk, [&](auto, auto n) {
+    constexpr int KD = decltype(n)::value;
+    delta_join_segments_kernel<KD><<<dim3((unsigned)(p.B * p.H), (unsigned)(p.dvp / 16)), KD * 4, 0, stream>>>(p, segments);
+    return launched("delta rule, segments");
   });
 }
 
@@ -461,7 +544,7 @@ int mebptt::delta::walk_back(const Args& p, int dtype, hipStream_t stream) {
   return with_size(dtype, p.dk, [&](auto t, auto n) {
     using T = decltype(t);
     constexpr int KD = decltype(n)::value;
-    if (eight_waves(p)) return launch<delta_walk_back_kernel<T, KD, 8>>(p, 8, BackLayout<T, KD, 8>::BYTES, "delta rule, back", stream);
-    return launch<delta_walk_back_kernel<T, KD, 4>>(p, 4, BackLayout<T, KD, 4>::BYTES, "delta rule, back", stream);
+    if (eight_waves(p, 1)) return launch<delta_walk_back_kernel<T, KD, 8>>(p, 8, BackLayout<T, KD, 8>::BYTES, "delta rule, back", stream, (int)ceil_div(p.dv, 128));
+    return launch<delta_walk_back_kernel<T, KD, 4>>(p, 4, BackLayout<T, KD, 4>::BYTES, "delta rule, back", stream, (int)ceil_div(p.dv, 64));
   });
 }

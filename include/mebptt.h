@@ -604,7 +604,7 @@ typedef struct {
 typedef struct {
   mebptt_seq dq, dk, dv, db;
   mebptt_seq da;           /* written if there is an a */
-  float *dA, *da_bias;     /* [H], with activate and an a; may be NULL */
+  float *dA, *da_bias;     /* [H], with activate; zeros without an a; may be NULL */
   float* dh0;              /* may be NULL */
 } mebptt_delta_grads;
 /* Bytes of the states that a forward call keeps for a backward call; of a forward call's workspace, or (backward != 0) of one that does for

@@ -371,7 +371,7 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
     p.to = slab ? carry : grads->dh0;
     if ((rc = walk_back(p, d->dtype, s)) || (rc = gradients(p, d->dtype, s))) return rc;
   }
-  if (!in->a.data || !d->activate || (!grads->dA && !grads->da_bias)) return MEBPTT_OK;
+  if (!grads->dA && !grads->da_bias) return MEBPTT_OK;   // (zeros without an a, which an a of no steps cannot be told from)
   const int64_t cols[2] = {d->H, d->H};
   float* const outs[2] = {grads->dA, grads->da_bias};
   return sum_parts(parts, chunks * d->B, 2, cols, outs, s);

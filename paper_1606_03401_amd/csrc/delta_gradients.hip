@@ -346,7 +346,7 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         ((T*)p.db.data)[s * p.db.stride_t + b * p.db.stride_b + h] = (T)(!in ? 0.0f : p.activate ? dbeta * beta * (1.0f - beta) : dbeta);
       }
       dlog = wave_sum(dlog);
-      da = wave_sum(da);
+      da = wave_sum(p.activate ? da : 0.0f);
       if (lane == 0) {
         parts[h] = dlog;
         parts[p.H + h] = da;

@@ -1,0 +1,177 @@
+"""GPU parity of the norms around a block with the gate and the residual's scale, through the C ABI's binding: rows and groups of one and odd sizes, both types of
+each tensor, strided and unaligned rows, everything that may be left out, in place, rows around an output left alone.
+
+Tolerances: sums of up to 16384 squares or products in trees of 32 bits, two norms one after the other: 2^-17 of the norm (placed.near); sums over rows are
+as long as there are rows.  A gradient behind a norm is what is left when its part along the norm's output is taken away (of one column: nearly nothing), and every
+term has been rounded: the terms' sizes count."""
+import numpy as np
+import pytest
+import torch
+from placed import DEV, NAN, TORCH, Placed, down, near, room, up
+
+from oracle import delta as od
+from paper_1606_03401_amd import binding as mb
+
+pytestmark = pytest.mark.gpu
+
+CODE = {"fp32": mb.FP32, "bf16": mb.BF16}
+SIZES = [(1, 1, 1), (3, 7, 7), (5, 64, 16), (2, 513, 27), (4, 650, 13), (3, 1024, 128), (2, 2048, 2048), (3, 2049, 683), (2, 4096, 128), (2, 8192, 4096), (1, 8200, 1640), (2, 16384, 128),
+         (1, 16383, 5461), (4103, 40, 8), (3, 96, 96), (2, 24, 2), (1200, 1032, 516)]
+
+
+class _Call:
+    def __init__(self, rows, width, group, x_dtype, r_dtype, layout="plain", gate=True, residual=True, scale=0.8):
+        m = self.m = Placed(rows * 7919 + width, layout)
+        X, R = TORCH[x_dtype], TORCH[r_dtype]
+        self.group, self.scale, s = group, scale, (rows, width)
+        self.x, self.z = m.normal(s, 0.7, X), m.normal(s, 1.0, X) if gate else None
+        self.w, self.wn = up(1 + 0.2 * m.rng.standard_normal(width)), up(1 + 0.2 * m.rng.standard_normal(width)) if residual else None
+        self.res = m.normal(s, 2.0, R) if residual else None
+        self.dy, self.dr_out = m.normal(s, 0.1, X), m.normal(s, 0.1, R) if residual else None
+        e = m.empty
+        self.y, self.out = e(s, X), e(s, R) if residual else None
+        self.dx, self.dz, self.dres = e(s, X), e(s, X) if gate else None, e(s, R) if residual else None
+        f = lambda *s: torch.full(s, NAN, device=DEV)  # noqa: E731
+        self.rstd, self.rn, self.dw, self.dwn = f(rows, width // group), f(rows) if residual else None, f(width), f(width) if residual else None
+        self.desc = mb.make_join_desc(rows, width, group, CODE[x_dtype], CODE[r_dtype], scale, 1e-5)
+        self.ws = room(mb.mebptt_join_workspace_bytes(self.desc))
+
+    def forward(self, **kw):
+        mb.mebptt_join_forward(self.desc, self.x, self.z, self.w, self.res, self.wn, self.y, self.out, self.rstd, self.rn, **kw)
+
+    def backward(self, **kw):
+        mb.mebptt_join_backward(self.desc, self.x, self.z, self.w, self.out, self.wn, self.rstd, self.rn, self.dy, self.dr_out, self.dx, self.dz, self.dw, self.dres,
+                                self.dwn, self.ws, **kw)
+
+    def check(self):
+        scale = float(np.float32(self.scale))
+        y, r, rstd, rn = od.join(down(self.x), down(self.z), down(self.w), down(self.res), down(self.wn), self.group, scale, 1e-5)
+        near(self.y, y, "y")
+        near(self.rstd, rstd, "rstd")
+        if self.res is not None:
+            near(self.out, r, "residual_out")
+            near(self.rn, rn, "rstd_next")
+        # the backward pass from what was stored (rstd_next is that of r before its rounding: half a step of 2^-8 in each of many values, which cancel)
+        d = od.join_backward(down(self.x), down(self.z), down(self.w), down(self.out), down(self.wn), down(self.dy), down(self.dr_out), self.group, scale, 1e-5)
+        rounded = self.out is not None and self.out.dtype == torch.bfloat16
+        for k, t in (("dx", self.dx), ("dz", self.dz), ("dresidual", self.dres), ("dweight", self.dw), ("dweight_next", self.dwn)):
+            if t is not None:
+                near(t, d[k], k, d.get(k + "_terms"), bits=8 if rounded else 17)
+        assert self.m.clean()
+
+
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("x_dtype,r_dtype", [("fp32", "fp32"), ("bf16", "fp32"), ("bf16", "bf16"), ("fp32", "bf16")])
+@pytest.mark.parametrize("size", SIZES)
+def test_join(size, x_dtype, r_dtype, layout):
+    c = _Call(*size, x_dtype, r_dtype, layout)
+    c.forward()
+    c.backward()
+    c.check()
+
+
+@pytest.mark.parametrize("gate,residual", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("x_dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("size", [(3, 7, 7), (9, 650, 13), (5, 1024, 128), (2, 4096, 4096), (1, 16384, 64)])
+def test_what_may_be_left_out(size, x_dtype, gate, residual):
+    c = _Call(*size, x_dtype, "fp32", gate=gate, residual=residual)
+    c.forward()
+    c.backward()
+    c.check()
+    y, dx = c.y.clone(), c.dx.clone()
+    # without factors, sums and weights; in place
+    mb.mebptt_join_forward(c.desc, c.x, c.z, c.w, c.res, c.wn, c.y, None, None, None)
+    assert torch.equal(c.y, y)
+    mb.mebptt_join_backward(c.desc, c.x, c.z, c.w, c.out, c.wn, c.rstd, c.rn, c.dy, c.dr_out, c.dy, c.dz, None, None, None, None)
+    assert torch.equal(c.dy, dx)
+    x = c.x.clone()
+    mb.mebptt_join_forward(c.desc, x, c.z, c.w, c.res, c.wn, x, c.res, None, None)
+    assert torch.equal(x, y) and (c.res is None or torch.equal(c.res, c.out))
+    c.w = None
+    if residual:
+        c.wn = None
+        c.res = c.out.clone()
+    c.dy = torch.randn_like(y)
+    c.forward()
+    c.backward()
+    c.check()
+
+
+def test_the_streams_gradient_in_place():
+    c = _Call(6, 650, 65, "bf16", "fp32")
+    c.forward()
+    c.backward()
+    want = c.dres.clone()
+    mb.mebptt_join_backward(c.desc, c.x, c.z, c.w, c.out, c.wn, c.rstd, c.rn, c.dy, c.dr_out, c.dx, c.dz, c.dw, c.dr_out, c.dwn, c.ws)
+    assert torch.equal(c.dr_out, want)
+
+
+def test_no_rows():
+    c = _Call(0, 64, 16, "bf16", "fp32")
+    c.forward()
+    c.backward()
+    assert not bool(c.dw.any()) and not bool(c.dwn.any())
+
+
+def test_values_that_are_not_finite_stay_in_their_group():
+    c = _Call(4, 256, 32, "fp32", "fp32", residual=False)
+    c.x[1, 40] = float("inf")
+    c.x[2, 100] = NAN
+    c.forward()
+    bad = ~c.y.isfinite()
+    where = torch.zeros_like(bad)
+    where[1, 40] = where[2, 96:128] = True
+    assert torch.equal(bad, where)
+
+
+def test_join_gradients_against_differences():
+    c = _Call(7, 90, 30, "fp32", "fp32")
+    c.forward()
+    c.backward()
+    loss = lambda: float((c.y.double() * c.dy.double()).sum() + (c.out.double() * c.dr_out.double()).sum())  # noqa: E731
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    for x, d in ((c.x, c.dx), (c.z, c.dz), (c.w, c.dw), (c.res, c.dres), (c.wn, c.dwn)):
+        way = torch.randn(x.shape, generator=g, device=DEV)
+        way *= 1e-2 * x.norm() / way.norm()
+        want, old, got = float((d.double() * way.double()).sum()), x.clone(), 0.0
+        for s in (1, -1):
+            x.copy_(old + s * way)
+            c.forward()
+            got += s * loss() / 2
+        x.copy_(old)
+        # a step of 1 % of the norm: the third derivative's share is about 1e-4 of the gradient's size along it
+        assert abs(got - want) <= 3e-3 * (abs(want) + float(d.norm() * way.norm()) * 0.05)
+
+
+def test_another_stream_and_a_graph():
+    c = _Call(300, 1024, 128, "bf16", "bf16")
+    names = ("y", "out", "dx", "dz", "dw", "dres", "dwn")
+    c.forward()
+    c.backward()
+    want = {n: getattr(c, n).clone() for n in names}
+
+    def same():
+        return all(torch.equal(getattr(c, n), want[n]) for n in names)
+
+    def wipe():
+        for n in names:
+            getattr(c, n).fill_(NAN)
+        c.ws.fill_(0xFF)
+    wipe()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c.forward(stream=side.cuda_stream)
+    c.backward(stream=side.cuda_stream)
+    side.synchronize()
+    assert same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward()
+        c.backward()
+    for _ in range(3):
+        wipe()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same()

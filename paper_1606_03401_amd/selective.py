@@ -18,6 +18,7 @@ from typing import Optional
 import torch
 
 from . import binding as mb
+from .optimiser import AdamW
 
 EPS = 1e-5
 
@@ -208,10 +209,14 @@ class Serving:
         return self._out(k, x.shape)
 
 
-def train(s: Sizes, t: int, B: int, steps: int, rate: float = 0.3, seed: int = 0):
-    """Gradient descent on a task that needs memory: out of a step is to be the input of eight steps before.  Returns (weights, the losses)."""
+def train(s: Sizes, t: int, B: int, steps: int, rate: float = 0.3, seed: int = 0, adamw: int = 0):
+    """Gradient descent on a task that needs memory: out of a step is to be the input of eight steps before.  adamw 32 or 8: AdamW instead, with states of so many
+    bits.  Returns (weights, the losses)."""
     w = make_weights(s, seed)
     run, losses = Training(s, t, B), []
+    if adamw:
+        into = {k: torch.empty_like(v) for k, v in w.items()}
+        opt = AdamW(list(w.values()), list(into.values()), rate, bits=adamw, clip=1.0, no_decay=[not k.startswith("W") for k in w], seed=seed)
     g = torch.Generator(device="cuda:0")
     g.manual_seed(seed + 1)
     for _ in range(steps):
@@ -222,8 +227,13 @@ def train(s: Sizes, t: int, B: int, steps: int, rate: float = 0.3, seed: int = 0
         err = out.float() - target.float()
         losses.append(float((err * err).mean()))
         grads, _, _ = run.backward(w, (2.0 / err.numel() * s.width * err).bfloat16())
-        for k, v in grads.items():
-            w[k] -= rate * v / (1.0 + v.norm())
+        if adamw:
+            for k, v in grads.items():
+                into[k].copy_(v)
+            opt.step()
+        else:
+            for k, v in grads.items():
+                w[k] -= rate * v / (1.0 + v.norm())
         w["A"].clamp_(max=-1e-3)
     return w, losses
 

@@ -276,8 +276,16 @@ struct Args {
 
 __device__ inline int ends_at(const Args& p, int b) { return p.lengths ? min(max(p.lengths[b], 0), p.t) : p.t; }
 
-// Rows that are no whole vectors, copied to ones that are: the launch's steps, [..][B][heads][r.width].
-int pad_rows(const mebptt_seq& from, const Args& p, int heads, int d, int width, int dtype, void* to, hipStream_t stream);
+// Rows that are no whole vectors, copied to ones that are, in one launch: the launch's steps, [..][B][heads][width].
+struct Padded {
+  struct One {
+    mebptt_seq from;
+    void* to;
+    int heads, d, width;
+  } one[4];
+  int n;
+};
+int pad_rows(const Padded& all, const Args& p, int dtype, hipStream_t stream);
 int prepare(const Args& p, int dtype, bool back, hipStream_t stream);
 enum { WALK = 0, AGAIN = 1, SURVEY = 2 };   // y; S and R of every chunk; what segments do to the state
 int walk(const Args& p, int dtype, int mode, hipStream_t stream);

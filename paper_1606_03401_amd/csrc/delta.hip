@@ -113,17 +113,14 @@ Args args_of(const mebptt_delta_desc* d, const mebptt_delta_inputs* in) {
   return p;
 }
 // Rows of a launch's steps as the kernels read them: in place, or copied to `room`, which moves on.
-int rows_of(Rows* to, const Args& p, const mebptt_delta_desc* d, const mebptt_seq& from, int heads, int n, char*& room, int64_t slab, hipStream_t stream) {
+Rows rows_of(Padded& all, const Args& p, const mebptt_delta_desc* d, const mebptt_seq& from, int heads, int n, char*& room, int64_t slab) {
   const int width = whole(d, n), V = d->dtype == MEBPTT_FP32 ? 4 : 8;
-  if (width == n && rows_aligned(from, d->dtype, V)) {
-    *to = {from.data, from.stride_t, from.stride_b, n, n};
-    return MEBPTT_OK;
-  }
+  if (width == n && rows_aligned(from, d->dtype, V)) return {from.data, from.stride_t, from.stride_b, n, n};
   char* at = room;
   room += row_bytes(d, slab, heads, n);
+  all.one[all.n++] = {from, at, heads, n, width};
   const int64_t sb = (int64_t)heads * width, st = d->B * sb;
-  *to = {at - (int64_t)p.c0 * C * st * (int64_t)elem_bytes(d->dtype), st, sb, width, width};    // (as if it held all steps)
-  return pad_rows(from, p, heads, n, width, d->dtype, at, stream);
+  return {at - (int64_t)p.c0 * C * st * (int64_t)elem_bytes(d->dtype), st, sb, width, width};    // (as if it held all steps)
 }
 
 // ---- single tokens -------------------------------------------------------------------------------------
@@ -306,9 +303,11 @@ int mebptt_delta_forward(const mebptt_delta_desc* d, const mebptt_delta_inputs* 
     p.moves = (float*)room, p.ends = (float*)(room + f.moves);
     p.starts = p.c1 - p.c0 > p.seg ? (float*)(room + f.moves + f.ends) : nullptr, p.start_rows = padded(d->dk), p.start_width = p.dvp;
     room += f.moves + f.ends + f.starts;
-    if ((rc = rows_of(&p.q, p, d, in->q, d->Hk, d->dk, room, f.slab, s)) || (rc = rows_of(&p.k, p, d, in->k, d->Hk, d->dk, room, f.slab, s)) ||
-        (rc = rows_of(&p.v, p, d, in->v, d->H, d->dv, room, f.slab, s)))
-      return rc;
+    Padded all = {};
+    p.q = rows_of(all, p, d, in->q, d->Hk, d->dk, room, f.slab);
+    p.k = rows_of(all, p, d, in->k, d->Hk, d->dk, room, f.slab);
+    p.v = rows_of(all, p, d, in->v, d->H, d->dv, room, f.slab);
+    if ((rc = pad_rows(all, p, d->dtype, s))) return rc;
     if ((rc = prepare(p, d->dtype, false, s))) return rc;
     if (p.starts && ((rc = walk(p, d->dtype, SURVEY, s)) || (rc = join_segments(p, d->dtype, s)))) return rc;
     if ((rc = walk(p, d->dtype, WALK, s))) return rc;
@@ -358,9 +357,12 @@ int mebptt_delta_backward(const mebptt_delta_desc* d, const mebptt_delta_inputs*
     p.c0 = (int)(slab * w.slab), p.c1 = (int)std::min(p.c0 + w.slab, chunks);
     p.parts = parts + (int64_t)p.c0 * d->B * 2 * d->H;
     char* room = at;
-    if ((rc = rows_of(&p.q, p, d, in->q, d->Hk, d->dk, room, w.slab, s)) || (rc = rows_of(&p.k, p, d, in->k, d->Hk, d->dk, room, w.slab, s)) ||
-        (rc = rows_of(&p.v, p, d, in->v, d->H, d->dv, room, w.slab, s)) || (rc = rows_of(&p.dy, p, d, dy, d->H, d->dv, room, w.slab, s)))
-      return rc;
+    Padded all = {};
+    p.q = rows_of(all, p, d, in->q, d->Hk, d->dk, room, w.slab);
+    p.k = rows_of(all, p, d, in->k, d->Hk, d->dk, room, w.slab);
+    p.v = rows_of(all, p, d, in->v, d->H, d->dv, room, w.slab);
+    p.dy = rows_of(all, p, d, dy, d->H, d->dv, room, w.slab);
+    if ((rc = pad_rows(all, p, d->dtype, s))) return rc;
     if ((rc = prepare(p, d->dtype, true, s))) return rc;
     const int64_t state = BH * d->dk * d->dv;
     p.seg = (int)w.seg;

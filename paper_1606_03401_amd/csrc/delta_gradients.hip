@@ -28,7 +28,7 @@ struct Layout {
   static constexpr int W = BLOCK;                                                                    // four matrices, over them
   static constexpr int SUMS = BLOCK + (2 * BLOCK_BYTES > 4 * NM * WSIZE ? 2 * BLOCK_BYTES : 4 * NM * WSIZE);
   static constexpr int GATE = SUMS + C * 8, ROWF = GATE + GATES * C * 4, COLS = ROWF + WAVES * C * 4, DOTS = COLS + 4 * C * 4,
-                       MORE = DOTS + 2 * WAVES * C * 4, BYTES = MORE + WAVES * 4;
+                       NORMS = DOTS + 4 * WAVES * C * 4, MORE = NORMS + 2 * C * 4, BYTES = MORE + WAVES * 4;
 };
 
 // An operand in the order in which it stands: lane l's eight values are 8 g .. 8 g + 7 of the 32.  (Both operands of such a product come from memory.)
@@ -112,12 +112,13 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
   T *W1 = (T*)(lds + L::W), *W1q = W1 + L::NM * WA, *W3 = W1q + L::NM * WA, *W3k = W3 + L::NM * WA;
   double* G = (double*)(lds + L::SUMS);
   float *gate = (float*)(lds + L::GATE), *rowF = (float*)(lds + L::ROWF), *cols = (float*)(lds + L::COLS), *dots = (float*)(lds + L::DOTS),
-        *more = (float*)(lds + L::MORE);
+        *norms = (float*)(lds + L::NORMS), *more = (float*)(lds + L::MORE);
   const int per = p.B * p.Hk, chunk = p.c0 + blockIdx.x / per, b = blockIdx.x % per / p.Hk, hk = blockIdx.x % p.Hk, group = SHARED ? p.H / p.Hk : 1;
   const int s0 = chunk * C, steps = min(p.t - s0, C), live = min(ends_at(p, b) - s0, C), BH = p.B * p.H;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE, g = lane / 16, c16 = lane % 16;
   const bool mine = wave < NT;               // waves with columns of dq and dk
-  const int jt = wave % 4, col = 16 * wave + c16;
+  // column tiles with many rows and with few are paired: waves w and w + 4 share a SIMD
+  const int jt = wave < 4 ? wave : 7 - wave, col = 16 * wave + c16;
   float* parts = p.parts + ((int64_t)(chunk - p.c0) * p.B + b) * 2 * p.H;
   T* dq = (T*)p.dq.data + (int64_t)s0 * p.dq.stride_t + b * p.dq.stride_b + hk * p.dk + col;
   T* dk = (T*)p.dkey.data + (int64_t)s0 * p.dkey.stride_t + b * p.dkey.stride_b + hk * p.dk + col;
@@ -132,17 +133,19 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
     for (int i = threadIdx.x; i < group; i += THREADS) parts[hk * group + i] = parts[p.H + hk * group + i] = 0.0f;
     return;
   }
-  {
-    Fetch<T, KD, THREADS> fk, fq;
-    fk.load(p.k, s0, b, hk, 0, live);
-    fq.load(p.q, s0, b, hk, 0, live);
+  Fetch<T, KD, THREADS> fk, fq;
+  fk.load(p.k, s0, b, hk, 0, live);
+  fq.load(p.q, s0, b, hk, 0, live);
+  static_assert(C * VB / 4 == THREADS, "a block is four values a thread");
+  if constexpr (SHARED) {
     fk.put(K, p.k, 0, live);
     fq.put(Q, p.q, 0, live);
   }
-  const int vs = threadIdx.x / (VB / 4), vc = threadIdx.x % (VB / 4) * 4;   // a thread's step and four columns of a block
-  static_assert(C * VB / 4 == THREADS, "a block is four values a thread");
   f32x4 dQ[4] = {}, dK[4] = {};
+  const int lane_ = lane, col_ = col;
   for (int h = hk * group, n = 0; n < group; ++h, ++n) {
+    const int lane = SHARED ? here(lane_) : lane_, g = lane / 16, c16 = lane % 16, col = 16 * wave + c16;
+    const int vs = (64 * wave + lane) / (VB / 4), vc = lane % (VB / 4) * 4;   // a thread's step and four columns of a block
     const int64_t at = (int64_t)(chunk - p.c0) * BH + b * p.H + h;
     const char* rec = p.records + at * Rec::BYTES;
     const float *Sg = p.S + at * KD * p.dvp, *dSg = p.dS + at * KD * p.dvp, *Rg = p.R + at * C * p.dvp, *Zg = p.Z + at * C * p.dvp;
@@ -170,9 +173,17 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       put_parts<L::NV>(dy + (1 + L::NV) * VA + vs * VLD + vc, VA, r);
     };
     fetch(0);
+    f32x4 factors;    // the gates and behind them G: whole vectors of a record
+    constexpr int FACTORS = (GATES * C * 4 + C * 8) / 16;
+    static_assert(FACTORS <= THREADS && L::GATE == L::SUMS + C * 8 && Rec::SUMS == Rec::GATE + GATES * C * 4, "a vector a thread");
+    const int fi = min((int)threadIdx.x, FACTORS - 1);
+    factors = *reinterpret_cast<const f32x4*>(rec + Rec::GATE + fi * 16);
+    if constexpr (!SHARED) {
+      fk.put(K, p.k, 0, live);
+      fq.put(Q, p.q, 0, live);
+    }
     __syncthreads();   // the head before has been read
-    for (int i = threadIdx.x; i < GATES * C; i += THREADS) gate[i] = reinterpret_cast<const float*>(rec + Rec::GATE)[i];
-    if (threadIdx.x < C) G[threadIdx.x] = reinterpret_cast<const double*>(rec + Rec::SUMS)[threadIdx.x];
+    *reinterpret_cast<f32x4*>(fi < GATES * C / 4 ? reinterpret_cast<char*>(gate) + fi * 16 : reinterpret_cast<char*>(G) + (fi * 16 - GATES * C * 4)) = factors;
     f32x4 YS[4] = {}, ZS[4] = {}, RS[4] = {}, AA[4] = {};
     float inner = 0.0f;
     for (int v0 = 0, buffer = 0; v0 < p.dvp; v0 += VB, buffer ^= 1) {
@@ -226,7 +237,7 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * rt + 4 * g + e;
           const bool in = wave < 4 ? j <= i : j < i;
-          const float d = in ? expf((float)(G[i] - Gj)) : 0.0f, u = (wave < 4 ? a[e] : -a[e]) * bej;
+          const float d = in ? __expf((float)(G[i] - Gj)) : 0.0f, u = (wave < 4 ? a[e] : -a[e]) * bej;
           m[e] *= fi[e] * skj * d;
           down += m[e] * (wave < 4 ? a[e] : -a[e]);
           const float f = u * m[e];
@@ -296,17 +307,27 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * rt + 4 * g + e;
-          const float k = (float)K[i * LD + col] * sk[e], q = (float)Q[i * LD + col] * sq[e];
+          const float kr = (float)K[i * LD + col], qr = (float)Q[i * LD + col], k = kr * sk[e], q = qr * sq[e];
+          // q~ . (gamma dY S^T) - k^ . (gamma Z S^T);  k^ . (gamma_C / gamma R dS'^T);  and for the norms' sake q . dq, k . dk
           const float one = over_columns(q * ys[e] - k * zs[e]), two = over_columns(k * rs[e]);
-          if (c16 == 0) {
-            dots[wave * C + i] = one;
-            dots[(WAVES + wave) * C + i] = two;
-          }
+          const float three = over_columns(qr * dQ[rt][e]), four = over_columns(kr * dK[rt][e]);
+          if (c16 < 4) dots[(c16 * WAVES + wave) * C + i] = c16 == 0 ? one : c16 == 1 ? two : c16 == 2 ? three : four;
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     __syncthreads();
+    if (p.normalise && (!SHARED || n == group - 1)) {   // over the waves, with the factors of both norms
+      if (threadIdx.x >= THREADS - 2 * C) {
+        const int i = threadIdx.x % C, k = (threadIdx.x - (THREADS - 2 * C)) / C;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NT; ++w) sum += dots[((2 + k) * WAVES + w) * C + i];
+        const float f = gate[(k ? SK : RQ) * C + i];
+        norms[k * C + i] = sum * f * f * (k ? 1.0f : p.scale);
+      }
+      __syncthreads();
+    }
     if (wave == 0) {
       const int i = lane;
       float rows = 0.0f, first = 0.0f, second = 0.0f, all = 0.0f;
@@ -353,40 +374,13 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       }
     }
   }
-  // through the norms of q and k
-  if (p.normalise) {
-    __syncthreads();
-    if (mine) {
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 16 * rt + 4 * g + e;
-          const float first = over_columns(dQ[rt][e] * (float)Q[i * LD + col]), second = over_columns(dK[rt][e] * (float)K[i * LD + col]);
-          if (c16 == 0) {
-            dots[wave * C + i] = first;
-            dots[(WAVES + wave) * C + i] = second;
-          }
-        }
-    }
-    __syncthreads();
-    if (threadIdx.x < 2 * C) {   // over the waves, with the factors of both norms
-      const int i = threadIdx.x % C, k = threadIdx.x / C;
-      float sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < NT; ++w) sum += dots[(k * WAVES + w) * C + i];
-      const float f = gate[(k ? SK : RQ) * C + i];
-      cols[k * C + i] = sum * f * f * (k ? 1.0f : p.scale);
-    }
-    __syncthreads();
-  }
-  if (!mine || col >= p.dk) return;
+  if (!mine || col_ >= p.dk) return;
 #pragma unroll
   for (int rt = 0; rt < 4; ++rt) {
     f32x4 dqt = p.scale * dQ[rt], dkt = dK[rt];
     if (p.normalise) {
       const f32x4 rq = *reinterpret_cast<const f32x4*>(gate + RQ * C + 16 * rt + 4 * g), rk = *reinterpret_cast<const f32x4*>(gate + SK * C + 16 * rt + 4 * g);
-      const f32x4 a = *reinterpret_cast<const f32x4*>(cols + 16 * rt + 4 * g), c = *reinterpret_cast<const f32x4*>(cols + C + 16 * rt + 4 * g);
+      const f32x4 a = *reinterpret_cast<const f32x4*>(norms + 16 * rt + 4 * g), c = *reinterpret_cast<const f32x4*>(norms + C + 16 * rt + 4 * g);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 16 * rt + 4 * g + e;

@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = 16 * wave + 4 * g + e;
-        const float d = j <= i ? expf((float)(G[i] - G[j])) * gate[SK * C + j] : 0.0f;
+        const float d = j <= i ? __expf((float)(G[i] - G[j])) * gate[SK * C + j] : 0.0f;
         kk[e] = j < i ? kk[e] * d * gate[SK * C + i] * gate[BE * C + j] : 0.0f;
         qk[e] = j <= i ? qk[e] * d * gate[SQ * C + i] : 0.0f;
       }
@@ -215,13 +215,14 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void delta_pad_kernel(mebptt_seq from, int B, int heads, int d, int width, int s0, int64_t n, T* to) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int c = (int)(i % width);
-    const int64_t row = i / width;
-    const int h = (int)(row % heads), b = (int)(row / heads % B);
-    const int64_t s = s0 + row / heads / B;
-    to[i] = c < d ? ((const T*)from.data)[s * from.stride_t + b * from.stride_b + h * d + c] : (T)0.0f;
+__global__ __launch_bounds__(256) void delta_pad_kernel(Padded all, int B, int s0, int steps) {
+  const Padded::One& p = all.one[blockIdx.y];
+  const int64_t rows = (int64_t)steps * B * p.heads;   // a wave each: where they are is the same for all lanes
+  const int lane = threadIdx.x % WAVE;
+  for (int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE); row < rows; row += (int64_t)gridDim.x * 4) {
+    const unsigned r = (unsigned)(row / p.heads), h = (unsigned)(row - (int64_t)r * p.heads), s = r / (unsigned)B, b = r - s * (unsigned)B;
+    const T* from = (const T*)p.from.data + (int64_t)(s0 + (int)s) * p.from.stride_t + (int64_t)b * p.from.stride_b + (int64_t)h * p.d;
+    for (int c = lane; c < p.width; c += WAVE) ((T*)p.to)[row * p.width + c] = c < p.d ? from[c] : (T)0.0f;
   }
 }
 
@@ -236,11 +237,14 @@ int launch(const Args& p, hipStream_t stream) {
 
 }  // namespace
 
-int mebptt::delta::pad_rows(const mebptt_seq& from, const Args& p, int heads, int d, int width, int dtype, void* to, hipStream_t stream) {
-  const int64_t n = (int64_t)std::min((p.c1 - p.c0) * C, p.t - p.c0 * C) * p.B * heads * width;
-  const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(n, 256), 1 << 16);
-  if (dtype == MEBPTT_FP32) delta_pad_kernel<float><<<grid, 256, 0, stream>>>(from, p.B, heads, d, width, p.c0 * C, n, (float*)to);
-  else delta_pad_kernel<__bf16><<<grid, 256, 0, stream>>>(from, p.B, heads, d, width, p.c0 * C, n, (__bf16*)to);
+int mebptt::delta::pad_rows(const Padded& all, const Args& p, int dtype, hipStream_t stream) {
+  if (!all.n) return MEBPTT_OK;
+  const int steps = std::min((p.c1 - p.c0) * C, p.t - p.c0 * C);
+  int64_t most = 1;
+  for (int i = 0; i < all.n; ++i) most = std::max(most, (int64_t)steps * p.B * all.one[i].heads);
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(most, 16), 1 << 14), (unsigned)all.n);
+  if (dtype == MEBPTT_FP32) delta_pad_kernel<float><<<grid, 256, 0, stream>>>(all, p.B, p.c0 * C, steps);
+  else delta_pad_kernel<__bf16><<<grid, 256, 0, stream>>>(all, p.B, p.c0 * C, steps);
   return launched("delta rule, rows");
 }
 

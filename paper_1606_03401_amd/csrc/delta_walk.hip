@@ -179,8 +179,8 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
 
   Fetch<T, KD, W * WAVE> ck, cq;
   Fetch<T, 16 * W, W * WAVE> cv;
-  Copy<frag_bytes<T>(T_PARTS), W * WAVE> ct;
-  Copy<frag_bytes<T>(P_PARTS), W * WAVE> cp;
+  // of the record: T, P and the gates as one, or T and the gates
+  Copy<MODE == WALK ? L::V - L::T_ : frag_bytes<T>(T_PARTS), W * WAVE> ct;
   Copy<WALK_GATES * C * 4, W * WAVE> cg;
   auto fetch = [&](int chunk) {
     const int live = end - chunk * C;
@@ -189,8 +189,7 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
     if (!unit) cv.load(p.v, (int64_t)chunk * C, b, h, c0, live);
     const char* rec = p.records + ((int64_t)(chunk - p.c0) * BH + bh) * R::BYTES;
     ct.load(rec + R::T_);
-    if (MODE == WALK) cp.load(rec + R::P);
-    cg.load(rec + R::GATE);
+    if (MODE != WALK) cg.load(rec + R::GATE);
   };
   if (first < behind) fetch(first);
   for (int chunk = first; chunk < behind; ++chunk) {
@@ -206,8 +205,8 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
     __syncthreads();   // the chunk before has been read
     ck.put(K, p.k, 0, live);
     ct.put(lds + L::T_);
-    if (MODE == WALK) cq.put(Q, p.q, 0, live), cp.put(lds + L::P);
-    cg.put(lds + L::GATE);
+    if (MODE == WALK) cq.put(Q, p.q, 0, live);
+    else cg.put(lds + L::GATE);
     if (!unit) cv.put(VL, p.v, c0, live);
     __syncthreads();
     fetch(min(chunk + 1, behind - 1));   // (not under a condition, see there)

@@ -14,7 +14,7 @@ constexpr int PIECE = 4096;           // whole blocks
 constexpr int THREADS = 256, V = 8;   // neighbouring values of a thread
 constexpr int SHARE = BLOCK / V;      // threads of a block: half a wave
 constexpr int64_t MAX_TENSORS = 65536;
-constexpr int NORM_GROUPS = 1024;
+constexpr int NORM_GROUPS = 2048;
 
 struct Entry {
   float* param;
@@ -26,6 +26,20 @@ struct Entry {
   int64_t block;           // number of its first block over all tensors
   int grad_bf16, state8, no_decay, vec;
 };
+// An entry as a kernel reads it: through scalar loads, once, in place of loads after each store that might have changed it, and with pointers of which
+// the compiler knows that they are to global memory.
+template <typename T>
+__device__ inline T* global(uint64_t address) { return (T*)(__attribute__((address_space(1))) T*)address; }
+template <typename T>
+__device__ inline T scalar(const void* p, int64_t at) { return ((const __attribute__((address_space(4))) T*)(uint64_t)p)[at]; }
+__device__ inline Entry entry_of(const Entry* entries, int32_t tensor) {
+  static_assert(sizeof(Entry) == 96 && offsetof(Entry, n) == 56 && offsetof(Entry, grad_bf16) == 80, "");
+  uint64_t w[12];
+#pragma unroll
+  for (int i = 0; i < 12; ++i) w[i] = scalar<uint64_t>(entries + tensor, i);
+  return {global<float>(w[0]), global<const void>(w[1]), global<void>(w[2]), global<void>(w[3]), global<float>(w[4]), global<float>(w[5]), global<__bf16>(w[6]),
+          (int64_t)w[7], (int64_t)w[8], (int64_t)w[9], (int)w[10], (int)(w[10] >> 32), (int)w[11], (int)(w[11] >> 32)};
+}
 // [entries][a piece's tensor]
 size_t map_at(int count) { return align_up((size_t)count * sizeof(Entry)); }
 
@@ -59,10 +73,18 @@ __device__ inline float value_of(uint32_t code, float scale) {
   const float size = low ? __uint_as_float((low + ((SIGNED ? 112u : 96u) << 3)) << 20) * scale : 0.0f;
   return SIGNED && (code & 128u) ? -size : size;
 }
-// One of the two neighbours of x / scale; `bits16` says which where the part cut off leaves a choice.
+// x / scale, correctly rounded, for x and scale of at least zero, by Markstein's correction: of a quotient that is off by one unit at most, the remainder
+// is exact in a fused multiply-add, and its product with the nearest number to 1 / scale settles the rounding.  The first step of the two makes it so.
+// (Where a remainder leaves fp32's range below, x / scale is under 2^-40 and only whether it is zero counts.)  A block's scale is shared, so its
+// reciprocal is taken once: 4 operations a value in place of a division's 11.
+constexpr float SMALL_SCALE = 0x1p-60f, LARGE_SCALE = 0x1p100f;   // beyond these plain division
+__device__ inline float quotient(float x, float scale, float inverse) {
+  const float q = x * inverse, q1 = fmaf(fmaf(-q, scale, x), inverse, q);
+  return fmaf(fmaf(-q1, scale, x), inverse, q1);
+}
+// One of the two neighbours of u = |x| / scale; `bits16` says which where the part cut off leaves a choice.
 template <bool SIGNED>
-__device__ inline uint32_t code_of(float x, float scale, uint32_t bits16) {
-  const float u = scale > 0.0f ? fabsf(x) / scale : fabsf(x);   // (at most 1.875 and a rounding)
+__device__ inline uint32_t code_of(float x, float u, uint32_t bits16) {   // (u is at most 1.875 and a rounding)
   const int code = (int)((__float_as_uint(u) + (bits16 << 4)) >> 20) - ((SIGNED ? 112 : 96) << 3);
   if constexpr (SIGNED) {
     constexpr float LEAST = 1.125f * 0x1p-15f;
@@ -124,9 +146,16 @@ __device__ inline void write_codes(uint8_t* p, float* scale, int64_t left, bool 
   const float s = top * (1.0f / 1.875f);
   if (left <= 0) return;
   if (first) *scale = s;
+  const bool plain = !(s >= SMALL_SCALE && s <= LARGE_SCALE);
+  const float inverse = 1.0f / s;
   uint32_t c[V];
+  if (plain) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) c[e] = code_of<SIGNED>(v[e], s, SIGNED ? bits[e] >> 16 : bits[e] & 0xFFFFu);
+    for (int e = 0; e < V; ++e) c[e] = code_of<SIGNED>(v[e], s > 0.0f ? fabsf(v[e]) / s : fabsf(v[e]), SIGNED ? bits[e] >> 16 : bits[e] & 0xFFFFu);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) c[e] = code_of<SIGNED>(v[e], quotient(fabsf(v[e]), s, inverse), SIGNED ? bits[e] >> 16 : bits[e] & 0xFFFFu);
+  }
   if constexpr (VEC) {
     if (left >= V) {
       *reinterpret_cast<u32x2*>(p) = u32x2{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
@@ -138,67 +167,85 @@ __device__ inline void write_codes(uint8_t* p, float* scale, int64_t left, bool 
     if (e < left) p[e] = (uint8_t)c[e];
 }
 
+struct Factors {
+  float factor, rate, keep, inv1, inv2;
+  uint32_t key;
+};
+// N chunks of V values of each thread, the first from value `start` on; every load stands before the first store.  WHOLE: all values exist.
 // One rounding to an operation, so that codes do not depend on what a compiler joins.
 #pragma clang fp contract(off)
-template <bool VEC>
-__device__ inline void piece_step(const Step& p, const Entry& t, int64_t start, float factor) {
-  const float rate = p.rate ? *p.rate : p.desc_rate;
-  const int64_t step = p.step ? (*p.step < 1 ? 1 : *p.step) : p.desc_step;
-  const float inv1 = p.beta1 > 0.0f ? -1.0f / expm1f((float)step * p.log1) : 1.0f, inv2 = p.beta2 > 0.0f ? -1.0f / expm1f((float)step * p.log2) : 1.0f;
-  const float keep = 1.0f - (t.no_decay ? 0.0f : rate * p.decay);
+template <int N, bool WHOLE, bool VEC, bool STATE8, typename TG>
+__device__ inline void chunks_step(const Step& p, const Entry& t, int64_t start, const Factors& f) {
+  float w[N][V], g[N][V], m[N][V], v[N][V];
+  int64_t at[N], left[N];
 #pragma unroll
-  for (int k = 0; k < PIECE; k += THREADS * V) {
-    const int64_t i = start + k + (int64_t)threadIdx.x * V, left = t.n - i;
-    if (start + k >= t.n) break;   // (the same for the whole workgroup)
-    const int64_t at = left > 0 ? i : 0;
-    float w[V], g[V], m[V], v[V];
-    read<float, VEC>(t.param + at, left, w);
-    if (t.grad_bf16) read<__bf16, VEC>((const __bf16*)t.grad + at, left, g);
-    else read<float, VEC>((const float*)t.grad + at, left, g);
-    const int64_t block = at / BLOCK;
-    if (t.state8) {
-      read_codes<true, VEC>((const uint8_t*)t.m + at, left, t.m_scale[block], m);
-      read_codes<false, VEC>((const uint8_t*)t.v + at, left, t.v_scale[block], v);
+  for (int k = 0; k < N; ++k) {
+    const int64_t i = start + k * (THREADS * V) + (int64_t)threadIdx.x * V;
+    left[k] = WHOLE ? V : t.n - i;
+    at[k] = left[k] > 0 ? i : 0;
+    read<TG, VEC>((const TG*)t.grad + at[k], left[k], g[k]);
+    if constexpr (STATE8) {
+      read_codes<true, VEC>((const uint8_t*)t.m + at[k], left[k], t.m_scale[at[k] / BLOCK], m[k]);
+      read_codes<false, VEC>((const uint8_t*)t.v + at[k], left[k], t.v_scale[at[k] / BLOCK], v[k]);
     } else {
-      read<float, VEC>((const float*)t.m + at, left, m);
-      read<float, VEC>((const float*)t.v + at, left, v);
+      read<float, VEC>((const float*)t.m + at[k], left[k], m[k]);
+      read<float, VEC>((const float*)t.v + at[k], left[k], v[k]);
     }
+    read<float, VEC>(t.param + at[k], left[k], w[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      g[e] *= factor;
-      m[e] = p.beta1 * m[e] + p.rest1 * g[e];
-      v[e] = p.beta2 * v[e] + p.rest2 * (g[e] * g[e]);
-      w[e] = w[e] * keep - rate * (m[e] * inv1) / (sqrtf(v[e] * inv2) + p.eps);
+      g[k][e] *= f.factor;
+      m[k][e] = p.beta1 * m[k][e] + p.rest1 * g[k][e];
+      v[k][e] = p.beta2 * v[k][e] + p.rest2 * (g[k][e] * g[k][e]);
+      w[k][e] = w[k][e] * f.keep - f.rate * (m[k][e] * f.inv1) / (sqrtf(v[k][e] * f.inv2) + p.eps);
     }
-    write<float, VEC>(t.param + at, left, w);
-    if (t.copy) write<__bf16, VEC>(t.copy + at, left, w);
-    if (t.state8) {
-      const uint32_t key = mix(p.seed + (uint32_t)step * 0x632BE5ABu + (uint32_t)(t.block + block) * 0x9E3779B9u);
+    write<float, VEC>(t.param + at[k], left[k], w[k]);
+    if (t.copy) write<__bf16, VEC>(t.copy + at[k], left[k], w[k]);
+    if constexpr (STATE8) {
+      const int64_t block = at[k] / BLOCK;
+      const uint32_t key = mix(f.key + (uint32_t)(t.block + block) * 0x9E3779B9u);
       uint32_t bits[V];
 #pragma unroll
-      for (int e = 0; e < V; ++e) bits[e] = mix(key + (uint32_t)(i % BLOCK + e) * 0x85157AF5u);
+      for (int e = 0; e < V; ++e) bits[e] = mix(key + (uint32_t)(threadIdx.x % SHARE * V + e) * 0x85157AF5u);
       const bool first = threadIdx.x % SHARE == 0;
-      write_codes<true, VEC>((uint8_t*)t.m + at, t.m_scale + block, left, first, m, bits);
-      write_codes<false, VEC>((uint8_t*)t.v + at, t.v_scale + block, left, first, v, bits);
+      write_codes<true, VEC>((uint8_t*)t.m + at[k], t.m_scale + block, left[k], first, m[k], bits);
+      write_codes<false, VEC>((uint8_t*)t.v + at[k], t.v_scale + block, left[k], first, v[k], bits);
     } else {
-      write<float, VEC>((float*)t.m + at, left, m);
-      write<float, VEC>((float*)t.v + at, left, v);
+      write<float, VEC>((float*)t.m + at[k], left[k], m[k]);
+      write<float, VEC>((float*)t.v + at[k], left[k], v[k]);
     }
   }
 }
-
-#pragma clang fp contract(fast)
-
-__global__ __launch_bounds__(THREADS) void adamw_step_kernel(Step p, int64_t pieces) {
-  const float factor = p.factor ? *p.factor : 1.0f;
-  if (!__builtin_isfinite(factor)) return;
-  for (int64_t k = blockIdx.x; k < pieces; k += gridDim.x) {
-    const Entry& t = p.entries[p.map[k]];
-    const int64_t start = (k - t.first) * PIECE;
-    if (t.vec) piece_step<true>(p, t, start, factor);
-    else piece_step<false>(p, t, start, factor);
+template <bool STATE8, typename TG>
+__device__ inline void piece_step(const Step& p, const Entry& t, int64_t start, const Factors& f) {
+  constexpr int N = PIECE / (THREADS * V);
+  if (t.vec && start + PIECE <= t.n) return chunks_step<N, true, true, STATE8, TG>(p, t, start, f);
+  for (int k = 0; k < N && start + k * (THREADS * V) < t.n; ++k) {   // (the same for the whole workgroup)
+    if (t.vec) chunks_step<1, false, true, STATE8, TG>(p, t, start + k * (THREADS * V), f);
+    else chunks_step<1, false, false, STATE8, TG>(p, t, start + k * (THREADS * V), f);
   }
 }
+__global__ __launch_bounds__(THREADS) void adamw_step_kernel(Step p, int64_t pieces) {
+  Factors f;
+  f.factor = p.factor ? *p.factor : 1.0f;
+  if (!__builtin_isfinite(f.factor)) return;
+  f.rate = p.rate ? *p.rate : p.desc_rate;
+  const int64_t step = p.step ? (*p.step < 1 ? 1 : *p.step) : p.desc_step;
+  f.inv1 = p.beta1 > 0.0f ? -1.0f / expm1f((float)step * p.log1) : 1.0f;
+  f.inv2 = p.beta2 > 0.0f ? -1.0f / expm1f((float)step * p.log2) : 1.0f;
+  f.key = p.seed + (uint32_t)step * 0x632BE5ABu;
+  for (int64_t k = blockIdx.x; k < pieces; k += gridDim.x) {
+    const Entry t = entry_of(p.entries, scalar<int32_t>(p.map, k));
+    const int64_t start = (k - t.first) * PIECE;
+    f.keep = 1.0f - (t.no_decay ? 0.0f : f.rate * p.decay);
+    if (t.state8) t.grad_bf16 ? piece_step<true, __bf16>(p, t, start, f) : piece_step<true, float>(p, t, start, f);
+    else t.grad_bf16 ? piece_step<false, __bf16>(p, t, start, f) : piece_step<false, float>(p, t, start, f);
+  }
+}
+#pragma clang fp contract(fast)
 
 // ---- norm ----------------------------------------------------------------------------------------------
 
@@ -219,7 +266,7 @@ __global__ __launch_bounds__(THREADS) void adamw_squares_kernel(const Entry* ent
   __shared__ double lds[THREADS / WAVE];
   double sum = 0.0;   // squares of large gradients leave fp32's range
   for (int64_t k = blockIdx.x; k < pieces; k += gridDim.x) {
-    const Entry& t = entries[map[k]];
+    const Entry t = entry_of(entries, scalar<int32_t>(map, k));
     const int64_t start = (k - t.first) * PIECE;
 #pragma unroll
     for (int j = 0; j < PIECE; j += THREADS * V) {

@@ -57,6 +57,11 @@ struct Place {
       at[c] = count[c] ? k * group + in : 0;
     }
   }
+  // Nothing that follows from the columns is kept from row to row: kept addresses of eight rows' chunks take more registers than there are.
+  __device__ inline void fresh() {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(at[c]));
+  }
 };
 template <typename T, bool VEC>
 struct Raw {
@@ -81,11 +86,23 @@ __device__ inline void widen(const Raw<T, VEC>& raw, int count, float (&v)[V]) {
 template <bool VEC, typename T>
 __device__ inline void store_chunk(T* row, int at, int count, int lanes, const float (&v)[V]) {
   if constexpr (VEC) {
-    if (count) store<V>(row + at, v);
+    if (count) store<V>(row + (unsigned)at, v);
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
-      if (e < count) row[at + lanes * e] = (T)v[e];
+      if (e < count) row[(unsigned)(at + lanes * e)] = (T)v[e];
+  }
+}
+
+// A weight's values, or ones.
+template <bool VEC>
+__device__ inline void load_weight(const float* weight, int at, int count, int lanes, float (&w)[V]) {
+#pragma unroll
+  for (int e = 0; e < V; ++e) w[e] = 1.0f;
+  if (weight) {
+    Raw<float, VEC> ws;
+    load_chunk<VEC>(weight, at, count, lanes, ws);
+    widen<VEC>(ws, count, w);
   }
 }
 
@@ -146,10 +163,11 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_forward_kernel(Join 
   constexpr int ROWS = WAVES == 1 ? 4 : 1;
   __shared__ float lds[WAVES * NC];
   const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);   // (uniform over a wave, and so are rows' addresses)
-  const Place<WAVES, NC, VEC> at(p.width, p.group, p.lanes, p.pieces);
+  Place<WAVES, NC, VEC> at(p.width, p.group, p.lanes, p.pieces);
   const int groups = p.width / p.group;
   const float per_group = 1.0f / (float)p.group;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + sub; row < p.rows; row += (int64_t)gridDim.x * ROWS) {
+    at.fresh();
     Raw<TX, VEC> xs[NC], zs[NC];
     Raw<TR, VEC> rs[NC];
 #pragma unroll
@@ -176,17 +194,15 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_forward_kernel(Join 
     for (int c = 0; c < NC; ++c) {
       const float rstd = rsqrtf(sums[c] * per_group + p.eps);
       if (p.rstd && at.count[c] && at.at[c] == at.slot[c] * p.group) p.rstd[row * groups + at.slot[c]] = rstd;
-      float w[V], z[V];
-      if (p.weight) {
-        Raw<float, VEC> ws;
-        load_chunk<VEC>(p.weight, at.at[c], at.count[c], p.lanes, ws);
-        widen<VEC>(ws, at.count[c], w);
-      }
-      if (p.z) widen<VEC>(zs[c], at.count[c], z);
+      float w[V];
+      load_weight<VEC>(p.weight, at.at[c], at.count[c], p.lanes, w);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        a[c][e] *= p.weight ? rstd * w[e] : rstd;
-        if (p.z) a[c][e] *= z[e] * sigmoid(z[e]);
+      for (int e = 0; e < V; ++e) a[c][e] *= rstd * w[e];
+      if (p.z) {
+        float z[V];
+        widen<VEC>(zs[c], at.count[c], z);
+#pragma unroll
+        for (int e = 0; e < V; ++e) a[c][e] *= z[e] * sigmoid(z[e]);
       }
       if constexpr (NEXT) {
         float r[V];
@@ -206,13 +222,9 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_forward_kernel(Join 
       for (int c = 0; c < NC; ++c) {
         if (p.residual_out) store_chunk<VEC>((TR*)p.residual_out + row * p.ldo, at.at[c], at.count[c], p.lanes, a[c]);
         float w[V];
-        if (p.weight_next) {
-          Raw<float, VEC> ws;
-          load_chunk<VEC>(p.weight_next, at.at[c], at.count[c], p.lanes, ws);
-          widen<VEC>(ws, at.count[c], w);
-        }
+        load_weight<VEC>(p.weight_next, at.at[c], at.count[c], p.lanes, w);
 #pragma unroll
-        for (int e = 0; e < V; ++e) a[c][e] *= p.weight_next ? rstd * w[e] : rstd;
+        for (int e = 0; e < V; ++e) a[c][e] *= rstd * w[e];
       }
     }
 #pragma unroll
@@ -227,7 +239,7 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_backward_kernel(Join
   __shared__ float lds[WAVES * NC];
   __shared__ float waves_dw[WAVES == 1 ? 3 * NC * V * WAVE : 1];
   const int sub = ROWS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-  const Place<WAVES, NC, VEC> at(p.width, p.group, p.lanes, p.pieces);
+  Place<WAVES, NC, VEC> at(p.width, p.group, p.lanes, p.pieces);
   const int groups = p.width / p.group;
   const float per_group = 1.0f / (float)p.group;
   float dw[NC][V], dwn[NEXT ? NC : 1][V];
@@ -236,6 +248,7 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_backward_kernel(Join
 #pragma unroll
     for (int e = 0; e < V; ++e) dw[c][e] = dwn[NEXT ? c : 0][e] = 0.0f;
   for (int64_t row = (int64_t)blockIdx.x * ROWS + sub; row < p.rows; row += (int64_t)gridDim.x * ROWS) {
+    at.fresh();
     Raw<TX, VEC> xs[NC], zs[NC], ys[NC];
     Raw<TR, VEC> rs[NC], os[NC];
 #pragma unroll
@@ -264,17 +277,13 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_backward_kernel(Join
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         float w[V];
-        if (p.weight_next) {
-          Raw<float, VEC> ws;
-          load_chunk<VEC>(p.weight_next, at.at[c], at.count[c], p.lanes, ws);
-          widen<VEC>(ws, at.count[c], w);
-        }
+        load_weight<VEC>(p.weight_next, at.at[c], at.count[c], p.lanes, w);
         widen<VEC>(rs[c], at.count[c], m[c]);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           m[c][e] *= rstd;
           dwn[c][e] += d[c][e] * m[c][e];
-          if (p.weight_next) d[c][e] *= w[e];
+          d[c][e] *= w[e];
           dot += d[c][e] * m[c][e];
         }
       }
@@ -296,29 +305,28 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_backward_kernel(Join
     for (int c = 0; c < NC; ++c) {
       rstd[c] = p.rstd[row * groups + (at.count[c] ? at.slot[c] : 0)];
       widen<VEC>(xs[c], at.count[c], n[c]);
-      float w[V], z[V], dz[V];
-      if (p.weight) {
-        Raw<float, VEC> ws;
-        load_chunk<VEC>(p.weight, at.at[c], at.count[c], p.lanes, ws);
-        widen<VEC>(ws, at.count[c], w);
-      }
-      if (p.z) widen<VEC>(zs[c], at.count[c], z);
+      float w[V];
+      load_weight<VEC>(p.weight, at.at[c], at.count[c], p.lanes, w);
       dots[c] = 0.0f;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        n[c][e] *= rstd[c];
-        float act = 1.0f;
-        if (p.z) {
-          const float s = sigmoid(z[e]);
-          act = z[e] * s;
-          dz[e] = d[c][e] * n[c][e] * (s * (1.0f + z[e] * (1.0f - s)));
-          if (p.weight) dz[e] *= w[e];
+      for (int e = 0; e < V; ++e) n[c][e] *= rstd[c];
+      if (p.z) {
+        float z[V], dz[V];
+        widen<VEC>(zs[c], at.count[c], z);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float s = sigmoid(z[e]), act = z[e] * s;
+          dz[e] = d[c][e] * n[c][e] * w[e] * (s * (1.0f + z[e] * (1.0f - s)));
+          d[c][e] *= act;
         }
-        dw[c][e] += d[c][e] * n[c][e] * act;
-        d[c][e] *= p.weight ? w[e] * act : act;
+        store_chunk<VEC>((TX*)p.dz + row * p.lddz, at.at[c], at.count[c], p.lanes, dz);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        dw[c][e] += d[c][e] * n[c][e];
+        d[c][e] *= w[e];
         dots[c] += d[c][e] * n[c][e];
       }
-      if (p.z) store_chunk<VEC>((TX*)p.dz + row * p.lddz, at.at[c], at.count[c], p.lanes, dz);
     }
     group_sums<WAVES, NC>(dots, p.lanes, p.pieces, lds);
 #pragma unroll
@@ -373,7 +381,7 @@ int to_power(int64_t v) {
   while (p < v) p *= 2;
   return p;
 }
-// The fewest waves whose threads hold the row in four chunks each, and then the fewest chunks.  (16 waves have 128 registers a thread.)
+// The fewest waves whose threads hold the row in four chunks each, and then the fewest chunks.
 bool shape_of(int width, int group, bool vec, Shape* out) {
   for (int waves : {1, 4, 16}) {
     Shape best = {};

@@ -11,8 +11,12 @@ namespace {
 constexpr int LM = C + 4;        // floats between rows of the 64 x 64 matrices
 constexpr float LEAST = -1e4f;   // exp of it is zero; sums of it stay far from infinity
 
+// M and P take the place of the rows of k and q that they come from: four workgroups to a compute unit in place of two, which is what hides the
+// waits between the short steps here.
 template <typename T, int KD>
-constexpr int lds_bytes() { return 2 * Lds<T>::row_bytes(KD) + 2 * C * LM * 4 + GATES * C * 4 + C * 8; }
+constexpr int matrix_bytes() { return 2 * (Lds<T>::row_bytes(KD) > C * LM * 4 ? Lds<T>::row_bytes(KD) : C * LM * 4); }
+template <typename T, int KD>
+constexpr int lds_bytes() { return matrix_bytes<T, KD>() + GATES * C * 4 + C * 8; }
 
 // c += a b of one 16 x 16 x 16 in fp32: a as rows in LDS, b as a result tile.
 __device__ inline void mma16(f32x4& c, const float* a, f32x4 b, int lane) {
@@ -34,7 +38,7 @@ __device__ inline void put_tile(float* a, f32x4 v, int lane) {
 // The pieces of a triangle, or of its transpose, in the order of the operands.
 template <typename T, int PARTS, bool TRANSPOSED>
 __device__ inline void put_frags(char* out, const float* m) {
-  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = here(threadIdx.x % WAVE), g = lane / 16;
   for (int f = wave; f < FRAGS; f += 4) {
     const int rt = TRANSPOSED ? (f < 4 ? f / 2 : f - 2) : (f < 2 ? f : f / 2 + 1);
     const int pb = TRANSPOSED ? (f < 4 ? f % 2 : 1) : (f < 2 ? 0 : f % 2);
@@ -58,35 +62,37 @@ __device__ inline void put_frags(char* out, const float* m) {
 }
 
 template <typename T, int KD, bool BACK>
-__global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
+__global__ __launch_bounds__(256, 4) void delta_prepare_kernel(Args p) {
   extern __shared__ __align__(16) char lds[];
   T* K = reinterpret_cast<T*>(lds);
   T* Q = reinterpret_cast<T*>(lds + Lds<T>::row_bytes(KD));
-  float* M = reinterpret_cast<float*>(lds + 2 * Lds<T>::row_bytes(KD));
+  float* M = reinterpret_cast<float*>(lds);
   float* P = M + C * LM;
-  double* G = reinterpret_cast<double*>(P + C * LM);
+  double* G = reinterpret_cast<double*>(lds + matrix_bytes<T, KD>());
   float* gate = reinterpret_cast<float*>(G + C);
   constexpr int LD = Lds<T>::ld(KD);
   const int BH = p.B * p.H, chunk = p.c0 + blockIdx.x / BH, bh = blockIdx.x % BH, b = bh / p.H, h = bh % p.H, hk = h / (p.H / p.Hk);
   const int s0 = chunk * C, live = min(ends_at(p, b) - s0, C);
   if (live <= 0) return;   // (nobody reads the record)
-  const int wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE, g = lane / 16;
   using R = Record<T, BACK>;
   char* out = p.records + (int64_t)blockIdx.x * R::BYTES;
 
   Fetch<T, KD, 256> fk, fq;
   fk.load(p.k, s0, b, hk, 0, live);
   fq.load(p.q, s0, b, hk, 0, live);
+  const int64_t step = s0 + min(lane, live - 1);   // (a and b are read before k and q are waited for)
+  const T raw_b = ((const T*)p.b.data)[step * p.b.stride_t + b * p.b.stride_b + h];
+  const T raw_a = p.a.data ? ((const T*)p.a.data)[step * p.a.stride_t + b * p.a.stride_b + h] : (T)0.0f;
   fk.put(K, p.k, 0, live);
   fq.put(Q, p.q, 0, live);
   if (wave == 0) {   // decays and betas of the steps
     float lg = 0.0f, beta = 0.0f;
     if (lane < live) {
-      const int64_t s = s0 + lane;
-      const float bv = (float)((const T*)p.b.data)[s * p.b.stride_t + b * p.b.stride_b + h];
+      const float bv = (float)raw_b;
       beta = p.activate ? 1.0f / (1.0f + expf(-bv)) : bv;
       if (p.a.data) {
-        lg = (float)((const T*)p.a.data)[s * p.a.stride_t + b * p.a.stride_b + h];
+        lg = (float)raw_a;
         if (p.activate) {
           lg += p.bias ? p.bias[h] : 0.0f;
           lg = p.A[h] * (fmaxf(lg, 0.0f) + log1pf(expf(-fabsf(lg))));
@@ -108,48 +114,66 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
     gate[LA * C + lane] = expf((float)(__shfl(sum, C - 1) - sum));
   }
   __syncthreads();
-  {   // lengths of k and q: four threads a row
-    const int row = threadIdx.x / 4, part = threadIdx.x % 4;
-    float kk = 0.0f, qq = 0.0f;
-    for (int c = part; c < KD; c += 4) {
-      const float x = (float)K[row * LD + c], y = (float)Q[row * LD + c];
-      kk += x * x;
-      qq += y * y;
+  // row tile `wave` of M beta and P; what stands above the diagonal is zero
+  f32x4 kk[4] = {}, qk[4] = {}, qq = {};
+  {
+    Op<T, 1> ki[KD / 32], qi[KD / 32];
+#pragma unroll
+    for (int c = 0; c < KD / 32; ++c) {
+      ki[c] = from_row(K + (16 * wave + lane % 16) * LD + 32 * c, g);
+      qi[c] = from_row(Q + (16 * wave + lane % 16) * LD + 32 * c, g);
+      mma(qq, qi[c], qi[c]);
     }
 #pragma unroll
-    for (int m = 1; m < 4; m <<= 1) kk += __shfl_xor(kk, m), qq += __shfl_xor(qq, m);
-    if (part == 0) {
-      const float rq = p.normalise ? 1.0f / sqrtf(qq + p.eps) : 1.0f;
-      gate[SK * C + row] = p.normalise ? 1.0f / sqrtf(kk + p.eps) : 1.0f;
+    for (int jt = 0; jt < 4; ++jt)
+      if (jt <= wave) {
+#pragma unroll
+        for (int c = 0; c < KD / 32; ++c) {
+          const auto kj = from_row(K + (16 * jt + lane % 16) * LD + 32 * c, g);
+          mma(kk[jt], ki[c], kj);
+          mma(qk[jt], qi[c], kj);
+        }
+      }
+  }
+  {   // squared lengths of k and q are the diagonals of their products with themselves
+    f32x4 k2 = kk[0];
+#pragma unroll
+    for (int jt = 1; jt < 4; ++jt) k2 = jt == wave ? kk[jt] : k2;
+    const int e = lane % 4;
+    if (lane % 16 / 4 == g) {
+      const float k = e == 0 ? k2[0] : e == 1 ? k2[1] : e == 2 ? k2[2] : k2[3], q = e == 0 ? qq[0] : e == 1 ? qq[1] : e == 2 ? qq[2] : qq[3];
+      const int row = 16 * wave + lane % 16;
+      const float rq = p.normalise ? 1.0f / sqrtf(q + p.eps) : 1.0f;
+      gate[SK * C + row] = p.normalise ? 1.0f / sqrtf(k + p.eps) : 1.0f;
       gate[SQ * C + row] = p.scale * rq;
       gate[RQ * C + row] = rq;
     }
   }
-  __syncthreads();
-  // row tile `wave` of M beta and P; what stands above the diagonal is zero
-  for (int jt = 0; jt < 4; ++jt) {
-    f32x4 kk = {}, qk = {};
-    if (jt <= wave) {
+  __syncthreads();   // k and q have been read
+  {
+    const int i0 = 16 * wave + 4 * g;
+    const f32x4 sk = *reinterpret_cast<const f32x4*>(gate + SK * C + i0), sq = *reinterpret_cast<const f32x4*>(gate + SQ * C + i0);
+    double Gi[4];
 #pragma unroll
-      for (int c = 0; c < KD; c += 32) {
-        const auto kj = from_row(K + (16 * jt + lane % 16) * LD + c, g);
-        mma(kk, from_row(K + (16 * wave + lane % 16) * LD + c, g), kj);
-        mma(qk, from_row(Q + (16 * wave + lane % 16) * LD + c, g), kj);
-      }
+    for (int e = 0; e < 4; ++e) Gi[e] = G[i0 + e];
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
       const int j = 16 * jt + lane % 16;
+      const float skj = gate[SK * C + j], bej = gate[BE * C + j];
+      const double Gj = G[j];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 16 * wave + 4 * g + e;
-        const float d = j <= i ? __expf((float)(G[i] - G[j])) * gate[SK * C + j] : 0.0f;
-        kk[e] = j < i ? kk[e] * d * gate[SK * C + i] * gate[BE * C + j] : 0.0f;
-        qk[e] = j <= i ? qk[e] * d * gate[SQ * C + i] : 0.0f;
+      for (int e = 0; e < 4; ++e) {   // (what is above the diagonal may be infinite before it is dropped)
+        const float d = __expf((float)(Gi[e] - Gj)) * skj, m = kk[jt][e] * d * sk[e] * bej, q = qk[jt][e] * d * sq[e];
+        kk[jt][e] = j < i0 + e ? m : 0.0f;
+        qk[jt][e] = j <= i0 + e ? q : 0.0f;
       }
+      put_tile(M + 16 * wave * LM + 16 * jt, kk[jt], lane);
+      put_tile(P + 16 * wave * LM + 16 * jt, qk[jt], lane);
     }
-    put_tile(M + 16 * wave * LM + 16 * jt, kk, lane);
-    put_tile(P + 16 * wave * LM + 16 * jt, qk, lane);
   }
   __syncthreads();
   // T over M.  Diagonal tiles by substitution, a column per lane; then from two diagonal blocks' inverses the block below: -T22 M21 T11.
+  const int lane_ = lane;
   {
     float* m = M + 16 * wave * (LM + 1);
     const int c = lane % 16;
@@ -158,9 +182,14 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
     for (int r = 0; r < 16; ++r) {
       float s = r == c ? 1.0f : 0.0f;
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-        if (j < r) s -= m[r * LM + j] * x[j];
+      for (int j = 0; j < r; j += 4) {
+        const f32x4 row = *reinterpret_cast<const f32x4*>(m + r * LM + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (j + e < r) s -= row[e] * x[j + e];
+      }
       x[r] = s;
+      if (r % 4 == 3) asm volatile("" : "+v"(x[r]) : : "memory");   // (all rows at once would not fit the registers)
     }
     __builtin_amdgcn_wave_barrier();
     if (lane < 16) {
@@ -170,6 +199,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
   }
   __syncthreads();
   if (wave < 2) {
+    const int lane = here(lane_);
     float* m = M + 32 * wave * (LM + 1);
     f32x4 w = {}, x = {};
     mma16(w, m + 16 * LM, tile(m, lane), lane);
@@ -180,6 +210,7 @@ __global__ __launch_bounds__(256) void delta_prepare_kernel(Args p) {
   __syncthreads();
   f32x4 low[2] = {};
   if (wave < 2) {   // column tile `wave` of the lower left 32 x 32
+    const int lane = here(lane_);
     f32x4 w[2] = {};
 #pragma unroll
     for (int i = 0; i < 2; ++i)

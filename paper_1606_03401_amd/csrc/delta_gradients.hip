@@ -173,6 +173,9 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       put_parts<L::NV>(dy + (1 + L::NV) * VA + vs * VLD + vc, VA, r);
     };
     fetch(0);
+    const int64_t step_a = s0 + min(lane, live - 1);   // (read here, so that the last wave's work waits for nothing)
+    const T raw_a = p.a.data ? ((const T*)p.a.data)[step_a * p.a.stride_t + b * p.a.stride_b + h] : (T)0.0f;
+    const float bias_h = p.a.data && p.activate && p.bias ? p.bias[h] : 0.0f, A_h = p.a.data && p.activate ? p.A[h] : 0.0f;
     f32x4 factors;    // the gates and behind them G: whole vectors of a record
     constexpr int FACTORS = (GATES * C * 4 + C * 8) / 16;
     static_assert(FACTORS <= THREADS && L::GATE == L::SUMS + C * 8 && Rec::SUMS == Rec::GATE + GATES * C * 4, "a vector a thread");
@@ -227,34 +230,37 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       T *first = wave < 4 ? W1 : W3, *second = wave < 4 ? W1q : W3k;
       const T* rows = wave < 4 ? Q : K;
       const float* factor = gate + (wave < 4 ? SQ : SK) * C;
-      for (int rt = jt; rt < 4; ++rt) {
-        f32x4 m = {};
+      Op<T, 1> kj[KD / 32];
 #pragma unroll
-        for (int c = 0; c < KD; c += 32) mma(m, from_row(rows + (16 * rt + c16) * LD + c, g), from_row(K + j * LD + c, g));
-        const f32x4 fi = *reinterpret_cast<const f32x4*>(factor + 16 * rt + 4 * g);
-        f32x4 a = rt == 0 ? AA[0] : rt == 1 ? AA[1] : rt == 2 ? AA[2] : AA[3], w1, w2;
+      for (int c = 0; c < KD / 32; ++c) kj[c] = from_row(K + j * LD + 32 * c, g);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 16 * rt + 4 * g + e;
-          const bool in = wave < 4 ? j <= i : j < i;
-          const float d = in ? __expf((float)(G[i] - Gj)) : 0.0f, u = (wave < 4 ? a[e] : -a[e]) * bej;
-          m[e] *= fi[e] * skj * d;
-          down += m[e] * (wave < 4 ? a[e] : -a[e]);
-          const float f = u * m[e];
-          w1[e] = u * d * skj;
-          w2[e] = u * d * fi[e];
-          colF += f;
-          const float row = over_columns(f);
-          if (c16 == 0) rowF[wave * C + i] = row;
+      for (int rt = 0; rt < 4; ++rt) {
+        const int i0 = 16 * rt + 4 * g;
+        f32x4 w1 = {}, w2 = {}, row = {};   // (above the diagonal too, as far as the products read)
+        if (rt >= jt) {
+          f32x4 m = {};
+#pragma unroll
+          for (int c = 0; c < KD / 32; ++c) mma(m, from_row(rows + (16 * rt + c16) * LD + 32 * c, g), kj[c]);
+          const f32x4 fi = *reinterpret_cast<const f32x4*>(factor + i0);
+          double Gi[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) Gi[e] = G[i0 + e];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool in = wave < 4 ? j <= i0 + e : j < i0 + e;
+            const float far = __expf((float)(Gi[e] - Gj)), d = in ? far : 0.0f, a = wave < 4 ? AA[rt][e] : -AA[rt][e], u = a * bej;
+            m[e] *= fi[e] * skj * d;
+            down += m[e] * a;
+            const float f = u * m[e];
+            w1[e] = u * d * skj;
+            w2[e] = u * d * fi[e];
+            colF += f;
+            row[e] = over_columns(f);
+          }
         }
-        put_parts<L::NM>(first + j * WLD + 16 * rt + 4 * g, WA, w1);
-        put_parts<L::NM>(second + j * WLD + 16 * rt + 4 * g, WA, w2);
-      }
-      for (int rt = 0; rt < jt; ++rt) {   // above the diagonal, as far as the products read
-        const f32x4 zero = {};
-        put_parts<L::NM>(first + j * WLD + 16 * rt + 4 * g, WA, zero);
-        put_parts<L::NM>(second + j * WLD + 16 * rt + 4 * g, WA, zero);
-        if (c16 < 4) rowF[wave * C + 16 * rt + 4 * g + c16] = 0.0f;
+        put_parts<L::NM>(first + j * WLD + i0, WA, w1);
+        put_parts<L::NM>(second + j * WLD + i0, WA, w2);
+        if (c16 == 0) *reinterpret_cast<f32x4*>(rowF + wave * C + i0) = row;
       }
       down += __shfl_xor(down, 16);
       colF += __shfl_xor(colF, 16);
@@ -355,10 +361,10 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       if (i < steps) {
         const bool in = i < live;
         if (p.a.data && in) {
-          const float raw = (float)((const T*)p.a.data)[s * p.a.stride_t + b * p.a.stride_b + h] + (p.activate && p.bias ? p.bias[h] : 0.0f);
+          const float raw = (float)raw_a + bias_h;
           if (p.activate) {
             dlog = dG * (fmaxf(raw, 0.0f) + log1pf(expf(-fabsf(raw))));
-            da = dG * p.A[h] / (1.0f + expf(-raw));
+            da = dG * A_h / (1.0f + expf(-raw));
           } else {
             da = dG;
           }

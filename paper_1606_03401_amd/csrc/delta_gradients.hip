@@ -28,10 +28,11 @@ struct Layout {
   static constexpr int W = BLOCK;                                                                    // four matrices, over them
   static constexpr int SUMS = BLOCK + (2 * BLOCK_BYTES > 4 * NM * WSIZE ? 2 * BLOCK_BYTES : 4 * NM * WSIZE);
   static constexpr int GATE = SUMS + C * 8, ROWF = GATE + GATES * C * 4, COLS = ROWF + WAVES * C * 4, DOTS = COLS + 4 * C * 4,
-                       NORMS = DOTS + 4 * WAVES * C * 4, MORE = NORMS + 2 * C * 4, BYTES = MORE + WAVES * 4;
+                       NORMS = DOTS + 3 * WAVES * C * 4, MORE = NORMS + 2 * C * 4, BYTES = MORE + WAVES * 4;
 };
 
-// An operand in the order in which it stands: lane l's eight values are 8 g .. 8 g + 7 of the 32.  (Both operands of such a product come from memory.)
+// An operand in the order in which it stands in a block: places 8 g .. 8 g + 7 hold columns 4 g .. and 16 + 4 g .., so that a load of S for one lane group
+// takes 64 neighbouring bytes of a row.
 template <int N>
 __device__ inline Op<__bf16, N> as_it_stands(const __bf16* p, int apart, int g) {
   Op<__bf16, N> o;
@@ -100,6 +101,25 @@ __device__ inline float over_columns(float v) {
   return v;
 }
 
+// Sums of 16 values over 16 neighbouring lanes; lane c's is that of value c.  In each step a lane hands the half that it does not keep to its mirror
+// image: 45 operations where 16 sums of their own take 64.
+__device__ inline float over_columns(float (&v)[16], int c16) {
+  auto half = [&](auto n, auto mirror) {
+    constexpr int N = decltype(n)::value;
+    const bool upper = c16 & N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float keep = upper ? v[i + N] : v[i], give = upper ? v[i] : v[i + N];
+      v[i] = keep + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(give), decltype(mirror)::value, 0xf, 0xf, false));
+    }
+  };
+  half(std::integral_constant<int, 8>{}, std::integral_constant<int, 0x140>{});   // 15 - c
+  half(std::integral_constant<int, 4>{}, std::integral_constant<int, 0x141>{});   // 7 - c of 8
+  half(std::integral_constant<int, 2>{}, std::integral_constant<int, 0x1B>{});    // 3 - c of 4
+  half(std::integral_constant<int, 1>{}, std::integral_constant<int, 0xB1>{});    // 1 - c of 2
+  return v[0];
+}
+
 // SHARED: more than one value head to a key head.  (Without the loop over them the compiler keeps what belongs to it out of registers.)
 template <typename T, int KD, bool SHARED>
 __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
@@ -154,23 +174,24 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
     typedef T Quad __attribute__((ext_vector_type(4), aligned(sizeof(T) * 4)));
     f32x4 z, r, x[2], y[2];
     Quad q4;
-    const unsigned off_v = (unsigned)(vs * p.dvp + vc) * 4u, off_s = (unsigned)((mine ? col : c16) * p.dvp + 8 * g) * 4u;
+    const unsigned off_v = (unsigned)(vs * p.dvp + vc) * 4u, off_s = (unsigned)((mine ? col : c16) * p.dvp + 4 * g) * 4u;
     auto fetch = [&](int v0) {
       z = *reinterpret_cast<const f32x4*>(near(Zg + v0, off_v));
       r = *reinterpret_cast<const f32x4*>(near(Rg + v0, off_v));
       q4 = *reinterpret_cast<const Quad*>(near(dyg, (off_y + (unsigned)min(v0 + vc, p.dy.width - 4)) * (unsigned)sizeof(T)));
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        x[i] = *reinterpret_cast<const f32x4*>(near(Sg + v0 + 4 * i, off_s));
-        y[i] = *reinterpret_cast<const f32x4*>(near(dSg + v0 + 4 * i, off_s));
+        x[i] = *reinterpret_cast<const f32x4*>(near(Sg + v0 + 16 * i, off_s));
+        y[i] = *reinterpret_cast<const f32x4*>(near(dSg + v0 + 16 * i, off_s));
       }
     };
     auto put = [&](int v0, int buffer) {
       T* dy = (T*)(lds + L::BLOCK + buffer * L::BLOCK_BYTES);
       if (vs >= live || v0 + vc >= p.dy.width) q4 = Quad{};
-      *reinterpret_cast<Quad*>(dy + vs * VLD + vc) = q4;
-      put_parts<L::NV>(dy + VA + vs * VLD + vc, VA, z);
-      put_parts<L::NV>(dy + (1 + L::NV) * VA + vs * VLD + vc, VA, r);
+      T* place = dy + vs * VLD + vc % 16 * 2 + vc / 16 * 4;
+      *reinterpret_cast<Quad*>(place) = q4;
+      put_parts<L::NV>(place + VA, VA, z);
+      put_parts<L::NV>(place + (1 + L::NV) * VA, VA, r);
     };
     fetch(0);
     const int64_t step_a = s0 + min(lane, live - 1);   // (read here, so that the last wave's work waits for nothing)
@@ -300,39 +321,62 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         products(W3, false, w, kc);
         products(W3k, true, w, kc);
       }
+      // q~ . (gamma dY S^T), k^ . (gamma Z S^T), k^ . (gamma_C / gamma R dS'^T) of each step, over this wave's columns
+      float v[16];
+      float* dot = dots + wave * C + 16 * (c16 / 4) + 4 * g + c16 % 4;
+      auto factors_of = [&](int which, int rt) { return *reinterpret_cast<const f32x4*>(gate + which * C + 16 * rt + 4 * g); };
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) {
-        const f32x4 ga = *reinterpret_cast<const f32x4*>(gate + GA * C + 16 * rt + 4 * g);
-        const f32x4 be = *reinterpret_cast<const f32x4*>(gate + BE * C + 16 * rt + 4 * g);
-        const f32x4 la = *reinterpret_cast<const f32x4*>(gate + LA * C + 16 * rt + 4 * g);
-        const f32x4 sk = *reinterpret_cast<const f32x4*>(gate + SK * C + 16 * rt + 4 * g);
-        const f32x4 sq = *reinterpret_cast<const f32x4*>(gate + SQ * C + 16 * rt + 4 * g);
-        const f32x4 ys = ga * YS[rt], zs = ga * ZS[rt], rs = la * RS[rt];
+        const f32x4 ys = factors_of(GA, rt) * YS[rt], sq = factors_of(SQ, rt);
         dQ[rt] += wx[rt] + ys;
-        dK[rt] += w[rt] + be * rs - zs;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * rt + e] = (float)Q[(16 * rt + 4 * g + e) * LD + col] * sq[e] * ys[e];
+      }
+      dot[0] = over_columns(v, c16);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 k[4];
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) {
+        const f32x4 zs = factors_of(GA, rt) * ZS[rt], sk = factors_of(SK, rt);
+        dK[rt] += w[rt] - zs;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int i = 16 * rt + 4 * g + e;
-          const float kr = (float)K[i * LD + col], qr = (float)Q[i * LD + col], k = kr * sk[e], q = qr * sq[e];
-          // q~ . (gamma dY S^T) - k^ . (gamma Z S^T);  k^ . (gamma_C / gamma R dS'^T);  and for the norms' sake q . dq, k . dk
-          const float one = over_columns(q * ys[e] - k * zs[e]), two = over_columns(k * rs[e]);
-          const float three = over_columns(qr * dQ[rt][e]), four = over_columns(kr * dK[rt][e]);
-          if (c16 < 4) dots[(c16 * WAVES + wave) * C + i] = c16 == 0 ? one : c16 == 1 ? two : c16 == 2 ? three : four;
+          k[rt][e] = (float)K[(16 * rt + 4 * g + e) * LD + col] * sk[e];
+          v[4 * rt + e] = k[rt][e] * zs[e];
         }
-        __builtin_amdgcn_sched_barrier(0);
       }
+      dot[WAVES * C] = over_columns(v, c16);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) {
+        const f32x4 rs = factors_of(LA, rt) * RS[rt];
+        dK[rt] += factors_of(BE, rt) * rs;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * rt + e] = k[rt][e] * rs[e];
+      }
+      dot[2 * WAVES * C] = over_columns(v, c16);
     }
     __syncthreads();
-    if (p.normalise && (!SHARED || n == group - 1)) {   // over the waves, with the factors of both norms
-      if (threadIdx.x >= THREADS - 2 * C) {
-        const int i = threadIdx.x % C, k = (threadIdx.x - (THREADS - 2 * C)) / C;
-        float sum = 0.0f;
+    if (p.normalise && wave >= 6) {
+      // q . dq and k . dk with the factors of both norms; the terms of dq and dk make sums that are there already, of rows and columns of F and those above
+      const int i = lane;
+      float sum = 0.0f;
+      if (wave == 6) {
 #pragma unroll
-        for (int w = 0; w < NT; ++w) sum += dots[((2 + k) * WAVES + w) * C + i];
-        const float f = gate[(k ? SK : RQ) * C + i];
-        norms[k * C + i] = sum * f * f * (k ? 1.0f : p.scale);
+        for (int w = 0; w < 4; ++w) sum += rowF[w * C + i];
+#pragma unroll
+        for (int w = 0; w < NT; ++w) sum += dots[w * C + i];
+        sum *= gate[RQ * C + i];
+      } else {
+        float e = 0.0f, zs = 0.0f;
+#pragma unroll
+        for (int w = 4; w < 8; ++w) sum += rowF[w * C + i];
+#pragma unroll
+        for (int w = 0; w < NT; ++w) zs += dots[(WAVES + w) * C + i], e += dots[(2 * WAVES + w) * C + i];
+        sum = (sum + cols[2 * C + i] + cols[3 * C + i] + gate[BE * C + i] * e - zs) * gate[SK * C + i];
       }
-      __syncthreads();
+      float* norm = norms + (wave - 6) * C + i;
+      *norm = SHARED && n ? *norm + sum : sum;
     }
     if (wave == 0) {
       const int i = lane;
@@ -341,8 +385,8 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       for (int w = 0; w < WAVES; ++w) rows += rowF[w * C + i];
 #pragma unroll
       for (int w = 0; w < NT; ++w) {
-        first += dots[w * C + i];
-        second += dots[(WAVES + w) * C + i];
+        first += dots[w * C + i] - dots[(WAVES + w) * C + i];
+        second += dots[(2 * WAVES + w) * C + i];
         all += more[w];
       }
       const float beta = gate[BE * C + i], e = beta * second;
@@ -380,6 +424,7 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       }
     }
   }
+  if (p.normalise) __syncthreads();   // `norms`
   if (!mine || col_ >= p.dk) return;
 #pragma unroll
   for (int rt = 0; rt < 4; ++rt) {

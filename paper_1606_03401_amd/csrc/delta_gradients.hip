@@ -5,7 +5,8 @@
 //     dbeta_j = sum_i (P o dY R^T)_ij - sum_i (M o E)_ij + (gamma_C / gamma k^)_j . (R dS'^T)_j,
 //     dG_i = sum_j F_ij - sum_j F_ji + q~_i . (gamma dY S^T)_i - k^_i . (gamma Z S^T)_i - e_i,   F = dP o P + dM o M,
 //     e_j = beta_j (gamma_C / gamma k^)_j . (R dS'^T)_j,   the last step's dG also sum e + gamma_C <dS', S>,   dg_s = sum_{i >= s} dG_i.
-// A workgroup of eight waves has a chunk of a sequence and one key head, and goes through the value heads that share it.  Wave w computes
+// A workgroup of eight waves, one to a compute unit, goes through chunks of sequences with one head each; or, where value heads share a key head, has one
+// chunk and key head and goes through its value heads.  Wave w computes
 // 16 columns of dq and dk; in what is 64 x 64, waves 0 .. 3 have column tiles of dY R^T and P, 4 .. 7 those of E and M.
 #include "delta.h"
 #include "dynamic_lds.h"
@@ -18,6 +19,7 @@ namespace {
 constexpr int WAVES = 8, THREADS = WAVES * WAVE;
 // Parts of R, Z, S and dS' in the products, and of W1 .. W3, which reach dq and dk only.
 constexpr int N32 = 3, NW = 2;
+constexpr int COMPUTE_UNITS = 256;
 constexpr int VB = 32;      // columns of a block of dY, Z and R
 
 template <typename T, int KD>
@@ -120,9 +122,37 @@ __device__ inline float over_columns(float (&v)[16], int c16) {
   return v[0];
 }
 
+// Sum over a wave in each lane: rows of 16 lanes, then the four rows.
+__device__ inline float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+__device__ inline float over_wave(float v) {
+  v = over_columns(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+// Sum of the values of this lane and those behind it.
+__device__ inline float from_lane_on(float v, int lane) {
+  auto add = [&](auto shift) {   // (lanes behind the row's end count as zero)
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(shift)::value, 0xf, 0xf, true));
+  };
+  add(std::integral_constant<int, 0x101>{});
+  add(std::integral_constant<int, 0x102>{});
+  add(std::integral_constant<int, 0x104>{});
+  add(std::integral_constant<int, 0x108>{});
+  const float last = lane_of(v, 48), two = lane_of(v, 32) + last, three = lane_of(v, 16) + two;
+  return v + (lane < 16 ? three : lane < 32 ? two : lane < 48 ? last : 0.0f);
+}
+
+// The kernel's first argument where the launch put it.
+__device__ inline const Args* fresh_arguments() {
+  auto* at = (const __attribute__((address_space(4))) Args*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return (const Args*)at;
+}
+
 // SHARED: more than one value head to a key head.  (Without the loop over them the compiler keeps what belongs to it out of registers.)
 template <typename T, int KD, bool SHARED>
-__global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
+__global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments) {
+  (void)arguments;
+  const Args* now = fresh_arguments();   // (read again for each head: kept over the loop, they would fill the scalar registers)
   extern __shared__ __align__(16) char lds[];
   using L = Layout<T, KD>;
   using Rec = Record<T, true>;
@@ -133,58 +163,113 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
   double* G = (double*)(lds + L::SUMS);
   float *gate = (float*)(lds + L::GATE), *rowF = (float*)(lds + L::ROWF), *cols = (float*)(lds + L::COLS), *dots = (float*)(lds + L::DOTS),
         *norms = (float*)(lds + L::NORMS), *more = (float*)(lds + L::MORE);
-  const int per = p.B * p.Hk, chunk = p.c0 + blockIdx.x / per, b = blockIdx.x % per / p.Hk, hk = blockIdx.x % p.Hk, group = SHARED ? p.H / p.Hk : 1;
-  const int s0 = chunk * C, steps = min(p.t - s0, C), live = min(ends_at(p, b) - s0, C), BH = p.B * p.H;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = threadIdx.x % WAVE, g = lane / 16, c16 = lane % 16;
+  const int per = now->B * now->Hk, items = (now->c1 - now->c0) * per, group = SHARED ? now->H / now->Hk : 1;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane_ = threadIdx.x % WAVE;
   const bool mine = wave < NT;               // waves with columns of dq and dk
   // column tiles with many rows and with few are paired: waves w and w + 4 share a SIMD
-  const int jt = wave < 4 ? wave : 7 - wave, col = 16 * wave + c16;
-  float* parts = p.parts + ((int64_t)(chunk - p.c0) * p.B + b) * 2 * p.H;
-  T* dq = (T*)p.dq.data + (int64_t)s0 * p.dq.stride_t + b * p.dq.stride_b + hk * p.dk + col;
-  T* dk = (T*)p.dkey.data + (int64_t)s0 * p.dkey.stride_t + b * p.dkey.stride_b + hk * p.dk + col;
-  if (live <= 0) {   // behind the sequence's end
-    if (mine && col < p.dk)
-      for (int s = g; s < steps; s += 4) dq[(int64_t)s * p.dq.stride_t] = dk[(int64_t)s * p.dkey.stride_t] = (T)0.0f;
-    for (int i = threadIdx.x; i < steps * group; i += THREADS) {
-      const int s = s0 + i / group, h = hk * group + i % group;
-      ((T*)p.db.data)[s * p.db.stride_t + b * p.db.stride_b + h] = (T)0.0f;
-      if (p.a.data) ((T*)p.da.data)[s * p.da.stride_t + b * p.da.stride_b + h] = (T)0.0f;
-    }
-    for (int i = threadIdx.x; i < group; i += THREADS) parts[hk * group + i] = parts[p.H + hk * group + i] = 0.0f;
-    return;
-  }
-  Fetch<T, KD, THREADS> fk, fq;
-  fk.load(p.k, s0, b, hk, 0, live);
-  fq.load(p.q, s0, b, hk, 0, live);
-  static_assert(C * VB / 4 == THREADS, "a block is four values a thread");
-  if constexpr (SHARED) {
-    fk.put(K, p.k, 0, live);
-    fq.put(Q, p.q, 0, live);
-  }
-  f32x4 dQ[4] = {}, dK[4] = {};
-  const int lane_ = lane, col_ = col;
-  for (int h = hk * group, n = 0; n < group; ++h, ++n) {
-    const int lane = SHARED ? here(lane_) : lane_, g = lane / 16, c16 = lane % 16, col = 16 * wave + c16;
-    const int vs = (64 * wave + lane) / (VB / 4), vc = lane % (VB / 4) * 4;   // a thread's step and four columns of a block
-    const int64_t at = (int64_t)(chunk - p.c0) * BH + b * p.H + h;
-    const char* rec = p.records + at * Rec::BYTES;
-    const float *Sg = p.S + at * KD * p.dvp, *dSg = p.dS + at * KD * p.dvp, *Rg = p.R + at * C * p.dvp, *Zg = p.Z + at * C * p.dvp;
-    const T* dyg = (const T*)p.dy.data + (int64_t)s0 * p.dy.stride_t + b * p.dy.stride_b + (int64_t)h * p.dy.head;
-    const unsigned off_y = (unsigned)(min(vs, live - 1) * (int)p.dy.stride_t);
-    typedef T Quad __attribute__((ext_vector_type(4), aligned(sizeof(T) * 4)));
-    f32x4 z, r, x[2], y[2];
-    Quad q4;
-    const unsigned off_v = (unsigned)(vs * p.dvp + vc) * 4u, off_s = (unsigned)((mine ? col : c16) * p.dvp + 4 * g) * 4u;
-    auto fetch = [&](int v0) {
-      z = *reinterpret_cast<const f32x4*>(near(Zg + v0, off_v));
-      r = *reinterpret_cast<const f32x4*>(near(Rg + v0, off_v));
-      q4 = *reinterpret_cast<const Quad*>(near(dyg, (off_y + (unsigned)min(v0 + vc, p.dy.width - 4)) * (unsigned)sizeof(T)));
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        x[i] = *reinterpret_cast<const f32x4*>(near(Sg + v0 + 16 * i, off_s));
-        y[i] = *reinterpret_cast<const f32x4*>(near(dSg + v0 + 16 * i, off_s));
+  const int jt = wave < 4 ? wave : 7 - wave;
+  struct Item {
+    int chunk, b, hk, s0, live;   // chunk: from the launch's first one on
+  };
+  auto item_at = [&](int item) {
+    const Args& p = *now;
+    Item w;
+    w.chunk = item / per;
+    w.b = (item - w.chunk * per) / p.Hk;
+    w.hk = item - w.chunk * per - w.b * p.Hk;
+    w.s0 = (p.c0 + w.chunk) * C;
+    w.live = min(ends_at(p, w.b) - w.s0, C);
+    return w;
+  };
+  auto parts_of = [&](const Item& w) { return now->parts + ((int64_t)w.chunk * now->B + w.b) * 2 * now->H; };
+  auto out_of = [&](const mebptt_seq& s, const Item& w) {
+    const Args& p = *now;
+    return (T*)s.data + (int64_t)w.s0 * s.stride_t + w.b * s.stride_b + w.hk * p.dk + 16 * wave + here(lane_) % 16;
+  };
+  // The first item from `item` on, of those that this workgroup takes, that has steps in it; gradients behind a sequence's end are zero.
+  auto next_live = [&](int item) {
+    const Args& p = *now;
+    for (; item < items; item += gridDim.x) {
+      const Item w = item_at(item);
+      if (w.live > 0) break;
+      const int steps = min(p.t - w.s0, C), lane = here(lane_);
+      if (mine && 16 * wave + lane % 16 < p.dk) {
+        T *dq = out_of(p.dq, w), *dk = out_of(p.dkey, w);
+        for (int s = lane / 16; s < steps; s += 4) dq[(int64_t)s * p.dq.stride_t] = dk[(int64_t)s * p.dkey.stride_t] = (T)0.0f;
       }
-    };
+      for (int i = threadIdx.x; i < steps * group; i += THREADS) {
+        const int s = w.s0 + i / group, h = w.hk * group + i % group;
+        ((T*)p.db.data)[s * p.db.stride_t + w.b * p.db.stride_b + h] = (T)0.0f;
+        if (p.a.data) ((T*)p.da.data)[s * p.da.stride_t + w.b * p.da.stride_b + h] = (T)0.0f;
+      }
+      float* parts = parts_of(w);
+      for (int i = threadIdx.x; i < group; i += THREADS) parts[w.hk * group + i] = parts[p.H + w.hk * group + i] = 0.0f;
+    }
+    return item;
+  };
+  static_assert(C * VB / 4 == THREADS, "a block is four values a thread");
+  constexpr int FACTORS = (GATES * C * 4 + C * 8) / 16;   // the gates and behind them G: whole vectors of a record
+  static_assert(FACTORS <= THREADS && L::GATE == L::SUMS + C * 8 && Rec::SUMS == Rec::GATE + GATES * C * 4, "a vector a thread");
+  // What an item needs first is read while the item before it is being finished.  (Where heads are shared no registers are left for that: dq and dk are kept
+  // from head to head.)
+  typedef T Quad __attribute__((ext_vector_type(4), aligned(sizeof(T) * 4)));
+  Fetch<T, KD, THREADS> fk, fq;
+  f32x4 z, r, x[2], y[2], factors;
+  Quad q4;
+  T raw_a;
+  // WHAT: 0 rows of dY, Z and R, 1 of S, 2 of dS'
+  auto fetch = [&](const Item& w, int h, int v0, auto what) {
+    constexpr int WHAT = decltype(what)::value;
+    const Args& p = *now;
+    const int lane = here(lane_), vs = (64 * wave + lane) / (VB / 4), vc = lane % (VB / 4) * 4;   // a thread's step and four columns of a block
+    const int64_t at = (int64_t)w.chunk * (p.B * p.H) + w.b * p.H + h;
+    if constexpr (WHAT == 0) {
+      const unsigned off_v = (unsigned)(vs * p.dvp + vc) * 4u, off_y = (unsigned)(min(vs, w.live - 1) * (int)p.dy.stride_t);
+      const T* dyg = (const T*)p.dy.data + (int64_t)w.s0 * p.dy.stride_t + w.b * p.dy.stride_b + (int64_t)h * p.dy.head;
+      z = *reinterpret_cast<const f32x4*>(near(p.Z + at * C * p.dvp + v0, off_v));
+      r = *reinterpret_cast<const f32x4*>(near(p.R + at * C * p.dvp + v0, off_v));
+      q4 = *reinterpret_cast<const Quad*>(near(dyg, (off_y + (unsigned)min(v0 + vc, p.dy.width - 4)) * (unsigned)sizeof(T)));
+    } else {
+      const unsigned off_s = (unsigned)((16 * (mine ? wave : 0) + lane % 16) * p.dvp + lane / 16 * 4) * 4u;
+      const float* from = (WHAT == 1 ? p.S : p.dS) + at * KD * p.dvp + v0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) (WHAT == 1 ? x : y)[i] = *reinterpret_cast<const f32x4*>(near(from + 16 * i, off_s));
+    }
+  };
+  constexpr std::integral_constant<int, 0> ROWS{};
+  constexpr std::integral_constant<int, 1> STATE{};
+  constexpr std::integral_constant<int, 2> STATE_GRAD{};
+  auto fetch_first = [&](const Item& w, int n) {
+    const Args& p = *now;
+    const int h = w.hk * group + n, lane = here(lane_);
+    if (n == 0) {
+      fk.load(p.k, w.s0, w.b, w.hk, 0, w.live);
+      fq.load(p.q, w.s0, w.b, w.hk, 0, w.live);
+    }
+    factors = *reinterpret_cast<const f32x4*>(p.records + ((int64_t)w.chunk * (p.B * p.H) + w.b * p.H + h) * Rec::BYTES + Rec::GATE +
+                                              min((int)threadIdx.x, FACTORS - 1) * 16);
+    fetch(w, h, 0, ROWS);
+    fetch(w, h, 0, STATE);
+    fetch(w, h, 0, STATE_GRAD);
+    raw_a = p.a.data ? ((const T*)p.a.data)[(w.s0 + min(lane, w.live - 1)) * p.a.stride_t + w.b * p.a.stride_b + h] : (T)0.0f;
+  };
+  int item = next_live(blockIdx.x), n = 0;
+  if (item >= items) return;
+  Item at = item_at(item);
+  if constexpr (!SHARED) fetch_first(at, 0);
+  f32x4 dQ[4], dK[4];
+  while (true) {
+    now = fresh_arguments();
+    const Args& p = *now;
+    if (!SHARED || n == 0) {
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) dQ[rt] = dK[rt] = f32x4{};
+    }
+    const int lane = here(lane_), g = lane / 16, c16 = lane % 16, col = 16 * wave + c16, h = at.hk * group + n;
+    const int b = at.b, s0 = at.s0, live = at.live, steps = min(p.t - s0, C);
+    const int vs = (64 * wave + lane) / (VB / 4), vc = lane % (VB / 4) * 4;
+    if constexpr (SHARED) fetch_first(at, n);
+    const T this_a = raw_a;
     auto put = [&](int v0, int buffer) {
       T* dy = (T*)(lds + L::BLOCK + buffer * L::BLOCK_BYTES);
       if (vs >= live || v0 + vc >= p.dy.width) q4 = Quad{};
@@ -193,20 +278,11 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       put_parts<L::NV>(place + VA, VA, z);
       put_parts<L::NV>(place + (1 + L::NV) * VA, VA, r);
     };
-    fetch(0);
-    const int64_t step_a = s0 + min(lane, live - 1);   // (read here, so that the last wave's work waits for nothing)
-    const T raw_a = p.a.data ? ((const T*)p.a.data)[step_a * p.a.stride_t + b * p.a.stride_b + h] : (T)0.0f;
-    const float bias_h = p.a.data && p.activate && p.bias ? p.bias[h] : 0.0f, A_h = p.a.data && p.activate ? p.A[h] : 0.0f;
-    f32x4 factors;    // the gates and behind them G: whole vectors of a record
-    constexpr int FACTORS = (GATES * C * 4 + C * 8) / 16;
-    static_assert(FACTORS <= THREADS && L::GATE == L::SUMS + C * 8 && Rec::SUMS == Rec::GATE + GATES * C * 4, "a vector a thread");
-    const int fi = min((int)threadIdx.x, FACTORS - 1);
-    factors = *reinterpret_cast<const f32x4*>(rec + Rec::GATE + fi * 16);
-    if constexpr (!SHARED) {
+    if (n == 0) {
       fk.put(K, p.k, 0, live);
       fq.put(Q, p.q, 0, live);
     }
-    __syncthreads();   // the head before has been read
+    const int fi = min((int)threadIdx.x, FACTORS - 1);
     *reinterpret_cast<f32x4*>(fi < GATES * C / 4 ? reinterpret_cast<char*>(gate) + fi * 16 : reinterpret_cast<char*>(G) + (fi * 16 - GATES * C * 4)) = factors;
     f32x4 YS[4] = {}, ZS[4] = {}, RS[4] = {}, AA[4] = {};
     float inner = 0.0f;
@@ -218,7 +294,10 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) inner += x[i][e] * y[i][e];
       __syncthreads();   // (and the block before the last one has been read)
-      fetch(min(v0 + VB, p.dvp - VB));   // (not under a condition: it would be waited for there)
+      const int ahead = min(v0 + VB, p.dvp - VB);   // (the last block again, not under a condition: it would be waited for there)
+      fetch(at, h, ahead, ROWS);
+      fetch(at, h, ahead, STATE);
+      fetch(at, h, ahead, STATE_GRAD);
       const T *DY = (const T*)(lds + L::BLOCK + buffer * L::BLOCK_BYTES), *ZL = DY + VA, *RL = ZL + L::NV * VA;
       const auto rj = as_it_stands<N32>(RL + (16 * jt + c16) * VLD, VA, g);
       Op<T, 1> dy[4];
@@ -292,12 +371,12 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         cols[(2 + wave / 4) * C + j] = colF;
       }
     }
-    inner = wave_sum(inner);
+    inner = over_wave(inner);
     if (lane == 0) more[wave] = inner;
     __syncthreads();
+    f32x4 wx[4] = {}, w[4] = {};
     if (mine) {
       // lower triangles have tiles 0 .. 3 of the first 32 columns and 2, 3 of the others, their transposes 0, 1 of the first and all of the others
-      f32x4 wx[4] = {}, w[4] = {};
 #pragma unroll
       for (int pb = 0; pb < 2; ++pb) {
         const auto kc = from_columns<LD>(K, 16 * wave, 32 * pb, lane), qc = from_columns<LD>(Q, 16 * wave, 32 * pb, lane);
@@ -321,6 +400,14 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         products(W3, false, w, kc);
         products(W3k, true, w, kc);
       }
+    }
+    now = fresh_arguments();
+    const bool last_head = !SHARED || n == group - 1;
+    const int item_then = SHARED ? items : next_live(item + gridDim.x);
+    const bool more_items = item_then < items;
+    const Item then = more_items ? item_at(item_then) : at;
+    if constexpr (!SHARED) fetch_first(then, 0);   // (not under a condition: it would be waited for there)
+    if (mine) {
       // q~ . (gamma dY S^T), k^ . (gamma Z S^T), k^ . (gamma_C / gamma R dS'^T) of each step, over this wave's columns
       float v[16];
       float* dot = dots + wave * C + 16 * (c16 / 4) + 4 * g + c16 % 4;
@@ -391,21 +478,17 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
       }
       const float beta = gate[BE * C + i], e = beta * second;
       float dG = rows - (cols[2 * C + i] + cols[3 * C + i]) + first - e;
-      const float ends = wave_sum(e);
+      const float ends = over_wave(e);
       if (i == C - 1) dG += ends + gate[GA * C + C - 1] * all;
-      // sum from this step to the last one
-#pragma unroll
-      for (int m = 1; m < WAVE; m <<= 1) {
-        const float behind = __shfl_down(dG, m);
-        if (lane + m < WAVE) dG += behind;
-      }
+      dG = from_lane_on(dG, i);   // sum from this step to the last one
       const float dbeta = cols[i] + cols[C + i] + second;
       float dlog = 0.0f, da = 0.0f;
       const int64_t s = s0 + i;
+      const float bias_h = p.a.data && p.activate && p.bias ? p.bias[h] : 0.0f, A_h = p.a.data && p.activate ? p.A[h] : 0.0f;
       if (i < steps) {
         const bool in = i < live;
         if (p.a.data && in) {
-          const float raw = (float)raw_a + bias_h;
+          const float raw = (float)this_a + bias_h;
           if (p.activate) {
             dlog = dG * (fmaxf(raw, 0.0f) + log1pf(expf(-fabsf(raw))));
             da = dG * A_h / (1.0f + expf(-raw));
@@ -416,36 +499,49 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args p) {
         if (p.a.data) ((T*)p.da.data)[s * p.da.stride_t + b * p.da.stride_b + h] = (T)da;
         ((T*)p.db.data)[s * p.db.stride_t + b * p.db.stride_b + h] = (T)(!in ? 0.0f : p.activate ? dbeta * beta * (1.0f - beta) : dbeta);
       }
-      dlog = wave_sum(dlog);
-      da = wave_sum(p.activate ? da : 0.0f);
+      dlog = over_wave(dlog);
+      da = over_wave(p.activate ? da : 0.0f);
       if (lane == 0) {
+        float* parts = parts_of(at);
         parts[h] = dlog;
         parts[p.H + h] = da;
       }
     }
-  }
-  if (p.normalise) __syncthreads();   // `norms`
-  if (!mine || col_ >= p.dk) return;
+    __syncthreads();   // `norms`; and this head has been read
+    if (last_head) {
+      if (mine && col < p.dk) {
+        T *dq = out_of(p.dq, at), *dk = out_of(p.dkey, at);
 #pragma unroll
-  for (int rt = 0; rt < 4; ++rt) {
-    f32x4 dqt = p.scale * dQ[rt], dkt = dK[rt];
-    if (p.normalise) {
-      const f32x4 rq = *reinterpret_cast<const f32x4*>(gate + RQ * C + 16 * rt + 4 * g), rk = *reinterpret_cast<const f32x4*>(gate + SK * C + 16 * rt + 4 * g);
-      const f32x4 a = *reinterpret_cast<const f32x4*>(norms + 16 * rt + 4 * g), c = *reinterpret_cast<const f32x4*>(norms + C + 16 * rt + 4 * g);
+        for (int rt = 0; rt < 4; ++rt) {
+          f32x4 dqt = p.scale * dQ[rt], dkt = dK[rt];
+          if (p.normalise) {
+            const f32x4 rq = *reinterpret_cast<const f32x4*>(gate + RQ * C + 16 * rt + 4 * g), rk = *reinterpret_cast<const f32x4*>(gate + SK * C + 16 * rt + 4 * g);
+            const f32x4 a = *reinterpret_cast<const f32x4*>(norms + 16 * rt + 4 * g), c = *reinterpret_cast<const f32x4*>(norms + C + 16 * rt + 4 * g);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = 16 * rt + 4 * g + e;
-        dqt[e] = rq[e] * (dqt[e] - (float)Q[i * LD + col] * a[e]);
-        dkt[e] = rk[e] * (dkt[e] - (float)K[i * LD + col] * c[e]);
+            for (int e = 0; e < 4; ++e) {
+              const int i = 16 * rt + 4 * g + e;
+              dqt[e] = rq[e] * (dqt[e] - (float)Q[i * LD + col] * a[e]);
+              dkt[e] = rk[e] * (dkt[e] - (float)K[i * LD + col] * c[e]);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = 16 * rt + 4 * g + e;
+            if (i < steps) {
+              dq[(int64_t)i * p.dq.stride_t] = (T)(i < live ? dqt[e] : 0.0f);
+              dk[(int64_t)i * p.dkey.stride_t] = (T)(i < live ? dkt[e] : 0.0f);
+            }
+          }
+        }
       }
+      if (!more_items) return;
+      __syncthreads();   // k, q, gates and `norms` have been read
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = 16 * rt + 4 * g + e;
-      if (i < steps) {
-        dq[(int64_t)i * p.dq.stride_t] = (T)(i < live ? dqt[e] : 0.0f);
-        dk[(int64_t)i * p.dkey.stride_t] = (T)(i < live ? dkt[e] : 0.0f);
-      }
+    if constexpr (SHARED) {
+      ++n;
+    } else {
+      item = item_then;
+      at = then;
     }
   }
 }
@@ -461,7 +557,9 @@ int mebptt::delta::gradients(const Args& p, int dtype, hipStream_t stream) {
       constexpr bool SHARED = decltype(shared)::value;
       const hipError_t e = allow_dynamic_lds<delta_gradients_kernel<T, KD, SHARED>>(BYTES);
       if (e != hipSuccess) return set_error(MEBPTT_EHIP, "LDS of the delta rule: %s", hipGetErrorString(e));
-      delta_gradients_kernel<T, KD, SHARED><<<(unsigned)((p.c1 - p.c0) * p.B * p.Hk), THREADS, BYTES, stream>>>(p);
+      const int64_t items = (int64_t)(p.c1 - p.c0) * p.B * p.Hk;
+      const unsigned groups = (unsigned)(SHARED ? items : std::min<int64_t>(items, COMPUTE_UNITS));
+      delta_gradients_kernel<T, KD, SHARED><<<groups, THREADS, BYTES, stream>>>(p);
       return launched("delta rule, gradients");
     };
     return p.H > p.Hk ? go(std::true_type{}) : go(std::false_type{});

@@ -294,10 +294,14 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
 #pragma unroll
         for (int e = 0; e < 4; ++e) inner += x[i][e] * y[i][e];
       __syncthreads();   // (and the block before the last one has been read)
-      const int ahead = min(v0 + VB, p.dvp - VB);   // (the last block again, not under a condition: it would be waited for there)
-      fetch(at, h, ahead, ROWS);
-      fetch(at, h, ahead, STATE);
-      fetch(at, h, ahead, STATE_GRAD);
+      // The next block, or the last one again: under a condition it would be waited for there.  (Shared heads leave fewer registers: a few loads at a time there.
+      // Where there are enough, that was no faster.)
+      const int ahead = min(v0 + VB, p.dvp - VB);
+      if constexpr (!SHARED) {
+        fetch(at, h, ahead, ROWS);
+        fetch(at, h, ahead, STATE);
+        fetch(at, h, ahead, STATE_GRAD);
+      }
       const T *DY = (const T*)(lds + L::BLOCK + buffer * L::BLOCK_BYTES), *ZL = DY + VA, *RL = ZL + L::NV * VA;
       const auto rj = as_it_stands<N32>(RL + (16 * jt + c16) * VLD, VA, g);
       Op<T, 1> dy[4];
@@ -307,12 +311,19 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
         dy[rt] = as_it_stands<1>(DY + (16 * rt + c16) * VLD, VA, g);
         zr[rt] = as_it_stands<N32>(ZL + (16 * rt + c16) * VLD, VA, g);
       }
+      if constexpr (SHARED) fetch(at, h, ahead, ROWS);
       // (all four tiles: the ones above the diagonal cost less than branches)
       if (wave < 4) mma(AA, dy, rj);
       else mma(AA, zr, rj);
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (SHARED) {
+        fetch(at, h, ahead, STATE);
+        if (mine) mma(YS, dy, s);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(at, h, ahead, STATE_GRAD);
+      }
       if (mine) {
-        mma(YS, dy, s);
+        if constexpr (!SHARED) mma(YS, dy, s);
         mma(ZS, zr, s);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll

@@ -137,7 +137,7 @@ struct Step {
 
 // A workgroup has 4 LC columns of one sequence's and head's state, a thread up to 128 LC / 256 of its rows in four columns: read once, all
 // loads on their way before the first is waited for, and written once.  With kS and qS from the same pass, y = scale (alpha qS + beta (q.k) r).
-// Bound: HBM.
+// Bound: HBM.  256 x 16 heads of 128 x 128: 114 us, 537 MB of states at 4.7 TB/s; 4 x 4 heads of 64 x 64: 6.6, a launch and two dependent reads.
 template <typename T, int LC, bool VEC>
 __global__ __launch_bounds__(256) void delta_step_kernel(Step p) {
   constexpr int RG = 256 / LC, ROWS = MAX_DK / RG;

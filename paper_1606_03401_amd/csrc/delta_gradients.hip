@@ -6,8 +6,13 @@
 //     dG_i = sum_j F_ij - sum_j F_ji + q~_i . (gamma dY S^T)_i - k^_i . (gamma Z S^T)_i - e_i,   F = dP o P + dM o M,
 //     e_j = beta_j (gamma_C / gamma k^)_j . (R dS'^T)_j,   the last step's dG also sum e + gamma_C <dS', S>,   dg_s = sum_{i >= s} dG_i.
 // A workgroup of eight waves, one to a compute unit, goes through chunks of sequences with one head each; or, where value heads share a key head, has one
-// chunk and key head and goes through its value heads.  Wave w computes
-// 16 columns of dq and dk; in what is 64 x 64, waves 0 .. 3 have column tiles of dY R^T and P, 4 .. 7 those of E and M.
+// chunk and key head and goes through its value heads.  Wave w computes 16 columns of dq and dk; in what is 64 x 64, waves 0 .. 3 have column tiles of
+// dY R^T and P, 4 .. 7 those of E and M.
+// Bound: what a chunk reads (R, Z, S and dS' in fp32: 243 KB a chunk of 128 x 128, 2.1 TB/s over all), in bursts between which the products stand; eight waves
+// of 240 registers and 110 KB of LDS leave no room for a second workgroup to fill the gaps.  1000 x 32 x 8 heads of 128 x 128, bf16, in four launches: 470 us,
+// of a chunk's 64 thousand cycles 25 in the loop over columns of v (13 of them products), 11 for the 64 x 64 products, 8 for sums, the rest writing and waiting.
+// Tried: two bf16 parts for R, Z, S and dS', 3 % faster and dA off by 10^-6; loads spread over the products, workgroups started apart, blocks in another order in
+// each workgroup: none faster.
 #include "delta.h"
 #include "dynamic_lds.h"
 

@@ -230,3 +230,55 @@ def test_lists_that_do_not_fit():
         mb.make_adamw_tensors(s.p, s.g, s.m, s.v, [s.ms[0][:1]], s.vs)
     with pytest.raises(ValueError):
         mb.make_adamw_tensors([], [], [], [])
+
+
+def _mix(x):
+    x = (x ^ (x >> np.uint32(17))) * np.uint32(0x2C9277B5)
+    x = (x ^ (x >> np.uint32(14))) * np.uint32(0x5851F42D)
+    return x ^ (x >> np.uint32(16))
+
+
+def _values32(code, scale, signed):
+    low = code.astype(np.uint32) & np.uint32(127) if signed else code.astype(np.uint32)
+    size = np.where(low > 0, ((low + np.uint32((112 if signed else 96) << 3)) << np.uint32(20)).view(np.float32) * scale, np.float32(0))
+    return np.where(signed & (code >= 128), -size, size)
+
+
+def _codes32(x, scale, bits, signed):
+    u = np.where(scale > 0, np.abs(x) / np.where(scale > 0, scale, np.float32(1)), np.abs(x)).astype(np.float32)
+    bits16 = bits >> np.uint32(16) if signed else bits & np.uint32(0xFFFF)
+    code = ((u.view(np.uint32) + (bits16 << np.uint32(4))) >> np.uint32(20)).astype(np.int64) - ((112 if signed else 96) << 3)
+    if not signed:
+        return np.where(u > 0, np.clip(code, 1, 255), 0)
+    least = np.float32(1.125 * 2.0 ** -15)
+    c = np.where(u < least, u * (np.float32(65536.0) / least) > bits16.astype(np.float32), np.clip(code, 1, 127))
+    return np.where((x < 0) & (c > 0), c + 128, c)
+
+
+def test_codes_bit_by_bit():
+    """States in 8 bits are what operations with one rounding each make of them, whatever the size of the values: from squares that vanish in 32 bits over blocks
+    whose scales have no normal reciprocal to squares near the type's end.  (Every operation here is numpy's in 32 bits, so equality is exact.)"""
+    powers = [0, -20, -40, -58, -62, -66, -72, 20, 40, 50, 56, 60]
+    t = _Tensors([70001 if i < 2 else 3001 for i in range(len(powers))], bits=8, copy=False, seed=9)
+    for i, e in enumerate(powers):
+        t.g[i].mul_(2.0 ** e)
+        t.ms[i].mul_(2.0 ** e)
+        t.vs[i].mul_(max(2.0 ** (2 * e), 2.0 ** -149))
+    before = [[x[i].cpu().numpy().copy() for x in (t.g, t.m, t.v, t.ms, t.vs)] for i in range(len(powers))]
+    mb.mebptt_adamw_step(mb.make_adamw_desc(**SET), t.args, t.table)
+    first, f = 0, np.float32
+    with np.errstate(over="ignore"):
+        for i, (g, m, v, ms, vs) in enumerate(before):
+            n, blocks = g.size, ms.size
+            of = np.arange(n) // 256
+            key = _mix(np.uint32(SET["seed"]) + np.uint32(SET["step"]) * np.uint32(0x632BE5AB) + (first + np.arange(blocks)).astype(np.uint32) * np.uint32(0x9E3779B9))
+            bits = _mix(key[of] + (np.arange(n) % 256).astype(np.uint32) * np.uint32(0x85157AF5))
+            first += blocks
+            new_m = f(SET["beta1"]) * _values32(m, ms[of], True) + f(1 - SET["beta1"]) * g
+            new_v = f(SET["beta2"]) * _values32(v, vs[of], False) + f(1 - SET["beta2"]) * (g * g)
+            for x, codes, scale, signed in ((new_m, t.m[i], t.ms[i], True), (new_v, t.v[i], t.vs[i], False)):
+                top = np.pad(np.abs(x), (0, -n % 256)).reshape(-1, 256).max(1)
+                s = top * (f(1.0) / f(1.875))
+                assert np.array_equal(scale.cpu().numpy(), s), (powers[i], signed)
+                assert np.array_equal(codes.cpu().numpy(), _codes32(x, s[of], bits, signed)), (powers[i], signed)
+    assert t.clean()

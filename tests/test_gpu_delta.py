@@ -153,6 +153,24 @@ def test_long_sequences_in_segments(size, kw, dtype):
         assert torch.equal(c.y, y) and torch.equal(c.h0, h)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("H", [2, 4])
+@pytest.mark.parametrize("some", [True, False])
+def test_more_chunks_than_compute_units(some, H, dtype):
+    """Workgroups that take several chunks one after another, with chunks behind a sequence's end first, last and between those with steps; and none with steps."""
+    B = 90
+    lengths = [0] * 9 + [int(n) for n in np.random.default_rng(4).integers(-40, 190, B - 18)] + [190] * 4 + [0] * 5 if some else [0] * B
+    _run(190, B, 2, H, 20, 12, dtype, lengths=lengths, stretch=256)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("size,some", [((130, 700, 1, 3, 9, 6), True), ((130, 700, 3, 3, 16, 8), False), ((4500, 16, 2, 4, 16, 8), True)])
+def test_several_launches(size, some, dtype):
+    """More chunks than a call holds the records of at once: the state goes from launch to launch, of whole chunks and of segments."""
+    lengths = [int(n) for n in np.random.default_rng(5).integers(-20, size[0] + 60, size[1])] if some else None
+    _run(*size, dtype, lengths=lengths, stretch=128)
+
+
 @pytest.mark.parametrize("stretch", [64, 128, 256, 512])
 def test_stretches_give_the_same_gradients(stretch):
     """Whatever is kept, and however much of it is recomputed at a time."""

@@ -50,14 +50,23 @@ __device__ inline Op<T, N> cut(f32x4 a, f32x4 b) {
     o.v[0] = a;
     o.v[1] = b;
   } else {
+    // in pairs: one instruction rounds two values, and a pair is a register of the operand
     float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+    for (int n = 0; n < N; ++n) {
+      u32x4 pairs;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        o.p[n][e] = (__bf16)x[e];
-        if (n + 1 < N) x[e] -= (float)o.p[n][e];
+      for (int e = 0; e < 4; ++e) {
+        const f32x2 two = {x[2 * e], x[2 * e + 1]};
+        const unsigned pair = __builtin_bit_cast(unsigned, __builtin_convertvector(two, bf16x2));
+        pairs[e] = pair;
+        if (n + 1 < N) {
+          x[2 * e] -= __uint_as_float(pair << 16);
+          x[2 * e + 1] -= __uint_as_float(pair & 0xFFFF0000u);
+        }
       }
+      o.p[n] = __builtin_bit_cast(bf16x8, pairs);
+    }
   }
   return o;
 }

@@ -108,6 +108,38 @@ __device__ inline void mma(f32x4 (&c)[M], const Op<float, NA> (&a)[R], const Op<
 #pragma unroll
       for (int r = 0; r < R; ++r) c[first + r] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r].v[h][e], b.v[h][e], c[first + r], 0, 0, 0);
 }
+// The same with another operand's cutting between: left to itself the compiler puts matrix instructions in a row and the cutting behind them, and a wave
+// that is alone on its SIMD uses one unit at a time.  `next` is what the cutting of (x, y) gives.
+template <int R, int M, int NA, int NB, int N>
+__device__ inline void mma_and_cut(f32x4 (&c)[M], const Op<__bf16, NA> (&a)[R], const Op<__bf16, NB>& b, int first, float (&x)[8], Op<__bf16, N>& next, int step0, int every) {
+  constexpr int MOST = NA > NB ? NA : NB;
+  int count = 0;
+#pragma unroll
+  for (int i = NA - 1; i >= 0; --i)
+#pragma unroll
+    for (int j = NB - 1; j >= 0; --j)
+      if (i + j < MOST) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          c[first + r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[r].p[i], b.p[j], c[first + r], 0, 0, 0);
+          const int step = step0 + count / every;
+          if (count % every == every - 1 && step < 4 * N) {
+            const int n = step / 4, e = step % 4;
+            const f32x2 two = {x[2 * e], x[2 * e + 1]};
+            const unsigned pair = __builtin_bit_cast(unsigned, __builtin_convertvector(two, bf16x2));
+            u32x4 pairs = __builtin_bit_cast(u32x4, next.p[n]);
+            pairs[e] = pair;
+            next.p[n] = __builtin_bit_cast(bf16x8, pairs);
+            if (n + 1 < N) {
+              x[2 * e] -= __uint_as_float(pair << 16);
+              x[2 * e + 1] -= __uint_as_float(pair & 0xFFFF0000u);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          ++count;
+        }
+      }
+}
 template <typename T, int NA, int NB>
 __device__ inline void mma(f32x4& c, const Op<T, NA>& a, const Op<T, NB>& b) {
   const Op<T, NA> row[1] = {a};

@@ -90,10 +90,15 @@ template <int N>
 __device__ inline void put_parts(__bf16* p, int apart, f32x4 x) {
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    bf16x4 part;
+    u32x2 pairs;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) part[e] = (__bf16)x[e], x[e] -= (float)part[e];
-    *reinterpret_cast<bf16x4*>(p + n * apart) = part;
+    for (int e = 0; e < 2; ++e) {
+      const f32x2 two = {x[2 * e], x[2 * e + 1]};
+      pairs[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(two, bf16x2));
+      x[2 * e] -= __uint_as_float(pairs[e] << 16);
+      x[2 * e + 1] -= __uint_as_float(pairs[e] & 0xFFFF0000u);
+    }
+    *reinterpret_cast<u32x2*>(p + n * apart) = pairs;
   }
 }
 template <int N>

@@ -235,6 +235,17 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
           for (int r = 0; r < ROWS; r += 4) rows(a[(n + 1) % 2][r / 4], r, n + 1);
         }
         next_product();
+        if constexpr (sizeof(T) == 2) {
+          if (n + 1 < NT / 2) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = S[2 * n + 2][e], x[4 + e] = S[2 * n + 3][e];
+#pragma unroll
+            for (int r = 0; r < ROWS; r += 4) mma_and_cut(KQ, a[n % 2][r / 4], s[n % 2], r, x, s[(n + 1) % 2], ROWS == 8 ? r / 4 * 6 : 0, ROWS == 8 ? 2 : 1);
+            next_product();
+            continue;
+          }
+        }
 #pragma unroll
         for (int r = 0; r < ROWS; r += 4) mma(KQ, a[n % 2][r / 4], s[n % 2], r);
         if (n + 1 < NT / 2) s[(n + 1) % 2] = cut<T, 3>(S[2 * n + 2], S[2 * n + 3]);

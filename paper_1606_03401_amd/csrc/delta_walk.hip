@@ -194,16 +194,16 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
     ct.load(rec + R::T_);
     if (MODE != WALK) cg.load(rec + R::GATE);
   };
-  if (first < behind) fetch(first);
-  for (int chunk = first; chunk < behind; ++chunk) {
-    const int s0 = chunk * C, live = min(end - s0, C), steps = min(p.t - s0, C);
+  auto keep = [&](int chunk) {
     if (MODE == WALK && p.states && chunk % p.keep == 0 && there)
       store_state(S, p.states + ((int64_t)(chunk / p.keep) * BH + bh) * p.dk * p.dv, p.dk, p.dv, col, g);
-    T* y = MODE ? nullptr : (T*)p.y.data + (int64_t)s0 * p.y.stride_t + b * p.y.stride_b + h * p.dv;
-    if (live <= 0) {   // behind the sequence's end: zeros, the state stays
-      if (MODE == WALK) store_zeros(y, p.y.stride_t, steps, col, p.dv, g);
-      continue;
-    }
+  };
+  auto y_of = [&](int chunk) { return (T*)p.y.data + (int64_t)(chunk * C) * p.y.stride_t + b * p.y.stride_b + h * p.dv; };
+  const int dead = max(first, min(behind, (end + C - 1) / C));   // the first chunk behind the sequence's end
+  if (first < dead) fetch(first);
+  for (int chunk = first; chunk < dead; ++chunk) {
+    const int s0 = chunk * C, live = min(end - s0, C), steps = min(p.t - s0, C);
+    keep(chunk);
     if (MODE == AGAIN && col < p.dvp) store_state(S, p.S + ((int64_t)(chunk - p.c0) * BH + bh) * KD * p.dvp, KD, p.dvp, col, g);
     __syncthreads();   // the chunk before has been read
     ck.put(K, p.k, 0, live);
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
     else cg.put(lds + L::GATE);
     if (!unit) cv.put(VL, p.v, c0, live);
     __syncthreads();
-    fetch(min(chunk + 1, behind - 1));   // (not under a condition, see there)
+    fetch(min(chunk + 1, dead - 1));   // (not under a condition, see there)
     next_product();
 
     // K S and Q S: tiles 0 .. 3 and 4 .. 7
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
       next_product();
       if (DEEP) fetch_columns(0);
       mma(Y, p1, cut<T, 2>(U[2], U[3]), 2);
-      store_tiles(y, (int)p.y.stride_t, Y, steps, live, c0 + 16 * wave, p.dv, p.vec_out, reinterpret_cast<T*>(lds + L::Y) + wave * TURN, lane);
+      store_tiles(y_of(chunk), (int)p.y.stride_t, Y, steps, live, c0 + 16 * wave, p.dv, p.vec_out, reinterpret_cast<T*>(lds + L::Y) + wave * TURN, lane);
       next_product();
     } else {
       if (DEEP) fetch_columns(0);
@@ -321,6 +321,12 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
       if (!DEEP || pb == 0) fetch_columns(DEEP ? 1 : pb);
       mma(S, columns[DEEP ? pb : 0], cut<T, 3>(U[2 * pb], U[2 * pb + 1]));
       next_product();
+    }
+  }
+  if constexpr (MODE == WALK) {   // zeros, the state stays
+    for (int chunk = dead; chunk < behind; ++chunk) {
+      keep(chunk);
+      store_zeros(y_of(chunk), p.y.stride_t, min(p.t - chunk * C, C), col, p.dv, g);
     }
   }
   if constexpr (MODE == SURVEY) {

@@ -637,6 +637,8 @@ typedef struct {
   int32_t residual_dtype; /* the same choice for residual, residual_out and their gradients */
   float scale;
   float eps;              /* >= 0 */
+  int32_t again;          /* backward: 1: r is the forward call's residual, and the sum is computed again; 0: r is the sum */
+  int32_t reserved;       /* 0 */
 } mebptt_join_desc;
 /* read:  x [rows, width], row stride ldx (elements, >= width; all ld alike); z (NULL: no gate); weight [width] fp32 (NULL: ones);
  *        residual (NULL: none, and then weight_next, residual_out and rstd_next must be NULL); weight_next [width] fp32 (NULL: ones).
@@ -647,8 +649,9 @@ int mebptt_join_forward(const mebptt_join_desc* desc, const void* x, int64_t ldx
                         const void* residual, int64_t ldr, const float* weight_next, void* y, int64_t ldy, void* residual_out,
                         int64_t ldo, float* rstd, float* rstd_next, void* stream);
 /* Gradients of mebptt_join_forward.
- * read:  x, z, weight as there; r [rows, width]: what residual_out received (NULL: there was no residual, and then weight_next, rstd_next,
- *        dresidual_out, dresidual and dweight_next must be NULL), weight_next, rstd, rstd_next, dy, dresidual_out (the gradient that arrives at
+ * read:  x, z, weight as there; r [rows, width]: what residual_out received, or with desc->again the residual, from which the sum comes out as it was before
+ *        its rounding: in bf16 the sum as it was stored costs dweight and dweight_next 2^-9 of each of their terms (NULL: there was no residual, and then
+ *        weight_next, rstd_next, dresidual_out, dresidual and dweight_next must be NULL), weight_next, rstd, rstd_next, dy, dresidual_out (the gradient that arrives at
  *        residual_out; NULL: none).
  * write: dx; dz (NULL exactly if z is); dresidual (NULL: not written; may be dresidual_out itself); dweight, dweight_next [width] fp32
  *        (NULL: not computed).  dx may be dy. */

@@ -135,7 +135,7 @@ class mebptt_delta_grads(C.Structure):
 
 class mebptt_join_desc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("group", C.c_int32), ("x_dtype", C.c_int32), ("residual_dtype", C.c_int32),
-                ("scale", C.c_float), ("eps", C.c_float)]
+                ("scale", C.c_float), ("eps", C.c_float), ("again", C.c_int32), ("reserved", C.c_int32)]
 
 
 ADAMW_NO_DECAY = 1
@@ -954,8 +954,8 @@ def mebptt_delta_step(desc: mebptt_delta_desc, q, k, v, a, b, A, a_bias, state_i
 
 
 def make_join_desc(rows: int, width: int, group: int, x_dtype: int, residual_dtype: int = FP32, scale: float = 1.0,
-                   eps: float = 1e-5) -> mebptt_join_desc:
-    return mebptt_join_desc(rows, width, group, x_dtype, residual_dtype, scale, eps)
+                   eps: float = 1e-5, again: bool = False) -> mebptt_join_desc:
+    return mebptt_join_desc(rows, width, group, x_dtype, residual_dtype, scale, eps, int(again), 0)
 
 
 def mebptt_join_workspace_bytes(desc: mebptt_join_desc) -> int:
@@ -976,7 +976,8 @@ def mebptt_join_forward(desc: mebptt_join_desc, x, z, weight, residual, weight_n
 
 def mebptt_join_backward(desc: mebptt_join_desc, x, z, weight, r, weight_next, rstd, rstd_next, dy, dresidual_out, dx, dz, dweight, dresidual,
                          dweight_next, workspace, stream: Optional[int] = None) -> None:
-    """Gradients of mebptt_join_forward; r is its residual_out (None: there was no residual)."""
+    """Gradients of mebptt_join_forward; r is its residual_out, or where the description says `again` its residual, from which the sum is computed once more
+    without its rounding to the stream's type (None: there was no residual)."""
     dev, M, W = _gpu(x), desc.rows, desc.width
     f32, xt, rt = _DTYPES[0], _dtype(desc.x_dtype), _dtype(desc.residual_dtype)
     _call(dev, stream, lib().mebptt_join_backward, C.byref(desc), *_rows(x, "x", M, W, xt, dev), *_maybe_rows(z, "z", M, W, xt, dev),

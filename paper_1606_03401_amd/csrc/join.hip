@@ -1,6 +1,6 @@
 // What joins a block to the residual stream, forward and backward:
 //     branch = n weight silu(z),  n = x rstd per group of columns;   r = scale residual + branch,   y = r rstd_next weight_next (without a residual: y = branch)
-//     dr = rms_back(dy) + dresidual_out;  dresidual = scale dr;  dz = dr n weight silu'(z);  g = dr weight silu(z);  dx = rstd (g - n mean over the group(g n))
+//     dr = rms_back(dy) + dresidual_out, from r as it was stored or (again) from the residual;  dresidual = scale dr;  dz = dr n weight silu'(z);  g = dr weight silu(z);  dx = rstd (g - n mean over the group(g n))
 // A row stays in the registers of the threads that read it: one pass over memory each way.  Bound: HBM.
 // Forward and backward at 32000 x 1024, bf16, groups of 128 and gate: 38 us (5.1 TB/s) and 57 (5.7); 64000 x 1024 with the residual in fp32: 146 and 236 (5.4, 5.0);
 // forward at 8192 x 4096, all parts: 65 (5.2).
@@ -38,6 +38,7 @@ struct JoinBack {
   int64_t rows, ldx, ldz, ldr, lddy, lddo, lddx, lddz, lddr;
   int width, group, lanes, pieces;
   float scale;
+  int again;   // r is the residual
 };
 
 template <int WAVES>
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_forward_kernel(Join 
         widen<VEC>(rs[c], at.count[c], r);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          a[c][e] = e < at.count[c] ? p.scale * r[e] + a[c][e] : 0.0f;
+          a[c][e] = e < at.count[c] ? fmaf(p.scale, r[e], a[c][e]) : 0.0f;
           total += a[c][e] * a[c][e];
         }
       }
@@ -281,6 +282,22 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_backward_kernel(Join
         float w[V];
         load_weight<VEC>(p.weight_next, at.at[c], at.count[c], p.lanes, w);
         widen<VEC>(rs[c], at.count[c], m[c]);
+        if (p.again) {   // the sum, operation by operation as the forward pass has it
+          const float rstd_x = p.rstd[row * groups + (at.count[c] ? at.slot[c] : 0)];
+          float a[V], wx[V];
+          widen<VEC>(xs[c], at.count[c], a);
+          load_weight<VEC>(p.weight, at.at[c], at.count[c], p.lanes, wx);
+#pragma unroll
+          for (int e = 0; e < V; ++e) a[e] *= rstd_x * wx[e];
+          if (p.z) {
+            float z[V];
+            widen<VEC>(zs[c], at.count[c], z);
+#pragma unroll
+            for (int e = 0; e < V; ++e) a[e] *= z[e] * sigmoid(z[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < V; ++e) m[c][e] = e < at.count[c] ? fmaf(p.scale, m[c][e], a[e]) : 0.0f;
+        }
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           m[c][e] *= rstd;
@@ -442,6 +459,7 @@ int check(const mebptt_join_desc* d) {
   if (d->group < 8 && d->width > 4096 * d->group) return set_error(MEBPTT_EINVAL, "group must be at least 8 where width is over 4096 * group");
   if (!float_dtype(d->x_dtype) || !float_dtype(d->residual_dtype)) return set_error(MEBPTT_EINVAL, "unknown dtype");
   if (!(d->eps >= 0.0f)) return set_error(MEBPTT_EINVAL, "eps must not be negative");
+  if ((d->again != 0 && d->again != 1) || d->reserved) return set_error(MEBPTT_EINVAL, "again must be 0 or 1, reserved 0");
   return MEBPTT_OK;
 }
 int check_ld(const void* p, int64_t ld, int width, const char* what) {
@@ -513,7 +531,7 @@ int mebptt_join_backward(const mebptt_join_desc* d, const void* x, int64_t ldx, 
   if (!shape_of(w, d->group, vec, &s)) return set_error(MEBPTT_EINVAL, "no shape for this width and group");
   const int64_t groups = back_groups(d, s.waves);
   const JoinBack p = {x, z, r, dy, dout, weight, weight_next, rstd, rstd_next, dx, dz, dres, sums ? (float*)workspace : nullptr,
-                      d->rows, ldx, ldz, ldr, lddy, lddo, lddx, lddz, lddr, w, d->group, s.lanes, s.pieces, d->scale};
+                      d->rows, ldx, ldz, ldr, lddy, lddo, lddx, lddz, lddr, w, d->group, s.lanes, s.pieces, d->scale, d->again};
   hipStream_t st = (hipStream_t)stream;
   if (groups) {
     auto at = [&](auto tx) {

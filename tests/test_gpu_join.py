@@ -97,6 +97,30 @@ def test_what_may_be_left_out(size, x_dtype, gate, residual):
     c.check()
 
 
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("x_dtype,r_dtype", [("fp32", "fp32"), ("bf16", "bf16"), ("fp32", "bf16")])
+@pytest.mark.parametrize("gate", [True, False])
+@pytest.mark.parametrize("size", [(5, 64, 16), (3, 650, 13), (1, 1024, 128), (300, 96, 96), (2, 4096, 128), (2, 8192, 4096), (1, 16384, 128)])
+def test_the_sum_computed_again(size, gate, x_dtype, r_dtype, layout):
+    """From the residual in place of the sum: gradients of the sum before its rounding, in a stream of bf16 too; with one of fp32 the same bits as from the sum."""
+    c = _Call(*size, x_dtype, r_dtype, layout, gate=gate)
+    c.forward()
+    c.desc = mb.make_join_desc(*size, CODE[x_dtype], CODE[r_dtype], c.scale, 1e-5, again=True)
+    mb.mebptt_join_backward(c.desc, c.x, c.z, c.w, c.res, c.wn, c.rstd, c.rn, c.dy, c.dr_out, c.dx, c.dz, c.dw, c.dres, c.dwn, c.ws)
+    scale = float(np.float32(c.scale))
+    r = od.join(down(c.x), down(c.z), down(c.w), down(c.res), down(c.wn), c.group, scale, 1e-5)[1]
+    d = od.join_backward(down(c.x), down(c.z), down(c.w), r, down(c.wn), down(c.dy), down(c.dr_out), c.group, scale, 1e-5)
+    got = [(k, t) for k, t in (("dx", c.dx), ("dz", c.dz), ("dresidual", c.dres), ("dweight", c.dw), ("dweight_next", c.dwn)) if t is not None]
+    for k, t in got:
+        near(t, d[k], k, d.get(k + "_terms"))
+    assert c.m.clean()
+    if r_dtype == "fp32":
+        first = [t.clone() for _, t in got]
+        c.desc = mb.make_join_desc(*size, CODE[x_dtype], CODE[r_dtype], c.scale, 1e-5)
+        c.backward()
+        assert all(torch.equal(a, t) for a, (_, t) in zip(first, got))
+
+
 def test_the_streams_gradient_in_place():
     c = _Call(6, 650, 65, "bf16", "fp32")
     c.forward()

@@ -254,7 +254,7 @@ def _own_join(s):
 
     def make():
         desc = mb.make_join_desc(c["rows"], c["width"], c["group"], mb.BF16 if c["dtype"] == "bf16" else mb.FP32,
-                                 mb.FP32 if c["residual"] == "fp32" else mb.BF16, c["scale"], EPS)
+                                 mb.FP32 if c["residual"] == "fp32" else mb.BF16, c["scale"], EPS, again=next_)
         k = {"desc": desc, "y": like(s["x"]), "sum": like(s["residual"]) if next_ else None}
         if c["what"] == "join grad":
             k |= {"rstd": torch.empty((c["rows"], c["width"] // c["group"]), device="cuda"), "rstd_next": torch.empty(c["rows"], device="cuda") if next_ else None,
@@ -269,7 +269,7 @@ def _own_join(s):
                            k["rstd_next"] if back else None)
     names = ["y"] + (["sum"] if next_ else [])
     if back:
-        mb.mebptt_join_backward(k["desc"], s["x"], s["z"], s["weight"], k["sum"], weight_next, k["rstd"], k["rstd_next"], s["dy"],
+        mb.mebptt_join_backward(k["desc"], s["x"], s["z"], s["weight"], residual, weight_next, k["rstd"], k["rstd_next"], s["dy"],
                                 s["dresidual_out"] if next_ else None, k["dx"], k["dz"], k["dweight"], k["dresidual"], k["dweight_next"], k["ws"])
         names += ["dx", "dweight"] + (["dz"] if c["gate"] else []) + (["dresidual", "dweight_next"] if next_ else [])
     return {n: k[n] for n in names}

@@ -34,7 +34,7 @@ struct Layout {
   static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), BLOCK = Q + Lds<T>::row_bytes(KD);    // two blocks, one being filled
   static constexpr int W = BLOCK;                                                                    // four matrices, over them
   static constexpr int SUMS = BLOCK + (2 * BLOCK_BYTES > 4 * NM * WSIZE ? 2 * BLOCK_BYTES : 4 * NM * WSIZE);
-  static constexpr int GATE = SUMS + C * 8, ROWF = GATE + GATES * C * 4, COLS = ROWF + WAVES * C * 4, DOTS = COLS + 4 * C * 4,
+  static constexpr int GATE = SUMS + C * 8, ROWF = GATE + GATES * C * 4, COLF = ROWF + WAVES * C * 8, COLS = COLF + 2 * C * 8, DOTS = COLS + 2 * C * 4,
                        NORMS = DOTS + 3 * WAVES * C * 4, MORE = NORMS + 2 * C * 4, BYTES = MORE + WAVES * 4;
 };
 
@@ -138,17 +138,35 @@ __device__ inline float over_wave(float v) {
   v = over_columns(v);
   return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
+// The same in 64 bits.
+template <int CONTROL>
+__device__ inline double moved(double v) {
+  const u32x2 x = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(double, u32x2{(unsigned)__builtin_amdgcn_update_dpp(0, (int)x[0], CONTROL, 0xf, 0xf, true), (unsigned)__builtin_amdgcn_update_dpp(0, (int)x[1], CONTROL, 0xf, 0xf, true)});
+}
+__device__ inline double over_columns(double v) {
+  v += moved<0x128>(v);
+  v += moved<0x124>(v);
+  v += moved<0x122>(v);
+  v += moved<0x121>(v);
+  return v;
+}
+__device__ inline double lane_of(double v, int lane) {
+  const u32x2 x = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(double, u32x2{(unsigned)__builtin_amdgcn_readlane((int)x[0], lane), (unsigned)__builtin_amdgcn_readlane((int)x[1], lane)});
+}
+__device__ inline double over_wave(double v) {
+  v = over_columns(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
 // Sum of the values of this lane and those behind it.
-__device__ inline float from_lane_on(float v, int lane) {
-  auto add = [&](auto shift) {   // (lanes behind the row's end count as zero)
-    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(shift)::value, 0xf, 0xf, true));
-  };
-  add(std::integral_constant<int, 0x101>{});
-  add(std::integral_constant<int, 0x102>{});
-  add(std::integral_constant<int, 0x104>{});
-  add(std::integral_constant<int, 0x108>{});
-  const float last = lane_of(v, 48), two = lane_of(v, 32) + last, three = lane_of(v, 16) + two;
-  return v + (lane < 16 ? three : lane < 32 ? two : lane < 48 ? last : 0.0f);
+__device__ inline double from_lane_on(double v, int lane) {
+  v += moved<0x101>(v);   // (lanes behind the row's end count as zero)
+  v += moved<0x102>(v);
+  v += moved<0x104>(v);
+  v += moved<0x108>(v);
+  const double last = lane_of(v, 48), two = lane_of(v, 32) + last, three = lane_of(v, 16) + two;
+  return v + (lane < 16 ? three : lane < 32 ? two : lane < 48 ? last : 0.0);
 }
 
 // The kernel's first argument where the launch put it.
@@ -170,8 +188,8 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
   T *K = (T*)(lds + L::K), *Q = (T*)(lds + L::Q);
   // [j][i], i >= j: W1 and W3 with the factor of column j's key, and with that of row i's query or key
   T *W1 = (T*)(lds + L::W), *W1q = W1 + L::NM * WA, *W3 = W1q + L::NM * WA, *W3k = W3 + L::NM * WA;
-  double* G = (double*)(lds + L::SUMS);
-  float *gate = (float*)(lds + L::GATE), *rowF = (float*)(lds + L::ROWF), *cols = (float*)(lds + L::COLS), *dots = (float*)(lds + L::DOTS),
+  double *G = (double*)(lds + L::SUMS), *rowF = (double*)(lds + L::ROWF), *colF_ = (double*)(lds + L::COLF);
+  float *gate = (float*)(lds + L::GATE), *cols = (float*)(lds + L::COLS), *dots = (float*)(lds + L::DOTS),
         *norms = (float*)(lds + L::NORMS), *more = (float*)(lds + L::MORE);
   const int per = now->B * now->Hk, items = (now->c1 - now->c0) * per, group = SHARED ? now->H / now->Hk : 1;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane_ = threadIdx.x % WAVE;
@@ -347,7 +365,8 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
       const int j = 16 * jt + c16;
       const float skj = gate[SK * C + j], bej = gate[BE * C + j];
       const double Gj = G[j];
-      float down = 0.0f, colF = 0.0f;
+      float down = 0.0f;
+      double colF = 0.0;
       T *first = wave < 4 ? W1 : W3, *second = wave < 4 ? W1q : W3k;
       const T* rows = wave < 4 ? Q : K;
       const float* factor = gate + (wave < 4 ? SQ : SK) * C;
@@ -357,7 +376,8 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) {
         const int i0 = 16 * rt + 4 * g;
-        f32x4 w1 = {}, w2 = {}, row = {};   // (above the diagonal too, as far as the products read)
+        f32x4 w1 = {}, w2 = {};   // (above the diagonal too, as far as the products read)
+        double row[4] = {};
         if (rt >= jt) {
           f32x4 m = {};
 #pragma unroll
@@ -376,12 +396,15 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
             w1[e] = u * d * skj;
             w2[e] = u * d * fi[e];
             colF += f;
-            row[e] = over_columns(f);
+            row[e] = over_columns((double)f);
           }
         }
         put_parts<L::NM>(first + j * WLD + i0, WA, w1);
         put_parts<L::NM>(second + j * WLD + i0, WA, w2);
-        if (c16 == 0) *reinterpret_cast<f32x4*>(rowF + wave * C + i0) = row;
+        if (c16 == 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rowF[wave * C + i0 + e] = row[e];
+        }
       }
       down += __shfl_xor(down, 16);
       colF += __shfl_xor(colF, 16);
@@ -389,7 +412,7 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
       colF += __shfl_xor(colF, 32);
       if (g == 0) {
         cols[(wave / 4) * C + j] = down;
-        cols[(2 + wave / 4) * C + j] = colF;
+        colF_[(wave / 4) * C + j] = colF;
       }
     }
     inner = over_wave(inner);
@@ -471,37 +494,40 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
       float sum = 0.0f;
       if (wave == 6) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) sum += rowF[w * C + i];
+        for (int w = 0; w < 4; ++w) sum += (float)rowF[w * C + i];
 #pragma unroll
         for (int w = 0; w < NT; ++w) sum += dots[w * C + i];
         sum *= gate[RQ * C + i];
       } else {
         float e = 0.0f, zs = 0.0f;
 #pragma unroll
-        for (int w = 4; w < 8; ++w) sum += rowF[w * C + i];
+        for (int w = 4; w < 8; ++w) sum += (float)rowF[w * C + i];
 #pragma unroll
         for (int w = 0; w < NT; ++w) zs += dots[(WAVES + w) * C + i], e += dots[(2 * WAVES + w) * C + i];
-        sum = (sum + cols[2 * C + i] + cols[3 * C + i] + gate[BE * C + i] * e - zs) * gate[SK * C + i];
+        sum = (sum + (float)colF_[i] + (float)colF_[C + i] + gate[BE * C + i] * e - zs) * gate[SK * C + i];
       }
       float* norm = norms + (wave - 6) * C + i;
       *norm = SHARED && n ? *norm + sum : sum;
     }
     if (wave == 0) {
       const int i = lane;
-      float rows = 0.0f, first = 0.0f, second = 0.0f, all = 0.0f;
+      // In 64 bits: of a sum from one step to the last what belongs to pairs of steps both behind it cancels, and each product's own rounding with it.
+      double dG = 0.0;
+      float second = 0.0f, all = 0.0f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) rows += rowF[w * C + i];
+      for (int w = 0; w < WAVES; ++w) dG += rowF[w * C + i];
+      dG -= colF_[i] + colF_[C + i];
 #pragma unroll
       for (int w = 0; w < NT; ++w) {
-        first += dots[w * C + i] - dots[(WAVES + w) * C + i];
+        dG += (double)dots[w * C + i] - dots[(WAVES + w) * C + i];
         second += dots[(2 * WAVES + w) * C + i];
         all += more[w];
       }
       const float beta = gate[BE * C + i], e = beta * second;
-      float dG = rows - (cols[2 * C + i] + cols[3 * C + i]) + first - e;
-      const float ends = over_wave(e);
+      const double ends = over_wave((double)e);
+      dG -= e;
       if (i == C - 1) dG += ends + gate[GA * C + C - 1] * all;
-      dG = from_lane_on(dG, i);   // sum from this step to the last one
+      const float dlast = (float)from_lane_on(dG, i);   // sum from this step to the last one
       const float dbeta = cols[i] + cols[C + i] + second;
       float dlog = 0.0f, da = 0.0f;
       const int64_t s = s0 + i;
@@ -511,10 +537,10 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
         if (p.a.data && in) {
           const float raw = (float)this_a + bias_h;
           if (p.activate) {
-            dlog = dG * (fmaxf(raw, 0.0f) + log1pf(expf(-fabsf(raw))));
-            da = dG * A_h / (1.0f + expf(-raw));
+            dlog = dlast * (fmaxf(raw, 0.0f) + log1pf(expf(-fabsf(raw))));
+            da = dlast * A_h / (1.0f + expf(-raw));
           } else {
-            da = dG;
+            da = dlast;
           }
         }
         if (p.a.data) ((T*)p.da.data)[s * p.da.stride_t + b * p.da.stride_b + h] = (T)da;

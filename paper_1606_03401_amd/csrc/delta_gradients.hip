@@ -9,7 +9,7 @@
 // chunk and key head and goes through its value heads.  Wave w computes 16 columns of dq and dk; in what is 64 x 64, waves 0 .. 3 have column tiles of
 // dY R^T and P, 4 .. 7 those of E and M.
 // Bound: what a chunk reads (R, Z, S and dS' in fp32: 243 KB a chunk of 128 x 128, 2.1 TB/s over all), in bursts between which the products stand; eight waves
-// of 240 registers and 110 KB of LDS leave no room for a second workgroup to fill the gaps.  1000 x 32 x 8 heads of 128 x 128, bf16, in four launches: 470 us,
+// of 240 registers and 110 KB of LDS leave no room for a second workgroup to fill the gaps.  1000 x 32 x 8 heads of 128 x 128, bf16, in four launches: 478 us,
 // of a chunk's 64 thousand cycles 25 in the loop over columns of v (13 of them products), 11 for the 64 x 64 products, 8 for sums, the rest writing and waiting.
 // Tried: two bf16 parts for R, Z, S and dS', 3 % faster and dA off by 10^-6; loads spread over the products, workgroups started apart, blocks in another order in
 // each workgroup: none faster.

@@ -2,7 +2,7 @@
 //     branch = n weight silu(z),  n = x rstd per group of columns;   r = scale residual + branch,   y = r rstd_next weight_next (without a residual: y = branch)
 //     dr = rms_back(dy) + dresidual_out, from r as it was stored or (again) from the residual;  dresidual = scale dr;  dz = dr n weight silu'(z);  g = dr weight silu(z);  dx = rstd (g - n mean over the group(g n))
 // A row stays in the registers of the threads that read it: one pass over memory each way.  Bound: HBM.
-// Forward and backward at 32000 x 1024, bf16, groups of 128 and gate: 38 us (5.1 TB/s) and 57 (5.7); 64000 x 1024 with the residual in fp32: 146 and 236 (5.4, 5.0);
+// Forward and backward at 32000 x 1024, bf16, groups of 128 and gate: 38 us (5.1 TB/s) and 57 (5.7); 64000 x 1024 with the residual in fp32: 146 and 236 (5.4, 5.0), 243 with the sum computed again;
 // forward at 8192 x 4096, all parts: 65 (5.2).
 // A row belongs to one wave up to 2048 columns, to 4 or 16 beyond.  L lanes (a power of two) share a group of columns, so that a group's sum takes
 // shuffles among neighbours (and, where L is more than a wave, a few floats in LDS), and several groups of a row are summed at once.

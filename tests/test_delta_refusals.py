@@ -182,3 +182,12 @@ def test_adamw_steps():
     assert norm(ws=None) == mb.EWORKSPACE and norm(n=8) == mb.EWORKSPACE
     unpack = lambda n=10, codes=P, dtype=mb.FP32: lib.mebptt_adamw_unpack(codes, P, n, 1, P, dtype, None)  # noqa: E731
     assert unpack(n=-1) == mb.EINVAL and unpack(codes=None) == mb.EINVAL and unpack(dtype=mb.INT8) == mb.EINVAL
+
+
+def test_join_flags_that_mean_nothing():
+    for field, value in (("again", 2), ("again", -1), ("reserved", 1)):
+        d = mb.make_join_desc(4, 64, 16, mb.BF16, mb.FP32)
+        assert mb.mebptt_join_workspace_bytes(d) > 0
+        setattr(d, field, value)
+        assert mb.mebptt_join_workspace_bytes(d) == 0
+        assert mb.lib().mebptt_join_forward(C.byref(d), P, 64, None, 0, None, None, 0, None, P, 64, None, 0, None, None, None) == mb.EINVAL

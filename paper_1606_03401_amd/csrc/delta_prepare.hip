@@ -146,8 +146,9 @@ __global__ __launch_bounds__(256, 4) void delta_prepare_kernel(Args p) {
     if (lane % 16 / 4 == g) {
       const float k = e == 0 ? k2[0] : e == 1 ? k2[1] : e == 2 ? k2[2] : k2[3], q = e == 0 ? qq[0] : e == 1 ? qq[1] : e == 2 ? qq[2] : qq[3];
       const int row = 16 * wave + lane % 16;
-      const float rq = p.normalise ? 1.0f / sqrtf(q + p.eps) : 1.0f;
-      gate[SK * C + row] = p.normalise ? 1.0f / sqrtf(k + p.eps) : 1.0f;
+      // (nothing of a step that does not exist: without an eps its length of zero would make infinities, and those NaNs of the chunk's other steps)
+      const float rq = row >= live ? 0.0f : p.normalise ? 1.0f / sqrtf(q + p.eps) : 1.0f;
+      gate[SK * C + row] = row >= live ? 0.0f : p.normalise ? 1.0f / sqrtf(k + p.eps) : 1.0f;
       gate[SQ * C + row] = p.scale * rq;
       gate[RQ * C + row] = rq;
     }

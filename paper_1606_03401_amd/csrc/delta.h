@@ -317,7 +317,10 @@ struct Args {
 
 __device__ inline int ends_at(const Args& p, int b) { return p.lengths ? min(max(p.lengths[b], 0), p.t) : p.t; }
 
-// Rows that are no whole vectors, copied to ones that are, in one launch: the launch's steps, [..][B][heads][width].
+// Steps of a launch.
+inline int launch_steps(const Args& p) { return std::min((p.c1 - p.c0) * C, p.t - p.c0 * C); }
+
+// Rows that are no whole vectors, copied to ones that are, in one launch: the launch's steps, [B][..][heads][width].
 struct Padded {
   struct One {
     mebptt_seq from;

@@ -112,14 +112,16 @@ Args args_of(const mebptt_delta_desc* d, const mebptt_delta_inputs* in) {
   p.activate = d->activate, p.normalise = d->normalise, p.scale = d->scale, p.eps = d->eps;
   return p;
 }
-// Rows of a launch's steps as the kernels read them: in place, or copied to `room`, which moves on.
+// Rows of a launch's steps as the kernels read them: in place, or copied to `room`, which moves on.  Copies have a sequence's steps next to each other, however
+// the caller's lie: offsets inside a chunk have 32 bits, and with all sequences between two steps they would leave them.
 Rows rows_of(Padded& all, const Args& p, const mebptt_delta_desc* d, const mebptt_seq& from, int heads, int n, char*& room, int64_t slab) {
   const int width = whole(d, n), V = d->dtype == MEBPTT_FP32 ? 4 : 8;
   if (width == n && rows_aligned(from, d->dtype, V)) return {from.data, from.stride_t, from.stride_b, n, n};
   char* at = room;
   room += row_bytes(d, slab, heads, n);
   all.one[all.n++] = {from, at, heads, n, width};
-  const int64_t sb = (int64_t)heads * width, st = d->B * sb;
+  static_assert((int64_t)MAX_HEADS * MAX_DV <= NEAR && MAX_DK <= MAX_DV && MAX_DV % 8 == 0, "a copy's steps are near each other");
+  const int64_t st = (int64_t)heads * width, sb = launch_steps(p) * st;
   return {at - (int64_t)p.c0 * C * st * (int64_t)elem_bytes(d->dtype), st, sb, width, width};    // (as if it held all steps)
 }
 

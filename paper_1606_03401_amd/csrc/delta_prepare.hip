@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256) void delta_pad_kernel(Padded all, int B, int s
     const int n = (int)min((int64_t)PAD_ROWS, rows - row0) * quads;
     for (int i = threadIdx.x; i < n; i += 256) {
       const unsigned row = (unsigned)i / (unsigned)quads, c = ((unsigned)i - row * quads) * 4;
-      const unsigned h1 = h0 + row, more = h1 / (unsigned)p.heads, h = h1 - more * p.heads, r = r0 + more, s = r / (unsigned)B, b = r - s * (unsigned)B;
+      const unsigned h1 = h0 + row, more = h1 / (unsigned)p.heads, h = h1 - more * p.heads, r = r0 + more, b = r / (unsigned)steps, s = r - b * (unsigned)steps;
       const T* from = (const T*)p.from.data + (int64_t)(s0 + (int)s) * p.from.stride_t + (int64_t)b * p.from.stride_b + (int64_t)h * p.d;
       Quad v;
 #pragma unroll
@@ -287,7 +287,7 @@ int launch(const Args& p, hipStream_t stream) {
 
 int mebptt::delta::pad_rows(const Padded& all, const Args& p, int dtype, hipStream_t stream) {
   if (!all.n) return MEBPTT_OK;
-  const int steps = std::min((p.c1 - p.c0) * C, p.t - p.c0 * C);
+  const int steps = launch_steps(p);
   int64_t most = 1;
   for (int i = 0; i < all.n; ++i) most = std::max(most, (int64_t)steps * p.B * all.one[i].heads);
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(most, PAD_ROWS), 1 << 14), (unsigned)all.n);

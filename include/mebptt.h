@@ -670,7 +670,9 @@ int mebptt_join_backward(const mebptt_join_desc* desc, const void* x, int64_t ld
  * is the block's largest new value / 1.875.  Values between two codes take one of them by chance, with the odds that keep the mean:
  * a v that changes by a thousandth a step would never move otherwise.  The chance is a hash of seed, step and the value's place, so
  * that the same call gives the same bits.  m below 1.125 * 2^-15 of its scale becomes that or zero in the same way, v below 1.125 * 2^-31 of its becomes
- * that, never zero, which would make the next step too large. */
+ * that, never zero, which would make the next step too large.  Where a value of a block is infinite, as the square of a gradient beyond 1.8e19 is, its scale is
+ * so, and every v but zeros stands for infinity from then on: its 256 parameters change by their decay only (one whose own gradient is infinite is NaN, with states of 32
+ * bits as well).  A NaN makes its block NaN. */
 enum { MEBPTT_ADAMW_NO_DECAY = 1 };
 typedef struct {
   float* param;

@@ -93,7 +93,7 @@ __device__ inline uint32_t code_of(float x, float u, uint32_t bits16) {   // (u 
     const uint32_t c = u < LEAST ? (u * (65536.0f / LEAST) > (float)bits16 ? 1u : 0u) : (uint32_t)min(max(code, 1), 127);
     return x < 0.0f && c ? c + 128u : c;
   } else {
-    return u > 0.0f ? (uint32_t)min(max(code, 1), 255) : 0u;
+    return x != 0.0f ? (uint32_t)min(max(code, 1), 255) : 0u;   // (u is 0 or NaN beside, and of, a value that left the range: its scale is infinite, and all that is not 0 stays so)
   }
 }
 

@@ -36,10 +36,12 @@ class AdamW:
         mb.mebptt_adamw_prepare(self.tensors, self.table)
 
     def step(self) -> None:
-        """One step on the current stream.  With a clip, gradients whose norm is not finite change nothing."""
-        self.count += 1
+        """One step on the current stream.  With a clip, gradients whose norm is not finite change nothing, and the step does not count."""
         if self.clip is not None:
             mb.mebptt_adamw_norm(self.tensors, self.table, self.clip, self.norm, self.ws)
+            self.count += self.norm[1:] == self.norm[1:]        # (the factor is NaN then)
+        else:
+            self.count += 1
         mb.mebptt_adamw_step(self.desc, self.tensors, self.table, self.norm[1:] if self.clip is not None else None, self.rate, self.count)
 
     def states(self):

@@ -1,4 +1,4 @@
-"""AdamW over all tensors of a model in two launches, with its states in 32 or 8 bits.
+"""AdamW over all tensors of a model, however many, in one launch (and two for the norm of all gradients), with its states in 32 or 8 bits.
 
 Owns the states and what the library's calls need; every tensor and gradient stays where it is, so that a step can be captured into a graph.  Rate and
 step count live on the GPU: set `rate` between steps (or replays), the count goes on by itself.
@@ -45,7 +45,7 @@ class AdamW:
         mb.mebptt_adamw_step(self.desc, self.tensors, self.table, self.norm[1:] if self.clip is not None else None, self.rate, self.count)
 
     def states(self):
-        """(m, v) of every tensor in float32, as a checkpoint keeps them."""
+        """(m, v) of every tensor in float32, to be looked at.  A checkpoint keeps what steps go on from, as it is: `m`, `v`, `m_scale`, `v_scale` and `count`, copied into a new object's."""
         if self.bits == 32:
             return [m.clone() for m in self.m], [v.clone() for v in self.v]
 

@@ -1,4 +1,4 @@
-"""AdamW's object: a step that its clip refuses has not been taken, whatever comes after it."""
+"""AdamW's object: a step that its clip refuses has not been taken, whatever comes after it; steps go on from what a checkpoint kept."""
 import pytest
 import torch
 from placed import DEV, NAN
@@ -67,3 +67,24 @@ def test_without_a_clip_every_step_counts(bits):
     for k in range(3):
         opt.step()
         assert int(opt.count) == k + 1
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_steps_go_on_from_a_checkpoint(bits):
+    """Bit by bit, also where values are rounded by chance."""
+    (a, pa, ga, given, ca), (b, pb, gb, _, cb) = _made(bits), _made(bits)
+    for k, grads in enumerate(given):
+        if k == 2:
+            for x, y in zip(pb + b.m + b.v, pa + a.m + a.v):
+                x.copy_(y)
+            for x, y in zip((b.m_scale + b.v_scale) if bits == 8 else [], (a.m_scale + a.v_scale) if bits == 8 else []):
+                x.copy_(y)
+            b.count.copy_(a.count)
+        for x, y, g in zip(ga, gb, grads):
+            x.copy_(g)
+            y.copy_(g)
+        a.step()
+    b.step()
+    assert all(torch.equal(x, y) for x, y in zip(_everything(a, pa, ca), _everything(b, pb, cb)))
+    for x, y in zip(sum(a.states(), []), sum(b.states(), [])):
+        assert torch.equal(x, y)

@@ -322,7 +322,9 @@ __global__ __launch_bounds__(threads_of<WAVES>()) void join_backward_kernel(Join
     float n[NC][V], rstd[NC], dots[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      rstd[c] = p.rstd[row * groups + (at.count[c] ? at.slot[c] : 0)];
+      // (0 for lanes that have no columns: another group's, were it not finite, would reach their own group's sum.  A select, since the load is there for all)
+      const float own = p.rstd[row * groups + (at.count[c] ? at.slot[c] : 0)];
+      rstd[c] = at.count[c] ? own : 0.0f;
       widen<VEC>(xs[c], at.count[c], n[c]);
       float w[V];
       load_weight<VEC>(p.weight, at.at[c], at.count[c], p.lanes, w);

@@ -273,14 +273,15 @@ __device__ inline Op<T, N> from_frag(const char* at, int f, int lane) {
   return o;
 }
 
-constexpr int T_PARTS = 3, P_PARTS = 2, PT_PARTS = 3;   // P reaches y only, which is rounded to bf16
+// Also of P, which reaches y only: with two its terms would have 16 bits, which a y shows that is little of what they are (10000 x 1 x 16 heads: 257 us, 247 with two).
+constexpr int PARTS = 3;
 // A chunk's record: forward [T | P | gates | G], backward [T | T^T | P^T | gates | G], G in 64 bits.
 template <typename T, bool BACK>
 struct Record {
   static constexpr int T_ = 0;
-  static constexpr int TT = frag_bytes<T>(T_PARTS);
-  static constexpr int P = BACK ? TT + frag_bytes<T>(T_PARTS) : TT;     // P, or its transpose
-  static constexpr int GATE = P + frag_bytes<T>(BACK ? PT_PARTS : P_PARTS);
+  static constexpr int TT = frag_bytes<T>(PARTS);
+  static constexpr int P = BACK ? TT + frag_bytes<T>(PARTS) : TT;     // P, or its transpose
+  static constexpr int GATE = P + frag_bytes<T>(PARTS);
   static constexpr int SUMS = GATE + GATES * C * 4;
   static constexpr int BYTES = SUMS + C * 8;
 };

@@ -22,18 +22,18 @@ using namespace mebptt::delta;
 namespace {
 
 constexpr int WAVES = 8, THREADS = WAVES * WAVE;
-// Parts of R, Z, S and dS' in the products, and of W1 .. W3, which reach dq and dk only.
-constexpr int N32 = 3, NW = 2;
+// Parts of R, Z, S, dS' and W1 .. W3 in the products.  (Two for W1 .. W3, which reach dq and dk only, took no less time.)
+constexpr int N32 = PARTS;
 constexpr int COMPUTE_UNITS = 256;
 constexpr int VB = 32;      // columns of a block of dY, Z and R
 
 template <typename T, int KD>
 struct Layout {
   static constexpr int VLD = VB + Lds<T>::PAD, VSIZE = C * VLD * (int)sizeof(T), NV = sizeof(T) == 2 ? N32 : 1, BLOCK_BYTES = (1 + 2 * NV) * VSIZE;
-  static constexpr int WLD = C + Lds<T>::PAD, WSIZE = C * WLD * (int)sizeof(T), NM = sizeof(T) == 2 ? NW : 1;
+  static constexpr int WLD = C + Lds<T>::PAD, WSIZE = C * WLD * (int)sizeof(T);
   static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), BLOCK = Q + Lds<T>::row_bytes(KD);    // two blocks, one being filled
   static constexpr int W = BLOCK;                                                                    // four matrices, over them
-  static constexpr int SUMS = BLOCK + (2 * BLOCK_BYTES > 4 * NM * WSIZE ? 2 * BLOCK_BYTES : 4 * NM * WSIZE);
+  static constexpr int SUMS = BLOCK + (2 * BLOCK_BYTES > 4 * NV * WSIZE ? 2 * BLOCK_BYTES : 4 * NV * WSIZE);
   static constexpr int GATE = SUMS + C * 8, ROWF = GATE + GATES * C * 4, COLF = ROWF + WAVES * C * 8, COLS = COLF + 2 * C * 8, DOTS = COLS + 2 * C * 4,
                        NORMS = DOTS + 3 * WAVES * C * 4, MORE = NORMS + 2 * C * 4, BYTES = MORE + WAVES * 4;
 };
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
   constexpr int LD = Lds<T>::ld(KD), NT = KD / 16, VLD = L::VLD, WLD = L::WLD, VA = L::VSIZE / (int)sizeof(T), WA = L::WSIZE / (int)sizeof(T);
   T *K = (T*)(lds + L::K), *Q = (T*)(lds + L::Q);
   // [j][i], i >= j: W1 and W3 with the factor of column j's key, and with that of row i's query or key
-  T *W1 = (T*)(lds + L::W), *W1q = W1 + L::NM * WA, *W3 = W1q + L::NM * WA, *W3k = W3 + L::NM * WA;
+  T *W1 = (T*)(lds + L::W), *W1q = W1 + L::NV * WA, *W3 = W1q + L::NV * WA, *W3k = W3 + L::NV * WA;
   double *G = (double*)(lds + L::SUMS), *rowF = (double*)(lds + L::ROWF), *colF_ = (double*)(lds + L::COLF);
   float *gate = (float*)(lds + L::GATE), *cols = (float*)(lds + L::COLS), *dots = (float*)(lds + L::DOTS),
         *norms = (float*)(lds + L::NORMS), *more = (float*)(lds + L::MORE);
@@ -399,8 +399,8 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
             row[e] = over_columns((double)f);
           }
         }
-        put_parts<L::NM>(first + j * WLD + i0, WA, w1);
-        put_parts<L::NM>(second + j * WLD + i0, WA, w2);
+        put_parts<L::NV>(first + j * WLD + i0, WA, w1);
+        put_parts<L::NV>(second + j * WLD + i0, WA, w2);
         if (c16 == 0) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) rowF[wave * C + i0 + e] = row[e];
@@ -425,16 +425,16 @@ __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments
       for (int pb = 0; pb < 2; ++pb) {
         const auto kc = from_columns<LD>(K, 16 * wave, 32 * pb, lane), qc = from_columns<LD>(Q, 16 * wave, 32 * pb, lane);
         constexpr int LOW = 4;
-        Op<T, NW> a[LOW];
+        Op<T, N32> a[LOW];
         auto products = [&](const T* m, bool transposed, f32x4(&to)[4], const Op<T, 1>& x) {
           // (what a triangle leaves empty is zero in LDS as far as it is read)
 #pragma unroll
           for (int rt = 0; rt < 4; ++rt)
-            a[rt] = transposed ? from_parts<NW>(m + (16 * rt + c16) * WLD + 32 * pb, WA, g) : from_part_columns<NW, WLD>(m, WA, 16 * rt, 32 * pb, lane);
+            a[rt] = transposed ? from_parts<N32>(m + (16 * rt + c16) * WLD + 32 * pb, WA, g) : from_part_columns<N32, WLD>(m, WA, 16 * rt, 32 * pb, lane);
           if (transposed ? pb == 1 : pb == 0) {
             mma(to, a, x);
           } else {
-            const Op<T, NW> part[2] = {a[transposed ? 0 : 2], a[transposed ? 1 : 3]};
+            const Op<T, N32> part[2] = {a[transposed ? 0 : 2], a[transposed ? 1 : 3]};
             mma(to, part, x, transposed ? 0 : 2);
           }
           __builtin_amdgcn_sched_barrier(0);

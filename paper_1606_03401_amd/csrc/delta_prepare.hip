@@ -39,7 +39,7 @@ __device__ inline void put_tile(float* a, f32x4 v, int lane) {
 }
 
 // The pieces of a triangle, or of its transpose, in the order of the operands.
-template <typename T, int PARTS, bool TRANSPOSED>
+template <typename T, bool TRANSPOSED>
 __device__ inline void put_frags(char* out, const float* m) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), lane = here(threadIdx.x % WAVE), g = lane / 16;
   for (int f = wave; f < FRAGS; f += 4) {
@@ -231,12 +231,12 @@ __global__ __launch_bounds__(256, 4) void delta_prepare_kernel(Args p) {
     for (int i = 0; i < 2; ++i) put_tile(M + (32 + 16 * i) * LM + 16 * wave, -low[i], lane);
   }
   __syncthreads();
-  put_frags<T, T_PARTS, false>(out + R::T_, M);
+  put_frags<T, false>(out + R::T_, M);
   if constexpr (BACK) {
-    put_frags<T, T_PARTS, true>(out + R::TT, M);
-    put_frags<T, PT_PARTS, true>(out + R::P, P);
+    put_frags<T, true>(out + R::TT, M);
+    put_frags<T, true>(out + R::P, P);
   } else {
-    put_frags<T, P_PARTS, false>(out + R::P, P);
+    put_frags<T, false>(out + R::P, P);
   }
   if (threadIdx.x < C) {
     const int i = threadIdx.x;

@@ -139,8 +139,8 @@ __device__ inline void store_state(const f32x4 (&S)[NT], float* to, int rows, in
 
 template <typename T, int KD, int W, int MODE>
 struct Layout {   // of LDS
-  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), T_ = MODE ? Q : Q + Lds<T>::row_bytes(KD), P = T_ + frag_bytes<T>(T_PARTS),
-                       GATE = MODE ? P : P + frag_bytes<T>(P_PARTS), V = GATE + WALK_GATES * C * 4, Y = V + Lds<T>::row_bytes(16 * W),
+  static constexpr int K = 0, Q = K + Lds<T>::row_bytes(KD), T_ = MODE ? Q : Q + Lds<T>::row_bytes(KD), P = T_ + frag_bytes<T>(PARTS),
+                       GATE = MODE ? P : P + frag_bytes<T>(PARTS), V = GATE + WALK_GATES * C * 4, Y = V + Lds<T>::row_bytes(16 * W),
                        BYTES = MODE || sizeof(T) == 4 ? Y : Y + W * TURN * 2;
 };
 
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
   Fetch<T, KD, W * WAVE> ck, cq;
   Fetch<T, 16 * W, W * WAVE> cv;
   // of the record: T, P and the gates as one, or T and the gates
-  Copy<MODE == WALK ? L::V - L::T_ : frag_bytes<T>(T_PARTS), W * WAVE> ct;
+  Copy<MODE == WALK ? L::V - L::T_ : frag_bytes<T>(PARTS), W * WAVE> ct;
   Copy<WALK_GATES * C * 4, W * WAVE> cg;
   auto fetch = [&](int chunk) {
     const int live = end - chunk * C;
@@ -269,14 +269,14 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
     if (!unit) load_tiles<Lds<T>::ld(16 * W)>(X, VL, 16 * wave, lane);
     f32x4 U[4] = {};
     {
-      Op<T, T_PARTS> t0[4], t1[2];
+      Op<T, PARTS> t0[4], t1[2];
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) t0[rt] = from_frag<T, T_PARTS>(lds + L::T_, lower(rt, 0), lane);
+      for (int rt = 0; rt < 4; ++rt) t0[rt] = from_frag<T, PARTS>(lds + L::T_, lower(rt, 0), lane);
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) X[rt] -= steps_of(gate, GA_SK, rt, g) * KQ[rt];
       next_product();
 #pragma unroll
-      for (int rt = 0; rt < 2; ++rt) t1[rt] = from_frag<T, T_PARTS>(lds + L::T_, lower(2 + rt, 1), lane);
+      for (int rt = 0; rt < 2; ++rt) t1[rt] = from_frag<T, PARTS>(lds + L::T_, lower(2 + rt, 1), lane);
       mma(U, t0, cut<T, 3>(X[0], X[1]));
       next_product();
       mma(U, t1, cut<T, 3>(X[2], X[3]), 2);
@@ -289,9 +289,9 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
     if (MODE == AGAIN && col < p.dvp) store_state(U, p.R + ((int64_t)(chunk - p.c0) * BH + bh) * C * p.dvp, C, p.dvp, col, g);
     if constexpr (MODE == WALK) {
       f32x4 Y[4];
-      Op<T, P_PARTS> p0[4], p1[2];
+      Op<T, PARTS> p0[4], p1[2];
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) p0[rt] = from_frag<T, P_PARTS>(lds + L::P, lower(rt, 0), lane);
+      for (int rt = 0; rt < 4; ++rt) p0[rt] = from_frag<T, PARTS>(lds + L::P, lower(rt, 0), lane);
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) {
         Y[rt] = steps_of(gate, GA_SQ, rt, g) * KQ[4 + rt];
@@ -299,11 +299,11 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, MODE>())) void delta_walk
       }
       if (DEEP) next_product();
 #pragma unroll
-      for (int rt = 0; rt < 2; ++rt) p1[rt] = from_frag<T, P_PARTS>(lds + L::P, lower(2 + rt, 1), lane);
-      mma(Y, p0, cut<T, 2>(U[0], U[1]));
+      for (int rt = 0; rt < 2; ++rt) p1[rt] = from_frag<T, PARTS>(lds + L::P, lower(2 + rt, 1), lane);
+      mma(Y, p0, cut<T, PARTS>(U[0], U[1]));
       next_product();
       if (DEEP) fetch_columns(0);
-      mma(Y, p1, cut<T, 2>(U[2], U[3]), 2);
+      mma(Y, p1, cut<T, PARTS>(U[2], U[3]), 2);
       store_tiles(y_of(chunk), (int)p.y.stride_t, Y, steps, live, c0 + 16 * wave, p.dv, p.vec_out, reinterpret_cast<T*>(lds + L::Y) + wave * TURN, lane);
       next_product();
     } else {
@@ -419,22 +419,22 @@ __global__ __launch_bounds__(W* WAVE, (per_simd<KD, W, WALK>())) void delta_walk
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) U[rt] *= steps_of(gate, LA_SK, rt, g);
     {
-      Op<T, PT_PARTS> p0[2], p1[4];
+      Op<T, PARTS> p0[2], p1[4];
 #pragma unroll
-      for (int rt = 0; rt < 2; ++rt) p0[rt] = from_frag<T, PT_PARTS>(lds + L::P, upper(rt, 0), lane);
+      for (int rt = 0; rt < 2; ++rt) p0[rt] = from_frag<T, PARTS>(lds + L::P, upper(rt, 0), lane);
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) p1[rt] = from_frag<T, PT_PARTS>(lds + L::P, upper(rt, 1), lane);
+      for (int rt = 0; rt < 4; ++rt) p1[rt] = from_frag<T, PARTS>(lds + L::P, upper(rt, 1), lane);
       mma(U, p0, cut<T, 1>(dY[0], dY[1]));   // (exact: dY has T's bits)
       mma(U, p1, cut<T, 1>(dY[2], dY[3]));
       next_product();
     }
     f32x4 Z[4] = {};
     {
-      Op<T, T_PARTS> t0[2], t1[4];
+      Op<T, PARTS> t0[2], t1[4];
 #pragma unroll
-      for (int rt = 0; rt < 2; ++rt) t0[rt] = from_frag<T, T_PARTS>(lds + L::T_, upper(rt, 0), lane);
+      for (int rt = 0; rt < 2; ++rt) t0[rt] = from_frag<T, PARTS>(lds + L::T_, upper(rt, 0), lane);
 #pragma unroll
-      for (int rt = 0; rt < 4; ++rt) t1[rt] = from_frag<T, T_PARTS>(lds + L::T_, upper(rt, 1), lane);
+      for (int rt = 0; rt < 4; ++rt) t1[rt] = from_frag<T, PARTS>(lds + L::T_, upper(rt, 1), lane);
 #pragma unroll
       for (int rt = 0; rt < 4; ++rt) U[rt] *= steps_of(gate, BE, rt, g);
       mma(Z, t0, cut<T, 3>(U[0], U[1]));

@@ -403,7 +403,7 @@ int to_power(int64_t v) {
   return p;
 }
 // The fewest waves whose threads hold the row in four chunks each, and then the fewest chunks.
-bool shape_of(int width, int group, bool vec, Shape* out) {
+bool shape_of(int width, int group, Shape* out) {
   for (int waves : {1, 4, 16}) {
     Shape best = {};
     for (int pieces : {1, 2, 4}) {
@@ -488,7 +488,7 @@ int mebptt_join_forward(const mebptt_join_desc* d, const void* x, int64_t ldx, c
                    rows_aligned(residual, ldr, d->residual_dtype, V) && rows_aligned(residual_out, ldo, d->residual_dtype, V) &&
                    rows_aligned(y, ldy, d->x_dtype, V) && rows_aligned(weight, 0, MEBPTT_FP32, V) && rows_aligned(weight_next, 0, MEBPTT_FP32, V);
   Shape s;
-  if (!shape_of(d->width, d->group, vec, &s)) return set_error(MEBPTT_EINVAL, "no shape for this width and group");
+  if (!shape_of(d->width, d->group, &s)) return set_error(MEBPTT_EINVAL, "no shape for this width and group");
   const Join p = {x, z, residual, weight, weight_next, y, residual_out, rstd, rstd_next, d->rows, ldx, ldz, ldr, ldy, ldo,
                   d->width, d->group, s.lanes, s.pieces, d->scale, d->eps};
   hipStream_t st = (hipStream_t)stream;
@@ -530,7 +530,7 @@ int mebptt_join_backward(const mebptt_join_desc* d, const void* x, int64_t ldx, 
                    rows_aligned(dx, lddx, d->x_dtype, V) && rows_aligned(dz, lddz, d->x_dtype, V) && rows_aligned(dres, lddr, d->residual_dtype, V) &&
                    rows_aligned(weight, 0, MEBPTT_FP32, V) && rows_aligned(weight_next, 0, MEBPTT_FP32, V);
   Shape s;
-  if (!shape_of(w, d->group, vec, &s)) return set_error(MEBPTT_EINVAL, "no shape for this width and group");
+  if (!shape_of(w, d->group, &s)) return set_error(MEBPTT_EINVAL, "no shape for this width and group");
   const int64_t groups = back_groups(d, s.waves);
   const JoinBack p = {x, z, r, dy, dout, weight, weight_next, rstd, rstd_next, dx, dz, dres, sums ? (float*)workspace : nullptr,
                       d->rows, ldx, ldz, ldr, lddy, lddo, lddx, lddz, lddr, w, d->group, s.lanes, s.pieces, d->scale, d->again};

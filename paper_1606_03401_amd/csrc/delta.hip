@@ -6,7 +6,7 @@ using namespace mebptt::delta;
 
 namespace {
 
-// Chunks whose records a forward call's workspace holds at once: 128 MB of them in bf16.
+// Chunks whose records a forward call's workspace holds at once: 163 MB of them in bf16.
 constexpr int64_t RECORDS = 4096;
 
 int check(const mebptt_delta_desc* d) {

@@ -8,9 +8,9 @@
 // A workgroup of eight waves, one to a compute unit, goes through chunks of sequences with one head each; or, where value heads share a key head, has one
 // chunk and key head and goes through its value heads.  Wave w computes 16 columns of dq and dk; in what is 64 x 64, waves 0 .. 3 have column tiles of
 // dY R^T and P, 4 .. 7 those of E and M.
-// Bound: what a chunk reads (R, Z, S and dS' in fp32: 243 KB a chunk of 128 x 128, 2.1 TB/s over all), in bursts between which the products stand; eight waves
-// of 240 registers and 110 KB of LDS leave no room for a second workgroup to fill the gaps.  1000 x 32 x 8 heads of 128 x 128, bf16, in four launches: 478 us,
-// of a chunk's 64 thousand cycles 25 in the loop over columns of v (13 of them products), 11 for the 64 x 64 products, 8 for sums, the rest writing and waiting.
+// Bound: what a chunk reads (R, Z, S and dS' in fp32: 243 KB a chunk of 128 x 128, 2 TB/s over all), in bursts between which the products stand; eight waves
+// of 240 registers and 157 KB of LDS leave no room for a second workgroup to fill the gaps.  1000 x 32 x 8 heads of 128 x 128, bf16, in four launches: 497 us,
+// of a chunk's 62 thousand cycles 25 in the loop over columns of v (13 of them products), 12 for the 64 x 64 products, 8 for sums, the rest writing and waiting.
 // Tried: two bf16 parts for R, Z, S and dS', 3 % faster and dA off by 10^-6; loads spread over the products, workgroups started apart, blocks in another order in
 // each workgroup: none faster.
 #include "delta.h"
@@ -22,7 +22,8 @@ using namespace mebptt::delta;
 namespace {
 
 constexpr int WAVES = 8, THREADS = WAVES * WAVE;
-// Parts of R, Z, S, dS' and W1 .. W3 in the products.  (Two for W1 .. W3, which reach dq and dk only, took no less time.)
+// Parts of R, Z, S, dS' and W1 .. W3 in the products.  (With two for W1 .. W3, which reach dq and dk only, a launch takes 120 us in place of 124, and a dq that is little of
+// its terms shows their 16 bits.)
 constexpr int N32 = PARTS;
 constexpr int COMPUTE_UNITS = 256;
 constexpr int VB = 32;      // columns of a block of dY, Z and R
@@ -176,7 +177,8 @@ __device__ inline const Args* fresh_arguments() {
   return (const Args*)at;
 }
 
-// SHARED: more than one value head to a key head.  (Without the loop over them the compiler keeps what belongs to it out of registers.)
+// SHARED: more than one value head to a key head.  (Without the loop over them the compiler keeps what belongs to it out of registers.  With it 24 values of a thread are in
+// scratch memory at 128 rows in bf16, 125 in fp32, 3 at 64.)
 template <typename T, int KD, bool SHARED>
 __global__ __launch_bounds__(THREADS) void delta_gradients_kernel(Args arguments) {
   (void)arguments;

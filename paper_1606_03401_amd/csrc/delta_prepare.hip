@@ -2,7 +2,7 @@
 // factors of its steps.  One workgroup of four waves per chunk, sequence and head.
 // Bound: short dependent steps (products, a substitution over 16 rows, two levels of joined blocks) with a barrier between any two; half of the
 // waves' time is waiting, which four or five workgroups on a compute unit fill.  1000 steps x 32 sequences x 8 heads of 128, bf16: 74 us (for the
-// backward pass, which needs T^T as well, 4 x 26), of which 202 MB take 39 at a copy's rate; 132 while k and q kept LDS of their own.
+// backward pass, which needs T^T as well, 4 x 26), of which 227 MB take 44 at a copy's rate; 132 while k and q kept LDS of their own.
 #include "delta.h"
 #include "dynamic_lds.h"
 

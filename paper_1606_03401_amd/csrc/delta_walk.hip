@@ -2,8 +2,8 @@
 // head, a wave 16 of them: all rows of the state in its registers, and with them everything that is computed in these columns.  Waves share a
 // chunk's keys, queries and matrices in LDS, nothing else.
 // Bound: the chain of products over a sequence's chunks, one workgroup to a compute unit; there the matrix instructions of three bf16 parts (of an fp32
-// state, to the state's full width) and the cutting take turns.  128 x 128, bf16: 1000 x 32 x 8 heads 141 us forward (the matrix unit busy 39 % of the time, the
-// vector unit 40 %), 4 x 40 to run it again with S and R written, 4 x 53 back; 10000 x 1 x 16 heads in eight segments 99 for the survey and 106.
+// state, to the state's full width) and the cutting take turns.  128 x 128, bf16: 1000 x 32 x 8 heads 151 us forward (the matrix unit busy 40 % of the time, the
+// vector unit as long), 4 x 39 to run it again with S and R written, 4 x 53 back; 10000 x 1 x 16 heads in eight segments 100 for the survey and 116.
 #include "delta.h"
 #include "dynamic_lds.h"
 

@@ -6,6 +6,8 @@
 // forward at 8192 x 4096, all parts: 65 (5.2).
 // A row belongs to one wave up to 2048 columns, to 4 or 16 beyond.  L lanes (a power of two) share a group of columns, so that a group's sum takes
 // shuffles among neighbours (and, where L is more than a wave, a few floats in LDS), and several groups of a row are summed at once.
+// The kernels of 16 waves, for rows of over 8192 columns, have 128 registers to a thread and keep the rest in scratch memory: up to 23 values forward and 522 backward, of rows or groups that
+// are no whole vectors 158 and 654.
 #include "ops.h"
 
 using namespace mebptt;
